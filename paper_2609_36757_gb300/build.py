@@ -25,8 +25,11 @@ DEBUG_BUILD = os.path.join(HERE, "_build_debug")
 DEBUG_LIB = os.path.join(HERE, "libfastvr_attn_debug.so")
 INCLUDE = os.path.join(ROOT, "include")
 
-SOURCES = ["fastvr_host.cpp", "kv_append.cu", "chunk_attn_fwd.cu",
-           "chunk_attn_static.cu", "one_step.cu", "chunk_attn_bwd.cu"]
+SOURCES = ["fastvr_host.cpp", "block_host.cpp", "kv_append.cu",
+           "chunk_attn_fwd.cu",
+           "chunk_attn_static.cu", "one_step.cu", "chunk_attn_bwd.cu",
+           "rotary.cu", "block_norm_fwd.cu", "block_norm_bwd.cu",
+           "q4_cache.cu", "q4_attn.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC",
          "-Xcompiler", "-fvisibility=hidden", "-I", INCLUDE, "-I", CSRC]

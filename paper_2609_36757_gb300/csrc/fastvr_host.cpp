@@ -23,10 +23,16 @@
 
 #include "../../include/fastvr_attn.h"
 #include "fastvr_internal.h"
+#include "fastvr_plan.h"
+
+using fastvr::aligned16;
+using fastvr::control_word;
+using fastvr::kControlBytes;
+using fastvr::num_slots;
+using fastvr::supported_dim;
+using fastvr::valid_config;
 
 namespace {
-
-constexpr size_t kControlBytes = 256;
 
 struct Segment {
   int64_t start, len;
@@ -34,44 +40,11 @@ struct Segment {
 
 }  // namespace
 
-struct fastvr_plan_s {
-  fastvr_attn_config_t cfg;
-  int64_t slots;         // S
-  int64_t slot_tokens;   // k * N
-  int64_t cache_tokens;  // S * k * N per head
-  size_t kv_bytes;       // bytes of the K region (= the V region)
-  char* base;            // caller's cache buffer
-  int64_t chunks;        // chunks appended since the last reset
-  int32_t last_frames;   // frames of the newest chunk
-  bool device_ready;
-  int device;
-  int64_t launches;        // kernels enqueued since creation
-  int32_t inject_stall;    // failure-detection test hook
-  uint64_t wait_limit_ns;  // 0 = kernel default
-  int64_t append_shift;    // debug builds: next append's destination shift
-};
-
 namespace {
 
 // Failure-detection hook for the calls without a plan (process-wide).
 std::atomic<int32_t> g_noplan_stall{0};
 std::atomic<uint64_t> g_noplan_wait_ns{0};
-
-bool valid_config(const fastvr_attn_config_t* c) {
-  return c != nullptr && c->batch > 0 && c->heads > 0 && c->head_dim > 0 &&
-         c->tokens_per_frame > 0 && c->frames_per_chunk > 0 &&
-         c->window_chunks >= -1 && !(c->softmax_scale < 0.f) &&
-         isfinite(c->softmax_scale) &&
-         (c->window_chunks >= 0 || c->max_chunks > 0);
-}
-
-bool supported_dim(int d) { return d == 64 || d == 128; }
-
-int64_t num_slots(const fastvr_attn_config_t& c) {
-  return c.window_chunks >= 0 ? (int64_t)c.window_chunks + 1 : c.max_chunks;
-}
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 // Visible segments of the newest chunk, in slot order, merged when adjacent.
 std::vector<Segment> visible_segments(const fastvr_plan_s& p) {
@@ -100,37 +73,66 @@ float* workspace(const fastvr_plan_s* p) {
   return reinterpret_cast<float*>(p->base + 2 * p->kv_bytes);
 }
 
-int* control_word(const fastvr_plan_s* p) {
-  return reinterpret_cast<int*>(p->base + 2 * p->kv_bytes +
-                                fastvr::workspace_bytes(p->cfg.head_dim));
+}  // namespace
+
+bool fastvr::valid_config(const fastvr_attn_config_t* c) {
+  return c != nullptr && c->batch > 0 && c->heads > 0 && c->head_dim > 0 &&
+         c->tokens_per_frame > 0 && c->frames_per_chunk > 0 &&
+         c->window_chunks >= -1 && !(c->softmax_scale < 0.f) &&
+         isfinite(c->softmax_scale) &&
+         (c->window_chunks >= 0 || c->max_chunks > 0);
 }
 
-fastvr_status_t ensure_device(fastvr_plan_s* p) {
-  if (p->device_ready) return FASTVR_OK;
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return FASTVR_ERR_CUDA;
-  int major = 0, minor = 0;
-  if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) !=
+int64_t fastvr::num_slots(const fastvr_attn_config_t& c) {
+  return c.window_chunks >= 0 ? (int64_t)c.window_chunks + 1 : c.max_chunks;
+}
+
+fastvr_status_t fastvr::check_device() {
+  int dev = 0, major = 0, minor = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) !=
           cudaSuccess ||
       cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) !=
           cudaSuccess)
     return FASTVR_ERR_CUDA;
-  if (major != 10 || minor != 3) return FASTVR_ERR_UNSUPPORTED;
-  cudaPointerAttributes attr;
-  if (cudaPointerGetAttributes(&attr, p->base) != cudaSuccess ||
-      attr.type != cudaMemoryTypeDevice || attr.device != dev) {
-    cudaGetLastError();
-    return FASTVR_ERR_INVALID_ARG;
+  return major == 10 && minor == 3 ? FASTVR_OK : FASTVR_ERR_UNSUPPORTED;
+}
+
+int fastvr::device_sms() {
+  int dev = 0, sms = 0;
+  cudaGetDevice(&dev);
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return sms > 0 ? sms : 152;
+}
+
+fastvr_status_t fastvr::ensure_device(fastvr_plan_s* p, size_t control_bytes,
+                                      struct CUstream_st* stream) {
+  if (p->device_ready) return FASTVR_OK;
+  const fastvr_status_t st = check_device();
+  if (st != FASTVR_OK) return st;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return FASTVR_ERR_CUDA;
+  const char* buffers[] = {p->base, p->workspace};
+  for (const char* buffer : buffers) {
+    if (buffer == nullptr) continue;  // bfloat16 plans have no second buffer
+    cudaPointerAttributes attr;
+    if (cudaPointerGetAttributes(&attr, buffer) != cudaSuccess ||
+        attr.type != cudaMemoryTypeDevice || attr.device != dev) {
+      cudaGetLastError();
+      return FASTVR_ERR_INVALID_ARG;
+    }
   }
-  // Clear the control block once; kernels only ever set it.
-  if (cudaMemset(control_word(p), 0, kControlBytes) != cudaSuccess)
-    return FASTVR_ERR_CUDA;
+  // Clear the control block once; kernels only ever set its status word and
+  // leave its counters at zero.
+  const cudaError_t e =
+      p->q4 ? cudaMemsetAsync(control_word(p), 0, control_bytes,
+                              reinterpret_cast<cudaStream_t>(stream))
+            : cudaMemset(control_word(p), 0, control_bytes);
+  if (e != cudaSuccess) return FASTVR_ERR_CUDA;
   p->device = dev;
   p->device_ready = true;
   return FASTVR_OK;
 }
-
-}  // namespace
 
 extern "C" {
 
@@ -187,6 +189,7 @@ fastvr_status_t fastvr_attn_plan(const fastvr_attn_config_t* cfg,
   p->cache_tokens = p->slots * p->slot_tokens;
   p->kv_bytes =
       (need - kControlBytes - fastvr::workspace_bytes(cfg->head_dim)) / 2;
+  p->control_off = need - kControlBytes;
   p->base = static_cast<char*>(kv_cache);
   p->chunks = 0;
   p->last_frames = 0;
@@ -202,7 +205,8 @@ fastvr_status_t fastvr_attn_plan(const fastvr_attn_config_t* cfg,
 fastvr_status_t fastvr_kv_append(fastvr_plan_t p, const void* k_new,
                                  const void* v_new, int32_t frames,
                                  struct CUstream_st* stream) {
-  if (p == nullptr || k_new == nullptr || v_new == nullptr || frames < 1 ||
+  if (p == nullptr || p->q4 || k_new == nullptr || v_new == nullptr ||
+      frames < 1 ||
       !aligned16(k_new) || !aligned16(v_new))
     return FASTVR_ERR_INVALID_ARG;
   if (frames > p->cfg.frames_per_chunk) return FASTVR_ERR_CAPACITY;
@@ -210,7 +214,7 @@ fastvr_status_t fastvr_kv_append(fastvr_plan_t p, const void* k_new,
     return FASTVR_ERR_SEQUENCE;  // the stream already ended with a ragged chunk
   if (p->cfg.window_chunks < 0 && p->chunks >= p->cfg.max_chunks)
     return FASTVR_ERR_CAPACITY;
-  fastvr_status_t st = ensure_device(p);
+  fastvr_status_t st = fastvr::ensure_device(p, kControlBytes, stream);
   if (st != FASTVR_OK) return st;
 
   fastvr::AppendParams a;
@@ -237,11 +241,11 @@ fastvr_status_t fastvr_kv_append(fastvr_plan_t p, const void* k_new,
 
 fastvr_status_t fastvr_chunk_attn_fwd(fastvr_plan_t p, const void* q, void* out,
                                       float* lse, struct CUstream_st* stream) {
-  if (p == nullptr || q == nullptr || out == nullptr || !aligned16(q) ||
-      !aligned16(out) || (((uintptr_t)lse) & 3u) != 0)
+  if (p == nullptr || p->q4 || q == nullptr || out == nullptr ||
+      !aligned16(q) || !aligned16(out) || (((uintptr_t)lse) & 3u) != 0)
     return FASTVR_ERR_INVALID_ARG;
   if (p->chunks == 0) return FASTVR_ERR_SEQUENCE;
-  fastvr_status_t st = ensure_device(p);
+  fastvr_status_t st = fastvr::ensure_device(p, kControlBytes, stream);
   if (st != FASTVR_OK) return st;
 
   const std::vector<Segment> segs = visible_segments(*p);
@@ -518,7 +522,7 @@ fastvr_status_t fastvr_debug_inject_stall(fastvr_plan_t p, int32_t stall,
 
 fastvr_status_t fastvr_debug_shift_next_append(fastvr_plan_t p,
                                               int64_t tokens) {
-  if (p == nullptr || tokens < 0 || tokens > p->slot_tokens)
+  if (p == nullptr || p->q4 || tokens < 0 || tokens > p->slot_tokens)
     return FASTVR_ERR_INVALID_ARG;
 #ifdef FASTVR_BOUNDS_CHECK
   p->append_shift = tokens;

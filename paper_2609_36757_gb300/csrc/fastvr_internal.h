@@ -184,4 +184,130 @@ int chunk_attn_parts(const AttnParams& p);
 cudaError_t launch_chunk_attn(const AttnParams& p, cudaStream_t stream,
                               int* launches);
 
+// ------------------------------------------- operators around the attention
+// (include/fastvr_block.h)
+
+constexpr int kRotaryMaxPairs = 256;
+
+struct RotaryArgs {
+  const void *q, *k;       // [batch, tokens, heads | kv_heads, head_dim]
+  void *q_out, *k_out;
+  Strides q_str, k_str, q_out_str, k_out_str;
+  const int32_t* positions;
+  int64_t pos_batch;
+  int32_t batch, tokens, heads, kv_heads, head_dim, pairs, axes, section[3];
+  bool f32, half, transpose;
+  float magnitude;
+  int sms;
+  uint64_t turn[kRotaryMaxPairs];  // theta / 2 pi modulo 1, in 2^-64 turns
+};
+cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t stream);
+
+constexpr int kNormNone = 0, kNormRms = 1, kNormLayer = 2;
+
+struct NormFwdParams {
+  const void *x, *y;
+  const float *gate, *scale, *shift, *pre_weight, *post_weight;
+  void *r, *h;
+  int64_t rows, group_tokens;
+  int32_t dim, pre, post;
+  float eps, residual_scale;
+};
+cudaError_t launch_norm_fwd(const NormFwdParams& p, bool res_f32,
+                            bool block_f32, cudaStream_t stream);
+
+struct NormBwdSplit {
+  int32_t slices;      // CTAs that share a group, or 1
+  int64_t cta_groups;  // whole groups of a CTA when slices is 1
+  int64_t ctas;
+};
+NormBwdSplit norm_bwd_split(int64_t all_groups, int64_t group_tokens, int sms);
+
+struct NormBwdParams {
+  const void *dr, *dh, *r, *y;
+  const float *gate, *scale, *pre_weight, *post_weight;
+  void *dx, *dy;
+  float *dgate, *dscale, *dshift, *dpre_weight, *dpost_weight;
+  float* partial;         // [ctas, 3, dim] when slices > 1
+  float* weight_partial;  // [ctas, 2, dim], or null when neither is wanted
+  int64_t all_groups, group_tokens, cta_groups, ctas;
+  int32_t slices, dim, pre, post;
+  float eps, residual_scale;
+};
+cudaError_t launch_norm_bwd(const NormBwdParams& p, bool res_f32,
+                            bool block_f32, cudaStream_t stream);
+
+// The 4-bit cache: codes [B, Hkv, cache_tokens, d/2] bytes, scales bfloat16
+// [B, Hkv, cache_tokens, d/32], for K and for V.
+struct Q4AppendParams {
+  const uint16_t *k, *v;
+  Strides k_str, v_str;
+  uint32_t *k_codes, *v_codes;
+  uint16_t *k_scales, *v_scales;
+  int32_t batch, tokens, heads, head_dim;
+  int64_t cache_tokens;
+  int64_t first_row;   // cache row of the first token (rows wrap)
+  int64_t code_words;  // 32-bit words of a code region (bounds checks)
+  int* status;
+};
+cudaError_t launch_q4_append(const Q4AppendParams& p, int sms,
+                             cudaStream_t stream);
+
+struct Q4ReadParams {
+  const uint32_t *k_codes, *v_codes;
+  const uint16_t *k_scales, *v_scales;
+  uint16_t *k_out, *v_out;
+  Strides out_str;
+  int32_t batch, tokens, heads, head_dim;
+  int64_t cache_tokens, first_row, code_words;
+  // Null, or the first visible chunk of each batch entry: see q4_cache.cu.
+  const int32_t* first_chunk;
+  int64_t lo_chunk, chunk_tokens;
+  int* status;
+};
+cudaError_t launch_q4_read(const Q4ReadParams& p, bool head_major, int sms,
+                           cudaStream_t stream);
+
+// Few query rows straight over the codes.
+constexpr int kQ4MaxParts = 1024;  // partial results of split key ranges
+constexpr int kQ4MaxSplits = 512;
+constexpr int kQ4PartRows = 32;    // rows of the largest row block
+inline size_t q4_partial_bytes(int head_dim) {
+  return (size_t)kQ4MaxParts * kQ4PartRows * (head_dim + 2) * sizeof(float);
+}
+struct Q4AttnParams {
+  const uint16_t* q;  // [B, q_tokens, heads, d]
+  uint16_t* out;
+  float* lse;
+  const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
+  const int32_t* first_chunk;
+  float* partial;  // kQ4MaxParts parts of kQ4PartRows rows of d + 2
+  int* tickets;    // kQ4MaxParts counters, zero between calls
+  int32_t batch_heads, heads, kv_heads, head_dim, q_tokens;
+  int32_t group;   // query heads per key head
+  int32_t rows;    // q_tokens * group
+  int64_t cache_tokens, first_row;  // first_row: oldest visible token's row
+  int64_t keys;                     // visible tokens
+  int64_t lo_chunk, chunk_tokens;
+  float scale_log2;
+  int32_t row_blocks, splits;  // filled in by the launch
+};
+cudaError_t launch_q4_attn(const Q4AttnParams& p, int sms,
+                           cudaStream_t stream);
+
+#ifdef __CUDACC__
+// The first of `keys` tokens (counted from the start of chunk lo_chunk) that
+// a batch entry sees when nothing before chunk first_chunk is visible to it.
+__device__ __forceinline__ int64_t first_visible_token(int32_t first_chunk,
+                                                       int64_t lo_chunk,
+                                                       int64_t chunk_tokens,
+                                                       int64_t keys) {
+  const int64_t hidden = (int64_t)first_chunk - lo_chunk;
+  if (hidden <= 0) return 0;
+  // hidden * chunk_tokens < 2^31 * 2^31
+  const int64_t t = hidden * chunk_tokens;
+  return t < keys ? t : keys;
+}
+#endif
+
 }  // namespace fastvr

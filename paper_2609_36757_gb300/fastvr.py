@@ -1,4 +1,5 @@
-"""Python binding of libfastvr_attn.so (the C ABI in include/fastvr_attn.h).
+"""Python binding of libfastvr_attn.so (the C ABI in include/fastvr_attn.h and
+include/fastvr_block.h).
 
 The functions below carry the C names and only marshal arguments: pointers are
 passed as integers (device addresses), streams as cudaStream_t handles.  Every
@@ -8,13 +9,16 @@ not been built.
 
 `StreamingAttention` is a convenience wrapper for torch tensors: it allocates
 the KV cache with torch (device memory is the caller's in the C ABI) and
-passes data pointers and the current CUDA stream through.
+passes data pointers and the current CUDA stream through;
+`StreamingAttention4` is the same over a cache held in 4 bits.  `rotary`,
+`gated_norm` and their gradients cover what runs before and after the
+attention in a block.
 """
 from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfastvr_attn.so")
@@ -41,10 +45,45 @@ class fastvr_attn_config_t(ctypes.Structure):
                 ("softmax_scale", ctypes.c_float)]
 
 
-# Every symbol the header declares, with (restype, argtypes).
+# Element types, rotary layouts and scalings, norms (include/fastvr_block.h).
+FASTVR_BF16, FASTVR_F32 = 0, 1
+ROTARY_LAYOUTS = {"interleaved": 0, "half": 1}
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+
+
+class fastvr_strides_t(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("token", ctypes.c_int64),
+                ("head", ctypes.c_int64)]
+
+
+class fastvr_rotary_config_t(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("section", ctypes.c_int32 * 3), ("scaling", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double * 3),
+                ("original_context", ctypes.c_double * 3),
+                ("beta_fast", ctypes.c_double),
+                ("beta_slow", ctypes.c_double),
+                ("magnitude", ctypes.c_double)]
+
+
+class fastvr_norm_config_t(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("pre", ctypes.c_int32), ("post", ctypes.c_int32),
+                ("residual_dtype", ctypes.c_int32),
+                ("block_dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("residual_scale", ctypes.c_float)]
+
+
+# Every symbol the headers declare, with (restype, argtypes).
 _VP, _I32, _I64, _SZ = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                         ctypes.c_size_t)
 _CFGP = ctypes.POINTER(fastvr_attn_config_t)
+_STRP = ctypes.POINTER(fastvr_strides_t)
+_ROTP = ctypes.POINTER(fastvr_rotary_config_t)
+_NRMP = ctypes.POINTER(fastvr_norm_config_t)
 SIGNATURES = {
     "fastvr_kv_cache_bytes": (_I32, [_CFGP, ctypes.POINTER(_SZ)]),
     "fastvr_attn_plan": (_I32, [_CFGP, _VP, _SZ, ctypes.POINTER(_VP)]),
@@ -78,6 +117,23 @@ SIGNATURES = {
     "fastvr_debug_inject_stall_noplan": (_I32, [_I32, ctypes.c_uint64]),
     "fastvr_plan_destroy": (None, [_VP]),
     "fastvr_status_string": (ctypes.c_char_p, [_I32]),
+    "fastvr_rotary_frequencies": (_I32, [_ROTP,
+                                         ctypes.POINTER(ctypes.c_double),
+                                         ctypes.POINTER(ctypes.c_double)]),
+    "fastvr_rotary": (_I32, [_ROTP] + [_I32] * 5 + [_VP, _STRP, _VP, _STRP,
+                                                    _VP, _I64, _VP, _STRP,
+                                                    _VP, _STRP, _I32, _VP]),
+    "fastvr_gated_norm_fwd": (_I32, [_NRMP] + [_VP] * 10),
+    "fastvr_gated_norm_bwd_scratch_bytes": (_I32, [_NRMP,
+                                                   ctypes.POINTER(_SZ)]),
+    "fastvr_gated_norm_bwd": (_I32, [_NRMP] + [_VP] * 16 + [_SZ, _VP]),
+    "fastvr_q4_cache_bytes": (_I32, [_CFGP, _I32, ctypes.POINTER(_SZ)]),
+    "fastvr_q4_workspace_bytes": (_I32, [_CFGP, _I32, ctypes.POINTER(_SZ)]),
+    "fastvr_q4_plan": (_I32, [_CFGP, _I32, _VP, _SZ, _VP, _SZ,
+                              ctypes.POINTER(_VP)]),
+    "fastvr_q4_append": (_I32, [_VP, _VP, _STRP, _VP, _STRP, _I32, _VP]),
+    "fastvr_q4_attn_fwd": (_I32, [_VP] * 6),
+    "fastvr_q4_read": (_I32, [_VP, _I64, _VP, _VP, _VP]),
 }
 
 
@@ -317,6 +373,95 @@ def fastvr_plan_destroy(plan: int) -> None:
     lib.fastvr_plan_destroy(plan)
 
 
+def fastvr_rotary_frequencies(cfg: fastvr_rotary_config_t):
+    """The rotary_dim / 2 angles per position (radians) in pair order, and
+    the magnitude."""
+    theta = (ctypes.c_double * max(1, cfg.rotary_dim // 2))()
+    mag = ctypes.c_double(0)
+    _check(lib.fastvr_rotary_frequencies(ctypes.byref(cfg), theta,
+                                         ctypes.byref(mag)),
+           "fastvr_rotary_frequencies")
+    return list(theta), mag.value
+
+
+def fastvr_rotary(cfg, batch, tokens, heads, kv_heads, dtype, q, q_str, k,
+                  k_str, positions, pos_batch, q_out, q_out_str, k_out,
+                  k_out_str, transpose, stream) -> None:
+    """Strides are fastvr_strides_t or None (contiguous)."""
+    _check(lib.fastvr_rotary(cfg, batch, tokens, heads, kv_heads, dtype, q,
+                             q_str, k, k_str, positions, pos_batch, q_out,
+                             q_out_str, k_out, k_out_str, transpose, stream),
+           "fastvr_rotary")
+
+
+def fastvr_gated_norm_fwd(cfg, x, y, gate, scale, shift, pre_weight,
+                          post_weight, r, h, stream) -> None:
+    _check(lib.fastvr_gated_norm_fwd(cfg, x, y, gate, scale, shift,
+                                     pre_weight, post_weight, r, h, stream),
+           "fastvr_gated_norm_fwd")
+
+
+def fastvr_gated_norm_bwd_scratch_bytes(cfg: fastvr_norm_config_t) -> int:
+    n = _SZ(0)
+    _check(lib.fastvr_gated_norm_bwd_scratch_bytes(cfg, ctypes.byref(n)),
+           "fastvr_gated_norm_bwd_scratch_bytes")
+    return n.value
+
+
+def fastvr_gated_norm_bwd(cfg, dr, dh, r, y, gate, scale, pre_weight,
+                          post_weight, dx, dy, dgate, dscale, dshift,
+                          dpre_weight, dpost_weight, scratch, scratch_bytes,
+                          stream) -> None:
+    _check(lib.fastvr_gated_norm_bwd(
+        cfg, dr, dh, r, y, gate, scale, pre_weight, post_weight, dx, dy,
+        dgate, dscale, dshift, dpre_weight, dpost_weight, scratch,
+        scratch_bytes, stream), "fastvr_gated_norm_bwd")
+
+
+def fastvr_q4_cache_bytes(cfg: fastvr_attn_config_t, kv_heads: int) -> int:
+    n = _SZ(0)
+    _check(lib.fastvr_q4_cache_bytes(ctypes.byref(cfg), kv_heads,
+                                     ctypes.byref(n)), "fastvr_q4_cache_bytes")
+    return n.value
+
+
+def fastvr_q4_workspace_bytes(cfg: fastvr_attn_config_t,
+                              kv_heads: int) -> int:
+    n = _SZ(0)
+    _check(lib.fastvr_q4_workspace_bytes(ctypes.byref(cfg), kv_heads,
+                                         ctypes.byref(n)),
+           "fastvr_q4_workspace_bytes")
+    return n.value
+
+
+def fastvr_q4_plan(cfg: fastvr_attn_config_t, kv_heads: int, cache: int,
+                   cache_bytes: int, workspace: int,
+                   workspace_bytes: int) -> int:
+    plan = _VP()
+    _check(lib.fastvr_q4_plan(ctypes.byref(cfg), kv_heads, cache, cache_bytes,
+                              workspace, workspace_bytes, ctypes.byref(plan)),
+           "fastvr_q4_plan")
+    return plan.value
+
+
+def fastvr_q4_append(plan: int, k: int, k_str, v: int, v_str, frames: int,
+                     stream: int) -> None:
+    """Strides are fastvr_strides_t or None (contiguous)."""
+    _check(lib.fastvr_q4_append(plan, k, k_str, v, v_str, frames, stream),
+           "fastvr_q4_append")
+
+
+def fastvr_q4_attn_fwd(plan: int, q: int, first_chunk: int, out: int,
+                       lse: int, stream: int) -> None:
+    _check(lib.fastvr_q4_attn_fwd(plan, q, first_chunk, out, lse, stream),
+           "fastvr_q4_attn_fwd")
+
+
+def fastvr_q4_read(plan: int, chunk: int, k: int, v: int,
+                   stream: int) -> None:
+    _check(lib.fastvr_q4_read(plan, chunk, k, v, stream), "fastvr_q4_read")
+
+
 def make_config(batch: int, heads: int, head_dim: int, tokens_per_frame: int,
                 frames_per_chunk: int, window_chunks: int = -1,
                 max_chunks: int = 0, softmax_scale: float = 0.0
@@ -382,6 +527,346 @@ class StreamingAttention:
                               0 if lse is None else lse.data_ptr(),
                               self._stream())
         return (out, lse) if want_lse or lse is not None else out
+
+    def reset(self) -> None:
+        fastvr_plan_reset(self.plan)
+
+    def launch_count(self) -> int:
+        return fastvr_plan_launch_count(self.plan)
+
+    def status(self) -> int:
+        return fastvr_get_status(self.plan)
+
+    def visible(self):
+        return fastvr_plan_visible(self.plan)
+
+    def state(self) -> Tuple[int, int]:
+        return fastvr_plan_get_state(self.plan)
+
+    def set_state(self, chunks: int, last_frames: int) -> None:
+        fastvr_plan_set_state(self.plan, chunks, last_frames)
+
+
+# ------------------------------------------- operators around the attention
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return FASTVR_BF16
+    if t.dtype == torch.float32:
+        return FASTVR_F32
+    raise ValueError("tensors must be bfloat16 or float32")
+
+
+def _head_strides(t, name: str):
+    """fastvr_strides_t of a [B, L, H, d] tensor whose heads are contiguous,
+    None when the whole tensor is."""
+    if not t.is_cuda or t.dim() != 4:
+        raise ValueError(f"{name} must be a CUDA tensor [B, L, H, d]")
+    if t.is_contiguous():
+        return None
+    b, l, h, e = t.stride()
+    if e != 1:
+        raise ValueError(f"the elements of a head of {name} must be contiguous")
+    return fastvr_strides_t(b, l, h)
+
+
+def make_rotary_config(head_dim: int, rotary_dim: Optional[int] = None,
+                       layout: str = "interleaved", sections=None,
+                       base: float = 10000.0, scaling: str = "none",
+                       factors=None, original_contexts=None,
+                       beta_fast: float = 32.0, beta_slow: float = 1.0,
+                       magnitude: float = 0.0) -> fastvr_rotary_config_t:
+    """Rotary positions of heads of head_dim elements, the first rotary_dim
+    of them rotated.  sections: pairs per axis (default: one axis); factors
+    and original_contexts: per axis, for the scalings that use them."""
+    rot = head_dim if rotary_dim is None else rotary_dim
+    sections = [rot // 2] if sections is None else list(sections)
+    n = len(sections)
+    if n > 3:
+        raise ValueError("at most three axes")
+    three = lambda v, fill: (list(v) if v is not None else [fill] * n) + \
+        [fill] * (3 - n)
+    return fastvr_rotary_config_t(
+        head_dim, rot, ROTARY_LAYOUTS[layout], n,
+        (ctypes.c_int32 * 3)(*three(sections, 0)), ROTARY_SCALINGS[scaling],
+        base, (ctypes.c_double * 3)(*three(factors, 1.0)),
+        (ctypes.c_double * 3)(*three(original_contexts, 0.0)), beta_fast,
+        beta_slow, magnitude)
+
+
+def rotary(cfg: fastvr_rotary_config_t, q, k, positions, out=None,
+           transpose: bool = False):
+    """Torch convenience for fastvr_rotary: q [B, L, H, d] and k [B, L, Hkv,
+    d] (or None), bfloat16 or float32, heads contiguous, any other strides
+    (slices of a fused projection); positions int32 [L, axes] or [B or 1, L,
+    axes].  Returns (q', k'), contiguous unless `out` gives the two outputs
+    (out=(q, k) works in place)."""
+    import torch
+    code = _dtype_code(q)
+    q_str = _head_strides(q, "q")
+    B, L, H, d = q.shape
+    Hk, k_str = 0, None
+    if d != cfg.head_dim:
+        raise ValueError(f"q has shape {tuple(q.shape)}")
+    if k is not None:
+        k_str = _head_strides(k, "k")
+        Hk = k.shape[2]
+        if k.shape != (B, L, Hk, d) or k.dtype != q.dtype:
+            raise ValueError("q and k differ in type or shape")
+    if positions.dtype != torch.int32 or not positions.is_cuda or \
+            not positions.is_contiguous():
+        raise ValueError("positions must be a contiguous int32 CUDA tensor")
+    if positions.dim() == 2:
+        rows = 1
+    else:
+        rows = positions.shape[0] if positions.dim() == 3 else -1
+    if positions.shape[-2:] != (L, cfg.axes) or rows not in (1, B):
+        raise ValueError(f"positions have shape {tuple(positions.shape)}")
+    if out is None:
+        q_out = torch.empty((B, L, H, d), dtype=q.dtype, device=q.device)
+        k_out = None if k is None else torch.empty(
+            (B, L, Hk, d), dtype=q.dtype, device=q.device)
+        q_out_str = k_out_str = None
+    else:
+        q_out, k_out = out
+        for o, i in ((q_out, q), (k_out, k)):
+            if (o is None) != (i is None) or o is not None and \
+                    (o.shape != i.shape or o.dtype != i.dtype):
+                raise ValueError("outputs differ from the inputs")
+        q_out_str = _head_strides(q_out, "the output for q")
+        k_out_str = None if k is None else _head_strides(
+            k_out, "the output for k")
+    fastvr_rotary(cfg, B, L, H, Hk, code, q.data_ptr(), q_str,
+                  0 if k is None else k.data_ptr(), k_str,
+                  positions.data_ptr(), L * cfg.axes if rows > 1 else 0,
+                  q_out.data_ptr(), q_out_str,
+                  0 if k is None else k_out.data_ptr(), k_out_str,
+                  int(transpose), torch.cuda.current_stream().cuda_stream)
+    return q_out, k_out
+
+
+def rotary_bwd(cfg: fastvr_rotary_config_t, dq, dk, positions, out=None):
+    """Gradients of rotary's inputs from those of its outputs."""
+    return rotary(cfg, dq, dk, positions, out, transpose=True)
+
+
+def make_norm_config(pre: str = "rms", post: str = "none", eps: float = 1e-6,
+                     residual_scale: float = 1.0) -> fastvr_norm_config_t:
+    """The norms of gated_norm; the shapes are taken from its tensors."""
+    return fastvr_norm_config_t(0, 0, 0, 0, NORMS[pre], NORMS[post], 0, 0,
+                                eps, residual_scale)
+
+
+def _norm_call(cfg, x, y, mods, weights):
+    """cfg for the tensors of a call, after their checks."""
+    import torch
+    if x.dim() != 3 or not x.is_cuda or not x.is_contiguous():
+        raise ValueError("x must be a contiguous CUDA tensor [B, L, D]")
+    B, L, D = x.shape
+    block = torch.bfloat16
+    for t in y:
+        if t is None:
+            continue
+        if t.shape != x.shape or not t.is_cuda or not t.is_contiguous():
+            raise ValueError("block tensors must be contiguous and of x's shape")
+        block = t.dtype
+    groups = 1
+    for t in mods:
+        if t is None:
+            continue
+        if t.dtype != torch.float32 or not t.is_cuda or \
+                not t.is_contiguous() or t.dim() != 3 or \
+                t.shape[0] != B or t.shape[2] != D:
+            raise ValueError("gate, scale and shift must be contiguous float32 "
+                             "CUDA tensors [B, G, D]")
+        groups = t.shape[1]
+    for t in mods:
+        if t is not None and t.shape[1] != groups:
+            raise ValueError("gate, scale and shift differ in groups")
+    for t in weights:
+        if t is not None and (t.dtype != torch.float32 or not t.is_cuda or
+                              t.shape != (D,) or not t.is_contiguous()):
+            raise ValueError("weights must be contiguous float32 CUDA "
+                             "tensors [D]")
+    code = {torch.bfloat16: FASTVR_BF16, torch.float32: FASTVR_F32}
+    if x.dtype not in code or block not in code:
+        raise ValueError("tensors must be bfloat16 or float32")
+    return fastvr_norm_config_t(B, L, D, groups, cfg.pre, cfg.post,
+                                code[x.dtype], code[block], cfg.eps,
+                                cfg.residual_scale)
+
+
+def _ptr(t) -> int:
+    return 0 if t is None else t.data_ptr()
+
+
+def gated_norm(cfg: fastvr_norm_config_t, x, y, gate=None, scale=None,
+               shift=None, pre_weight=None, post_weight=None, block_dtype=None,
+               want_r: bool = True, want_h: bool = True):
+    """Torch convenience for fastvr_gated_norm_fwd: x [B, L, D] (bfloat16 or
+    float32) and y the same shape (or None: no block output), gate, scale and
+    shift float32 [B, G, D], weights float32 [D].  Returns (r, h), None for
+    the one not wanted; h has y's type (block_dtype without y)."""
+    import torch
+    c = _norm_call(cfg, x, (y,), (gate, scale, shift),
+                   (pre_weight, post_weight))
+    block = (block_dtype or torch.bfloat16) if y is None else y.dtype
+    if y is None:
+        c.block_dtype = FASTVR_F32 if block == torch.float32 else FASTVR_BF16
+    r = torch.empty_like(x) if want_r else None
+    h = torch.empty(x.shape, dtype=block, device=x.device) if want_h else None
+    fastvr_gated_norm_fwd(c, x.data_ptr(), _ptr(y), _ptr(gate), _ptr(scale),
+                          _ptr(shift), _ptr(pre_weight), _ptr(post_weight),
+                          _ptr(r), _ptr(h),
+                          torch.cuda.current_stream().cuda_stream)
+    return r, h
+
+
+class NormGrads(NamedTuple):
+    """Gradients of gated_norm; None where the forward had no such input."""
+    dx: object
+    dy: object
+    dgate: object
+    dscale: object
+    dshift: object
+    dpre_weight: object
+    dpost_weight: object
+
+
+def gated_norm_bwd(cfg: fastvr_norm_config_t, dr, dh, r, y, gate=None,
+                   scale=None, pre_weight=None, post_weight=None,
+                   want_dshift: Optional[bool] = None) -> NormGrads:
+    """Torch convenience for fastvr_gated_norm_bwd: dr, dh the gradients of r
+    and h (either may be None), r the forward's r.  dshift is formed when
+    scale is given, or as want_dshift says (the groups are then gate's or
+    scale's, or one)."""
+    import torch
+    if dr is not None and (dr.shape != r.shape or dr.dtype != r.dtype or
+                           not dr.is_contiguous()):
+        raise ValueError("dr must be contiguous and of r's type and shape")
+    c = _norm_call(cfg, r, (dh, y), (gate, scale), (pre_weight, post_weight))
+    if dh is not None and y is not None and dh.dtype != y.dtype:
+        raise ValueError("dh and y differ in type")
+    new = lambda *s: torch.empty(s, dtype=torch.float32, device=r.device)
+    like = lambda t: None if t is None else torch.empty_like(t)
+    B, L, D = r.shape
+    if want_dshift is None:
+        want_dshift = scale is not None
+    dshift = new(B, c.groups, D) if want_dshift else None
+    g = NormGrads(torch.empty_like(r), like(y),
+                  None if y is None else like(gate), like(scale), dshift,
+                  like(pre_weight), None if y is None else like(post_weight))
+    nbytes = fastvr_gated_norm_bwd_scratch_bytes(c)
+    scratch = new((nbytes + 3) // 4)
+    fastvr_gated_norm_bwd(c, _ptr(dr), _ptr(dh), r.data_ptr(), _ptr(y),
+                          _ptr(gate), _ptr(scale), _ptr(pre_weight),
+                          _ptr(post_weight), *(_ptr(t) for t in g),
+                          scratch.data_ptr(), nbytes,
+                          torch.cuda.current_stream().cuda_stream)
+    return g
+
+
+class StreamingAttention4:
+    """One video stream, or a batch of them, over a KV cache held in 4 bits.
+
+    append(k, v) takes bfloat16 CUDA tensors [B, f*N, kv_heads, d] (heads
+    contiguous, any other strides; f up to k, or several whole chunks at
+    once), forward(q) contiguous [B, f*N, heads, d]; both enqueue on the
+    current CUDA stream.  `workspace` (a uint8 CUDA tensor of at least
+    fastvr_q4_workspace_bytes) may be shared by streams whose calls do not
+    overlap on the GPU; by default one is allocated."""
+
+    def __init__(self, cfg: fastvr_attn_config_t,
+                 kv_heads: Optional[int] = None, device=None, workspace=None):
+        import torch
+        self.cfg = cfg
+        self.kv_heads = cfg.heads if kv_heads is None else kv_heads
+        device = device or "cuda"
+        self.nbytes = fastvr_q4_cache_bytes(cfg, self.kv_heads)
+        need = fastvr_q4_workspace_bytes(cfg, self.kv_heads)
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        self.workspace = workspace
+        self.cache = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        self.plan = fastvr_q4_plan(cfg, self.kv_heads, self.cache.data_ptr(),
+                                   self.nbytes, workspace.data_ptr(),
+                                   workspace.numel() *
+                                   workspace.element_size())
+
+    def __del__(self):
+        plan = getattr(self, "plan", None)
+        if plan:
+            fastvr_plan_destroy(plan)
+            self.plan = None
+
+    def append(self, k, v) -> None:
+        import torch
+        c = self.cfg
+        if k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+            raise ValueError("k and v must be bfloat16")
+        k_str, v_str = _head_strides(k, "k"), _head_strides(v, "v")
+        B, L, H, d = k.shape
+        if v.shape != k.shape:
+            raise ValueError("k and v differ in shape")
+        if (B, H, d) != (c.batch, self.kv_heads, c.head_dim) or \
+                L % c.tokens_per_frame:
+            raise ValueError(f"k has shape {tuple(k.shape)}")
+        fastvr_q4_append(self.plan, k.data_ptr(), k_str, v.data_ptr(), v_str,
+                         L // c.tokens_per_frame,
+                         torch.cuda.current_stream().cuda_stream)
+
+    def forward(self, q, first_chunk=None, out=None, lse=None,
+                want_lse: bool = False):
+        """Attention of the newest chunk's queries; first_chunk, int32 [B]:
+        the first chunk that each batch entry sees."""
+        import torch
+        c = self.cfg
+        if q.dtype != torch.bfloat16 or not q.is_cuda or \
+                not q.is_contiguous() or q.dim() != 4:
+            raise ValueError("q must be a contiguous bfloat16 CUDA tensor "
+                             "[B, L, H, d]")
+        B, L, H, d = q.shape
+        _, frames = self.state()
+        if (B, H, d) != (c.batch, c.heads, c.head_dim) or \
+                frames and L != frames * c.tokens_per_frame:
+            raise ValueError(f"q has shape {tuple(q.shape)}")
+        if first_chunk is not None and (
+                first_chunk.dtype != torch.int32 or not first_chunk.is_cuda or
+                first_chunk.shape != (B,) or not first_chunk.is_contiguous()):
+            raise ValueError("first_chunk must be a contiguous int32 CUDA "
+                             "tensor [B]")
+        if out is None:
+            out = torch.empty_like(q)
+        elif out.shape != q.shape or out.dtype != q.dtype or \
+                not out.is_contiguous():
+            raise ValueError("out must be contiguous and like q")
+        if lse is None and want_lse:
+            lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device)
+        elif lse is not None and (lse.shape != (B, H, L) or
+                                  lse.dtype != torch.float32 or
+                                  not lse.is_contiguous()):
+            raise ValueError("lse must be contiguous float32 [B, H, L]")
+        fastvr_q4_attn_fwd(self.plan, q.data_ptr(), _ptr(first_chunk),
+                           out.data_ptr(), _ptr(lse),
+                           torch.cuda.current_stream().cuda_stream)
+        return (out, lse) if lse is not None else out
+
+    def read(self, chunk: Optional[int] = None):
+        """(k, v) bfloat16 [B, f*N, kv_heads, d]: the values held for a chunk
+        (default: the newest)."""
+        import torch
+        c = self.cfg
+        chunks, frames = self.state()
+        chunk = chunks - 1 if chunk is None else chunk
+        if chunk != chunks - 1:
+            frames = c.frames_per_chunk
+        shape = (c.batch, frames * c.tokens_per_frame, self.kv_heads,
+                 c.head_dim)
+        k, v = (torch.empty(shape, dtype=torch.bfloat16,
+                            device=self.cache.device) for _ in range(2))
+        fastvr_q4_read(self.plan, chunk, k.data_ptr(), v.data_ptr(),
+                       torch.cuda.current_stream().cuda_stream)
+        return k, v
 
     def reset(self) -> None:
         fastvr_plan_reset(self.plan)
