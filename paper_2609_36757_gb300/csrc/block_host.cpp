@@ -173,6 +173,10 @@ fastvr_status_t q4_layout(const fastvr_attn_config_t* c, int32_t kv_heads,
   l->scales = round256((size_t)values / 32 * 2);
   l->cache = 2 * l->codes + 2 * l->scales + kQ4ControlBytes;
   l->workspace = round256(fastvr::q4_partial_bytes(c->head_dim));
+  if (rows > fastvr::kQ4DirectRows)
+    l->workspace =
+        std::max(l->workspace, 2 * round256((size_t)values * 2) +
+                                   fastvr::workspace_bytes(c->head_dim));
   return FASTVR_OK;
 }
 
@@ -202,6 +206,64 @@ void fill_read(const fastvr_plan_s* p, fastvr::Q4ReadParams* r) {
   r->code_words = (int64_t)p->cfg.batch * p->kv_heads * p->cache_tokens *
                   p->cfg.head_dim / 8;
   r->status = fastvr::control_word(p);
+}
+
+// The visible keys and values in bfloat16 into the workspace, oldest first,
+// then the tile kernel over them.
+cudaError_t attend_expanded(fastvr_plan_s* p, const fastvr::Q4AttnParams& d,
+                            cudaStream_t stream) {
+  fastvr::Q4ReadParams r;
+  fill_read(p, &r);
+  const int hd = d.head_dim;
+  const size_t region =
+      round256((size_t)r.batch * r.heads * p->cache_tokens * hd * 2);
+  r.k_out = reinterpret_cast<uint16_t*>(p->workspace);
+  r.v_out = reinterpret_cast<uint16_t*>(p->workspace + region);
+  r.tokens = (int32_t)d.keys;
+  r.out_str.token = hd;
+  r.out_str.head = d.keys * hd;
+  r.out_str.batch = r.heads * r.out_str.head;
+  r.first_row = d.first_row;
+  r.first_chunk = d.first_chunk;
+  r.lo_chunk = d.lo_chunk;
+  r.chunk_tokens = d.chunk_tokens;
+  cudaError_t e =
+      fastvr::launch_q4_read(r, true, fastvr::device_sms(), stream);
+  if (e != cudaSuccess) return e;
+  p->launches += 1;
+
+  fastvr::AttnParams a;
+  memset(&a, 0, sizeof(a));
+  a.q = d.q;
+  a.o = d.out;
+  a.lse = d.lse;
+  a.k = r.k_out;
+  a.v = r.v_out;
+  a.batch = r.batch;
+  a.heads = d.heads;
+  a.head_dim = hd;
+  a.q_tokens = d.q_tokens;
+  a.q_str.head = hd;
+  a.q_str.token = (int64_t)d.heads * hd;
+  a.q_str.batch = (int64_t)d.q_tokens * d.heads * hd;
+  a.kv_str = r.out_str;
+  a.kv_tokens = d.keys;
+  a.num_segments = 1;
+  a.seg_len[0] = (int32_t)d.keys;
+  a.scale_log2 = d.scale_log2;
+  a.status = fastvr::control_word(p);
+  a.workspace = reinterpret_cast<float*>(p->workspace + 2 * region);
+  a.workspace_parts = fastvr::kMaxParts;
+  a.wait_limit_ns = p->wait_limit_ns;
+  a.inject_stall = p->inject_stall;
+  a.kv_group = d.group;
+  a.first_chunk = d.first_chunk;
+  a.lo_chunk = d.lo_chunk;
+  a.chunk_tokens = (int32_t)d.chunk_tokens;
+  int launched = 0;
+  e = fastvr::launch_chunk_attn(a, stream, &launched);
+  p->launches += launched;
+  return e;
 }
 
 }  // namespace
@@ -523,6 +585,10 @@ fastvr_status_t fastvr_q4_attn_fwd(fastvr_plan_t p, const void* q,
   a.lo_chunk = lo;
   a.chunk_tokens = p->slot_tokens;
   a.scale_log2 = c.softmax_scale * 1.4426950408889634f;
+  if (a.rows > fastvr::kQ4DirectRows)
+    return attend_expanded(p, a, to_stream(stream)) == cudaSuccess
+               ? FASTVR_OK
+               : FASTVR_ERR_CUDA;
   if (fastvr::launch_q4_attn(a, fastvr::device_sms(), to_stream(stream)) !=
       cudaSuccess)
     return FASTVR_ERR_CUDA;

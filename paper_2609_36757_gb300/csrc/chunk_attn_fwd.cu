@@ -121,6 +121,11 @@ struct TcParams {
   // One-shot (training-form) launches: the whole sequence of seq_tokens
   // tokens, chunks of chunk_tokens tokens, window W (-1: unbounded).
   int32_t seq_tokens, chunk_tokens, window, batch;
+  int32_t kv_group;  // query heads that share a key head
+  // Late-start launches (kStart): the first chunk that each batch entry sees,
+  // the keys being one segment that starts with chunk lo_chunk.
+  const int32_t* first_chunk;
+  int64_t lo_chunk;
 };
 
 // The work of one CTA.
@@ -129,7 +134,8 @@ struct Work {
   int j0, n;   // first key tile (index into the visible tiles) and count
   int nqt;     // query tiles with at least one row in the chunk (1 or 2)
   int part;    // -1: whole unit, final output; else workspace slot
-  int kv0, kv1;  // one-shot: the unit's key token range [kv0, kv1)
+  int kv0, kv1;  // one-shot: the unit's key token range [kv0, kv1);
+                 // late start: kv0 is the first visible token
   bool rev;    // walk the key tiles last to first
 };
 
@@ -177,7 +183,9 @@ __device__ __forceinline__ Work oneshot_work(const TcParams& p) {
   return w;
 }
 
-template <bool kOneShot>
+// kStart: keys before the batch entry's first visible token are not read (nor
+// is any, when it sees none: n = 0); reads global memory.
+template <bool kOneShot, bool kStart>
 __device__ __forceinline__ Work cta_work(const TcParams& p) {
   if (kOneShot) return oneshot_work(p);
   Work w;
@@ -197,8 +205,16 @@ __device__ __forceinline__ Work cta_work(const TcParams& p) {
   w.b = unit / (p.q_pairs * p.heads);
   w.q0 = pair * kQTiles * kBM;
   w.nqt = (p.q_tokens - w.q0 > kBM) ? 2 : 1;
-  w.j0 = (int)((int64_t)idx * p.total_tiles / nparts);
-  w.n = (int)((int64_t)(idx + 1) * p.total_tiles / nparts) - w.j0;
+  int tiles = p.total_tiles, skip = 0;
+  if (kStart) {
+    w.kv0 = (int)first_visible_token(p.first_chunk[w.b], p.lo_chunk,
+                                     p.chunk_tokens, p.seg_len[0]);
+    skip = w.kv0 < p.seg_len[0] ? w.kv0 / kBN : tiles;
+    tiles -= skip;
+  }
+  w.j0 = (int)((int64_t)idx * tiles / nparts);
+  w.n = (int)((int64_t)(idx + 1) * tiles / nparts) - w.j0;
+  w.j0 += skip;
   w.part = part;
   w.rev = part < 0 && odd_wave(p);
   return w;
@@ -289,6 +305,7 @@ template <int D, bool kIsK, bool kOneShot>
 __device__ void producer(const TcParams& p, uint8_t* smem, Shared* S,
                          const Work& w) {
   const int h = w.h, b = w.b;
+  const int h_kv = p.kv_group == 1 ? h : h / p.kv_group;
   using L = Layout<D>;
   constexpr int kStages = kIsK ? kKStages : kVStages;
   uint64_t* full = kIsK ? S->k_full : S->v_full;
@@ -322,7 +339,7 @@ __device__ void producer(const TcParams& p, uint8_t* smem, Shared* S,
     for (int bx = 0; bx < L::kNB; ++bx)
       tma_load_4d_hint(kIsK ? &p.k_map[seg] : &p.v_map[seg],
                        smem + (kIsK ? L::k(st, bx) : L::v(st, bx)), &full[st],
-                       bx * 64, tok0, h, b, keep);
+                       bx * 64, tok0, h_kv, b, keep);
     ++issued;
   }
   // Every issued load has landed before the CTA may exit (a no-op wait in
@@ -603,11 +620,12 @@ __device__ __forceinline__ void mask_range_max32(uint32_t (&sc)[32], int c,
 // Streaming: j0, n index the launch's visible tiles.  One-shot: the tiles of
 // [kv0, kv1); a row of chunk c sees keys of chunks max(0, c - W) .. c, so a
 // row can be fully masked in a tile (its reference then stays at -inf).
+// Late start: keys before kv0 are masked; every tile has a visible key.
 // Per key tile: read S (shared by both query tiles) into registers and
 // release it at once, exponentiate, wait until the previous PV of this tile
 // has consumed P_t (and brought O_t up to date), rescale O_t if the
 // reference moved, then store P_t.
-template <int D, bool kOneShot>
+template <int D, bool kOneShot, bool kStart>
 __device__ void softmax_role(const TcParams& p, Shared* S, uint32_t tmem,
                              int t, int nqt, int wq, int lane, int j0, int n,
                              int kv0, int kv1, int q0, bool rev) {
@@ -656,6 +674,10 @@ __device__ void softmax_role(const TcParams& p, Shared* S, uint32_t tmem,
       const int hi = min(vis_hi - tok0, valid);
 #pragma unroll
       for (int c = 0; c < 4; ++c) mask_range_max32(s[c], c, lo, hi, mx);
+    } else if (kStart) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        mask_range_max32(s[c], c, kv0 - tok0, valid, mx);
     } else {
 #pragma unroll
       for (int c = 0; c < 4; ++c) mask_max32(s[c], c, valid, mx);
@@ -724,10 +746,11 @@ __device__ void softmax_role(const TcParams& p, Shared* S, uint32_t tmem,
     ++p_arrived;
   }
   const bool have = ok && wait_bar(&S->o_full, 0, S, p.status);
-  const Work w = cta_work<kOneShot>(p);
+  const Work w = cta_work<kOneShot, kStart>(p);
   const int r_unit = t * kBM + wq * 32 + lane;  // row within the unit
   const int row = w.q0 + r_unit;
   const float inv_l = 1.f / l;
+  const bool none = kStart && n == 0;  // sees no key: O = 0, LSE = -inf
   if (w.part >= 0) {
     // Partial result of a key range: O / l in fp32 (transposed, so a warp's
     // stores are contiguous) and the log2-domain log-sum-exp.
@@ -745,7 +768,8 @@ __device__ void softmax_role(const TcParams& p, Shared* S, uint32_t tmem,
         const int64_t x = (int64_t)w.part * D * kUnitRows +
                           (int64_t)(c * 32 + i) * kUnitRows + r_unit;
         if (in_bounds(x, (int64_t)p.ws_parts * D * kUnitRows, p.status))
-          ws_o[(c * 32 + i) * kUnitRows + r_unit] = __uint_as_float(r[i]) * inv_l;
+          ws_o[(c * 32 + i) * kUnitRows + r_unit] =
+              none ? 0.f : __uint_as_float(r[i]) * inv_l;
       }
     }
     if (in_bounds((int64_t)w.part * kUnitRows + r_unit,
@@ -772,8 +796,9 @@ __device__ void softmax_role(const TcParams& p, Shared* S, uint32_t tmem,
       uint32_t pk[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        pk[i] = pack_bf16(__uint_as_float(r[2 * i]) * inv_l,
-                          __uint_as_float(r[2 * i + 1]) * inv_l);
+        pk[i] = none ? 0u
+                     : pack_bf16(__uint_as_float(r[2 * i]) * inv_l,
+                                 __uint_as_float(r[2 * i + 1]) * inv_l);
       uint8_t* line = tile + (c / 2) * kBox + rt * 128;
 #pragma unroll
       for (int q = 0; q < 4; ++q)
@@ -870,7 +895,7 @@ combine_kernel(const __grid_constant__ TcParams p) {
       for (int x = 0; x < kCols; ++x) acc[x] = fmaf(wi, v[u][x], acc[x]);
     }
   }
-  const float inv = 1.f / wsum;
+  const float inv = wsum == 0.f ? 0.f : 1.f / wsum;  // 0: no visible key
 #pragma unroll
   for (int x = 0; x < kCols; x += 2)
     *reinterpret_cast<uint32_t*>(&tile[r][g * kCols + x]) =
@@ -895,7 +920,7 @@ combine_kernel(const __grid_constant__ TcParams p) {
   }
 }
 
-template <int D, bool kOneShot>
+template <int D, bool kOneShot, bool kStart = false>
 __global__ void __launch_bounds__(kThreads, 1)
 chunk_attn_tc_kernel(const __grid_constant__ TcParams p) {
   using L = Layout<D>;
@@ -905,7 +930,8 @@ chunk_attn_tc_kernel(const __grid_constant__ TcParams p) {
   Shared* S = reinterpret_cast<Shared*>(smem + L::shared_off);
   const int warp = threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
-  const Work w = cta_work<kOneShot>(p);
+  Work w;
+  if (!kStart) w = cta_work<kOneShot, false>(p);
 
   if (warp == 9) {
     tmem_alloc(&S->tmem_base, kTmemCols);
@@ -939,6 +965,7 @@ chunk_attn_tc_kernel(const __grid_constant__ TcParams p) {
   // belong to the previous kernel on the stream until it has completed.
   pdl_trigger();
   pdl_wait();
+  if (kStart) w = cta_work<kOneShot, kStart>(p);
 
   if (warp == 8) {
     if (lane == 0) producer<D, true, kOneShot>(p, smem, S, w);
@@ -953,8 +980,9 @@ chunk_attn_tc_kernel(const __grid_constant__ TcParams p) {
   } else {
     // A query tile that lies past the end of the chunk has no work.
     if (warp / 4 < w.nqt)
-      softmax_role<D, kOneShot>(p, S, tmem, warp / 4, w.nqt, warp % 4, lane,
-                                w.j0, w.n, w.kv0, w.kv1, w.q0, w.rev);
+      softmax_role<D, kOneShot, kStart>(p, S, tmem, warp / 4, w.nqt, warp % 4,
+                                        lane, w.j0, w.n, w.kv0, w.kv1, w.q0,
+                                        w.rev);
   }
   tc_fence_before();
   __syncthreads();
@@ -1029,14 +1057,16 @@ cudaError_t launch_d(const AttnParams& a, cudaStream_t stream, int* launches) {
       !make_map(&p.o_map, a.o, D, a.q_tokens, a.heads, a.batch,
                 a.q_str.token * es, a.q_str.head * es, a.q_str.batch * es))
     return cudaErrorInvalidValue;
+  p.kv_group = std::max(1, a.kv_group);
+  const int kv_heads = a.heads / p.kv_group;
   int tiles = 0;
   for (int s = 0; s < kMaxSegments; ++s) {
     const int src = s < a.num_segments ? s : 0;
     // The map ends where the segment ends: keys past it read as zeros.
     const int64_t end = a.seg_start[src] + a.seg_len[src];
-    if (!make_map(&p.k_map[s], a.k, D, end, a.heads, a.batch,
+    if (!make_map(&p.k_map[s], a.k, D, end, kv_heads, a.batch,
                   a.kv_str.token * es, a.kv_str.head * es, a.kv_str.batch * es) ||
-        !make_map(&p.v_map[s], a.v, D, end, a.heads, a.batch,
+        !make_map(&p.v_map[s], a.v, D, end, kv_heads, a.batch,
                   a.kv_str.token * es, a.kv_str.head * es, a.kv_str.batch * es))
       return cudaErrorInvalidValue;
     p.seg_start[s] = (int32_t)a.seg_start[src];
@@ -1067,13 +1097,17 @@ cudaError_t launch_d(const AttnParams& a, cudaStream_t stream, int* launches) {
               &p.split);
   p.ws_lse = p.ws + (size_t)a.workspace_parts * D * kUnitRows;
   const int grid = p.units_full + (units - p.units_full) * p.split;
+  p.first_chunk = a.first_chunk;
+  p.lo_chunk = a.lo_chunk;
+  p.chunk_tokens = a.chunk_tokens;
+  auto kernel = a.first_chunk == nullptr
+                    ? chunk_attn_tc_kernel<D, false, false>
+                    : chunk_attn_tc_kernel<D, false, true>;
   const int smem = Layout<D>::bytes;
   cudaError_t e = cudaFuncSetAttribute(
-      chunk_attn_tc_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-      smem);
+      kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(chunk_attn_tc_kernel<D, false>, dim3(grid), dim3(kThreads),
-                 smem, stream, p);
+  e = launch_pdl(kernel, dim3(grid), dim3(kThreads), smem, stream, p);
   if (e != cudaSuccess) return e;
   *launches = 1;
   if (p.split > 1) {
@@ -1122,6 +1156,7 @@ cudaError_t launch_oneshot_d(const OneShotParams& a, cudaStream_t stream) {
   p.seq_tokens = a.seq_tokens;
   p.chunk_tokens = a.chunk_tokens;
   p.window = a.window;
+  p.kv_group = 1;
   p.q_pairs = (a.seq_tokens + kQTiles * kBM - 1) / (kQTiles * kBM);
   p.split = 1;
   p.sms = sm_count();

@@ -132,6 +132,12 @@ struct AttnParams {
   int32_t workspace_parts;
   uint64_t wait_limit_ns; // bound of every in-kernel wait (0 = default)
   int32_t inject_stall;   // test hook: stall the MMA issuer until timeout
+  int32_t kv_group;       // query heads that share a key head (0: 1)
+  // Null, or the first chunk that each batch entry sees; the keys are then
+  // one segment whose first token is that of chunk lo_chunk.
+  const int32_t* first_chunk;
+  int64_t lo_chunk;
+  int32_t chunk_tokens;
 };
 
 cudaError_t launch_kv_append(const AppendParams& p, cudaStream_t stream);
@@ -268,7 +274,11 @@ struct Q4ReadParams {
 cudaError_t launch_q4_read(const Q4ReadParams& p, bool head_major, int sms,
                            cudaStream_t stream);
 
-// Few query rows straight over the codes.
+// Calls with at most kQ4DirectRows query rows (tokens times query heads per
+// key head) go straight over the codes (q4_attn.cu); longer ones write the
+// visible keys and values in bfloat16 to the workspace and run the tile
+// kernel over them.
+constexpr int kQ4DirectRows = 128;
 constexpr int kQ4MaxParts = 1024;  // partial results of split key ranges
 constexpr int kQ4MaxSplits = 512;
 constexpr int kQ4PartRows = 32;    // rows of the largest row block
