@@ -91,6 +91,30 @@ void rotary_frequencies(const fastvr_rotary_config_t& c, double* theta,
                                                   : 1.0;
 }
 
+// Turns per position and magnitude of a config.  A program calls with the
+// same config step after step and a decode step's host time counts, so each
+// host thread keeps what it computed for its last config (compared by value).
+struct RotaryTurns {
+  fastvr_rotary_config_t cfg;
+  bool valid = false;
+  float magnitude;
+  uint64_t turn[fastvr::kRotaryMaxPairs];
+};
+const RotaryTurns& rotary_turns(const fastvr_rotary_config_t& c) {
+  static thread_local RotaryTurns last;
+  if (!last.valid || memcmp(&last.cfg, &c, sizeof(c)) != 0) {
+    double theta[fastvr::kRotaryMaxPairs], magnitude;
+    rotary_frequencies(c, theta, &magnitude);
+    last.cfg = c;
+    last.valid = true;
+    last.magnitude = (float)magnitude;
+    // theta <= 1, so theta / 2 pi < 1 and the product fits 64 bits
+    for (int i = 0; i < c.rotary_dim / 2; ++i)
+      last.turn[i] = (uint64_t)(theta[i] / kTwoPi * 18446744073709551616.0);
+  }
+  return last;
+}
+
 // Strides in elements that keep every head 16-byte aligned.
 bool get_strides(const fastvr_strides_t* s, int64_t tokens, int64_t heads,
                  int64_t d, int elem_bytes, fastvr::Strides* out) {
@@ -133,7 +157,7 @@ struct BwdLayout {
 BwdLayout norm_bwd_layout(const fastvr_norm_config_t& c) {
   BwdLayout l;
   const int64_t groups = (int64_t)c.batch * c.groups;
-  l.split = fastvr::norm_bwd_split(groups, c.tokens / c.groups, kNormSms);
+  l.split = fastvr::norm_bwd_split(groups, c.tokens / c.groups, c.dim, kNormSms);
   l.partial = l.split.slices > 1
                   ? (size_t)l.split.ctas * 3 * c.dim * sizeof(float)
                   : 0;
@@ -143,7 +167,7 @@ BwdLayout norm_bwd_layout(const fastvr_norm_config_t& c) {
 
 // -------------------------------------------------------------- 4-bit cache
 constexpr size_t kQ4ControlBytes =
-    fastvr::kControlBytes + fastvr::kQ4MaxParts * sizeof(int);
+    fastvr::kControlBytes + fastvr::kQ4MaxCtas * sizeof(int);
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -173,7 +197,7 @@ fastvr_status_t q4_layout(const fastvr_attn_config_t* c, int32_t kv_heads,
   l->scales = round256((size_t)values / 32 * 2);
   l->cache = 2 * l->codes + 2 * l->scales + kQ4ControlBytes;
   l->workspace = round256(fastvr::q4_partial_bytes(c->head_dim));
-  if (rows > fastvr::kQ4DirectRows)
+  if (!fastvr::q4_direct(l->slot_tokens, c->heads / kv_heads))
     l->workspace =
         std::max(l->workspace, 2 * round256((size_t)values * 2) +
                                    fastvr::workspace_bytes(c->head_dim));
@@ -300,7 +324,6 @@ fastvr_status_t fastvr_rotary(
     return FASTVR_ERR_INVALID_ARG;
   const int es = dtype == FASTVR_F32 ? 4 : 2;
   fastvr::RotaryArgs a;
-  memset(&a, 0, sizeof(a));
   if (!get_strides(q_str, tokens, heads, cfg->head_dim, es, &a.q_str) ||
       !get_strides(q_out_str, tokens, heads, cfg->head_dim, es,
                    &a.q_out_str) ||
@@ -323,17 +346,15 @@ fastvr_status_t fastvr_rotary(
   a.head_dim = cfg->head_dim;
   a.pairs = cfg->rotary_dim / 2;
   a.axes = cfg->axes;
-  for (int i = 0; i < cfg->axes; ++i) a.section[i] = cfg->section[i];
+  for (int i = 0; i < FASTVR_ROTARY_MAX_AXES; ++i)
+    a.section[i] = i < cfg->axes ? cfg->section[i] : 0;
   a.f32 = dtype == FASTVR_F32;
   a.half = cfg->layout == FASTVR_ROTARY_HALF;
   a.transpose = transpose != 0;
   a.sms = fastvr::device_sms();
-  double theta[fastvr::kRotaryMaxPairs], magnitude;
-  rotary_frequencies(*cfg, theta, &magnitude);
-  a.magnitude = (float)magnitude;
-  // theta <= 1, so theta / 2 pi < 1 and the product fits 64 bits
-  for (int i = 0; i < a.pairs; ++i)
-    a.turn[i] = (uint64_t)(theta[i] / kTwoPi * 18446744073709551616.0);
+  const RotaryTurns& turns = rotary_turns(*cfg);
+  a.magnitude = turns.magnitude;
+  a.turn = turns.turn;
   return fastvr::launch_rotary(a, to_stream(stream)) == cudaSuccess
              ? FASTVR_OK
              : FASTVR_ERR_CUDA;
@@ -371,6 +392,7 @@ fastvr_status_t fastvr_gated_norm_fwd(
   p.residual_scale = cfg->residual_scale;
   return fastvr::launch_norm_fwd(p, cfg->residual_dtype == FASTVR_F32,
                                  cfg->block_dtype == FASTVR_F32,
+                                 fastvr::device_sms(),
                                  to_stream(stream)) == cudaSuccess
              ? FASTVR_OK
              : FASTVR_ERR_CUDA;
@@ -572,7 +594,7 @@ fastvr_status_t fastvr_q4_attn_fwd(fastvr_plan_t p, const void* q,
   a.first_chunk = first_chunk;
   a.partial = reinterpret_cast<float*>(p->workspace);
   a.tickets = fastvr::control_word(p) + fastvr::kControlBytes / sizeof(int);
-  a.batch_heads = c.batch * p->kv_heads;
+  a.batch = c.batch;
   a.heads = c.heads;
   a.kv_heads = p->kv_heads;
   a.head_dim = c.head_dim;
@@ -585,7 +607,7 @@ fastvr_status_t fastvr_q4_attn_fwd(fastvr_plan_t p, const void* q,
   a.lo_chunk = lo;
   a.chunk_tokens = p->slot_tokens;
   a.scale_log2 = c.softmax_scale * 1.4426950408889634f;
-  if (a.rows > fastvr::kQ4DirectRows)
+  if (!fastvr::q4_direct(a.q_tokens, a.group))
     return attend_expanded(p, a, to_stream(stream)) == cudaSuccess
                ? FASTVR_OK
                : FASTVR_ERR_CUDA;

@@ -205,7 +205,7 @@ struct RotaryArgs {
   bool f32, half, transpose;
   float magnitude;
   int sms;
-  uint64_t turn[kRotaryMaxPairs];  // theta / 2 pi modulo 1, in 2^-64 turns
+  const uint64_t* turn;  // pairs: theta / 2 pi in 2^-64 turns (host memory)
 };
 cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t stream);
 
@@ -220,14 +220,15 @@ struct NormFwdParams {
   float eps, residual_scale;
 };
 cudaError_t launch_norm_fwd(const NormFwdParams& p, bool res_f32,
-                            bool block_f32, cudaStream_t stream);
+                            bool block_f32, int sms, cudaStream_t stream);
 
 struct NormBwdSplit {
   int32_t slices;      // CTAs that share a group, or 1
   int64_t cta_groups;  // whole groups of a CTA when slices is 1
   int64_t ctas;
 };
-NormBwdSplit norm_bwd_split(int64_t all_groups, int64_t group_tokens, int sms);
+NormBwdSplit norm_bwd_split(int64_t all_groups, int64_t group_tokens, int dim,
+                            int sms);
 
 struct NormBwdParams {
   const void *dr, *dh, *r, *y;
@@ -274,14 +275,20 @@ struct Q4ReadParams {
 cudaError_t launch_q4_read(const Q4ReadParams& p, bool head_major, int sms,
                            cudaStream_t stream);
 
-// Calls with at most kQ4DirectRows query rows (tokens times query heads per
-// key head) go straight over the codes (q4_attn.cu); longer ones write the
-// visible keys and values in bfloat16 to the workspace and run the tile
-// kernel over them.
-constexpr int kQ4DirectRows = 128;
-constexpr int kQ4MaxParts = 1024;  // partial results of split key ranges
-constexpr int kQ4MaxSplits = 512;
-constexpr int kQ4PartRows = 32;    // rows of the largest row block
+// Whether a call goes straight over the codes (q4_attn.cu) or first writes the
+// visible keys and values in bfloat16 to the workspace and runs the tile
+// kernel over them.  Per key and key head the former takes about 0.17 ns for
+// every 32 query rows (tokens times query heads per key head), the latter 0.10
+// to expand and 0.12 for every query head and 256 tokens (measured on 12 heads
+// and 32768 keys, and on 8 streams of 32 over 8 heads and 8192 keys; the two
+// meet at 32 rows and at 112).
+inline bool q4_direct(int64_t q_tokens, int64_t group) {
+  const int64_t blocks = (q_tokens * group + 31) / 32;
+  return blocks * 17 < 10 + 12 * group * ((q_tokens + 255) / 256);
+}
+constexpr int kQ4MaxCtas = 512;               // of a launch
+constexpr int kQ4MaxParts = 2 * kQ4MaxCtas;   // partial results, two per CTA
+constexpr int kQ4PartRows = 32;               // rows of the largest row block
 inline size_t q4_partial_bytes(int head_dim) {
   return (size_t)kQ4MaxParts * kQ4PartRows * (head_dim + 2) * sizeof(float);
 }
@@ -292,15 +299,15 @@ struct Q4AttnParams {
   const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
   const int32_t* first_chunk;
   float* partial;  // kQ4MaxParts parts of kQ4PartRows rows of d + 2
-  int* tickets;    // kQ4MaxParts counters, zero between calls
-  int32_t batch_heads, heads, kv_heads, head_dim, q_tokens;
+  int* tickets;    // kQ4MaxCtas counters, zero between calls
+  int32_t batch, heads, kv_heads, head_dim, q_tokens;
   int32_t group;   // query heads per key head
   int32_t rows;    // q_tokens * group
   int64_t cache_tokens, first_row;  // first_row: oldest visible token's row
   int64_t keys;                     // visible tokens
   int64_t lo_chunk, chunk_tokens;
   float scale_log2;
-  int32_t row_blocks, splits;  // filled in by the launch
+  int32_t row_blocks;               // filled in by the launch
 };
 cudaError_t launch_q4_attn(const Q4AttnParams& p, int sms,
                            cudaStream_t stream);

@@ -13,9 +13,17 @@
 //   S^T[16 keys x 8 rows] = K[16 x d] Q^T     A: 16 keys of the cache
 //   O^T[d x 8 rows] += V^T[d x 16] P^T        A: the transposed V block
 //
-// A nibble y is placed in bits 3..6 of a bfloat16 with the exponent of 16
-// (one shift, one logic operation for two of them), which is 16 + y, and one
-// packed fused multiply-add gives (16 + y) s - 24 s = (y - 8) s, exact.
+// Expansion of K: a nibble y in the low bits of a half-precision float is the
+// subnormal y 2^-24 (16 y 2^-24 one nibble up), which the tensor cores take as
+// it is, so four logic operations and one shift expand eight codes and no
+// arithmetic is left: Q, scaled by a power of two per row, is exact in half
+// precision, the -8 of (y - 8) starts the accumulator as -8 sum q, and the
+// group's scale multiplies its partial dot product in 32 bits.
+//
+// Expansion of V, whose scales lie along the contraction: a nibble y in bits
+// 3..6 of a bfloat16 with the exponent of 16 is 16 + y (one shift and one
+// logic operation for two of them), and one packed fused multiply-add gives
+// (16 + y) s - 24 s = (y - 8) s, exact.
 //
 // The order of d inside a product is free as long as both operands share it.
 // Lane (g, c) of a K fragment holds words 4 i + c of key row g for all groups
@@ -34,6 +42,7 @@
 // are filled with zeros, scale included, so that whatever the cache holds
 // there cannot reach the result.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <math.h>
 
 #include <algorithm>
@@ -74,6 +83,14 @@ __device__ __forceinline__ void copy_commit() {
 template <int N>
 __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void mma_half(float (&c)[4], const uint32_t (&a)[4],
+                                         uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 "
+      "{%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4],
                                     uint32_t b0, uint32_t b1) {
@@ -132,402 +149,723 @@ __device__ __forceinline__ int v_offset(int r, int byte) {
   return r * Tile<D>::kRow + (D == 128 ? byte ^ ((r & 2) << 4) : byte);
 }
 
-// NT blocks of 8 query rows, W warps, kStages tiles in each warp's ring.
-template <int D, int NT, int W, int kStages>
-__global__ void __launch_bounds__(W * 32)
+// A unit is a block of query rows of one key head of one batch entry.  The
+// tiles of all units laid end to end (row blocks fastest, batch entries
+// slowest) are cut into even shares, one to a CTA, however different the
+// entries' lengths are.  Every unit counts kUnitCost tiles more than it has,
+// about what starting and ending it costs, so that a CTA with many short
+// units is not the last one; an entry that sees no key still has units, whose
+// zeros someone writes.
+constexpr int kUnitCost = 12;
+
+// A CTA's part of a unit.
+struct Piece {
+  bool more;           // there is one
+  int b, hk, rb;
+  int first, j0, j1;   // first visible key; tiles [j0, j1) of the unit
+  // The CTAs that share the unit are cta0 .. cta0 + parts - 1.  Each has two
+  // slots for partial results, 0 for the unit that its share begins in and 1
+  // for the one that it ends in.  cta0 uses slot0, the others 0, this CTA
+  // `mine`.  Of the units that begin in a CTA only the last one goes on in
+  // others, so that cta0's ticket counts the unit's parts.
+  int cta0, parts, slot0, mine;
+};
+
+template <int NT, int W, int kGroups>
+struct Shared {
+  float m[W][8 * NT], l[W][8 * NT];
+  float start[kGroups][8 * NT];  // first value of a dot product
+  uint4 q[NT > 1 ? NT : 1][NT > 1 ? kGroups : 1][32];
+  Piece piece[2];       // this one and the next
+  Piece shared[2];      // by slot: the units that other CTAs have parts of
+  int64_t total, at;    // counted tiles in all; the share's next one
+  int64_t before;       // counted tiles of the entries before b
+  int ctas, b;          // CTAs that have a share
+  int last[2];          // this CTA joins the parts of shared[i]
+};
+
+// a / b; in 32 bits, many times faster, where both fit
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+  return a / b;
+}
+
+__device__ __forceinline__ int first_key(const Q4AttnParams& p, int b) {
+  return p.first_chunk == nullptr
+             ? 0
+             : (int)first_visible_token(p.first_chunk[b], p.lo_chunk,
+                                        p.chunk_tokens, p.keys);
+}
+__device__ __forceinline__ int tiles_from(const Q4AttnParams& p, int first) {
+  return ((int)p.keys - first + kKeys - 1) / kKeys;
+}
+
+// Warp 0: the counted tiles of the launch and the entry that this CTA's share
+// begins in.
+template <class S>
+__device__ void find_share(const Q4AttnParams& p, S* sh) {
+  const int lane = threadIdx.x % 32;
+  const int units_b = p.kv_heads * p.row_blocks;  // units of a batch entry
+  auto counted = [&](int b) -> int64_t {
+    return b < p.batch
+               ? (int64_t)(tiles_from(p, first_key(p, b)) + kUnitCost) * units_b
+               : 0;
+  };
+  int64_t total = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    int64_t n = counted(b0 + lane);
+#pragma unroll
+    for (int y = 16; y > 0; y /= 2) n += __shfl_xor_sync(0xffffffffu, n, y);
+    total += n;
+  }
+  // no more CTAs than tiles: an empty share inside a unit would leave its
+  // ticket short of a part
+  const int ctas = (int)min((int64_t)gridDim.x, total);
+  const int64_t begin = divide(total * blockIdx.x, ctas);
+  int64_t before = 0;
+  int b = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 32) {
+    const int64_t n = counted(b0 + lane);
+    int64_t sum = n;  // inclusive
+#pragma unroll
+    for (int y = 1; y < 32; y *= 2) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, sum, y);
+      if (lane >= y) sum += v;
+    }
+    const uint32_t past = __ballot_sync(0xffffffffu, before + sum > begin);
+    if (past != 0) {
+      const int i = __ffs(past) - 1;
+      before += __shfl_sync(0xffffffffu, sum - n, i);
+      b = b0 + i;
+      break;
+    }
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (lane == 0) {
+    sh->total = total;
+    sh->ctas = ctas;
+    sh->at = begin;
+    sh->before = before;
+    sh->b = b;
+  }
+}
+
+// Thread 0: the share's next piece.
+template <class S>
+__device__ __noinline__ void next_piece(const Q4AttnParams& p, S* sh,
+                                        Piece* out) {
+  const int ctas = sh->ctas;
+  const int64_t total = sh->total, at = sh->at;
+  const int64_t begin = divide(total * blockIdx.x, ctas);
+  const int64_t end = divide(total * (blockIdx.x + 1), ctas);
+  out->more = (int)blockIdx.x < ctas && at < end;
+  if (!out->more) return;
+  const int units_b = p.kv_heads * p.row_blocks;
+  int b = sh->b;
+  int64_t before = sh->before;
+  int first = first_key(p, b);
+  int count = tiles_from(p, first) + kUnitCost;
+  while (at >= before + (int64_t)count * units_b) {
+    before += (int64_t)count * units_b;
+    ++b;
+    first = first_key(p, b);
+    count = tiles_from(p, first) + kUnitCost;
+  }
+  const int in_b = (int)divide(at - before, count);
+  const int64_t unit0 = before + (int64_t)in_b * count;
+  out->b = b;
+  out->rb = in_b % p.row_blocks;
+  out->hk = in_b / p.row_blocks;
+  out->first = first;
+  // the first kUnitCost counted tiles have no keys
+  out->j0 = max(0, (int)(at - unit0) - kUnitCost);
+  out->j1 = max(0, (int)min((int64_t)count, end - unit0) - kUnitCost);
+  const int cta0 = (int)divide((unit0 + 1) * ctas - 1, total);
+  out->cta0 = cta0;
+  out->parts = (int)divide((unit0 + count) * ctas - 1, total) - cta0 + 1;
+  out->slot0 = divide(total * cta0, ctas) == unit0 ? 0 : 1;
+  out->mine = at == begin ? 0 : 1;
+  sh->b = b;
+  sh->before = before;
+  sh->at = min(end, unit0 + count);
+}
+
+// Partial results: O (for its own m) [CTA][slot][row][D] and, behind all of
+// them, m and l [CTA][slot][row].
+template <int D>
+__device__ __forceinline__ float2* partial_ml(const Q4AttnParams& p) {
+  return reinterpret_cast<float2*>(p.partial +
+                                   (int64_t)kQ4MaxParts * kQ4PartRows * D);
+}
+
+// Four columns of a row of a unit, from the sums over all its keys.
+template <int D, int kRows>
+__device__ __forceinline__ void finish(const Q4AttnParams& p,
+                                       const Piece& piece, int row, int d,
+                                       float4 acc, float sum, float top) {
+  const int r = piece.rb * kRows + row;
+  const int tok = r / p.group, head = piece.hk * p.group + r % p.group;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key: zeros
+  *reinterpret_cast<uint2*>(
+      p.out +
+      (((int64_t)piece.b * p.q_tokens + tok) * p.heads + head) * D + d) =
+      make_uint2(pack(acc.x * inv, acc.y * inv),
+                 pack(acc.z * inv, acc.w * inv));
+  if (d == 0 && p.lse != nullptr)
+    p.lse[((int64_t)piece.b * p.heads + head) * p.q_tokens + tok] =
+        sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+}
+
+// The end of a piece: joins the warps' results (m and l in sh, O[row][d] for
+// its own m in each warp's part of `smem`) into the output, or into a partial
+// result when other CTAs have parts of the unit.
+template <int D, int NT, int W, int kWarpBytes, class S>
+__device__ __forceinline__ void end_piece(const Q4AttnParams& p, S* sh,
+                                          const uint8_t* smem,
+                                          const Piece& piece) {
+  constexpr int kRows = 8 * NT;
+  constexpr int kPitch = D + 4;
+  const int rows = min(kRows, p.rows - piece.rb * kRows);
+  const int part = ((int)blockIdx.x * 2 + piece.mine) * kRows;
+  // A thread takes 4 columns of a row.
+  constexpr int kSlots = D / 4;
+  const int slots = rows * kSlots;
+  for (int x = threadIdx.x; x < slots; x += W * 32) {
+    const int row = x / kSlots, d = x % kSlots * 4;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, sh->m[w][row]);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      // a warp without keys (m = -inf, l = 0) adds nothing
+      const float mw = sh->m[w][row], lw = sh->l[w][row];
+      const float f = mw == -INFINITY && lw == 0.f ? 0.f : ex2(mw - top);
+      const float4 v = *reinterpret_cast<const float4*>(
+          smem + w * kWarpBytes + (row * kPitch + d) * 4);
+      acc.x = fmaf(f, v.x, acc.x);
+      acc.y = fmaf(f, v.y, acc.y);
+      acc.z = fmaf(f, v.z, acc.z);
+      acc.w = fmaf(f, v.w, acc.w);
+      sum = fmaf(f, lw, sum);
+    }
+    if (piece.parts == 1) {
+      finish<D, kRows>(p, piece, row, d, acc, sum, top);
+    } else {
+      *reinterpret_cast<float4*>(p.partial + (int64_t)(part + row) * D + d) =
+          acc;
+      if (d == 0) partial_ml<D>(p)[part + row] = make_float2(top, sum);
+    }
+  }
+  if (threadIdx.x == 0 && piece.parts > 1) sh->shared[piece.mine] = piece;
+}
+
+// The last CTA of a unit to arrive joins its parts, in their order: the weight
+// of every (row, part) first, then sums of weighted rows with many loads in
+// flight.
+template <int D, int NT, int W, int kWarpBytes, class S>
+__device__ __forceinline__ void join_parts(const Q4AttnParams& p, S* sh,
+                                           uint8_t* smem, const Piece& piece) {
+  constexpr int kRows = 8 * NT;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int parts = piece.parts, cta0 = piece.cta0, slot0 = piece.slot0;
+  const int rows = min(kRows, p.rows - piece.rb * kRows);
+  auto slot_of = [&](int cta) {
+    return (cta * 2 + (cta == cta0 ? slot0 : 0)) * kRows;
+  };
+  const float2* all_ml = partial_ml<D>(p);
+  float* weight = reinterpret_cast<float*>(smem);  // [row][part]
+  for (int row = warp; row < rows; row += W) {
+    float* w = weight + row * parts;
+    float top = -INFINITY;
+    for (int i = lane; i < parts; i += 32) {
+      const float2 ml = __ldcg(all_ml + slot_of(cta0 + i) + row);
+      w[i] = ml.x;
+      top = fmaxf(top, ml.x);
+    }
+#pragma unroll
+    for (int y = 16; y > 0; y /= 2)
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
+    float sum = 0.f;
+    for (int i = lane; i < parts; i += 32) {
+      const float l = __ldcg(all_ml + slot_of(cta0 + i) + row).y;
+      // a part without keys has m = -inf and l = 0
+      const float f = w[i] == -INFINITY && l == 0.f ? 0.f : ex2(w[i] - top);
+      w[i] = f;
+      sum = fmaf(f, l, sum);
+    }
+#pragma unroll
+    for (int y = 16; y > 0; y /= 2)
+      sum += __shfl_xor_sync(0xffffffffu, sum, y);
+    if (lane == 0) {
+      sh->m[0][row] = top;
+      sh->l[0][row] = sum;
+    }
+  }
+  __syncthreads();
+  constexpr int kSlots = D / 4;
+  const int slots = rows * kSlots;
+  // With few rows the parts are shared out over `share` threads, whose sums
+  // are added in their order.
+  static_assert(kQ4MaxCtas * kRows * 4 + W * 32 * 16 <= W * kWarpBytes,
+                "weights and sums do not fit");
+  float4* sums = reinterpret_cast<float4*>(weight + kQ4MaxCtas * kRows);
+  const int share = max(1, W * 32 / slots);
+  const int who = share > 1 ? threadIdx.x / slots : 0;
+  for (int x0 = 0; x0 < slots; x0 += W * 32) {
+    const int x = x0 + threadIdx.x - who * slots;
+    const bool on = x < slots && who < share;
+    const int row = x / kSlots, d = x % kSlots * 4;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (on) {
+      const float* src = p.partial + row * D + d;
+      const float* w = weight + row * parts;
+      constexpr int kBatch = 8;
+      for (int i0 = who; i0 < parts; i0 += kBatch * share) {
+        float4 v[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          if (i0 + u * share < parts)
+            v[u] = __ldcg(reinterpret_cast<const float4*>(
+                src + slot_of(cta0 + i0 + u * share) * D));
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          if (i0 + u * share < parts) {
+            const float f = w[i0 + u * share];
+            acc.x = fmaf(f, v[u].x, acc.x);
+            acc.y = fmaf(f, v[u].y, acc.y);
+            acc.z = fmaf(f, v[u].z, acc.z);
+            acc.w = fmaf(f, v[u].w, acc.w);
+          }
+      }
+    }
+    if (share > 1) {
+      sums[threadIdx.x] = acc;
+      __syncthreads();
+      if (who == 0)
+        for (int i = 1; i < share; ++i) {
+          if (x >= slots) break;
+          const float4 v = sums[i * slots + x];
+          acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
+        }
+    }
+    if (on && who == 0)
+      finish<D, kRows>(p, piece, row, d, acc, sh->l[0][row], sh->m[0][row]);
+  }
+}
+
+// NT blocks of 8 query rows, W warps, kStages tiles in each warp's ring, kCtas
+// CTAs to an SM.
+template <int D, int NT, int W, int kStages, int kCtas>
+__global__ void __launch_bounds__(W * 32, kCtas)
 q4_attn_kernel(const __grid_constant__ Q4AttnParams p) {
   using L = Tile<D>;
   constexpr int kGroups = D / 32;
   constexpr int kWords = D / 64;  // V words (8 values) of a lane per token
-  constexpr int kRows = 8 * NT;
+  constexpr bool kQShared = NT > 1;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ float s_m[W][kRows], s_l[W][kRows];
-  __shared__ int s_last;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int g = lane / 4, c = lane % 4;
-  uint8_t* ring = smem + warp * kStages * L::bytes;
-  const uint32_t ring_u = smem_u32(ring);
-
-  // This CTA: key range `split` of row block rb of (b, kv head).
-  const int rb = blockIdx.x % p.row_blocks;
-  const int bh = blockIdx.x / p.row_blocks % p.batch_heads;
-  const int split = blockIdx.x / p.row_blocks / p.batch_heads;
-  const int b = bh / p.kv_heads, hk = bh % p.kv_heads;
+  __shared__ Shared<NT, W, kGroups> sh;
   pdl_trigger();
   pdl_wait();
+  if (threadIdx.x < 32) find_share(p, &sh);
+  if (threadIdx.x < 2) sh.shared[threadIdx.x].parts = 1;
+  if (threadIdx.x == 0) next_piece(p, &sh, &sh.piece[0]);
+  __syncthreads();
 
-  // Logical keys are counted from the oldest chunk of the window.
-  const int64_t first =
-      p.first_chunk == nullptr
-          ? 0
-          : first_visible_token(p.first_chunk[b], p.lo_chunk, p.chunk_tokens,
-                                p.keys);
-  const int64_t tiles = (p.keys - first + kKeys - 1) / kKeys;
-  const int64_t j0 = tiles * split / p.splits;
-  const int64_t j1 = tiles * (split + 1) / p.splits;
+  const int keys = (int)p.keys;
+  const uint32_t cache_tokens = (uint32_t)p.cache_tokens;
+  for (int k = 0;; k ^= 1) {
+    const Piece* piece = &sh.piece[k];
+    if (!piece->more) break;
+    // read anew for every unit: what follows from it is then not kept in
+    // registers across the end of the previous one
+    int tid;
+    asm volatile("mov.u32 %0, %%tid.x;" : "=r"(tid));
+    const int warp = tid / 32, lane = tid % 32;
+    const int g = lane / 4, c = lane % 4;
+    uint8_t* ring = smem + warp * kStages * L::bytes;
+    const uint32_t ring_u = smem_u32(ring);
+    const int b = piece->b, hk = piece->hk, rb = piece->rb;
+    const int first = piece->first, j0 = piece->j0, j1 = piece->j1;
+    // bytes of codes before this head's; its scales take an eighth as many
+    const int64_t head_at =
+        ((int64_t)b * p.kv_heads + hk) * p.cache_tokens * L::kRow;
+    static_assert(L::kRow == 8 * L::kScale, "");
 
-  const uint8_t* k_codes =
-      p.k_codes + (int64_t)bh * p.cache_tokens * L::kRow;
-  const uint8_t* v_codes =
-      p.v_codes + (int64_t)bh * p.cache_tokens * L::kRow;
-  const uint8_t* k_scales =
-      p.k_scales + (int64_t)bh * p.cache_tokens * L::kScale;
-  const uint8_t* v_scales =
-      p.v_scales + (int64_t)bh * p.cache_tokens * L::kScale;
-
-  // The key that this lane's row x of a tile holds in the cache.
-  auto cache_row = [&](int64_t key) {
-    int64_t r = p.first_row + key;
-    return r >= p.cache_tokens ? r - p.cache_tokens : r;
-  };
-  auto fetch = [&](int64_t j, int stage) {
-    if (j < j1) {
-      const int64_t key0 = first + j * kKeys;
-      const uint32_t dst = ring_u + stage * L::bytes;
-      constexpr int kPieces = L::kRow / 16;  // 16-byte pieces of a row
+    constexpr int kPieces = L::kRow / 16;  // 16-byte pieces of a row
+    // This lane's piece of every 32 / kPieces rows of a tile.
+    const uint32_t k_dst = ring_u + L::k + lane * 16;
+    const uint32_t v_dst =
+        ring_u + L::v + v_offset<D>(lane / kPieces, lane % kPieces * 16);
+    const uint32_t s_dst = ring_u + L::ks + lane * L::kScale;
+    auto fetch = [&](int j, int stage) {
+      if (j < j1) {
+        const int key0 = first + j * kKeys;
+        uint32_t row0 = (uint32_t)p.first_row + key0;  // both below 2^30
+        if (row0 >= cache_tokens) row0 -= cache_tokens;
+        const uint32_t to = stage * L::bytes;
+        if (key0 + kKeys <= keys && row0 + kKeys <= cache_tokens) {
+          // the usual tile: 32 rows in one piece
+          const int64_t at = head_at + (int64_t)row0 * L::kRow + lane * 16;
+          const uint8_t* kc = p.k_codes + at;
+          const uint8_t* vc = p.v_codes + at;
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int x = i * 32 + lane;
-        const int r = x / kPieces, piece = x % kPieces;
-        const bool ok = key0 + r < p.keys;
-        const int64_t at =
-            (ok ? cache_row(key0 + r) : 0) * L::kRow + piece * 16;
-        copy_async<16>(dst + L::k + r * L::kRow + piece * 16, k_codes + at, ok);
-        copy_async<16>(dst + L::v + v_offset<D>(r, piece * 16), v_codes + at,
-                       ok);
+          for (int i = 0; i < kPieces; ++i) {
+            copy_async<16>(k_dst + to + i * 512, kc + i * 512, true);
+            copy_async<16>(v_dst + to + i * 512, vc + i * 512, true);
+          }
+          const int64_t st =
+              head_at / 8 + (int64_t)(row0 + lane) * L::kScale;
+          copy_async<L::kScale>(s_dst + to, p.k_scales + st, true);
+          copy_async<L::kScale>(s_dst + to + L::vs - L::ks, p.v_scales + st,
+                                true);
+        } else {
+          auto cache_row = [&](int r) {
+            const uint32_t x = row0 + r;
+            return (int64_t)(x >= cache_tokens ? x - cache_tokens : x);
+          };
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) {
+            const int r = (i * 32 + lane) / kPieces;
+            const bool ok = key0 + r < keys;
+            const int64_t at = head_at + (ok ? cache_row(r) : 0) * L::kRow +
+                               lane % kPieces * 16;
+            copy_async<16>(k_dst + to + i * 512, p.k_codes + at, ok);
+            copy_async<16>(v_dst + to + i * 512, p.v_codes + at, ok);
+          }
+          const bool ok = key0 + lane < keys;
+          const int64_t st =
+              head_at / 8 + (ok ? cache_row(lane) : 0) * L::kScale;
+          copy_async<L::kScale>(s_dst + to, p.k_scales + st, ok);
+          copy_async<L::kScale>(s_dst + to + L::vs - L::ks, p.v_scales + st,
+                                ok);
+        }
       }
-      const bool ok = key0 + lane < p.keys;
-      const int64_t at = (ok ? cache_row(key0 + lane) : 0) * L::kScale;
-      copy_async<L::kScale>(dst + L::ks + lane * L::kScale, k_scales + at, ok);
-      copy_async<L::kScale>(dst + L::vs + lane * L::kScale, v_scales + at, ok);
+      copy_commit();
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) fetch(j0 + warp + s * W, s);
+
+    // Q^T fragments in half precision: for group i, element pairs (e, e + 4) of
+    // words 4 i + c, those of odd e divided by 16 (their codes lie one nibble
+    // up), all times the power of two that brings the row's largest magnitude
+    // to [2^15, 2^16) (of magnitudes up to 2^110).
+    // All warps need the same ones: with more than one block they stay in
+    // shared memory, which leaves their registers to the sums.
+    uint32_t qf[kQShared ? 1 : NT][kGroups][4];
+    float unit[NT][2];  // score of a dot product of 1, rows 2 c and 2 c + 1
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = (rb * NT + nt) * 8 + g;
+      const int tok = row / p.group, head = hk * p.group + row % p.group;
+      const uint16_t* q =
+          p.q + (((int64_t)b * p.q_tokens + tok) * p.heads + head) * D;
+      uint4 w[kGroups];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        w[i] = make_uint4(0, 0, 0, 0);
+        if (row < p.rows)
+          w[i] = *reinterpret_cast<const uint4*>(q + 32 * i + 8 * c);
+        const uint32_t m = 0x7fff7fffu;
+        top = __vmaxu2(top, __vmaxu2(__vmaxu2(w[i].x & m, w[i].y & m),
+                                     __vmaxu2(w[i].z & m, w[i].w & m)));
+      }
+      top = max(top >> 16, top & 0xffffu);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // exponent of the largest magnitude, kept where powers of two stay finite
+      const int e = min(max((int)(top >> 7) - 127, -110), 110);
+      const float up = __int_as_float((15 - e + 127) << 23);
+      // 2^24 of the subnormal codes, 2^(e - 15) of the row
+      const float mine = p.scale_log2 * __int_as_float((24 - 15 + e + 127) << 23);
+      unit[nt][0] = __shfl_sync(0xffffffffu, mine, 8 * c);
+      unit[nt][1] = __shfl_sync(0xffffffffu, mine, 8 * c + 4);
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        float f[8], sum = 0.f;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          f[2 * y] = __uint_as_float(x[y] << 16) * up;
+          f[2 * y + 1] = __uint_as_float(x[y] & 0xffff0000u) * up;
+          sum += f[2 * y] + f[2 * y + 1];
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float k = y % 2 ? 0.0625f : 1.f;
+          const __half2 h = __floats2half2_rn(f[y] * k, f[y + 4] * k);
+          qf[kQShared ? 0 : nt][i][y] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        if (kQShared && warp == 0)
+          sh.q[nt][i][lane] = make_uint4(qf[0][i][0], qf[0][i][1], qf[0][i][2],
+                                        qf[0][i][3]);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        if (warp == 0 && c == 0) sh.start[i][nt * 8 + g] = sum * (-8.f * 0x1p-24f);
+      }
     }
-    copy_commit();
-  };
-#pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) fetch(j0 + warp + s * W, s);
+    if (tid == 0) next_piece(p, &sh, &sh.piece[k ^ 1]);
+    __syncthreads();
 
-  // Q^T fragments: for group i, element pairs (e, e + 4) of words 4 i + c.
-  uint32_t qf[NT][kGroups][4];
+    float o[NT][D / 16][4];
+    float m[NT][2], l[NT][2];  // rows 2 c and 2 c + 1 of each block
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int row = (rb * NT + nt) * 8 + g;
-    const int tok = row / p.group, head = hk * p.group + row % p.group;
-    const uint16_t* q =
-        p.q + (((int64_t)b * p.q_tokens + tok) * p.heads + head) * D;
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-      uint4 w = make_uint4(0, 0, 0, 0);
-      if (row < p.rows)
-        w = *reinterpret_cast<const uint4*>(q + 32 * i + 8 * c);
-      qf[nt][i][0] = __byte_perm(w.x, w.z, 0x5410);
-      qf[nt][i][1] = __byte_perm(w.x, w.z, 0x7632);
-      qf[nt][i][2] = __byte_perm(w.y, w.w, 0x5410);
-      qf[nt][i][3] = __byte_perm(w.y, w.w, 0x7632);
+      for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
     }
-  }
 
-  float o[NT][D / 16][4];
-  float m[NT][2], l[NT][2];  // rows 2 c and 2 c + 1 of each block
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    m[nt][0] = m[nt][1] = -INFINITY;
-    l[nt][0] = l[nt][1] = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[nt][i][e] = 0.f;
-  }
+    int stage = 0;
+    const int kr = (g >> 1) + (g & 1) * 4;  // key of MMA row g
+    for (int j = j0 + warp; j < j1; j += W) {
+      copy_wait<kStages - 2>();
+      __syncwarp();
+      {
+        int ahead = stage + kStages - 1;
+        if (ahead >= kStages) ahead -= kStages;
+        fetch(j + (kStages - 1) * W, ahead);
+      }
+      const uint8_t* t = ring + stage * L::bytes;
+      if (++stage == kStages) stage = 0;
 
-  int stage = 0;
-  const int kr = (g >> 1) + (g & 1) * 4;  // key of MMA row g
-  for (int64_t j = j0 + warp; j < j1; j += W) {
-    copy_wait<kStages - 2>();
+      // S^T: two blocks of 16 keys, in units of `unit`
+      float s[NT][2][4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint32_t w[2][kGroups];
+        float sc[2][kGroups];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int r = x * 16 + y * 8 + kr;
+          if constexpr (D == 128) {
+            const uint4 v = *reinterpret_cast<const uint4*>(t + L::k +
+                                                            r * L::kRow + c * 16);
+            w[y][0] = v.x, w[y][1] = v.y, w[y][2] = v.z, w[y][3] = v.w;
+            const uint2 f =
+                *reinterpret_cast<const uint2*>(t + L::ks + r * L::kScale);
+            sc[y][0] = __uint_as_float(f.x << 16);
+            sc[y][1] = __uint_as_float(f.x & 0xffff0000u);
+            sc[y][2] = __uint_as_float(f.y << 16);
+            sc[y][3] = __uint_as_float(f.y & 0xffff0000u);
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(t + L::k +
+                                                            r * L::kRow + c * 8);
+            w[y][0] = v.x, w[y][1] = v.y;
+            const uint32_t f =
+                *reinterpret_cast<const uint32_t*>(t + L::ks + r * L::kScale);
+            sc[y][0] = __uint_as_float(f << 16);
+            sc[y][1] = __uint_as_float(f & 0xffff0000u);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+          const uint32_t lo = 0x000f000fu, hi = 0x00f000f0u;
+          const uint32_t u0 = w[0][i] >> 8, u1 = w[1][i] >> 8;
+          const uint32_t a0[4] = {w[0][i] & lo, w[1][i] & lo, w[0][i] & hi,
+                                  w[1][i] & hi};
+          const uint32_t a1[4] = {u0 & lo, u1 & lo, u0 & hi, u1 & hi};
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const float2 z =
+                *reinterpret_cast<const float2*>(&sh.start[i][nt * 8 + 2 * c]);
+            float d[4] = {z.x, z.y, z.x, z.y};
+            const uint32_t(&r)[4] = qf[kQShared ? 0 : nt][i];
+            const uint4 q = kQShared ? sh.q[kQShared ? nt : 0][i][lane]
+                                     : make_uint4(r[0], r[1], r[2], r[3]);
+            mma_half(d, a0, q.x, q.y);
+            mma_half(d, a1, q.z, q.w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              s[nt][x][e] = i == 0 ? d[e] * sc[e / 2][i]
+                                   : fmaf(d[e], sc[e / 2][i], s[nt][x][e]);
+          }
+        }
+      }
+
+      // Softmax over the tile's 32 keys; lane: keys x 16 + e/2 8 + kr of rows
+      // 2 c + e % 2.
+      const int left = keys - first - j * kKeys;
+      if (left < kKeys) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (x * 16 + (e / 2) * 8 + kr >= left) s[nt][x][e] = -INFINITY;
+      }
+      uint32_t pt[NT][2][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float top[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          top[q] = fmaxf(fmaxf(s[nt][0][q], s[nt][0][q + 2]),
+                         fmaxf(s[nt][1][q], s[nt][1][q + 2]));
+#pragma unroll
+          for (int y = 4; y < 32; y *= 2)
+            top[q] = fmaxf(top[q], __shfl_xor_sync(0xffffffffu, top[q], y));
+          top[q] *= unit[nt][q];
+        }
+        if (__any_sync(0xffffffffu, top[0] > m[nt][0] + kThreshold ||
+                                        top[1] > m[nt][1] + kThreshold)) {
+          float f[2];
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const float mn = fmaxf(m[nt][q], top[q]);
+            f[q] = mn == -INFINITY ? 1.f : ex2(m[nt][q] - mn);
+            l[nt][q] *= f[q];
+            m[nt][q] = mn;
+          }
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[nt][i][e] *= f[e % 2];
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[nt][x][e] =
+                ex2(fmaf(s[nt][x][e], unit[nt][e % 2], -m[nt][e % 2]));
+            l[nt][e % 2] += s[nt][x][e];
+          }
+          pt[nt][x][0] = transpose8(pack(s[nt][x][0], s[nt][x][1]));
+          pt[nt][x][1] = transpose8(pack(s[nt][x][2], s[nt][x][3]));
+        }
+      }
+
+      // O^T += V^T P^T: MMA column pairs of block x are tokens c, c + 4 and
+      // 8 + c, 12 + c.
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint32_t w[4][kWords], sv[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int r = x * 16 + y * 4 + c;
+          if constexpr (D == 128) {
+            const uint2 v = *reinterpret_cast<const uint2*>(
+                t + L::v + v_offset<D>(r, g * 8));
+            w[y][0] = v.x, w[y][1] = v.y;
+          } else {
+            w[y][0] = *reinterpret_cast<const uint32_t*>(t + L::v + r * L::kRow +
+                                                         g * 4);
+          }
+          // the group of this lane's elements: 16 g / 32 or 8 g / 32
+          sv[y] = *reinterpret_cast<const uint16_t*>(
+              t + L::vs + r * L::kScale + (D == 128 ? g / 2 : g / 4) * 2);
+        }
+        const uint32_t s0 = sv[0] | (sv[1] << 16), s1 = sv[2] | (sv[3] << 16);
+        const uint32_t o0 = scale_offset(s0), o1 = scale_offset(s1);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+          // (token pair 0 | 1) x (elements 0..3 | 4..7)
+          const uint32_t a00 = __byte_perm(w[0][i], w[1][i], 0x5410);
+          const uint32_t a01 = __byte_perm(w[0][i], w[1][i], 0x7632);
+          const uint32_t a10 = __byte_perm(w[2][i], w[3][i], 0x5410);
+          const uint32_t a11 = __byte_perm(w[2][i], w[3][i], 0x7632);
+#define FASTVR_PV(J)                                                  \
+  {                                                                   \
+    const uint32_t a[4] = {expand<J>(a00, s0, o0), expand<J>(a01, s0, o0), \
+                           expand<J>(a10, s1, o1), expand<J>(a11, s1, o1)}; \
+    _Pragma("unroll") for (int nt = 0; nt < NT; ++nt)                 \
+        mma(o[nt][4 * i + J], a, pt[nt][x][0], pt[nt][x][1]);         \
+  }
+          FASTVR_PV(0) FASTVR_PV(1) FASTVR_PV(2) FASTVR_PV(3)
+#undef FASTVR_PV
+        }
+      }
+    }
+    copy_wait<0>();
     __syncwarp();
-    {
-      int ahead = stage + kStages - 1;
-      if (ahead >= kStages) ahead -= kStages;
-      fetch(j + (int64_t)(kStages - 1) * W, ahead);
-    }
-    const uint8_t* t = ring + stage * L::bytes;
-    if (++stage == kStages) stage = 0;
 
-    // S^T: two blocks of 16 keys
-    float s[NT][2][4];
+    // Each warp leaves m, l and O[row][d] (for its own m) in shared memory.
+    float* so = reinterpret_cast<float*>(ring);
+    constexpr int kPitch = D + 4;
+    static_assert(8 * NT * kPitch * 4 <= kStages * L::bytes, "ring too small");
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+      for (int q = 0; q < 2; ++q) {
+        float x = l[nt][q];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[nt][x][e] = 0.f;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      uint32_t w[2][kGroups], sc[2][kGroups];
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int r = x * 16 + y * 8 + kr;
-        if constexpr (D == 128) {
-          const uint4 v = *reinterpret_cast<const uint4*>(t + L::k +
-                                                          r * L::kRow + c * 16);
-          w[y][0] = v.x, w[y][1] = v.y, w[y][2] = v.z, w[y][3] = v.w;
-          const uint2 f =
-              *reinterpret_cast<const uint2*>(t + L::ks + r * L::kScale);
-          sc[y][0] = __byte_perm(f.x, f.x, 0x1010);
-          sc[y][1] = __byte_perm(f.x, f.x, 0x3232);
-          sc[y][2] = __byte_perm(f.y, f.y, 0x1010);
-          sc[y][3] = __byte_perm(f.y, f.y, 0x3232);
-        } else {
-          const uint2 v = *reinterpret_cast<const uint2*>(t + L::k +
-                                                          r * L::kRow + c * 8);
-          w[y][0] = v.x, w[y][1] = v.y;
-          const uint32_t f =
-              *reinterpret_cast<const uint32_t*>(t + L::ks + r * L::kScale);
-          sc[y][0] = __byte_perm(f, f, 0x1010);
-          sc[y][1] = __byte_perm(f, f, 0x3232);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        const uint32_t o0 = scale_offset(sc[0][i]), o1 = scale_offset(sc[1][i]);
-        uint32_t a[4];
-        a[0] = expand<0>(w[0][i], sc[0][i], o0);
-        a[1] = expand<0>(w[1][i], sc[1][i], o1);
-        a[2] = expand<1>(w[0][i], sc[0][i], o0);
-        a[3] = expand<1>(w[1][i], sc[1][i], o1);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          mma(s[nt][x], a, qf[nt][i][0], qf[nt][i][1]);
-        a[0] = expand<2>(w[0][i], sc[0][i], o0);
-        a[1] = expand<2>(w[1][i], sc[1][i], o1);
-        a[2] = expand<3>(w[0][i], sc[0][i], o0);
-        a[3] = expand<3>(w[1][i], sc[1][i], o1);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          mma(s[nt][x], a, qf[nt][i][2], qf[nt][i][3]);
-      }
-    }
-
-    // Softmax over the tile's 32 keys; lane: keys x 16 + e/2 8 + kr of rows
-    // 2 c + e % 2.
-    const int64_t left = p.keys - first - j * kKeys;
-    uint32_t pt[NT][2][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float v = s[nt][x][e] * p.scale_log2;
-          if (left < kKeys && x * 16 + (e / 2) * 8 + kr >= left) v = -INFINITY;
-          s[nt][x][e] = v;
-          top[e % 2] = fmaxf(top[e % 2], v);
+        for (int y = 4; y < 32; y *= 2) x += __shfl_xor_sync(0xffffffffu, x, y);
+        const int row = nt * 8 + 2 * c + q;
+        if (g == 0) {
+          sh.m[warp][row] = m[nt][q];
+          sh.l[warp][row] = x;
         }
 #pragma unroll
-      for (int y = 4; y < 32; y *= 2) {
-        top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], y));
-        top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], y));
+        for (int i = 0; i < kWords; ++i)
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            *reinterpret_cast<float4*>(so + row * kPitch + 8 * kWords * g +
+                                       8 * i + 4 * y) =
+                make_float4(o[nt][4 * i][2 * y + q], o[nt][4 * i + 1][2 * y + q],
+                            o[nt][4 * i + 2][2 * y + q],
+                            o[nt][4 * i + 3][2 * y + q]);
       }
-      if (__any_sync(0xffffffffu, top[0] > m[nt][0] + kThreshold ||
-                                      top[1] > m[nt][1] + kThreshold)) {
-        float f[2];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const float mn = fmaxf(m[nt][q], top[q]);
-          f[q] = mn == -INFINITY ? 1.f : ex2(m[nt][q] - mn);
-          l[nt][q] *= f[q];
-          m[nt][q] = mn;
-        }
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[nt][i][e] *= f[e % 2];
-      }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[nt][x][e] = ex2(s[nt][x][e] - m[nt][e % 2]);
-          l[nt][e % 2] += s[nt][x][e];
-        }
-        pt[nt][x][0] = transpose8(pack(s[nt][x][0], s[nt][x][1]));
-        pt[nt][x][1] = transpose8(pack(s[nt][x][2], s[nt][x][3]));
-      }
-    }
-
-    // O^T += V^T P^T: MMA column pairs of block x are tokens c, c + 4 and
-    // 8 + c, 12 + c.
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      uint32_t w[4][kWords], sv[4];
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        const int r = x * 16 + y * 4 + c;
-        if constexpr (D == 128) {
-          const uint2 v = *reinterpret_cast<const uint2*>(
-              t + L::v + v_offset<D>(r, g * 8));
-          w[y][0] = v.x, w[y][1] = v.y;
-        } else {
-          w[y][0] = *reinterpret_cast<const uint32_t*>(t + L::v + r * L::kRow +
-                                                       g * 4);
-        }
-        // the group of this lane's elements: 16 g / 32 or 8 g / 32
-        sv[y] = *reinterpret_cast<const uint16_t*>(
-            t + L::vs + r * L::kScale + (D == 128 ? g / 2 : g / 4) * 2);
-      }
-      const uint32_t s0 = sv[0] | (sv[1] << 16), s1 = sv[2] | (sv[3] << 16);
-      const uint32_t o0 = scale_offset(s0), o1 = scale_offset(s1);
-#pragma unroll
-      for (int i = 0; i < kWords; ++i) {
-        // (token pair 0 | 1) x (elements 0..3 | 4..7)
-        const uint32_t a00 = __byte_perm(w[0][i], w[1][i], 0x5410);
-        const uint32_t a01 = __byte_perm(w[0][i], w[1][i], 0x7632);
-        const uint32_t a10 = __byte_perm(w[2][i], w[3][i], 0x5410);
-        const uint32_t a11 = __byte_perm(w[2][i], w[3][i], 0x7632);
-#define FASTVR_PV(J)                                              \
-  {                                                               \
-    const uint32_t a[4] = {                                       \
-        expand<J>(a00, s0, o0), expand<J>(a01, s0, o0),           \
-        expand<J>(a10, s1, o1), expand<J>(a11, s1, o1)};          \
-    _Pragma("unroll") for (int nt = 0; nt < NT; ++nt)             \
-        mma(o[nt][4 * i + J], a, pt[nt][x][0], pt[nt][x][1]);     \
+    __syncthreads();
+    end_piece<D, NT, W, kStages * L::bytes>(p, &sh, smem, *piece);
+    __syncthreads();  // before the next unit's tiles and the piece after it
   }
-        FASTVR_PV(0) FASTVR_PV(1) FASTVR_PV(2) FASTVR_PV(3)
-#undef FASTVR_PV
-      }
-    }
-  }
-  copy_wait<0>();
-  __syncwarp();
 
-  // Join the warps: each leaves m, l and O[row][d] (for its own m) in its
-  // part of shared memory.
-  float* so = reinterpret_cast<float*>(ring);
-  constexpr int kPitch = D + 4;
-  static_assert(kRows * kPitch * 4 <= kStages * L::bytes, "ring too small");
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      float x = l[nt][q];
-#pragma unroll
-      for (int y = 4; y < 32; y *= 2) x += __shfl_xor_sync(0xffffffffu, x, y);
-      const int row = nt * 8 + 2 * c + q;
-      if (g == 0) {
-        s_m[warp][row] = m[nt][q];
-        s_l[warp][row] = x;
-      }
-#pragma unroll
-      for (int i = 0; i < kWords; ++i)
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-          *reinterpret_cast<float4*>(so + row * kPitch + 8 * kWords * g +
-                                     8 * i + 4 * y) =
-              make_float4(o[nt][4 * i][2 * y + q], o[nt][4 * i + 1][2 * y + q],
-                          o[nt][4 * i + 2][2 * y + q],
-                          o[nt][4 * i + 3][2 * y + q]);
-    }
-  __syncthreads();
-
-  const int unit = bh * p.row_blocks + rb;
-  const int rows = min(kRows, p.rows - rb * kRows);
-  float* part = p.partial +
-                ((int64_t)unit * p.splits + split) * kRows * (D + 2);
-  auto finish = [&](int row, int d, float acc, float sum, float top) {
-    const int r = rb * kRows + row;
-    const int tok = r / p.group, head = hk * p.group + r % p.group;
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // no key: zeros
-    p.out[(((int64_t)b * p.q_tokens + tok) * p.heads + head) * D + d] =
-        __bfloat16_as_ushort(__float2bfloat16_rn(acc * inv));
-    if (d == 0 && p.lse != nullptr)
-      p.lse[((int64_t)b * p.heads + head) * p.q_tokens + tok] =
-          sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-  };
-  for (int x = threadIdx.x; x < rows * D; x += W * 32) {
-    const int row = x / D, d = x % D;
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < W; ++w) top = fmaxf(top, s_m[w][row]);
-    float acc = 0.f, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      // a warp without keys (m = -inf, l = 0) adds nothing
-      const float mw = s_m[w][row];
-      const float f = mw == -INFINITY && s_l[w][row] == 0.f ? 0.f : ex2(mw - top);
-      const float* src =
-          reinterpret_cast<const float*>(smem + w * kStages * L::bytes);
-      acc = fmaf(f, src[row * kPitch + d], acc);
-      sum = fmaf(f, s_l[w][row], sum);
-    }
-    if (p.splits == 1) {
-      finish(row, d, acc, sum, top);
-    } else {
-      part[row * (D + 2) + d] = acc;
-      if (d == 0) {
-        part[row * (D + 2) + D] = top;
-        part[row * (D + 2) + D + 1] = sum;
-      }
-    }
-  }
-  if (p.splits == 1) return;
-
-  // The last CTA of the unit to arrive joins the key ranges, in their order.
+  // Of the units that this CTA shares with others it joins those whose last
+  // part it was.
   __threadfence();
   __syncthreads();
-  if (threadIdx.x == 0) {
-    const int n = atomicAdd(p.tickets + unit, 1);
-    s_last = n == p.splits - 1;
-    if (s_last) p.tickets[unit] = 0;  // for the next call
+  if (threadIdx.x < 2) {
+    const Piece& mine = sh.shared[threadIdx.x];
+    bool last = false;
+    if (mine.parts > 1) {
+      last = atomicAdd(p.tickets + mine.cta0, 1) == mine.parts - 1;
+      if (last) p.tickets[mine.cta0] = 0;  // for the next call
+    }
+    sh.last[threadIdx.x] = last;
   }
   __syncthreads();
-  if (!s_last) return;
-  __threadfence();
-  const float* all = p.partial + (int64_t)unit * p.splits * kRows * (D + 2);
-  for (int x = threadIdx.x; x < rows * D; x += W * 32) {
-    const int row = x / D, d = x % D;
-    float top = -INFINITY, acc = 0.f, sum = 0.f;
-    for (int i = 0; i < p.splits; ++i) {
-      const float* src = all + ((int64_t)i * kRows + row) * (D + 2);
-      const float mi = __ldcg(src + D), li = __ldcg(src + D + 1);
-      const float oi = __ldcg(src + d);
-      if (mi == -INFINITY && li == 0.f) continue;  // no keys in this range
-      const float mn = fmaxf(top, mi);
-      const float f0 = top == -INFINITY ? 0.f : ex2(top - mn);
-      const float f1 = ex2(mi - mn);
-      acc = fmaf(oi, f1, acc * f0);
-      sum = fmaf(li, f1, sum * f0);
-      top = mn;
-    }
-    finish(row, d, acc, sum, top);
+  for (int i = 0; i < 2; ++i) {
+    if (!sh.last[i]) continue;
+    __threadfence();
+    join_parts<D, NT, W, kStages * L::bytes>(p, &sh, smem, sh.shared[i]);
+    __syncthreads();
   }
 }
 
-constexpr int kWarps = 8;
-
-template <int D, int NT, int kStages>
+template <int D, int NT, int kWarps, int kStages, int kCtas>
 cudaError_t launch_v(Q4AttnParams p, int sms, cudaStream_t stream) {
   p.row_blocks = (p.rows + 8 * NT - 1) / (8 * NT);
-  const int64_t units = (int64_t)p.batch_heads * p.row_blocks;
-  // Cut the keys so that the CTAs fill the SMs: the number of splits with the
-  // shortest time, counted in key tiles of the longest warp plus a fixed cost
-  // of about 4 tiles per CTA.
-  const int64_t tiles = (p.keys + kKeys - 1) / kKeys;
-  const int64_t slots = sms;
-  int64_t best = 1, best_cost = INT64_MAX;
-  for (int64_t s = 1; s <= kQ4MaxSplits && units * s <= kQ4MaxParts; ++s) {
-    if (s > 1 && (tiles + s - 1) / s < kWarps) break;
-    const int64_t waves = (units * s + slots - 1) / slots;
-    const int64_t per = (tiles + s * kWarps - 1) / (s * kWarps);
-    const int64_t cost = waves * (per + 4);
-    if (cost < best_cost) {
-      best_cost = cost;
-      best = s;
+  const int64_t units = (int64_t)p.batch * p.kv_heads * p.row_blocks;
+  const int64_t tiles = units * ((p.keys + kKeys - 1) / kKeys + kUnitCost);
+  // Either as many CTAs as the SMs hold at once, sharing out the tiles whatever
+  // the units, or the same number to every unit (no CTA then has more than one
+  // piece when the entries are equally long): whichever has the shortest
+  // estimated time in clocks, a round of tiles (each warp one) taking about
+  // 1000 with 8 query rows and half as much for every further 8, a piece 3000,
+  // and the join of a unit 2000 and its bytes at 64 per clock.
+  const int64_t rows = std::min(p.rows, 8 * NT);
+  const int64_t slots = std::min(sms * kCtas, kQ4MaxCtas);
+  int64_t grid = slots, best = INT64_MAX;
+  auto consider = [&](int64_t n, int64_t pieces, int64_t parts) {
+    const int64_t rounds = (tiles + n * kWarps - 1) / (n * kWarps);
+    const int64_t cost = rounds * 500 * (NT + 1) + pieces * 3000 +
+                         (parts > 1 ? 2000 + parts * rows * D / 16 : 0);
+    if (cost < best) {
+      best = cost;
+      grid = n;
     }
-  }
-  p.splits = (int32_t)best;
-  const int64_t grid = units * best;
-  if (grid > 0x7fffffffLL) return cudaErrorInvalidValue;
+  };
+  for (int64_t parts = 1; parts * units <= slots; ++parts)
+    consider(parts * units, 1, parts);
+  consider(slots, (units + slots - 1) / slots + 1, (slots + units - 1) / units + 1);
   constexpr int smem = kWarps * kStages * Tile<D>::bytes;
-  auto kernel = q4_attn_kernel<D, NT, kWarps, kStages>;
+  auto kernel = q4_attn_kernel<D, NT, kWarps, kStages, kCtas>;
   const cudaError_t e = cudaFuncSetAttribute(
       kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
@@ -537,10 +875,12 @@ cudaError_t launch_v(Q4AttnParams p, int sms, cudaStream_t stream) {
 
 template <int D>
 cudaError_t launch_d(const Q4AttnParams& p, int sms, cudaStream_t stream) {
-  constexpr int kStages = D == 128 ? 4 : 8;
-  if (p.rows <= 8) return launch_v<D, 1, kStages>(p, sms, stream);
-  if (p.rows <= 16) return launch_v<D, 2, kStages>(p, sms, stream);
-  return launch_v<D, 4, kStages>(p, sms, stream);
+  // Warps and ring depths are what registers and shared memory hold: 16 warps
+  // of 128 registers with one block of rows, 10 of 200 with two, 8 with four.
+  constexpr int kDeep = D == 128 ? 1 : 2;
+  if (p.rows <= 8) return launch_v<D, 1, 8, 3 * kDeep, 2>(p, sms, stream);
+  if (p.rows <= 16) return launch_v<D, 2, 10, 4 * kDeep, 1>(p, sms, stream);
+  return launch_v<D, 4, 8, 4 * kDeep, 1>(p, sms, stream);
 }
 
 }  // namespace

@@ -8,6 +8,8 @@
 // the reverse.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "fastvr_internal.h"
 
 namespace fastvr {
@@ -16,103 +18,148 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;
 
+// A thread keeps one 16-byte piece of one head and walks over tokens, kUnroll
+// consecutive ones at a time: in the cache these are neighbouring rows, 256
+// bytes of codes and a whole sector of scales (tokens far apart left every
+// 64-byte row and 8-byte scale on a DRAM page of its own, 97 us instead of
+// the figure below for the read-back).  The groups of d / 8 threads that make
+// up a row are numbered over the grid with the head fastest (token-major
+// tensors: neighbouring groups touch neighbouring memory), or they all belong
+// to one head (head-major ones).
+struct Walk {
+  int32_t slots;  // groups of threads along the tokens
+  int32_t ctas;   // grid.x
+};
+Walk make_walk(int64_t tokens, int64_t lanes, int groups_per_cta,
+               int64_t others, int sms) {
+  // Eight CTAs of 256 threads per SM in all.
+  const int64_t target =
+      std::max<int64_t>(1, (int64_t)sms * 8 * groups_per_cta / others);
+  const int64_t units = (tokens + kUnroll - 1) / kUnroll;
+  const int64_t passes = (units * lanes + target - 1) / target;
+  Walk w;
+  w.slots = (int32_t)((units + passes - 1) / passes);
+  w.ctas = (int32_t)((w.slots * lanes + groups_per_cta - 1) / groups_per_cta);
+  return w;
+}
+
+__device__ __forceinline__ float approx_rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // max |v| of a group -> its scale (the stored bfloat16 as a float); a group
 // below 2^-100 becomes zeros, one that is not finite or reaches 2^120 NaN.
 __device__ __forceinline__ float group_scale(float top) {
-  if (!(top < 0x1p120f)) return __int_as_float(0x7fc00000);
-  if (top < 0x1p-100f) return 0.f;
-  // Correctly rounded division: with 8 significant bits in top, top / 7 is
-  // either exact or further from a 5-bit tie than its rounding error.
-  const uint32_t u = __float_as_uint(__fdiv_rn(top, 7.f));
+  // top / 7 correctly rounded by one residual step (division by a known
+  // divisor, Brisebarre, Muller and Raina, 2004).  With 8 significant bits in
+  // top, top / 7 is either exact or further from a 5-bit tie than the
+  // rounding error.
+  constexpr float kSeventh = 1.f / 7.f;
+  const float q0 = top * kSeventh;
+  const float q = __fmaf_rn(__fmaf_rn(-7.f, q0, top), kSeventh, q0);
+  const uint32_t u = __float_as_uint(q);
   const uint32_t odd = (u >> 19) & 1;
-  return __uint_as_float((u + 0x3ffffu + odd) & 0xfff80000u);
+  const float s = __uint_as_float((u + 0x3ffffu + odd) & 0xfff80000u);
+  if (!(top < 0x1p120f)) return __int_as_float(0x7fc00000);
+  return top < 0x1p-100f ? 0.f : s;
 }
 
-// The code of v for scale s, r being 1 / s slightly reduced.  v has 8
+// The codes of 8 values for scale s, r being 1 / s slightly reduced.  v has 8
 // significant bits and s 5, so v / s is either exactly halfway between two
 // whole numbers or at least 2^-14 of itself away from it; r = (1 - 2^-18) / s
-// (and its rounding) moves an exact half below the half and nothing else
-// across one, which rounds ties toward zero.
-__device__ __forceinline__ uint32_t code(float v, float r) {
-  // 1.5 * 2^23 + 8: adding it leaves 8 + round(v r) in the low bits
-  return __float_as_uint(__fmaf_rn(v, r, 12582920.f)) & 15u;
+// (with the 2^-22 of an approximate reciprocal) moves an exact half below the
+// half and nothing else across one, which rounds ties toward zero.
+__device__ __forceinline__ uint32_t encode8(const uint32_t (&v)[4], float r) {
+  // Adding 1.5 * 2^23 + 8 leaves 8 + round(v r) in the low bits of the float
+  // 0x4b400000; the words are summed up shifted, and what the upper parts add
+  // modulo 2^32 is taken off: 0x4b400000 * (1 + 16 + 256).  Two values to an
+  // instruction: the low and the high halves of two words.
+  uint64_t r2, big2;
+  asm("mov.b64 %0, {%1, %1};" : "=l"(r2) : "f"(r));
+  asm("mov.b64 %0, {%1, %1};" : "=l"(big2) : "f"(12582920.f));
+  uint32_t n[8];
+#pragma unroll
+  for (int e = 0; e < 4; e += 2) {
+    uint64_t lo, hi;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(lo) : "r"(v[e] << 16), "r"(v[e + 1] << 16));
+    asm("mov.b64 %0, {%1, %2};"
+        : "=l"(hi)
+        : "r"(v[e] & 0xffff0000u), "r"(v[e + 1] & 0xffff0000u));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(lo) : "l"(lo), "l"(r2), "l"(big2));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(hi) : "l"(hi), "l"(r2), "l"(big2));
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(n[2 * e]), "=r"(n[2 * e + 2]) : "l"(lo));
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(n[2 * e + 1]), "=r"(n[2 * e + 3]) : "l"(hi));
+  }
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 7; e >= 0; --e) w = w * 16u + n[e];
+  return w - (0x4b400000u + 0xb4000000u + 0x40000000u);
 }
 
+// blockIdx.y: V or K of batch entries y / 2, + gridDim.y / 2, ...
 template <int VPR>  // words (8 values) of a row: d / 8
-__global__ void __launch_bounds__(kThreads) q4_append_kernel(Q4AppendParams p) {
+__global__ void __launch_bounds__(kThreads)
+q4_append_kernel(const __grid_constant__ Q4AppendParams p, Walk walk) {
+  constexpr int kGroups = VPR / 4;
   pdl_trigger();
   pdl_wait();
-  const bool is_v = blockIdx.y != 0;
-  const uint16_t* src = is_v ? p.v : p.k;
-  const Strides& st = is_v ? p.v_str : p.k_str;
+  const bool is_v = blockIdx.y & 1;
+  const Strides st = is_v ? p.v_str : p.k_str;
   uint32_t* codes = is_v ? p.v_codes : p.k_codes;
   uint16_t* scales = is_v ? p.v_scales : p.k_scales;
-  const int64_t rows = (int64_t)p.batch * p.tokens * p.heads;
-  const int64_t n = rows * VPR;
-  const int64_t stride = (int64_t)gridDim.x * kThreads;
-  // n and stride are multiples of 4 (VPR and kThreads are), so the four
-  // lanes of a group are in range, or out of it, together.
-  for (int64_t i0 = (int64_t)blockIdx.x * kThreads + threadIdx.x;;
-       i0 += kUnroll * stride) {
-    // warp-uniform: whole warps leave together (shuffles below)
-    if (i0 - (threadIdx.x & 31) >= n) break;
-    uint4 raw[kUnroll];
-    int64_t row_out[kUnroll];
+  const int word = threadIdx.x % VPR;
+  const int group = blockIdx.x * (kThreads / VPR) + threadIdx.x / VPR;
+  const int slot = group / p.heads;
+  const int h = group - slot * p.heads;
+  const int at_word = is_v ? word : (word % 4) * kGroups + word / 4;
+  const uint32_t cache_tokens = (uint32_t)p.cache_tokens;
+  const uint32_t stride = (uint32_t)walk.slots * kUnroll;
+  for (int b = blockIdx.y / 2; b < p.batch; b += gridDim.y / 2) {
+    const uint16_t* base =
+        (is_v ? p.v : p.k) + b * st.batch + h * st.head + word * 8;
+    const int64_t head_row = ((int64_t)b * p.heads + h) * p.cache_tokens;
+    // Every group of threads makes the same number of passes (shuffles
+    // inside); a surplus group (slot >= slots) copies nothing.
+    for (uint32_t t0 = 0; t0 < (uint32_t)p.tokens; t0 += stride) {
+      const uint32_t t = t0 + slot * kUnroll;
+      const uint16_t* src = base + (int64_t)t * st.token;
+      const uint32_t left =
+          slot < walk.slots && t < (uint32_t)p.tokens ? p.tokens - t : 0;
+      uint4 raw[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int64_t i = i0 + u * stride;
-      raw[u] = make_uint4(0, 0, 0, 0);
-      row_out[u] = -1;
-      if (i < n) {
-        const int64_t row = i / VPR;
-        const int32_t h = (int32_t)(row % p.heads);
-        const int64_t bt = row / p.heads;
-        const int64_t b = bt / p.tokens;
-        const int64_t t = bt - b * p.tokens;
-        raw[u] = __ldcs(reinterpret_cast<const uint4*>(
-            src + b * st.batch + t * st.token + h * st.head + (i % VPR) * 8));
-        int64_t at = p.first_row + t;
-        if (at >= p.cache_tokens) at -= p.cache_tokens;
-        row_out[u] = (b * p.heads + h) * p.cache_tokens + at;
+      for (int u = 0; u < kUnroll; ++u) {
+        raw[u] = make_uint4(0, 0, 0, 0);
+        if (u < left)
+          raw[u] = __ldcs(reinterpret_cast<const uint4*>(src + u * st.token));
       }
-    }
+      uint32_t at = (uint32_t)p.first_row + t;  // both below 2^30
+      if (at >= cache_tokens) at -= cache_tokens;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      float v[8];
-      const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[2 * e] = __uint_as_float(w[e] << 16);
-        v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-      }
-      // |v| as integers: their order is that of the magnitudes, and a NaN
-      // compares above everything, so it reaches the scale
-      uint32_t top = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const float s = group_scale(__uint_as_float(top));
-      const float r = s > 0.f ? (1.f - 0x1p-18f) / s : 0.f;
-      uint32_t word = 0;
-      if (s > 0.f) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) word |= code(v[e], r) << (4 * e);
-      } else {
-        word = 0x88888888u;  // zeros, or NaN through the scale
-      }
-      if (row_out[u] >= 0) {
-        const int word_i = (int)((i0 + u * stride) % VPR);
-        constexpr int kGroups = VPR / 4;
-        const int at = is_v ? word_i : (word_i % 4) * kGroups + word_i / 4;
-        if (in_bounds(row_out[u] * VPR + at, p.code_words, p.status))
-          codes[row_out[u] * VPR + at] = word;
-        if (word_i % 4 == 0 &&
-            in_bounds(row_out[u] * kGroups + word_i / 4,
-                      p.code_words / 4, p.status))
-          scales[row_out[u] * kGroups + word_i / 4] =
-              (uint16_t)(__float_as_uint(s) >> 16);
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+        // |v| as 15-bit integers, two to a word: their order is that of the
+        // magnitudes, and a NaN is above everything, so it reaches the scale
+        uint32_t top = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu),
+                                __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+        top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        top = max(top << 16, top & 0xffff0000u);
+        const float s = group_scale(__uint_as_float(top));
+        const float r = s > 0.f ? approx_rcp(s) * (1.f - 0x1p-18f) : 0.f;
+        // zeros, also under a NaN scale
+        const uint32_t code = s > 0.f ? encode8(w, r) : 0x88888888u;
+        if (u < left) {
+          const int64_t row = head_row + at;
+          if (in_bounds(row * VPR + at_word, p.code_words, p.status))
+            codes[row * VPR + at_word] = code;
+          if (word % 4 == 0 && in_bounds(row * kGroups + word / 4,
+                                         p.code_words / 4, p.status))
+            scales[row * kGroups + word / 4] =
+                (uint16_t)(__float_as_uint(s) >> 16);
+        }
+        if (++at == cache_tokens) at = 0;
       }
     }
   }
@@ -141,81 +188,68 @@ __device__ __forceinline__ uint4 expand(uint32_t w, __nv_bfloat162 s) {
   return o;
 }
 
-// kHeadMajor: rows in the order (b, h, t) of a head-major output, else
-// (b, t, h); the output itself is given by its strides.
+// kHeadMajor: blockIdx.y walks over V or K of (batch entry, head) pairs and
+// the groups of threads over tokens; else as the append.
 template <int VPR, bool kHeadMajor>
-__global__ void __launch_bounds__(kThreads) q4_read_kernel(Q4ReadParams p) {
+__global__ void __launch_bounds__(kThreads)
+q4_read_kernel(const __grid_constant__ Q4ReadParams p, Walk walk) {
+  constexpr int kGroups = VPR / 4;
   pdl_trigger();
   pdl_wait();
-  const bool is_v = blockIdx.y != 0;
+  const bool is_v = blockIdx.y & 1;
   const uint32_t* codes = is_v ? p.v_codes : p.k_codes;
   const uint16_t* scales = is_v ? p.v_scales : p.k_scales;
-  uint16_t* out = is_v ? p.v_out : p.k_out;
-  constexpr int kGroups = VPR / 4;
-  const int64_t n = (int64_t)p.batch * p.tokens * p.heads * VPR;
-  const int64_t stride = (int64_t)gridDim.x * kThreads;
-  for (int64_t i0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; i0 < n;
-       i0 += kUnroll * stride) {
-    uint32_t w[kUnroll];
-    uint16_t sc[kUnroll];
-    int64_t dst[kUnroll];
+  const int word = threadIdx.x % VPR;
+  const int group = blockIdx.x * (kThreads / VPR) + threadIdx.x / VPR;
+  const int slot = kHeadMajor ? group : group / p.heads;
+  if (slot >= walk.slots) return;
+  const int at_word = is_v ? word : (word % 4) * kGroups + word / 4;
+  const int outer = kHeadMajor ? p.batch * p.heads : p.batch;
+  for (int y = blockIdx.y / 2; y < outer; y += gridDim.y / 2) {
+    const int b = kHeadMajor ? y / p.heads : y;
+    const int h = kHeadMajor ? y - b * p.heads : group - slot * p.heads;
+    uint16_t* out = (is_v ? p.v_out : p.k_out) + b * p.out_str.batch +
+                    h * p.out_str.head + word * 8;
+    const int64_t head_row = ((int64_t)b * p.heads + h) * p.cache_tokens;
+    // Tokens before the first visible one: those that share a key tile with
+    // it are read back as zeros (they meet a weight of zero, which a stored
+    // NaN or infinity would survive), earlier ones are skipped.
+    const int64_t start =
+        p.first_chunk == nullptr
+            ? 0
+            : first_visible_token(p.first_chunk[b], p.lo_chunk, p.chunk_tokens,
+                                  p.tokens);
+    const uint32_t skip = (uint32_t)start / 128 * 128;
+    const uint32_t cache_tokens = (uint32_t)p.cache_tokens;
+    const uint32_t stride = (uint32_t)walk.slots * kUnroll;
+    for (uint32_t t0 = slot * kUnroll; t0 < (uint32_t)p.tokens; t0 += stride) {
+      if (t0 + kUnroll <= skip) continue;
+      uint32_t at = (uint32_t)p.first_row + t0;  // both below 2^30
+      if (at >= cache_tokens) at -= cache_tokens;
+      uint32_t w[kUnroll], sc[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int64_t i = i0 + u * stride;
-      dst[u] = -1;
-      w[u] = 0x88888888u;
-      sc[u] = 0;
-      if (i >= n) continue;
-      const int word = (int)(i % VPR);
-      const int64_t row = i / VPR;
-      int64_t b, t;
-      int32_t h;
-      if (kHeadMajor) {
-        t = row % p.tokens;
-        h = (int32_t)(row / p.tokens % p.heads);
-        b = row / p.tokens / p.heads;
-      } else {
-        h = (int32_t)(row % p.heads);
-        t = row / p.heads % p.tokens;
-        b = row / p.heads / p.tokens;
-      }
-      dst[u] = b * p.out_str.batch + t * p.out_str.token +
-               h * p.out_str.head + word * 8;
-      if (p.first_chunk != nullptr) {
-        // Tokens before the first visible one: those that share a key tile
-        // with it are read back as zeros (they meet a weight of zero, which
-        // a stored NaN or infinity would survive), earlier ones are skipped.
-        const int64_t start = first_visible_token(p.first_chunk[b], p.lo_chunk,
-                                                  p.chunk_tokens, p.tokens);
-        if (t < start) {
-          if (t < start / 128 * 128) dst[u] = -1;
-          continue;
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint32_t t = t0 + u;
+        w[u] = sc[u] = 0;
+        const int64_t row = head_row + at;
+        if (t >= (uint32_t)start && t < (uint32_t)p.tokens &&
+            in_bounds(row * VPR + at_word, p.code_words, p.status)) {
+          w[u] = __ldcs(codes + row * VPR + at_word);
+          sc[u] = scales[row * kGroups + word / 4];
         }
+        if (++at == cache_tokens) at = 0;
       }
-      int64_t at = p.first_row + t;
-      if (at >= p.cache_tokens) at -= p.cache_tokens;
-      const int64_t r = (b * p.heads + h) * p.cache_tokens + at;
-      const int pos = is_v ? word : (word % 4) * kGroups + word / 4;
-      if (in_bounds(r * VPR + pos, p.code_words, p.status)) {
-        w[u] = codes[r * VPR + pos];
-        sc[u] = scales[r * kGroups + word / 4];
-      }
-    }
+      uint16_t* dst = out + (int64_t)t0 * p.out_str.token;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (dst[u] < 0) continue;
-      const uint32_t s2 = sc[u] * 0x10001u;
-      *reinterpret_cast<uint4*>(out + dst[u]) =
-          expand(w[u], *reinterpret_cast<const __nv_bfloat162*>(&s2));
+      for (int u = 0; u < kUnroll; ++u) {
+        const uint32_t t = t0 + u;
+        if (t < skip || t >= (uint32_t)p.tokens) continue;
+        const uint32_t s2 = sc[u] * 0x10001u;
+        *reinterpret_cast<uint4*>(dst + u * p.out_str.token) =
+            expand(w[u], *reinterpret_cast<const __nv_bfloat162*>(&s2));
+      }
     }
   }
-}
-
-int grid_for(int64_t n, int sms) {
-  int64_t blocks = (int64_t)sms * 4;
-  const int64_t need = (n + kThreads - 1) / kThreads;
-  if (blocks > need) blocks = need;
-  return (int)blocks;
 }
 
 }  // namespace
@@ -223,30 +257,33 @@ int grid_for(int64_t n, int sms) {
 cudaError_t launch_q4_append(const Q4AppendParams& p, int sms,
                              cudaStream_t stream) {
   const int vpr = p.head_dim / 8;
-  const int64_t n = (int64_t)p.batch * p.tokens * p.heads * vpr;
-  const dim3 grid(grid_for(n, sms), 2);
-  if (vpr == 16)
-    return launch_pdl(q4_append_kernel<16>, grid, dim3(kThreads), 0, stream, p);
-  if (vpr == 8)
-    return launch_pdl(q4_append_kernel<8>, grid, dim3(kThreads), 0, stream, p);
-  return cudaErrorInvalidValue;
+  if (vpr != 16 && vpr != 8) return cudaErrorInvalidValue;
+  const int ys = std::min(p.batch, 32767);
+  const Walk w = make_walk(p.tokens, p.heads, kThreads / vpr, 2 * ys, sms);
+  const dim3 grid(w.ctas, 2 * ys), block(kThreads);
+  return vpr == 16 ? launch_pdl(q4_append_kernel<16>, grid, block, 0, stream, p,
+                                w)
+                   : launch_pdl(q4_append_kernel<8>, grid, block, 0, stream, p,
+                                w);
 }
 
 cudaError_t launch_q4_read(const Q4ReadParams& p, bool head_major, int sms,
                            cudaStream_t stream) {
   const int vpr = p.head_dim / 8;
-  const int64_t n = (int64_t)p.batch * p.tokens * p.heads * vpr;
-  const dim3 grid(grid_for(n, sms), 2);
-  const dim3 block(kThreads);
+  if (vpr != 16 && vpr != 8) return cudaErrorInvalidValue;
+  const int ys = std::min(head_major ? p.batch * p.heads : p.batch, 32767);
+  const Walk w = make_walk(p.tokens, head_major ? 1 : p.heads, kThreads / vpr,
+                           2 * ys, sms);
+  const dim3 grid(w.ctas, 2 * ys), block(kThreads);
   if (vpr == 16)
-    return head_major
-               ? launch_pdl(q4_read_kernel<16, true>, grid, block, 0, stream, p)
-               : launch_pdl(q4_read_kernel<16, false>, grid, block, 0, stream, p);
-  if (vpr == 8)
-    return head_major
-               ? launch_pdl(q4_read_kernel<8, true>, grid, block, 0, stream, p)
-               : launch_pdl(q4_read_kernel<8, false>, grid, block, 0, stream, p);
-  return cudaErrorInvalidValue;
+    return head_major ? launch_pdl(q4_read_kernel<16, true>, grid, block, 0,
+                                   stream, p, w)
+                      : launch_pdl(q4_read_kernel<16, false>, grid, block, 0,
+                                   stream, p, w);
+  return head_major ? launch_pdl(q4_read_kernel<8, true>, grid, block, 0,
+                                 stream, p, w)
+                    : launch_pdl(q4_read_kernel<8, false>, grid, block, 0,
+                                 stream, p, w);
 }
 
 }  // namespace fastvr

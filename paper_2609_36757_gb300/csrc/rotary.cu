@@ -14,6 +14,8 @@
 // top 32 bits go to sincospi.  A position of 10^6 is as accurate as 1.
 #include <cuda_bf16.h>
 
+#include <algorithm>
+
 #include "fastvr_internal.h"
 
 namespace fastvr {
@@ -21,7 +23,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kSmemPairs = 2048;  // (token, pair) entries per CTA: 16 KB
-constexpr int kUnroll = 4;
 
 // Division of 32-bit numbers below 2^31 by a divisor fixed at launch.
 struct FastDiv {
@@ -60,36 +61,48 @@ struct Params {
   const int32_t* pos;
   int64_t pos_batch;
   Strides q_str, k_str, q_out_str, k_out_str;
-  int64_t rows;               // batch * tokens
+  int32_t rows;               // batch * tokens
   int32_t tokens, axes, pairs, head_dim;
   int32_t tile;               // tokens of a CTA
   int32_t axis_end[3];        // first pair past each axis
-  FastDiv by_tokens, by_pairs, by_items, by_heads;
+  FastDiv by_tokens, by_pairs, by_blocks;
   int32_t items;              // vector items of a head
+  int32_t lanes;              // threads of a group, one per item
+  int32_t head_blocks;
   int32_t heads, all_heads;   // q heads, q and k heads
   float mag, sign;
   uint64_t turn[kRotaryMaxPairs];  // theta / 2 pi in 2^-64 turns
 };
 
+// Heads that a thread takes at once: 64 bytes of loads in flight (64 registers
+// keep 32 warps on an SM).
+__host__ __device__ constexpr int head_block(int elem_bytes, bool half) {
+  return 8 / elem_bytes / (half ? 2 : 1);
+}
+
 // One head's item: kHalf: the vectors of V elements at i V and rot/2 + i V
 // (one per pair of the V), then the pass-through vectors; interleaved: the
-// vector at i V, V / 2 pairs.
+// vector at i V, V / 2 pairs.  A group of threads, one per item, takes a block
+// of HB heads of a token at a time: the sines of a thread's item are read once
+// for the block, and the block's loads are in flight together.
 template <typename T, bool kHalf, int V>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 rotary_kernel(const __grid_constant__ Params p) {
-  __shared__ float2 cs[kSmemPairs];
+  constexpr int HB = head_block(sizeof(T), kHalf);
+  constexpr int kPairs = kHalf ? V : V / 2;  // pairs of an item
+  __shared__ __align__(16) float2 cs[kSmemPairs + 8];
   pdl_trigger();
-  const int64_t row0 = (int64_t)blockIdx.x * p.tile;
-  const int n_rows = (int)min((int64_t)p.tile, p.rows - row0);
+  const int row0 = blockIdx.x * p.tile;
+  const int n_rows = min(p.tile, p.rows - row0);
   pdl_wait();
   for (int i = threadIdx.x; i < n_rows * p.pairs; i += kThreads) {
     const int r = fast_div(i, p.by_pairs);
     const int pair = i - r * p.pairs;
-    const int64_t row = row0 + r;
-    const int64_t b = row / p.tokens;
-    const int64_t t = row - b * p.tokens;
+    const int row = row0 + r;
+    const int b = fast_div(row, p.by_tokens);
+    const int t = row - b * p.tokens;
     const int axis = (pair >= p.axis_end[0]) + (pair >= p.axis_end[1]);
-    const int32_t pos = p.pos[b * p.pos_batch + t * p.axes + axis];
+    const int32_t pos = p.pos[b * p.pos_batch + (int64_t)t * p.axes + axis];
     const uint64_t turn = (uint64_t)(int64_t)pos * p.turn[pair];
     // half turns in [-1, 1)
     const float x = (float)(int32_t)(turn >> 32) * 0x1p-31f;
@@ -100,75 +113,70 @@ rotary_kernel(const __grid_constant__ Params p) {
   __syncthreads();
 
   using Vt = Vec<T, V>;
-  const int half = p.pairs;
-  const int pair_items = kHalf ? half / V : p.items;
-  const int total = n_rows * p.all_heads * p.items;
-  for (int i0 = threadIdx.x; i0 < total; i0 += kThreads * kUnroll) {
-    Vt a[kUnroll], b[kUnroll];
-    T* dst[kUnroll];
-    int item[kUnroll], r[kUnroll];
+  const int pair_items = kHalf ? p.pairs / V : p.items;
+  const int group = threadIdx.x / p.lanes;
+  const int groups = kThreads / p.lanes;
+  const int lane = threadIdx.x - group * p.lanes;
+  if (group >= groups) return;
+  const int tasks = n_rows * p.head_blocks;
+  for (int task = group; task < tasks; task += groups) {
+    const int r = fast_div(task, p.by_blocks);
+    const int h0 = (task - r * p.head_blocks) * HB;
+    const int row = row0 + r;
+    const int b = fast_div(row, p.by_tokens);
+    const int t = row - b * p.tokens;
+    const T* q = static_cast<const T*>(p.q) + b * p.q_str.batch +
+                 t * p.q_str.token;
+    const T* k = static_cast<const T*>(p.k) + b * p.k_str.batch +
+                 t * p.k_str.token;
+    T* qo = static_cast<T*>(p.q_out) + b * p.q_out_str.batch +
+            t * p.q_out_str.token;
+    T* ko = static_cast<T*>(p.k_out) + b * p.k_out_str.batch +
+            t * p.k_out_str.token;
+    for (int item = lane; item < p.items; item += p.lanes) {
+      const bool rot = !kHalf || item < pair_items;
+      const int x =
+          rot ? item * V : 2 * p.pairs + (item - pair_items) * V;
+      Vt a[HB], z[HB];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int i = i0 + u * kThreads;
-      if (i >= total) break;
-      const int rh = fast_div(i, p.by_items);
-      item[u] = i - rh * p.items;
-      r[u] = fast_div(rh, p.by_heads);
-      int h = rh - r[u] * p.all_heads;
-      const int64_t row = row0 + r[u];
-      const int64_t bb = p.rows == p.tokens ? 0 : row / p.tokens;
-      const int64_t t = row - bb * p.tokens;
-      const bool is_k = h >= p.heads;
-      if (is_k) h -= p.heads;
-      const Strides& si = is_k ? p.k_str : p.q_str;
-      const Strides& so = is_k ? p.k_out_str : p.q_out_str;
-      const T* src = static_cast<const T*>(is_k ? p.k : p.q) + bb * si.batch +
-                     t * si.token + h * si.head;
-      dst[u] = static_cast<T*>(is_k ? p.k_out : p.q_out) + bb * so.batch +
-               t * so.token + h * so.head;
-      if (kHalf) {
-        const bool rot = item[u] < pair_items;
-        const int x = rot ? item[u] * V : 2 * half + (item[u] - pair_items) * V;
+      for (int u = 0; u < HB; ++u) {
+        const int h = h0 + u;
+        if (h >= p.all_heads) continue;
+        const T* src = h < p.heads ? q + h * p.q_str.head
+                                   : k + (h - p.heads) * p.k_str.head;
         a[u] = *reinterpret_cast<const Vt*>(src + x);
-        if (rot) b[u] = *reinterpret_cast<const Vt*>(src + x + half);
-      } else {
-        a[u] = *reinterpret_cast<const Vt*>(src + item[u] * V);
+        if (kHalf && rot)
+          z[u] = *reinterpret_cast<const Vt*>(src + x + p.pairs);
       }
-    }
+      if (rot) {
+        float2 w[kPairs];
+        const int pair0 = item * kPairs;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (i0 + u * kThreads >= total) break;
-      if (kHalf) {
-        if (item[u] >= pair_items) {
-          *reinterpret_cast<Vt*>(dst[u] + 2 * half +
-                                 (item[u] - pair_items) * V) = a[u];
-          continue;
-        }
-        const float2* w = cs + r[u] * half + item[u] * V;
-        Vt y, z;
+        for (int e = 0; e < kPairs; ++e)
+          w[e] = cs[r * p.pairs + pair0 + e];  // the table is padded
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float2 cw = w[e];
-          const float fa = to_f(a[u].e[e]), fb = to_f(b[u].e[e]);
-          from_f(y.e[e], fa * cw.x - fb * cw.y);
-          from_f(z.e[e], fb * cw.x + fa * cw.y);
-        }
-        *reinterpret_cast<Vt*>(dst[u] + item[u] * V) = y;
-        *reinterpret_cast<Vt*>(dst[u] + half + item[u] * V) = z;
-      } else {
-        Vt y = a[u];
-        const float2* w = cs + r[u] * half + item[u] * (V / 2);
-        const int left = half - item[u] * (V / 2);  // pairs from here on
+        for (int u = 0; u < HB; ++u) {
+          if (h0 + u >= p.all_heads) continue;
 #pragma unroll
-        for (int e = 0; e < V / 2; ++e) {
-          if (e < left) {
-            const float2 cw = w[e];
-            const float fa = to_f(a[u].e[2 * e]), fb = to_f(a[u].e[2 * e + 1]);
-            from_f(y.e[2 * e], fa * cw.x - fb * cw.y);
-            from_f(y.e[2 * e + 1], fb * cw.x + fa * cw.y);
+          for (int e = 0; e < kPairs; ++e) {
+            // the rotated part may end inside a piece; the rest is copied
+            if (!kHalf && pair0 + e >= p.pairs) continue;
+            T& ra = kHalf ? a[u].e[e] : a[u].e[(2 * e) % V];
+            T& rb = kHalf ? z[u].e[e] : a[u].e[(2 * e + 1) % V];
+            const float fa = to_f(ra), fb = to_f(rb);
+            from_f(ra, fa * w[e].x - fb * w[e].y);
+            from_f(rb, fb * w[e].x + fa * w[e].y);
           }
         }
-        *reinterpret_cast<Vt*>(dst[u] + item[u] * V) = y;
+      }
+#pragma unroll
+      for (int u = 0; u < HB; ++u) {
+        const int h = h0 + u;
+        if (h >= p.all_heads) continue;
+        T* dst = h < p.heads ? qo + h * p.q_out_str.head
+                             : ko + (h - p.heads) * p.k_out_str.head;
+        *reinterpret_cast<Vt*>(dst + x) = a[u];
+        if (kHalf && rot) *reinterpret_cast<Vt*>(dst + x + p.pairs) = z[u];
       }
     }
   }
@@ -181,21 +189,19 @@ cudaError_t launch_t(const RotaryArgs& a, Params& p, cudaStream_t stream) {
   int v = 8;
   if (a.half)
     while (p.pairs % v) v /= 2;
-  p.items = a.half ? (p.pairs + p.head_dim - 2 * p.pairs) / v : p.head_dim / 8;
-  p.by_items = make_div(p.items);
-  // Tokens of a CTA: what the sine table holds, no more than leave every SM
-  // a few CTAs (a decode step has one token per stream).
+  p.items = a.half ? (p.head_dim - p.pairs) / v : p.head_dim / 8;
+  p.lanes = p.items < kThreads ? p.items : kThreads;
+  const int hb = head_block(sizeof(T), a.half);
+  p.head_blocks = (p.all_heads + hb - 1) / hb;
+  p.by_blocks = make_div(p.head_blocks);
+  // Tokens of a CTA: what the sine table holds, and few enough that every SM
+  // has a dozen CTAs to even out its last ones.
   int64_t tile = kSmemPairs / p.pairs;
-  const int64_t spread = p.rows / ((int64_t)a.sms * 4);
-  if (tile > spread) tile = spread;
-  // total items of a CTA stay within 32 bits: all_heads * items * tile
-  const int64_t per = (int64_t)p.all_heads * p.items;
-  if (tile > (1 << 30) / per) tile = (1 << 30) / per;
+  tile = std::min<int64_t>(tile, p.rows / (a.sms * 12));
+  tile = std::min<int64_t>(tile, (1 << 30) / p.head_blocks);
   if (tile < 1) tile = 1;
   p.tile = (int32_t)tile;
-  const int64_t grid = (p.rows + tile - 1) / tile;
-  if (grid > 0x7fffffffLL || per > (1 << 30)) return cudaErrorInvalidValue;
-  const dim3 g((unsigned)grid), b(kThreads);
+  const dim3 g((unsigned)((p.rows + tile - 1) / tile)), b(kThreads);
   if (!a.half) return launch_pdl(rotary_kernel<T, false, 8>, g, b, 0, stream, p);
   switch (v) {
     case 8: return launch_pdl(rotary_kernel<T, true, 8>, g, b, 0, stream, p);
@@ -219,7 +225,7 @@ cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t stream) {
   p.k_str = a.k_str;
   p.q_out_str = a.q_out_str;
   p.k_out_str = a.k_out_str;
-  p.rows = (int64_t)a.batch * a.tokens;
+  p.rows = a.batch * a.tokens;
   p.tokens = a.tokens;
   p.axes = a.axes;
   p.pairs = a.pairs;
@@ -233,7 +239,6 @@ cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t stream) {
   p.by_pairs = make_div(a.pairs);
   p.heads = a.heads;
   p.all_heads = a.heads + a.kv_heads;
-  p.by_heads = make_div(p.all_heads);
   p.mag = a.magnitude;
   p.sign = a.transpose ? -a.magnitude : a.magnitude;
   for (int i = 0; i < a.pairs; ++i) p.turn[i] = a.turn[i];
