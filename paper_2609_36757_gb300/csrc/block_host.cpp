@@ -385,6 +385,7 @@ fastvr_status_t fastvr_gated_norm_fwd(
   p.h = h;
   p.rows = (int64_t)cfg->batch * cfg->tokens;
   p.group_tokens = cfg->tokens / cfg->groups;
+  p.by_group_tokens = fastvr::make_div((uint32_t)p.group_tokens);
   p.dim = cfg->dim;
   p.pre = cfg->pre;
   p.post = cfg->post;

@@ -4,9 +4,57 @@
 #include <cuda_bf16.h>
 
 #include "fastvr_internal.h"
+#include "vec_math.cuh"
 
 namespace fastvr {
 namespace norm {
+
+// 8 float32 values, two to a register pair.
+struct F8 {
+  F2 v[4];
+};
+__device__ __forceinline__ F8 splat(float x) {
+  F8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = f2(x);
+  return r;
+}
+__device__ __forceinline__ F8 add(const F8& a, const F8& b) {
+  F8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = add(a.v[i], b.v[i]);
+  return r;
+}
+__device__ __forceinline__ F8 mul(const F8& a, const F8& b) {
+  F8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = mul(a.v[i], b.v[i]);
+  return r;
+}
+__device__ __forceinline__ F8 fma(const F8& a, const F8& b, const F8& c) {
+  F8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.v[i] = fma(a.v[i], b.v[i], c.v[i]);
+  return r;
+}
+// The same with one factor, or a factor and a summand, for all.
+__device__ __forceinline__ F8 mul(const F8& a, float b) {
+  return mul(a, splat(b));
+}
+__device__ __forceinline__ F8 fma(const F8& a, float b, const F8& c) {
+  return fma(a, splat(b), c);
+}
+__device__ __forceinline__ F8 fma(const F8& a, float b, float c) {
+  return fma(a, splat(b), splat(c));
+}
+__device__ __forceinline__ float sum(const F8& a) {
+  return sum(add(add(a.v[0], a.v[1]), add(a.v[2], a.v[3])));
+}
+__device__ __forceinline__ float dot(const F8& a, const F8& b) {
+  return sum(fma(a.v[3], b.v[3],
+                 fma(a.v[2], b.v[2],
+                     fma(a.v[1], b.v[1], mul(a.v[0], b.v[0])))));
+}
 
 // 8 consecutive elements in memory: 16 bytes of bfloat16 or 32 of float32.
 template <typename T>
@@ -18,13 +66,13 @@ struct Raw8<__nv_bfloat16> {
     u = *reinterpret_cast<const uint4*>(
         static_cast<const __nv_bfloat16*>(base) + i);
   }
-  __device__ __forceinline__ void widen(float (&f)[8]) const {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      f[2 * e] = __uint_as_float(w[e] << 16);
-      f[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-    }
+  __device__ __forceinline__ F8 widen() const {
+    F8 r;
+    r.v[0] = f2(bf16_lo(u.x), bf16_hi(u.x));
+    r.v[1] = f2(bf16_lo(u.y), bf16_hi(u.y));
+    r.v[2] = f2(bf16_lo(u.z), bf16_hi(u.z));
+    r.v[3] = f2(bf16_lo(u.w), bf16_hi(u.w));
+    return r;
   }
 };
 template <>
@@ -36,45 +84,82 @@ struct Raw8<float> {
     a = p[0];
     b = p[1];
   }
-  __device__ __forceinline__ void widen(float (&f)[8]) const {
-    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w;
-    f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+  __device__ __forceinline__ F8 widen() const {
+    F8 r;
+    r.v[0] = f2(a.x, a.y);
+    r.v[1] = f2(a.z, a.w);
+    r.v[2] = f2(b.x, b.y);
+    r.v[3] = f2(b.z, b.w);
+    return r;
   }
 };
 
 __device__ __forceinline__ void store8(__nv_bfloat16* base, int64_t i,
-                                       const float (&f)[8]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
-    w[e] = *reinterpret_cast<const uint32_t*>(&v);
-  }
-  *reinterpret_cast<uint4*>(base + i) = make_uint4(w[0], w[1], w[2], w[3]);
+                                       const F8& f) {
+  *reinterpret_cast<uint4*>(base + i) =
+      make_uint4(bf16_pack(f.v[0]), bf16_pack(f.v[1]), bf16_pack(f.v[2]),
+                 bf16_pack(f.v[3]));
 }
-__device__ __forceinline__ void store8(float* base, int64_t i,
-                                       const float (&f)[8]) {
+__device__ __forceinline__ void store8(float* base, int64_t i, const F8& f) {
+  float x[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) split(f.v[e], x[2 * e], x[2 * e + 1]);
   float4* p = reinterpret_cast<float4*>(base + i);
-  p[0] = make_float4(f[0], f[1], f[2], f[3]);
-  p[1] = make_float4(f[4], f[5], f[6], f[7]);
+  p[0] = make_float4(x[0], x[1], x[2], x[3]);
+  p[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
 
 // 8 floats of an optional vector, `absent` where there is none.
-__device__ __forceinline__ void load8_or(const float* base, int64_t i,
-                                         float absent, float (&f)[8]) {
-  if (base == nullptr) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = absent;
-    return;
-  }
+__device__ __forceinline__ F8 load8_or(const float* base, int64_t i,
+                                       float absent) {
+  if (base == nullptr) return splat(absent);
   Raw8<float> r;
   r.load(base, i);
-  r.widen(f);
+  return r.widen();
 }
 
-__device__ __forceinline__ float sum8(const float (&f)[8]) {
-  return ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-}
+// Vectors of 8 floats that belong to a thread, in shared memory: what is used
+// once per row leaves its registers to the rows in flight (a spilled register
+// costs more than such a read).  The halves lie apart, so that the lanes of a
+// warp touch consecutive 16 bytes.
+struct Private {
+  float4* base;  // [vector][half][thread]
+  __device__ __forceinline__ F8 get(int i) const {
+    const float4 a = base[2 * i * blockDim.x + threadIdx.x];
+    const float4 b = base[(2 * i + 1) * blockDim.x + threadIdx.x];
+    F8 r;
+    r.v[0] = f2(a.x, a.y);
+    r.v[1] = f2(a.z, a.w);
+    r.v[2] = f2(b.x, b.y);
+    r.v[3] = f2(b.z, b.w);
+    return r;
+  }
+  __device__ __forceinline__ void set(int i, const F8& f) const {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) split(f.v[e], x[2 * e], x[2 * e + 1]);
+    base[2 * i * blockDim.x + threadIdx.x] =
+        make_float4(x[0], x[1], x[2], x[3]);
+    base[(2 * i + 1) * blockDim.x + threadIdx.x] =
+        make_float4(x[4], x[5], x[6], x[7]);
+  }
+};
+
+// N such vectors, in registers where kRegs.
+template <bool kRegs, int N>
+struct Kept {
+  F8 r[kRegs ? N : 1];
+  Private m;
+  __device__ __forceinline__ F8 get(int i) const {
+    return kRegs ? r[kRegs ? i : 0] : m.get(i);
+  }
+  __device__ __forceinline__ void set(int i, const F8& f) {
+    if (kRegs)
+      r[kRegs ? i : 0] = f;
+    else
+      m.set(i, f);
+  }
+};
 
 // Sums of a and of b over the L lanes of a row within a warp, at the price of
 // about one: the halves of the lanes first trade what they do not keep.
@@ -98,9 +183,10 @@ __device__ __forceinline__ void both_sums(float& a, float& b) {
   b = hi ? v : o;
 }
 
-// A row's threads, 8 columns each: TPR of them.  Up to 32: 128 / TPR rows side
-// by side in a CTA of 128 threads, their sums within a warp.  Above: one row
-// to a CTA of (at most) TPR threads, its sums across the warps.
+// A row's threads: TPR of them with NV vectors of 8 columns each, vector i at
+// column (i TPR + thread) 8.  Up to 32: 128 / TPR rows side by side in a CTA of
+// 128 threads, their sums within a warp.  Above: a row to a CTA, its sums
+// across the warps.
 template <int TPR>
 struct Shape {
   static constexpr int kThreads = TPR <= 32 ? 128 : TPR;
@@ -108,36 +194,40 @@ struct Shape {
   static constexpr int kRows = TPR <= 32 ? 128 / TPR : 1;
   static constexpr bool kMany = TPR > 32;
   static constexpr int kWarps = kMany ? TPR / 32 : 1;
+  // (all of many warps' parts at once take too many registers)
+  static constexpr int kUnroll = kWarps <= 8 ? kWarps : 4;
 };
 
 // What a thread knows of its row's columns.
+template <int TPR, int NV>
 struct Cols {
-  int c;           // first of its 8 columns
-  bool on;         // they exist
-  int warps;       // warps of the row
-  float inv_dim, inv_warp;  // 1 / columns of the row, of this warp
-  float last;      // columns of the row's last warp
-};
-template <int TPR>
-__device__ __forceinline__ Cols make_cols(int dim) {
   using S = Shape<TPR>;
-  Cols k;
-  k.c = (S::kRows > 1 ? threadIdx.x % TPR : threadIdx.x) * 8;
-  k.on = k.c < dim;
-  k.warps = S::kMany ? blockDim.x / 32 : 1;
-  k.inv_dim = 1.f / (float)dim;
-  const int warp = S::kMany ? threadIdx.x / 32 : 0;
-  k.inv_warp = 1.f / (float)min(S::kMany ? 256 : dim, dim - warp * 256);
-  k.last = (float)(dim - (k.warps - 1) * 256);
-  return k;
-}
+  int dim, c;  // c: its first column
+  float inv_dim, inv_warp;  // 1 / columns of the row, of this warp
+  const float* counts;      // columns of each warp of the row
+  // `n`: kWarps floats of shared memory, filled before the first exchange
+  __device__ __forceinline__ Cols(int d, float* n) : dim(d), counts(n) {
+    c = (S::kRows > 1 ? threadIdx.x % TPR : threadIdx.x) * 8;
+    inv_dim = 1.f / (float)d;
+    int mine = d;
+    if (S::kMany) {
+      mine = 0;
+      for (int i = 0; i < NV; ++i)
+        mine += min(256, max(0, d - (i * TPR + (int)threadIdx.x / 32 * 32) * 8));
+    }
+    inv_warp = 1.f / (float)max(mine, 1);
+    if (threadIdx.x % 32 == 0 && (S::kMany || threadIdx.x == 0))
+      n[S::kMany ? threadIdx.x / 32 : 0] = (float)mine;
+  }
+  __device__ __forceinline__ int at(int i) const { return c + i * TPR * 8; }
+  __device__ __forceinline__ bool on(int i) const { return at(i) < dim; }
+};
 
 // Sums over the row of a and of b, on every thread; `part` (kWarps entries)
 // is this exchange's own: two exchanges with another part between them need
 // one barrier each.
 template <int TPR>
-__device__ __forceinline__ void row_sums(float& a, float& b, const Cols& k,
-                                         float2* part) {
+__device__ __forceinline__ void row_sums(float& a, float& b, float2* part) {
   using S = Shape<TPR>;
   if constexpr (!S::kMany) {
     both_sums<S::kLanes>(a, b);
@@ -146,14 +236,11 @@ __device__ __forceinline__ void row_sums(float& a, float& b, const Cols& k,
     if (threadIdx.x % 16 == 0)
       reinterpret_cast<float*>(part)[threadIdx.x / 16] = v;
     __syncthreads();
-    a = b = 0.f;
-#pragma unroll
+    F2 all = f2(0.f);
+#pragma unroll(S::kUnroll)
     for (int w = 0; w < S::kWarps; ++w)
-      if (w < k.warps) {
-        const float2 x = part[w];
-        a += x.x;
-        b += x.y;
-      }
+      all = add(all, f2(part[w].x, part[w].y));
+    split(all, a, b);
   }
 }
 
@@ -164,71 +251,70 @@ __device__ __forceinline__ void row_sums(float& a, float& b, const Cols& k,
 struct Stats {
   float mu_a, mu_b, sq_a, sq_b;
 };
-template <int TPR>
-__device__ __forceinline__ Stats row_stats(const float (&a)[8],
-                                           const float (&b)[8], bool mean_a,
-                                           bool mean_b, const Cols& k,
+template <int TPR, int NV>
+__device__ __forceinline__ Stats row_stats(const F8 (&a)[NV], const F8 (&b)[NV],
+                                           bool mean_a, bool mean_b,
+                                           const Cols<TPR, NV>& k,
                                            float4* part) {
   using S = Shape<TPR>;
   Stats st;
   st.mu_a = st.mu_b = 0.f;
   if (mean_a || mean_b) {
-    st.mu_a = mean_a ? sum8(a) : 0.f;
-    st.mu_b = mean_b ? sum8(b) : 0.f;
+    F8 x = a[0], y = b[0];
+#pragma unroll
+    for (int i = 1; i < NV; ++i) {
+      x = add(x, a[i]);
+      y = add(y, b[i]);
+    }
+    st.mu_a = mean_a ? sum(x) : 0.f;
+    st.mu_b = mean_b ? sum(y) : 0.f;
     both_sums<S::kLanes>(st.mu_a, st.mu_b);
     st.mu_a *= k.inv_warp;
     st.mu_b *= k.inv_warp;
   }
-  st.sq_a = st.sq_b = 0.f;
-  if (k.on) {
+  F8 qa = splat(0.f), qb = qa;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = a[e] - st.mu_a, y = b[e] - st.mu_b;
-      st.sq_a = fmaf(x, x, st.sq_a);
-      st.sq_b = fmaf(y, y, st.sq_b);
+  for (int i = 0; i < NV; ++i)
+    if (k.on(i)) {
+      const F8 x = add(a[i], splat(-st.mu_a)), y = add(b[i], splat(-st.mu_b));
+      qa = fma(x, x, qa);
+      qb = fma(y, y, qb);
     }
-  }
+  st.sq_a = sum(qa);
+  st.sq_b = sum(qb);
   if constexpr (!S::kMany) {
     both_sums<S::kLanes>(st.sq_a, st.sq_b);
   } else {
+    // part[w] = (mean of a, of b, squares of a, of b) in warp w
     const float v = keep_sums<32>(st.sq_a, st.sq_b);
-    if (threadIdx.x % 16 == 0)  // lane 0: of a, lane 16: of b
-      reinterpret_cast<float2*>(part)[threadIdx.x / 16] =
-          make_float2(threadIdx.x & 16 ? st.mu_b : st.mu_a, v);
-    __syncthreads();
-    float sa = 0.f, sb = 0.f;
-    st.sq_a = st.sq_b = 0.f;
-#pragma unroll
-    for (int w = 0; w < S::kWarps; ++w)
-      if (w < k.warps) {
-        const float4 x = part[w];
-        const float n = w == k.warps - 1 ? k.last : 256.f;
-        sa = fmaf(n, x.x, sa);
-        sb = fmaf(n, x.z, sb);
-        st.sq_a += x.y;
-        st.sq_b += x.w;
-      }
-    if (mean_a || mean_b) {
-      st.mu_a = sa * k.inv_dim;
-      st.mu_b = sb * k.inv_dim;
-#pragma unroll
-      for (int w = 0; w < S::kWarps; ++w)
-        if (w < k.warps) {
-          const float n = w == k.warps - 1 ? k.last : 256.f;
-          const float4 x = part[w];
-          const float da = x.x - st.mu_a, db = x.z - st.mu_b;
-          st.sq_a = fmaf(n * da, da, st.sq_a);
-          st.sq_b = fmaf(n * db, db, st.sq_b);
-        }
+    if (threadIdx.x % 16 == 0) {  // lane 0: of a, lane 16: of b
+      float* to = reinterpret_cast<float*>(part + threadIdx.x / 32) +
+                  (threadIdx.x & 16 ? 1 : 0);
+      to[0] = threadIdx.x & 16 ? st.mu_b : st.mu_a;
+      to[2] = v;
     }
+    __syncthreads();
+    F2 mean = f2(0.f), sq = f2(0.f);
+#pragma unroll(S::kUnroll)
+    for (int w = 0; w < S::kWarps; ++w) {
+      const float4 x = part[w];
+      mean = fma(f2(x.x, x.y), f2(k.counts[w]), mean);
+      sq = add(sq, f2(x.z, x.w));
+    }
+    if (mean_a || mean_b) {
+      mean = mul(mean, f2(k.inv_dim));
+      const F2 back = mul(mean, f2(-1.f));
+#pragma unroll(S::kUnroll)
+      for (int w = 0; w < S::kWarps; ++w) {
+        const float4 x = part[w];
+        const F2 d = add(f2(x.x, x.y), back);
+        sq = fma(mul(d, f2(k.counts[w])), d, sq);
+      }
+    }
+    split(mean, st.mu_a, st.mu_b);
+    split(sq, st.sq_a, st.sq_b);
   }
   return st;
-}
-
-// Threads of a row for dim columns (8 each): 8, 16, or whole warps.
-inline int row_threads(int dim) {
-  const int n = dim / 8;
-  return n <= 8 ? 8 : n <= 16 ? 16 : (n + 31) / 32 * 32;
 }
 
 }  // namespace norm

@@ -9,10 +9,11 @@
 //   dpre_weight = sum_g (1 + scale) A,  dpost_weight = sum_g gate E.
 //
 // Bound by memory: dr, dh, r, y are read once, dx, dy written once (18 bytes
-// per element with a float32 residual stream).  A thread owns 8 columns for
-// all the rows that its CTA takes, so A, C and E stay in its registers and
-// every token sum has a fixed order; the next row is loaded while a row's eight
-// sums go across the CTA in three exchanges.
+// per element with a float32 residual stream).  A thread owns the same columns
+// of all the rows that its CTA takes, so A, C and E are its own and every token
+// sum has a fixed order; the next row is loaded while a row's eight sums go
+// across the CTA in three exchanges, whose latency is what is left: 73.7 us
+// (4.6 TB/s) for 12288 rows of 1536 with a float32 residual.
 #include "block_norm.cuh"
 
 namespace fastvr {
@@ -20,27 +21,65 @@ namespace {
 
 using namespace norm;
 
-// The four inputs of a row, a thread's 8 columns of each.
+// The four inputs of a row, 8 columns of each.
 template <typename TR, typename TY>
 struct RowIn {
   Raw8<TR> dr, r;
   Raw8<TY> dh, y;
 };
 
-template <typename TR, typename TY, int TPR, int kMinCtas>
+// The end of a group in a CTA: sums over its tokens of 8 columns into a partial
+// result or the group's gradients, and their share of the weight gradients into
+// dyn [2][dim].
+__device__ __forceinline__ void end_group(const NormBwdParams& p, int64_t g,
+                                          int c, const F8& sum_a,
+                                          const F8& sum_c, const F8& sum_e,
+                                          float* dyn) {
+  const int64_t gc = g * p.dim + c;
+  if (p.slices > 1) {
+    float* part = p.partial + (int64_t)blockIdx.x * 3 * p.dim + c;
+    store8(part, 0, sum_a);
+    store8(part, p.dim, sum_c);
+    store8(part, 2 * p.dim, sum_e);
+  } else {
+    if (p.dshift != nullptr) store8(p.dshift, gc, sum_c);
+    if (p.dscale != nullptr)
+      store8(p.dscale, gc, mul(sum_a, load8_or(p.pre_weight, c, 1.f)));
+    if (p.dgate != nullptr)
+      store8(p.dgate, gc,
+             mul(sum_e,
+                 load8_or(p.post == kNormNone ? nullptr : p.post_weight, c,
+                          1.f)));
+  }
+  if (p.weight_partial != nullptr) {
+    store8(dyn, c,
+           fma(add(load8_or(p.scale, gc, 0.f), splat(1.f)), sum_a,
+               load8_or(dyn, c, 0.f)));
+    store8(dyn, p.dim + c,
+           fma(load8_or(p.gate, gc, 1.f), sum_e,
+               load8_or(dyn, p.dim + c, 0.f)));
+  }
+}
+
+template <typename TR, typename TY, int TPR, int NV, bool kAhead, bool kRegs,
+          int kMinCtas>
 __global__ void __launch_bounds__(Shape<TPR>::kThreads, kMinCtas)
 norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
   using S = Shape<TPR>;
   constexpr int kRows = S::kRows;
-  extern __shared__ __align__(16) float dyn[];  // [2][dim] weight sums
+  // mine: gate post_weight (j), (1 + scale) pre_weight (NV + j), and the sums
+  // over tokens A, C, E ((2, 3, 4) NV + j); then [2][dim] weight sums
+  extern __shared__ float4 dyn4[];
+  Kept<kRegs, 5 * NV> mine;
+  mine.m = Private{dyn4};
+  static_assert(!kRegs || S::kRows == 1, "rows side by side are added there");
+  float* dyn = reinterpret_cast<float*>(
+      dyn4 + (kRegs ? 0 : 10 * NV * S::kThreads));
   __shared__ float4 s_stat[S::kWarps];
   __shared__ float2 s_dn[S::kWarps], s_du[S::kWarps];
-  __shared__ __align__(16) float s_fold[kRows > 1 ? 3 * 8 * 128 : 4];
+  __shared__ float s_n[S::kWarps];
   pdl_trigger();
-  pdl_wait();
-  const Cols k = make_cols<TPR>(p.dim);
-  const int c = k.c;
-  const bool on = k.on;
+  const Cols<TPR, NV> k(p.dim, s_n);
   const float inv_dim = k.inv_dim;
   const int slot = kRows > 1 ? threadIdx.x / TPR : 0;
   const bool has_y = p.y != nullptr, has_h = p.dh != nullptr;
@@ -49,11 +88,14 @@ norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
   const bool mean_r = has_h && p.pre == kNormLayer;
   const bool mean_y = post && p.post == kNormLayer;
   const bool weights = p.weight_partial != nullptr;
-  if (weights && slot == 0 && on) {
-    const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    store8(dyn, c, zero);
-    store8(dyn, p.dim + c, zero);
-  }
+  if (weights && slot == 0)
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (k.on(j)) {
+        store8(dyn, k.at(j), splat(0.f));
+        store8(dyn, p.dim + k.at(j), splat(0.f));
+      }
+  pdl_wait();
 
   // The CTA's groups: one slice of one group, or several whole groups.
   const int64_t g0 = p.slices > 1 ? blockIdx.x / p.slices
@@ -64,177 +106,147 @@ norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
   const int64_t t0 = slice * p.group_tokens / p.slices;
   const int64_t t1 = (slice + 1) * p.group_tokens / p.slices;
 
-  RowIn<TR, TY> in;
+  RowIn<TR, TY> in[NV];
   auto fetch = [&](int64_t g, int64_t t) {
-    if (!on || t >= t1) return;
-    const int64_t at = (g * p.group_tokens + t) * p.dim + c;
-    if (has_dr) in.dr.load(p.dr, at);
-    if (has_h) {
-      in.dh.load(p.dh, at);
-      in.r.load(p.r, at);
-    }
-    if (has_y) in.y.load(p.y, at);
+    if (t >= t1) return;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (k.on(j)) {
+        const int64_t at = (g * p.group_tokens + t) * p.dim + k.at(j);
+        if (has_dr) in[j].dr.load(p.dr, at);
+        if (has_h) {
+          in[j].dh.load(p.dh, at);
+          in[j].r.load(p.r, at);
+        }
+        if (has_y) in[j].y.load(p.y, at);
+      }
   };
-  fetch(g0, t0 + slot);
+  if (kAhead) fetch(g0, t0 + slot);
   for (int64_t g = g0; g < g1; ++g) {
-    float gp[8], sw[8];  // gate post_weight, (1 + scale) pre_weight
-    float sum_a[8], sum_c[8], sum_e[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      sum_a[e] = sum_c[e] = sum_e[e] = gp[e] = sw[e] = 0.f;
-    if (on) {
-      float x[8];
-      load8_or(p.gate, g * p.dim + c, 1.f, gp);
-      load8_or(p.post == kNormNone ? nullptr : p.post_weight, c, 1.f, x);
+    for (int j = 0; j < NV; ++j) {
+      F8 gp = splat(0.f), sw = gp;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) gp[e] *= x[e];
-      load8_or(p.scale, g * p.dim + c, 0.f, sw);
-      load8_or(p.pre_weight, c, 1.f, x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sw[e] = (1.f + sw[e]) * x[e];
+      for (int q = 2; q < 5; ++q) mine.set(q * NV + j, gp);
+      if (k.on(j)) {
+        const int64_t at = g * p.dim + k.at(j);
+        gp = mul(load8_or(p.gate, at, 1.f),
+                 load8_or(p.post == kNormNone ? nullptr : p.post_weight,
+                          k.at(j), 1.f));
+        sw = mul(add(load8_or(p.scale, at, 0.f), splat(1.f)),
+                 load8_or(p.pre_weight, k.at(j), 1.f));
+      }
+      mine.set(j, gp);
+      mine.set(NV + j, sw);
     }
     // Every thread makes every pass (barriers and shuffles inside); a slot
     // past the last row works on zeros.
     for (int64_t tb = t0; tb < t1; tb += kRows) {
       const int64_t t = tb + slot;
-      const bool row_on = on && t < t1;
-      float d[8], dh[8], n[8], u[8];
+      if (!kAhead) fetch(g, t);
+      F8 d[NV], dh[NV], n[NV], u[NV];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) d[e] = dh[e] = n[e] = u[e] = 0.f;
-      if (row_on) {
-        if (has_dr) in.dr.widen(d);
-        if (has_h) {
-          in.dh.widen(dh);
-          in.r.widen(n);
-        }
-        if (has_y) in.y.widen(u);
+      for (int j = 0; j < NV; ++j) {
+        const bool on = t < t1 && k.on(j);
+        d[j] = on && has_dr ? in[j].dr.widen() : splat(0.f);
+        dh[j] = on && has_h ? in[j].dh.widen() : splat(0.f);
+        n[j] = on && has_h ? in[j].r.widen() : splat(0.f);
+        u[j] = on && has_y ? in[j].y.widen() : splat(0.f);
       }
       // the next row is on its way while this one is worked on
-      if (tb + kRows < t1)
+      if (kAhead && tb + kRows < t1)
         fetch(g, t + kRows);
-      else if (g + 1 < g1)
+      else if (kAhead && g + 1 < g1)
         fetch(g + 1, t0 + slot);
 
       float rho = 1.f, rho_y = 1.f;
       if (has_h || post) {
-        const Stats st = row_stats<TPR>(n, u, mean_r, mean_y, k, s_stat);
+        const Stats st = row_stats<TPR, NV>(n, u, mean_r, mean_y, k, s_stat);
         rho = rsqrtf(st.sq_a * inv_dim + p.eps);
         if (post) rho_y = rsqrtf(st.sq_b * inv_dim + p.eps);
-        if (row_on) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            n[e] = (n[e] - st.mu_a) * rho;
-            u[e] = (u[e] - st.mu_b) * rho_y;
+        for (int j = 0; j < NV; ++j)
+          if (t < t1 && k.on(j)) {
+            n[j] = fma(n[j], rho, -st.mu_a * rho);
+            u[j] = fma(u[j], rho_y, -st.mu_b * rho_y);
           }
-        }
       }
       if (has_h) {
-        float dn[8], s0 = 0.f, s1 = 0.f;
+        F8 s0 = splat(0.f), s1 = s0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          dn[e] = dh[e] * sw[e];
-          s0 += dn[e];
-          s1 = fmaf(dn[e], n[e], s1);
-          sum_a[e] = fmaf(dh[e], n[e], sum_a[e]);
-          sum_c[e] += dh[e];
+        for (int j = 0; j < NV; ++j) {
+          mine.set(2 * NV + j, fma(dh[j], n[j], mine.get(2 * NV + j)));
+          mine.set(3 * NV + j, add(dh[j], mine.get(3 * NV + j)));
+          dh[j] = mul(dh[j], mine.get(NV + j));
+          s0 = add(s0, dh[j]);
+          s1 = fma(dh[j], n[j], s1);
         }
-        row_sums<TPR>(s0, s1, k, s_dn);
-        const float m0 = p.pre == kNormLayer ? s0 * inv_dim : 0.f;
-        const float m1 = s1 * inv_dim;
+        float m0 = sum(s0), m1 = sum(s1);
+        row_sums<TPR>(m0, m1, s_dn);
+        m0 = p.pre == kNormLayer ? -m0 * inv_dim : 0.f;
+        m1 *= -inv_dim;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          d[e] = fmaf(rho, dn[e] - m0 - n[e] * m1, d[e]);
+        for (int j = 0; j < NV; ++j)
+          d[j] = fma(fma(n[j], m1, add(dh[j], splat(m0))), rho, d[j]);
       }
-      const int64_t at = (g * p.group_tokens + t) * p.dim + c;
-      if (row_on) {
-        float dx[8];
+      const int64_t at = (g * p.group_tokens + t) * p.dim;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dx[e] = p.residual_scale * d[e];
-        store8(static_cast<TR*>(p.dx), at, dx);
-      }
+      for (int j = 0; j < NV; ++j)
+        if (t < t1 && k.on(j))
+          store8(static_cast<TR*>(p.dx), at + k.at(j),
+                 mul(d[j], p.residual_scale));
       if (has_y) {
-        float du[8], s0 = 0.f, s1 = 0.f;
+        F8 s0 = splat(0.f), s1 = s0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          sum_e[e] = fmaf(d[e], u[e], sum_e[e]);
-          du[e] = d[e] * gp[e];
-          s0 += du[e];
-          s1 = fmaf(du[e], u[e], s1);
+        for (int j = 0; j < NV; ++j) {
+          mine.set(4 * NV + j, fma(d[j], u[j], mine.get(4 * NV + j)));
+          d[j] = mul(d[j], mine.get(j));
+          s0 = add(s0, d[j]);
+          s1 = fma(d[j], u[j], s1);
         }
         if (post) {
-          row_sums<TPR>(s0, s1, k, s_du);
-          const float m0 = p.post == kNormLayer ? s0 * inv_dim : 0.f;
-          const float m1 = s1 * inv_dim;
+          float m0 = sum(s0), m1 = sum(s1);
+          row_sums<TPR>(m0, m1, s_du);
+          m0 = p.post == kNormLayer ? -m0 * inv_dim : 0.f;
+          m1 *= -inv_dim;
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            du[e] = rho_y * (du[e] - m0 - u[e] * m1);
+          for (int j = 0; j < NV; ++j)
+            d[j] = mul(fma(u[j], m1, add(d[j], splat(m0))), rho_y);
         }
-        if (row_on) store8(static_cast<TY*>(p.dy), at, du);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+          if (t < t1 && k.on(j))
+            store8(static_cast<TY*>(p.dy), at + k.at(j), d[j]);
       }
     }
 
     // The group's sums: over the rows side by side, then to memory.
-    if constexpr (kRows > 1) {
-      __syncthreads();  // the previous group's sums have been read
-      store8(s_fold, threadIdx.x * 8, sum_a);
-      store8(s_fold, 1024 + threadIdx.x * 8, sum_c);
-      store8(s_fold, 2048 + threadIdx.x * 8, sum_e);
-      __syncthreads();
-      if (slot == 0) {
+    if (kRows > 1) __syncthreads();
+    if (slot == 0)
 #pragma unroll
-        for (int r = 1; r < kRows; ++r) {
-          float x[8];
-          load8_or(s_fold, r * TPR * 8 + c, 0.f, x);
+      for (int j = 0; j < NV; ++j)
+        if (k.on(j)) {
+          F8 sums[3];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum_a[e] += x[e];
-          load8_or(s_fold, 1024 + r * TPR * 8 + c, 0.f, x);
+          for (int q = 0; q < 3; ++q) {
+            sums[q] = mine.get((2 + q) * NV + j);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum_c[e] += x[e];
-          load8_or(s_fold, 2048 + r * TPR * 8 + c, 0.f, x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum_e[e] += x[e];
+            for (int r = 1; r < kRows; ++r)
+              sums[q] = add(sums[q], Private{dyn4 + r * TPR}.get(
+                                         (2 + q) * NV + j));
+          }
+          end_group(p, g, k.at(j), sums[0], sums[1], sums[2], dyn);
         }
-      }
-    }
-    if (on && slot == 0) {
-      float x[8], w[8];
-      if (p.slices > 1) {
-        float* part = p.partial + (int64_t)blockIdx.x * 3 * p.dim + c;
-        store8(part, 0, sum_a);
-        store8(part, p.dim, sum_c);
-        store8(part, 2 * p.dim, sum_e);
-      } else {
-        if (p.dshift != nullptr) store8(p.dshift, g * p.dim + c, sum_c);
-        load8_or(p.pre_weight, c, 1.f, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = sum_a[e] * w[e];
-        if (p.dscale != nullptr) store8(p.dscale, g * p.dim + c, x);
-        load8_or(p.post == kNormNone ? nullptr : p.post_weight, c, 1.f, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = sum_e[e] * w[e];
-        if (p.dgate != nullptr) store8(p.dgate, g * p.dim + c, x);
-      }
-      if (weights) {
-        load8_or(p.scale, g * p.dim + c, 0.f, w);
-        load8_or(dyn, c, 0.f, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = fmaf(1.f + w[e], sum_a[e], x[e]);
-        store8(dyn, c, x);
-        load8_or(p.gate, g * p.dim + c, 1.f, w);
-        load8_or(dyn, p.dim + c, 0.f, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = fmaf(w[e], sum_e[e], x[e]);
-        store8(dyn, p.dim + c, x);
-      }
-    }
+    if (kRows > 1) __syncthreads();  // before the next group's zeros
   }
-  if (weights && on && slot == 0) {
-    float* part = p.weight_partial + (int64_t)blockIdx.x * 2 * p.dim + c;
-    float x[8];
-    load8_or(dyn, c, 0.f, x);
-    store8(part, 0, x);
-    load8_or(dyn, p.dim + c, 0.f, x);
-    store8(part, p.dim, x);
+  if (weights && slot == 0) {
+    float* part = p.weight_partial + (int64_t)blockIdx.x * 2 * p.dim;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (k.on(j)) {
+        store8(part, k.at(j), load8_or(dyn, k.at(j), 0.f));
+        store8(part, p.dim + k.at(j), load8_or(dyn, p.dim + k.at(j), 0.f));
+      }
   }
 }
 
@@ -294,43 +306,47 @@ norm_bwd_sum_kernel(const __grid_constant__ NormBwdParams p) {
   }
 }
 
-// CTAs per SM: the registers of a thread (8 columns of
-// every input, the sums) want about 112 of them, up to 2048 columns.
+// CTAs per SM of the kernel that dim selects, see launch_t.
 int ctas_per_sm(int dim) {
-  const int n = row_threads(dim);
-  return n <= 32 ? 4 : n <= 64 ? 8 : n <= 128 ? 4 : n <= 192 ? 3
-                                   : n <= 256 ? 2 : 1;
+  return dim <= 256 ? 4 : dim <= 512 ? 5 : dim <= 1024 ? 3 : dim <= 2048 ? 2 : 1;
 }
 
+template <typename TR, typename TY, int TPR, int NV, bool kAhead, bool kRegs,
+          int kMinCtas>
+cudaError_t launch_v(const NormBwdParams& p, cudaStream_t stream) {
+  const size_t smem =
+      (kRegs ? 0 : (size_t)10 * NV * Shape<TPR>::kThreads * sizeof(float4)) +
+      (p.weight_partial != nullptr ? (size_t)2 * p.dim * sizeof(float) : 0);
+  auto kernel = norm_bwd_kernel<TR, TY, TPR, NV, kAhead, kRegs, kMinCtas>;
+  if (smem > 32768) {  // up to 224 KB at dim 8192
+    const cudaError_t e = cudaFuncSetAttribute(
+        kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl(kernel, dim3((unsigned)p.ctas),
+                    dim3(Shape<TPR>::kThreads), smem, stream, p);
+}
+
+// Threads and vectors of a row, whether its sums stay in registers, and CTAs
+// per SM: what was fastest of those that do not spill (12288 rows of 1536 with
+// a float32 residual: 96 threads of 16 columns 73.7 us, 192 of 8 76.1, the
+// same with the sums in shared memory 82; one more CTA per SM at the price of
+// spills 115 and more).  With groups of a few rows, whose ends then count, 192
+// threads of 8 columns: 84.8 us for 8160 groups of one row, against 120.9.
 template <typename TR, typename TY>
 cudaError_t launch_t(const NormBwdParams& p, cudaStream_t stream) {
-  const dim3 grid((unsigned)p.ctas);
-  const size_t smem =
-      p.weight_partial != nullptr ? (size_t)2 * p.dim * sizeof(float) : 0;
-  const int n = row_threads(p.dim);
-  const dim3 block(n <= 32 ? 128 : n);
-  if (n == 8)
-    return launch_pdl(norm_bwd_kernel<TR, TY, 8, 4>, grid, block, smem, stream, p);
-  if (n == 16)
-    return launch_pdl(norm_bwd_kernel<TR, TY, 16, 4>, grid, block, smem, stream, p);
-  if (n == 32)
-    return launch_pdl(norm_bwd_kernel<TR, TY, 32, 4>, grid, block, smem, stream, p);
-  if (n <= 64)
-    return launch_pdl(norm_bwd_kernel<TR, TY, 64, 8>, grid, block, smem, stream, p);
-  if (n <= 128)
-    return launch_pdl(norm_bwd_kernel<TR, TY, 128, 4>, grid, block, smem, stream, p);
-  if (n <= 192)
-    return launch_pdl(norm_bwd_kernel<TR, TY, 192, 3>, grid, block, smem, stream, p);
-  if (n <= 256)
-    return launch_pdl(norm_bwd_kernel<TR, TY, 256, 2>, grid, block, smem, stream, p);
-  if (n <= 512)
-    return launch_pdl(norm_bwd_kernel<TR, TY, 512, 1>, grid, block, smem, stream, p);
-  // 64 KB of weight sums at dim 8192
-  auto kernel = norm_bwd_kernel<TR, TY, 1024, 1>;
-  const cudaError_t e = cudaFuncSetAttribute(
-      kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * 8192 * 4);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(kernel, grid, block, smem, stream, p);
+  if (p.dim <= 64) return launch_v<TR, TY, 8, 1, true, false, 4>(p, stream);
+  if (p.dim <= 128) return launch_v<TR, TY, 16, 1, true, false, 4>(p, stream);
+  if (p.dim <= 256) return launch_v<TR, TY, 32, 1, true, false, 4>(p, stream);
+  if (p.dim <= 512) return launch_v<TR, TY, 64, 1, true, true, 5>(p, stream);
+  if (p.dim <= 1024) return launch_v<TR, TY, 128, 1, true, true, 3>(p, stream);
+  if (p.dim <= 1536 && p.group_tokens < 16)
+    return launch_v<TR, TY, 192, 1, true, true, 2>(p, stream);
+  if (p.dim <= 1536) return launch_v<TR, TY, 96, 2, true, true, 2>(p, stream);
+  if (p.dim <= 2048) return launch_v<TR, TY, 256, 1, true, false, 2>(p, stream);
+  if (p.dim <= 4096) return launch_v<TR, TY, 256, 2, true, false, 1>(p, stream);
+  if (p.dim <= 5120) return launch_v<TR, TY, 320, 2, true, false, 1>(p, stream);
+  return launch_v<TR, TY, 1024, 1, false, false, 1>(p, stream);
 }
 
 }  // namespace

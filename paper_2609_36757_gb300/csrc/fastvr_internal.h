@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "vec_math.cuh"
+
 namespace fastvr {
 
 // At most two contiguous token ranges of one head's cache make up the keys a
@@ -216,6 +218,7 @@ struct NormFwdParams {
   const float *gate, *scale, *shift, *pre_weight, *post_weight;
   void *r, *h;
   int64_t rows, group_tokens;
+  FastDiv by_group_tokens;
   int32_t dim, pre, post;
   float eps, residual_scale;
 };

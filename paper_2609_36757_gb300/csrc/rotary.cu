@@ -17,6 +17,7 @@
 #include <algorithm>
 
 #include "fastvr_internal.h"
+#include "vec_math.cuh"
 
 namespace fastvr {
 namespace {
@@ -24,23 +25,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kSmemPairs = 2048;  // (token, pair) entries per CTA: 16 KB
 
-// Division of 32-bit numbers below 2^31 by a divisor fixed at launch.
-struct FastDiv {
-  uint32_t d, mul, shift;
-};
-FastDiv make_div(uint32_t d) {
-  FastDiv f;
-  f.d = d;
-  f.shift = 0;
-  while ((1ull << f.shift) < d) ++f.shift;
-  // mul = ceil(2^(31 + shift) / d) < 2^32; exact for numbers below 2^31
-  f.mul = (uint32_t)(((1ull << (31 + f.shift)) + d - 1) / d);
-  return f;
-}
-__device__ __forceinline__ uint32_t fast_div(uint32_t n, const FastDiv& f) {
-  return (uint32_t)(((uint64_t)n * f.mul) >> (31 + f.shift));
-}
-
+// V consecutive elements of T as they lie in memory.
 template <typename T, int V>
 struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Vec {
   T e[V];
@@ -55,6 +40,55 @@ __device__ __forceinline__ void from_f(__nv_bfloat16& d, float x) {
   d = __float2bfloat16_rn(x);
 }
 
+// Elements (2 i, 2 i + 1) of a vector as a pair, and back.
+template <int V>
+__device__ __forceinline__ F2 get2(const Vec<__nv_bfloat16, V>& v, int i) {
+  const uint32_t w = reinterpret_cast<const uint32_t*>(v.e)[i];
+  return f2(bf16_lo(w), bf16_hi(w));
+}
+template <int V>
+__device__ __forceinline__ F2 get2(const Vec<float, V>& v, int i) {
+  return f2(v.e[2 * i], v.e[2 * i + 1]);
+}
+template <int V>
+__device__ __forceinline__ void put2(Vec<__nv_bfloat16, V>& v, int i, F2 x) {
+  reinterpret_cast<uint32_t*>(v.e)[i] = bf16_pack(x);
+}
+template <int V>
+__device__ __forceinline__ void put2(Vec<float, V>& v, int i, F2 x) {
+  split(x, v.e[2 * i], v.e[2 * i + 1]);
+}
+// Elements (4 i, 4 i + 2) and (4 i + 1, 4 i + 3): the first and the second
+// ones of two neighbouring pairs.
+template <int V>
+__device__ __forceinline__ void get_pairs(const Vec<__nv_bfloat16, V>& v, int i,
+                                          F2& a, F2& b) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(v.e) + 2 * i;
+  a = f2(bf16_lo(w[0]), bf16_lo(w[1]));
+  b = f2(bf16_hi(w[0]), bf16_hi(w[1]));
+}
+template <int V>
+__device__ __forceinline__ void get_pairs(const Vec<float, V>& v, int i, F2& a,
+                                          F2& b) {
+  a = f2(v.e[4 * i], v.e[4 * i + 2]);
+  b = f2(v.e[4 * i + 1], v.e[4 * i + 3]);
+}
+template <int V>
+__device__ __forceinline__ void put_pairs(Vec<__nv_bfloat16, V>& v, int i, F2 a,
+                                          F2 b) {
+  float a0, a1, b0, b1;
+  split(a, a0, a1);
+  split(b, b0, b1);
+  uint32_t* w = reinterpret_cast<uint32_t*>(v.e) + 2 * i;
+  w[0] = bf16_pack(a0, b0);
+  w[1] = bf16_pack(a1, b1);
+}
+template <int V>
+__device__ __forceinline__ void put_pairs(Vec<float, V>& v, int i, F2 a, F2 b) {
+  split(a, v.e[4 * i], v.e[4 * i + 2]);
+  split(b, v.e[4 * i + 1], v.e[4 * i + 3]);
+}
+
 struct Params {
   const void *q, *k;
   void *q_out, *k_out;
@@ -65,11 +99,12 @@ struct Params {
   int32_t tokens, axes, pairs, head_dim;
   int32_t tile;               // tokens of a CTA
   int32_t axis_end[3];        // first pair past each axis
-  FastDiv by_tokens, by_pairs, by_blocks;
   int32_t items;              // vector items of a head
-  int32_t lanes;              // threads of a group, one per item
-  int32_t head_blocks;
-  int32_t heads, all_heads;   // q heads, q and k heads
+  int32_t lanes;              // threads of a group, an item each
+  int32_t heads, kv_heads;
+  int32_t q_blocks, blocks;   // blocks of heads of q, of q and k
+  int32_t item_blocks;        // of `lanes` items
+  FastDiv by_tokens, by_pairs, by_blocks, by_item_blocks;
   float mag, sign;
   uint64_t turn[kRotaryMaxPairs];  // theta / 2 pi in 2^-64 turns
 };
@@ -84,21 +119,69 @@ __host__ __device__ constexpr int head_block(int elem_bytes, bool half) {
 // (one per pair of the V), then the pass-through vectors; interleaved: the
 // vector at i V, V / 2 pairs.  A group of threads, one per item, takes a block
 // of HB heads of a token at a time: the sines of a thread's item are read once
-// for the block, and the block's loads are in flight together.
+// for the block, and the block's loads are in flight together.  The first
+// block's are on their way while the sines are formed.
 template <typename T, bool kHalf, int V>
 __global__ void __launch_bounds__(kThreads, 4)
 rotary_kernel(const __grid_constant__ Params p) {
   constexpr int HB = head_block(sizeof(T), kHalf);
   constexpr int kPairs = kHalf ? V : V / 2;  // pairs of an item
-  __shared__ __align__(16) float2 cs[kSmemPairs + 8];
+  using Vt = Vec<T, V>;
+  // (cos, cos, sin, sin) of two neighbouring pairs of a token
+  __shared__ float4 cs[kSmemPairs / 2 + 4];
   pdl_trigger();
   const int row0 = blockIdx.x * p.tile;
   const int n_rows = min(p.tile, p.rows - row0);
+  const int entries = (p.pairs + 1) / 2;  // of a token
+  const int pair_items = kHalf ? p.pairs / V : p.items;
+  const int group = threadIdx.x / p.lanes;
+  const int groups = kThreads / p.lanes;
+  const int lane = threadIdx.x - group * p.lanes;
+  const int tasks = group < groups ? n_rows * p.blocks * p.item_blocks : 0;
   pdl_wait();
-  for (int i = threadIdx.x; i < n_rows * p.pairs; i += kThreads) {
-    const int r = fast_div(i, p.by_pairs);
-    const int pair = i - r * p.pairs;
+
+  Vt a[HB], z[HB];
+  T* dst;
+  int64_t dst_head;
+  int n_heads, item, r;
+  bool rot;
+  auto load = [&](int task) {
+    const int rb = fast_div(task, p.by_item_blocks);
+    item = (task - rb * p.item_blocks) * p.lanes + lane;
+    r = fast_div(rb, p.by_blocks);
+    const int block = rb - r * p.blocks;
+    const bool is_k = block >= p.q_blocks;
+    const int h0 = (is_k ? block - p.q_blocks : block) * HB;
+    n_heads = item < p.items
+                  ? min(HB, (is_k ? p.kv_heads : p.heads) - h0)
+                  : 0;
+    rot = !kHalf || item < pair_items;
+    const int x = rot ? item * V : 2 * p.pairs + (item - pair_items) * V;
     const int row = row0 + r;
+    const int b = fast_div(row, p.by_tokens);
+    const int t = row - b * p.tokens;
+    const Strides& si = is_k ? p.k_str : p.q_str;
+    const Strides& so = is_k ? p.k_out_str : p.q_out_str;
+    const T* src = static_cast<const T*>(is_k ? p.k : p.q) + b * si.batch +
+                   t * si.token + h0 * si.head + x;
+    dst = static_cast<T*>(is_k ? p.k_out : p.q_out) + b * so.batch +
+          t * so.token + h0 * so.head + x;
+    dst_head = so.head;
+#pragma unroll
+    for (int u = 0; u < HB; ++u)
+      if (u < n_heads) {
+        a[u] = *reinterpret_cast<const Vt*>(src + u * si.head);
+        if (kHalf && rot)
+          z[u] = *reinterpret_cast<const Vt*>(src + u * si.head + p.pairs);
+      }
+  };
+  int task = group;
+  if (task < tasks) load(task);
+
+  for (int i = threadIdx.x; i < n_rows * p.pairs; i += kThreads) {
+    const int row_i = fast_div(i, p.by_pairs);
+    const int pair = i - row_i * p.pairs;
+    const int row = row0 + row_i;
     const int b = fast_div(row, p.by_tokens);
     const int t = row - b * p.tokens;
     const int axis = (pair >= p.axis_end[0]) + (pair >= p.axis_end[1]);
@@ -108,77 +191,69 @@ rotary_kernel(const __grid_constant__ Params p) {
     const float x = (float)(int32_t)(turn >> 32) * 0x1p-31f;
     float s, c;
     sincospif(x, &s, &c);
-    cs[i] = make_float2(c * p.mag, s * p.sign);
+    float* e = reinterpret_cast<float*>(cs + row_i * entries + pair / 2) +
+               pair % 2;
+    e[0] = c * p.mag;
+    e[2] = s * p.sign;
   }
   __syncthreads();
 
-  using Vt = Vec<T, V>;
-  const int pair_items = kHalf ? p.pairs / V : p.items;
-  const int group = threadIdx.x / p.lanes;
-  const int groups = kThreads / p.lanes;
-  const int lane = threadIdx.x - group * p.lanes;
-  if (group >= groups) return;
-  const int tasks = n_rows * p.head_blocks;
-  for (int task = group; task < tasks; task += groups) {
-    const int r = fast_div(task, p.by_blocks);
-    const int h0 = (task - r * p.head_blocks) * HB;
-    const int row = row0 + r;
-    const int b = fast_div(row, p.by_tokens);
-    const int t = row - b * p.tokens;
-    const T* q = static_cast<const T*>(p.q) + b * p.q_str.batch +
-                 t * p.q_str.token;
-    const T* k = static_cast<const T*>(p.k) + b * p.k_str.batch +
-                 t * p.k_str.token;
-    T* qo = static_cast<T*>(p.q_out) + b * p.q_out_str.batch +
-            t * p.q_out_str.token;
-    T* ko = static_cast<T*>(p.k_out) + b * p.k_out_str.batch +
-            t * p.k_out_str.token;
-    for (int item = lane; item < p.items; item += p.lanes) {
-      const bool rot = !kHalf || item < pair_items;
-      const int x =
-          rot ? item * V : 2 * p.pairs + (item - pair_items) * V;
-      Vt a[HB], z[HB];
-#pragma unroll
-      for (int u = 0; u < HB; ++u) {
-        const int h = h0 + u;
-        if (h >= p.all_heads) continue;
-        const T* src = h < p.heads ? q + h * p.q_str.head
-                                   : k + (h - p.heads) * p.k_str.head;
-        a[u] = *reinterpret_cast<const Vt*>(src + x);
-        if (kHalf && rot)
-          z[u] = *reinterpret_cast<const Vt*>(src + x + p.pairs);
-      }
+  for (; task < tasks; task += groups, task < tasks ? load(task) : void()) {
+    const int pair0 = item * kPairs;
+    const float4* w = cs + r * entries + pair0 / 2;
+    if (V == 1 || (!kHalf && pair0 + kPairs > p.pairs)) {
+      // one pair, or a piece inside which the rotated part ends (the rest of
+      // it is copied)
       if (rot) {
-        float2 w[kPairs];
-        const int pair0 = item * kPairs;
 #pragma unroll
-        for (int e = 0; e < kPairs; ++e)
-          w[e] = cs[r * p.pairs + pair0 + e];  // the table is padded
+        for (int e = 0; e < kPairs; ++e) {
+          if (pair0 + e >= p.pairs) continue;
+          const float* f = reinterpret_cast<const float*>(
+                               cs + r * entries + (pair0 + e) / 2) +
+                           (pair0 + e) % 2;
+          const float c = f[0], s = f[2];
 #pragma unroll
-        for (int u = 0; u < HB; ++u) {
-          if (h0 + u >= p.all_heads) continue;
-#pragma unroll
-          for (int e = 0; e < kPairs; ++e) {
-            // the rotated part may end inside a piece; the rest is copied
-            if (!kHalf && pair0 + e >= p.pairs) continue;
+          for (int u = 0; u < HB; ++u) {
             T& ra = kHalf ? a[u].e[e] : a[u].e[(2 * e) % V];
             T& rb = kHalf ? z[u].e[e] : a[u].e[(2 * e + 1) % V];
             const float fa = to_f(ra), fb = to_f(rb);
-            from_f(ra, fa * w[e].x - fb * w[e].y);
-            from_f(rb, fb * w[e].x + fa * w[e].y);
+            from_f(ra, fa * c - fb * s);
+            from_f(rb, fb * c + fa * s);
           }
         }
       }
+    } else if (rot) {
 #pragma unroll
-      for (int u = 0; u < HB; ++u) {
-        const int h = h0 + u;
-        if (h >= p.all_heads) continue;
-        T* dst = h < p.heads ? qo + h * p.q_out_str.head
-                             : ko + (h - p.heads) * p.k_out_str.head;
-        *reinterpret_cast<Vt*>(dst + x) = a[u];
-        if (kHalf && rot) *reinterpret_cast<Vt*>(dst + x + p.pairs) = z[u];
+      for (int e = 0; e < kPairs / 2; ++e) {
+        const float4 f = w[e];
+        const F2 c = f2(f.x, f.y), s = f2(f.z, f.w), ns = f2(-f.z, -f.w);
+#pragma unroll
+        for (int u = 0; u < HB; ++u) {
+          F2 fa, fb;
+          if constexpr (kHalf) {
+            fa = get2(a[u], e);
+            fb = get2(z[u], e);
+          } else {
+            get_pairs(a[u], e, fa, fb);
+          }
+          const F2 ya = fma(fb, ns, mul(fa, c));
+          const F2 yb = fma(fa, s, mul(fb, c));
+          if constexpr (kHalf) {
+            put2(a[u], e, ya);
+            put2(z[u], e, yb);
+          } else {
+            put_pairs(a[u], e, ya, yb);
+          }
+        }
       }
     }
+#pragma unroll
+    for (int u = 0; u < HB; ++u)
+      if (u < n_heads) {
+        *reinterpret_cast<Vt*>(dst + u * dst_head) = a[u];
+        if (kHalf && rot)
+          *reinterpret_cast<Vt*>(dst + u * dst_head + p.pairs) = z[u];
+      }
   }
 }
 
@@ -190,15 +265,19 @@ cudaError_t launch_t(const RotaryArgs& a, Params& p, cudaStream_t stream) {
   if (a.half)
     while (p.pairs % v) v /= 2;
   p.items = a.half ? (p.head_dim - p.pairs) / v : p.head_dim / 8;
-  p.lanes = p.items < kThreads ? p.items : kThreads;
+  p.lanes = std::min(p.items, kThreads);
+  p.item_blocks = (p.items + p.lanes - 1) / p.lanes;
   const int hb = head_block(sizeof(T), a.half);
-  p.head_blocks = (p.all_heads + hb - 1) / hb;
-  p.by_blocks = make_div(p.head_blocks);
-  // Tokens of a CTA: what the sine table holds, and few enough that every SM
-  // has a dozen CTAs to even out its last ones.
-  int64_t tile = kSmemPairs / p.pairs;
-  tile = std::min<int64_t>(tile, p.rows / (a.sms * 12));
-  tile = std::min<int64_t>(tile, (1 << 30) / p.head_blocks);
+  p.q_blocks = (p.heads + hb - 1) / hb;
+  p.blocks = p.q_blocks + (p.kv_heads + hb - 1) / hb;
+  p.by_blocks = make_div(p.blocks);
+  p.by_item_blocks = make_div(p.item_blocks);
+  // Tokens of a CTA: what the sine table holds, at most 8, and few enough
+  // that every SM has eight CTAs to even out its last ones.
+  const int entries = (p.pairs + 1) / 2;
+  int64_t tile = std::min(8, kSmemPairs / 2 / entries);
+  tile = std::min<int64_t>(tile, p.rows / (a.sms * 8));
+  tile = std::min<int64_t>(tile, (1 << 30) / ((int64_t)p.blocks * p.item_blocks));
   if (tile < 1) tile = 1;
   p.tile = (int32_t)tile;
   const dim3 g((unsigned)((p.rows + tile - 1) / tile)), b(kThreads);
@@ -238,7 +317,7 @@ cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t stream) {
   p.by_tokens = make_div(a.tokens);
   p.by_pairs = make_div(a.pairs);
   p.heads = a.heads;
-  p.all_heads = a.heads + a.kv_heads;
+  p.kv_heads = a.kv_heads;
   p.mag = a.magnitude;
   p.sign = a.transpose ? -a.magnitude : a.magnitude;
   for (int i = 0; i < a.pairs; ++i) p.turn[i] = a.turn[i];
