@@ -16,9 +16,10 @@ namespace fastvr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;
+constexpr int kUnroll = 4;      // tokens of a thread at once: append
+constexpr int kReadUnroll = 8;  // and read-back, which loads 6 bytes for each
 
-// A thread keeps one 16-byte piece of one head and walks over tokens, kUnroll
+// A thread keeps one 16-byte piece of one head and walks over tokens, 4 or 8
 // consecutive ones at a time: in the cache these are neighbouring rows, 256
 // bytes of codes and a whole sector of scales (tokens far apart left every
 // 64-byte row and 8-byte scale on a DRAM page of its own, 97 us instead of
@@ -31,11 +32,11 @@ struct Walk {
   int32_t ctas;   // grid.x
 };
 Walk make_walk(int64_t tokens, int64_t lanes, int groups_per_cta,
-               int64_t others, int sms) {
+               int64_t others, int unroll, int sms) {
   // Eight CTAs of 256 threads per SM in all.
   const int64_t target =
       std::max<int64_t>(1, (int64_t)sms * 8 * groups_per_cta / others);
-  const int64_t units = (tokens + kUnroll - 1) / kUnroll;
+  const int64_t units = (tokens + unroll - 1) / unroll;
   const int64_t passes = (units * lanes + target - 1) / target;
   Walk w;
   w.slots = (int32_t)((units + passes - 1) / passes);
@@ -136,6 +137,11 @@ q4_append_kernel(const __grid_constant__ Q4AppendParams p, Walk walk) {
       }
       uint32_t at = (uint32_t)p.first_row + t;  // both below 2^30
       if (at >= cache_tokens) at -= cache_tokens;
+      // rows of the pass from `wrap` on lie at the start of the head
+      const uint32_t wrap = cache_tokens - at;
+      const int64_t row0 = head_row + at;
+      uint32_t* code_to = codes + row0 * VPR + at_word;
+      uint16_t* scale_to = scales + row0 * kGroups + word / 4;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
@@ -151,15 +157,15 @@ q4_append_kernel(const __grid_constant__ Q4AppendParams p, Walk walk) {
         // zeros, also under a NaN scale
         const uint32_t code = s > 0.f ? encode8(w, r) : 0x88888888u;
         if (u < left) {
-          const int64_t row = head_row + at;
-          if (in_bounds(row * VPR + at_word, p.code_words, p.status))
-            codes[row * VPR + at_word] = code;
-          if (word % 4 == 0 && in_bounds(row * kGroups + word / 4,
-                                         p.code_words / 4, p.status))
-            scales[row * kGroups + word / 4] =
-                (uint16_t)(__float_as_uint(s) >> 16);
+          const int64_t back = u < wrap ? 0 : p.cache_tokens;
+          if (in_bounds((row0 + u - back) * VPR + at_word, p.code_words,
+                        p.status)) {
+            code_to[u * VPR - back * VPR] = code;
+            if (word % 4 == 0)
+              scale_to[u * kGroups - back * kGroups] =
+                  (uint16_t)(__float_as_uint(s) >> 16);
+          }
         }
-        if (++at == cache_tokens) at = 0;
       }
     }
   }
@@ -221,27 +227,32 @@ q4_read_kernel(const __grid_constant__ Q4ReadParams p, Walk walk) {
                                   p.tokens);
     const uint32_t skip = (uint32_t)start / 128 * 128;
     const uint32_t cache_tokens = (uint32_t)p.cache_tokens;
-    const uint32_t stride = (uint32_t)walk.slots * kUnroll;
-    for (uint32_t t0 = slot * kUnroll; t0 < (uint32_t)p.tokens; t0 += stride) {
-      if (t0 + kUnroll <= skip) continue;
+    constexpr int U = kReadUnroll;
+    const uint32_t stride = (uint32_t)walk.slots * U;
+    for (uint32_t t0 = slot * U; t0 < (uint32_t)p.tokens; t0 += stride) {
+      if (t0 + U <= skip) continue;
       uint32_t at = (uint32_t)p.first_row + t0;  // both below 2^30
       if (at >= cache_tokens) at -= cache_tokens;
-      uint32_t w[kUnroll], sc[kUnroll];
+      const uint32_t wrap = cache_tokens - at;
+      const int64_t row0 = head_row + at;
+      const uint32_t* code_at = codes + row0 * VPR + at_word;
+      const uint16_t* scale_at = scales + row0 * kGroups + word / 4;
+      uint32_t w[U], sc[U];
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
+      for (int u = 0; u < U; ++u) {
         const uint32_t t = t0 + u;
         w[u] = sc[u] = 0;
-        const int64_t row = head_row + at;
+        const int64_t back = u < wrap ? 0 : p.cache_tokens;
         if (t >= (uint32_t)start && t < (uint32_t)p.tokens &&
-            in_bounds(row * VPR + at_word, p.code_words, p.status)) {
-          w[u] = __ldcs(codes + row * VPR + at_word);
-          sc[u] = scales[row * kGroups + word / 4];
+            in_bounds((row0 + u - back) * VPR + at_word, p.code_words,
+                      p.status)) {
+          w[u] = __ldcs(code_at + u * VPR - back * VPR);
+          sc[u] = scale_at[u * kGroups - back * kGroups];
         }
-        if (++at == cache_tokens) at = 0;
       }
       uint16_t* dst = out + (int64_t)t0 * p.out_str.token;
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
+      for (int u = 0; u < U; ++u) {
         const uint32_t t = t0 + u;
         if (t < skip || t >= (uint32_t)p.tokens) continue;
         const uint32_t s2 = sc[u] * 0x10001u;
@@ -259,7 +270,8 @@ cudaError_t launch_q4_append(const Q4AppendParams& p, int sms,
   const int vpr = p.head_dim / 8;
   if (vpr != 16 && vpr != 8) return cudaErrorInvalidValue;
   const int ys = std::min(p.batch, 32767);
-  const Walk w = make_walk(p.tokens, p.heads, kThreads / vpr, 2 * ys, sms);
+  const Walk w = make_walk(p.tokens, p.heads, kThreads / vpr, 2 * ys,
+                           kUnroll, sms);
   const dim3 grid(w.ctas, 2 * ys), block(kThreads);
   return vpr == 16 ? launch_pdl(q4_append_kernel<16>, grid, block, 0, stream, p,
                                 w)
@@ -273,7 +285,7 @@ cudaError_t launch_q4_read(const Q4ReadParams& p, bool head_major, int sms,
   if (vpr != 16 && vpr != 8) return cudaErrorInvalidValue;
   const int ys = std::min(head_major ? p.batch * p.heads : p.batch, 32767);
   const Walk w = make_walk(p.tokens, head_major ? 1 : p.heads, kThreads / vpr,
-                           2 * ys, sms);
+                           2 * ys, kReadUnroll, sms);
   const dim3 grid(w.ctas, 2 * ys), block(kThreads);
   if (vpr == 16)
     return head_major ? launch_pdl(q4_read_kernel<16, true>, grid, block, 0,

@@ -100,6 +100,7 @@ struct Params {
   int32_t tile;               // tokens of a CTA
   int32_t axis_end[3];        // first pair past each axis
   int32_t items;              // vector items of a head
+  int32_t pass_step;          // half layout: see rotary_kernel; or 0
   int32_t lanes;              // threads of a group, an item each
   int32_t heads, kv_heads;
   int32_t q_blocks, blocks;   // blocks of heads of q, of q and k
@@ -116,8 +117,9 @@ __host__ __device__ constexpr int head_block(int elem_bytes, bool half) {
 }
 
 // One head's item: kHalf: the vectors of V elements at i V and rot/2 + i V
-// (one per pair of the V), then the pass-through vectors; interleaved: the
-// vector at i V, V / 2 pairs.  A group of threads, one per item, takes a block
+// (one per pair of the V), then the pass-through vectors, two to an item as
+// well (pass_step apart) when their number is even; interleaved: the vector at
+// i V, V / 2 pairs.  A group of threads, one per item, takes a block
 // of HB heads of a token at a time: the sines of a thread's item are read once
 // for the block, and the block's loads are in flight together.  The first
 // block's are on their way while the sines are formed.
@@ -143,7 +145,7 @@ rotary_kernel(const __grid_constant__ Params p) {
   Vt a[HB], z[HB];
   T* dst;
   int64_t dst_head;
-  int n_heads, item, r;
+  int n_heads, item, r, second;  // second: distance of the item's other vector
   bool rot;
   auto load = [&](int task) {
     const int rb = fast_div(task, p.by_item_blocks);
@@ -157,6 +159,7 @@ rotary_kernel(const __grid_constant__ Params p) {
                   : 0;
     rot = !kHalf || item < pair_items;
     const int x = rot ? item * V : 2 * p.pairs + (item - pair_items) * V;
+    second = rot ? p.pairs : p.pass_step;
     const int row = row0 + r;
     const int b = fast_div(row, p.by_tokens);
     const int t = row - b * p.tokens;
@@ -171,8 +174,8 @@ rotary_kernel(const __grid_constant__ Params p) {
     for (int u = 0; u < HB; ++u)
       if (u < n_heads) {
         a[u] = *reinterpret_cast<const Vt*>(src + u * si.head);
-        if (kHalf && rot)
-          z[u] = *reinterpret_cast<const Vt*>(src + u * si.head + p.pairs);
+        if (kHalf && second)
+          z[u] = *reinterpret_cast<const Vt*>(src + u * si.head + second);
       }
   };
   int task = group;
@@ -251,8 +254,8 @@ rotary_kernel(const __grid_constant__ Params p) {
     for (int u = 0; u < HB; ++u)
       if (u < n_heads) {
         *reinterpret_cast<Vt*>(dst + u * dst_head) = a[u];
-        if (kHalf && rot)
-          *reinterpret_cast<Vt*>(dst + u * dst_head + p.pairs) = z[u];
+        if (kHalf && second)
+          *reinterpret_cast<Vt*>(dst + u * dst_head + second) = z[u];
       }
   }
 }
@@ -264,7 +267,13 @@ cudaError_t launch_t(const RotaryArgs& a, Params& p, cudaStream_t stream) {
   int v = 8;
   if (a.half)
     while (p.pairs % v) v /= 2;
-  p.items = a.half ? (p.head_dim - p.pairs) / v : p.head_dim / 8;
+  p.items = p.head_dim / 8;
+  p.pass_step = 0;
+  if (a.half) {
+    const int pass = (p.head_dim - 2 * p.pairs) / v;  // vectors
+    p.pass_step = pass % 2 == 0 ? pass / 2 * v : 0;
+    p.items = p.pairs / v + (pass % 2 == 0 ? pass / 2 : pass);
+  }
   p.lanes = std::min(p.items, kThreads);
   p.item_blocks = (p.items + p.lanes - 1) / p.lanes;
   const int hb = head_block(sizeof(T), a.half);
