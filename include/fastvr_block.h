@@ -37,7 +37,8 @@ extern "C" {
 #define FASTVR_F32 1
 
 /* Strides of a [batch, token, head, d] tensor in elements; the d elements of
- * a head are contiguous.  Every stride is a multiple of 16 bytes. */
+ * a head are contiguous.  Every stride (of a dimension with more than one
+ * entry) is a multiple of 16 bytes; an output's is not 0. */
 typedef struct {
   int64_t batch, token, head;
 } fastvr_strides_t;
@@ -133,7 +134,8 @@ FASTVR_API fastvr_status_t fastvr_rotary(
  * post and pre are the norms above, each followed by an optional weight
  * vector.  Tensors are contiguous [batch, tokens, dim]. */
 typedef struct {
-  int32_t batch, tokens, dim; /* dim: a multiple of 8, 8 .. 8192            */
+  int32_t batch, tokens, dim; /* dim: a multiple of 8, 8 .. 8192;
+                                 batch * tokens below 2^30                  */
   int32_t groups;             /* 1 .. tokens, divides tokens                */
   int32_t pre, post;          /* FASTVR_NORM_*; pre is RMS or LAYER         */
   int32_t residual_dtype;     /* x, r, dr, dx: FASTVR_BF16 or FASTVR_F32    */
@@ -210,7 +212,8 @@ FASTVR_API fastvr_status_t fastvr_gated_norm_bwd(
 
 /* Bytes of cache and of workspace for cfg with kv_heads key/value heads
  * (cfg->heads query heads, a multiple of kv_heads: consecutive query heads
- * share one).  A workspace may serve any number of plans whose calls do not
+ * share one).  A head's cache holds fewer than 2^30 tokens, S*k*N, and a
+ * chunk has fewer than 2^30 query rows per key head.  A workspace may serve any number of plans whose calls do not
  * overlap on the GPU; nothing is kept in it between calls.
  * Host only.  Errors: INVALID_ARG, UNSUPPORTED (head_dim not 64 or 128). */
 FASTVR_API fastvr_status_t fastvr_q4_cache_bytes(
@@ -250,7 +253,8 @@ FASTVR_API fastvr_status_t fastvr_q4_append(fastvr_plan_t plan, const void* k,
  * array int32 [B] (4-byte aligned): batch entry b sees no chunk before
  * first_chunk[b] (a stream that joined the batch then; any value).  An entry
  * whose first_chunk is later than c sees nothing: its out is 0 and its lse
- * -infinity.  What the cache holds at hidden places does not matter.
+ * -infinity.  What the cache holds at hidden places does not matter.  out
+ * does not overlap q; magnitudes in q are below 2^100.
  * Calls with few query rows (frames * N * heads / kv_heads) read the codes
  * directly; longer ones first write the visible keys and values in bfloat16
  * to the workspace.  A plan whose chunks are all short needs a workspace of

@@ -115,20 +115,26 @@ const RotaryTurns& rotary_turns(const fastvr_rotary_config_t& c) {
   return last;
 }
 
-// Strides in elements that keep every head 16-byte aligned.
-bool get_strides(const fastvr_strides_t* s, int64_t tokens, int64_t heads,
-                 int64_t d, int elem_bytes, fastvr::Strides* out) {
+// Strides in elements that keep every head 16-byte aligned; those of a
+// dimension of one entry do not matter.  A tensor that is written may not have
+// several entries in one place.
+bool get_strides(const fastvr_strides_t* s, int64_t batch, int64_t tokens,
+                 int64_t heads, int64_t d, int elem_bytes, bool written,
+                 fastvr::Strides* out) {
   if (s == nullptr) {
     out->head = d;
     out->token = heads * d;
     out->batch = tokens * heads * d;
     return true;
   }
-  const int64_t unit = 16 / elem_bytes;
-  if (s->batch % unit || s->token % unit || s->head % unit) return false;
-  out->batch = s->batch;
-  out->token = s->token;
-  out->head = s->head;
+  const int64_t size[] = {batch, tokens, heads};
+  const int64_t given[] = {s->batch, s->token, s->head};
+  int64_t* to[] = {&out->batch, &out->token, &out->head};
+  for (int i = 0; i < 3; ++i) {
+    *to[i] = size[i] > 1 ? given[i] : 0;
+    if (*to[i] % (16 / elem_bytes) != 0) return false;
+    if (written && size[i] > 1 && given[i] == 0) return false;
+  }
   return true;
 }
 
@@ -143,7 +149,7 @@ bool valid_norm(const fastvr_norm_config_t* c) {
           c->residual_dtype == FASTVR_F32) &&
          (c->block_dtype == FASTVR_BF16 || c->block_dtype == FASTVR_F32) &&
          c->eps > 0.f && isfinite(c->eps) && isfinite(c->residual_scale) &&
-         (int64_t)c->batch * c->tokens <= 0x7fffffffLL;
+         (int64_t)c->batch * c->tokens <= INT32_MAX / 2;
 }
 
 // CTAs of the backward do not depend on the device at hand: the scratch size
@@ -324,11 +330,12 @@ fastvr_status_t fastvr_rotary(
     return FASTVR_ERR_INVALID_ARG;
   const int es = dtype == FASTVR_F32 ? 4 : 2;
   fastvr::RotaryArgs a;
-  if (!get_strides(q_str, tokens, heads, cfg->head_dim, es, &a.q_str) ||
-      !get_strides(q_out_str, tokens, heads, cfg->head_dim, es,
+  const int d = cfg->head_dim;
+  if (!get_strides(q_str, batch, tokens, heads, d, es, false, &a.q_str) ||
+      !get_strides(q_out_str, batch, tokens, heads, d, es, true,
                    &a.q_out_str) ||
-      !get_strides(k_str, tokens, kv_heads, cfg->head_dim, es, &a.k_str) ||
-      !get_strides(k_out_str, tokens, kv_heads, cfg->head_dim, es,
+      !get_strides(k_str, batch, tokens, kv_heads, d, es, false, &a.k_str) ||
+      !get_strides(k_out_str, batch, tokens, kv_heads, d, es, true,
                    &a.k_out_str))
     return FASTVR_ERR_INVALID_ARG;
   const fastvr_status_t st = fastvr::check_device();
@@ -537,8 +544,10 @@ fastvr_status_t fastvr_q4_append(fastvr_plan_t p, const void* k,
   fastvr::Q4AppendParams a;
   memset(&a, 0, sizeof(a));
   const int64_t tokens = (int64_t)frames * c.tokens_per_frame;
-  if (!get_strides(k_str, tokens, p->kv_heads, c.head_dim, 2, &a.k_str) ||
-      !get_strides(v_str, tokens, p->kv_heads, c.head_dim, 2, &a.v_str))
+  if (!get_strides(k_str, c.batch, tokens, p->kv_heads, c.head_dim, 2, false,
+                   &a.k_str) ||
+      !get_strides(v_str, c.batch, tokens, p->kv_heads, c.head_dim, 2, false,
+                   &a.v_str))
     return FASTVR_ERR_INVALID_ARG;
   const fastvr_status_t st = ready(p, stream);
   if (st != FASTVR_OK) return st;
@@ -569,7 +578,7 @@ fastvr_status_t fastvr_q4_append(fastvr_plan_t p, const void* k,
 fastvr_status_t fastvr_q4_attn_fwd(fastvr_plan_t p, const void* q,
                                    const int32_t* first_chunk, void* out,
                                    float* lse, struct CUstream_st* stream) {
-  if (p == nullptr || !p->q4 || q == nullptr || out == nullptr ||
+  if (p == nullptr || !p->q4 || q == nullptr || out == nullptr || q == out ||
       !aligned16(q) || !aligned16(out) || !aligned4(first_chunk) ||
       !aligned4(lse))
     return FASTVR_ERR_INVALID_ARG;
@@ -635,7 +644,8 @@ fastvr_status_t fastvr_q4_read(fastvr_plan_t p, int64_t chunk, void* k,
   r.tokens = (chunk == p->chunks - 1 ? p->last_frames
                                      : p->cfg.frames_per_chunk) *
              p->cfg.tokens_per_frame;
-  get_strides(nullptr, r.tokens, r.heads, r.head_dim, 2, &r.out_str);
+  get_strides(nullptr, r.batch, r.tokens, r.heads, r.head_dim, 2, true,
+              &r.out_str);
   r.first_row = chunk % p->slots * p->slot_tokens;
   if (fastvr::launch_q4_read(r, false, fastvr::device_sms(),
                              to_stream(stream)) != cudaSuccess)

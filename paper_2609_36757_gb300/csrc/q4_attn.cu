@@ -550,7 +550,7 @@ q4_attn_kernel(const __grid_constant__ Q4AttnParams p) {
     // Q^T fragments in half precision: for group i, element pairs (e, e + 4) of
     // words 4 i + c, those of odd e divided by 16 (their codes lie one nibble
     // up), all times the power of two that brings the row's largest magnitude
-    // to [2^15, 2^16) (of magnitudes up to 2^110).
+    // to [2^15, 2^16) (of magnitudes up to 2^100).
     // All warps need the same ones: with more than one block they stay in
     // shared memory, which leaves their registers to the sums.
     uint32_t qf[kQShared ? 1 : NT][kGroups][4];
@@ -576,7 +576,7 @@ q4_attn_kernel(const __grid_constant__ Q4AttnParams p) {
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       // exponent of the largest magnitude, kept where powers of two stay finite
-      const int e = min(max((int)(top >> 7) - 127, -110), 110);
+      const int e = min(max((int)(top >> 7) - 127, -100), 100);
       const float up = __int_as_float((15 - e + 127) << 23);
       // 2^24 of the subnormal codes, 2^(e - 15) of the row
       const float mine = p.scale_log2 * __int_as_float((24 - 15 + e + 127) << 23);

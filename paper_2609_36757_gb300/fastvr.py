@@ -859,8 +859,8 @@ class StreamingAttention4:
         if out is None:
             out = torch.empty_like(q)
         elif out.shape != q.shape or out.dtype != q.dtype or \
-                not out.is_contiguous():
-            raise ValueError("out must be contiguous and like q")
+                not out.is_contiguous() or out.data_ptr() == q.data_ptr():
+            raise ValueError("out must be contiguous, like q and not q")
         if lse is None and want_lse:
             lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device)
         elif lse is not None and (lse.shape != (B, H, L) or

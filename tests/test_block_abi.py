@@ -46,6 +46,12 @@ def test_rotary_refuses_unaligned_strides(fv):
     for name in ("q_str", "k_str", "q_out_str", "k_out_str"):
         _refused(fv, fv.FASTVR_ERR_INVALID_ARG, fv.fastvr_rotary, cfg,
                  **{**ROT_ARGS, name: bad})
+    # outputs with several tokens (or heads) in one place
+    for bad in (fv.fastvr_strides_t(512, 0, 64),
+                fv.fastvr_strides_t(512, 128, 0)):
+        for name in ("q_out_str", "k_out_str"):
+            _refused(fv, fv.FASTVR_ERR_INVALID_ARG, fv.fastvr_rotary, cfg,
+                     **{**ROT_ARGS, name: bad})
 
 
 @pytest.mark.parametrize("kw", [
@@ -76,7 +82,7 @@ def _norm_cfg(fv, **kw):
     dict(groups=0), dict(groups=4), dict(groups=7), dict(pre=0), dict(pre=3),
     dict(post=-1), dict(residual_dtype=2), dict(block_dtype=-1),
     dict(eps=0.0), dict(eps=float("nan")), dict(residual_scale=float("inf")),
-    dict(batch=1 << 16, tokens=3 << 15),
+    dict(batch=1 << 15, tokens=3 << 14),
 ])
 def test_norm_config_refused(fv, kw):
     cfg = _norm_cfg(fv, **kw)
@@ -163,7 +169,8 @@ def test_q4_sequencing(fv):
     app = lambda frames, k=FAKE, v=FAKE, s=None: fv.fastvr_q4_append(
         plan, k, s, v, None, frames, 0)
     try:
-        _refused(fv, SEQ, fv.fastvr_q4_attn_fwd, plan, FAKE, 0, FAKE, 0, 0)
+        _refused(fv, SEQ, fv.fastvr_q4_attn_fwd, plan, FAKE, 0, FAKE + 4096, 0,
+                 0)
         _refused(fv, SEQ, fv.fastvr_q4_read, plan, 0, FAKE, FAKE, 0)
         _refused(fv, ARG, app, 0)
         _refused(fv, CAP, app, 3)        # neither <= k nor a multiple
@@ -175,15 +182,16 @@ def test_q4_sequencing(fv):
         _refused(fv, SEQ, app, 2)        # after a ragged chunk
         _refused(fv, SEQ, fv.fastvr_q4_read, plan, 1, FAKE, FAKE, 0)
         _refused(fv, SEQ, fv.fastvr_q4_read, plan, 5, FAKE, FAKE, 0)
-        for a in [(0, 0, FAKE, 0), (FAKE + 8, 0, FAKE, 0), (FAKE, 2, FAKE, 0),
-                  (FAKE, 0, 0, 0), (FAKE, 0, FAKE, 2)]:
+        OUT = FAKE + 4096
+        for a in [(0, 0, OUT, 0), (FAKE + 8, 0, OUT, 0), (FAKE, 2, OUT, 0),
+                  (FAKE, 0, 0, 0), (FAKE, 0, OUT, 2), (FAKE, 0, FAKE, 0)]:
             _refused(fv, ARG, fv.fastvr_q4_attn_fwd, plan, *a, 0)
         # the bfloat16 calls and the 4-bit ones do not take each other's plans
         _refused(fv, ARG, fv.fastvr_kv_append, plan, FAKE, FAKE, 1, 0)
         _refused(fv, ARG, fv.fastvr_chunk_attn_fwd, plan, FAKE, FAKE, 0, 0)
         bf = fv.fastvr_attn_plan(cfg, FAKE, fv.fastvr_kv_cache_bytes(cfg))
         _refused(fv, ARG, fv.fastvr_q4_append, bf, FAKE, None, FAKE, None, 1, 0)
-        _refused(fv, ARG, fv.fastvr_q4_attn_fwd, bf, FAKE, 0, FAKE, 0, 0)
+        _refused(fv, ARG, fv.fastvr_q4_attn_fwd, bf, FAKE, 0, FAKE + 4096, 0, 0)
         _refused(fv, ARG, fv.fastvr_q4_read, bf, 0, FAKE, FAKE, 0)
         fv.fastvr_plan_destroy(bf)
         # the shared calls do take it

@@ -303,6 +303,49 @@ def test_offsets_past_32_bits():
     assert att.status() == FV.FASTVR_OK
 
 
+def test_workspace_offsets_past_32_bits():
+    """A chunk of 350 queries over 700 000 tokens of 24 heads: the expanded
+    keys take 2.15e9 elements.  The newest chunks, checked on the last head."""
+    from paper_2609_36757_gb300 import fastvr as FV
+    H, d, N, chunks, seen = 24, 128, 350, 2000, 3
+    cfg = FV.make_config(1, H, d, N, 1, -1, chunks)
+    att = FV.StreamingAttention4(cfg)
+    assert H * d * N * chunks > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(6)
+    tail = torch.randn(2, 1, seen * N, H, d, generator=g,
+                       device="cuda").to(torch.bfloat16)
+    att.cache.zero_()
+    att.set_state(chunks - seen, 1)
+    att.append(tail[0], tail[1])
+    q = torch.randn(1, N, H, d, generator=g, device="cuda").to(torch.bfloat16)
+    for first, lo in ((chunks - seen, 0), (chunks - 1, 2 * N)):
+        o, lse = att.forward(q, want_lse=True, first_chunk=torch.tensor(
+            [first], dtype=torch.int32, device="cuda"))
+        kk, vv = (Q4.values(f64(t[0, lo:, -1:])) for t in tail)
+        ref, rl, mass, top = Q4.attention(f64(q[0, ::50, -1:]), kk, vv,
+                                          d ** -0.5, np.ones(len(kk), bool))
+        bound = 2.0 ** -8 * (mass + np.abs(ref)) + 2e-5 * (
+            1 + top.T[..., None]) * mass
+        assert (np.abs(f64(o[0, ::50, -1:]) - ref) <= bound).all()
+        assert (np.abs(f64(lse[0, -1:, ::50]) - rl) <= 2e-5 * (1 + top)).all()
+    # everything visible: the zeros before count 1 each in the sum
+    o, lse = att.forward(q, want_lse=True)
+    s = f64(q[0, ::50, -1]) @ Q4.values(f64(tail[0][0, :, -1])).T * d ** -0.5
+    want = np.log((chunks - seen) * N + np.exp(s).sum(-1))
+    assert np.abs(f64(lse[0, -1, ::50]) - want).max() <= 2e-5 * (
+        1 + np.abs(s).max())
+    assert att.status() == FV.FASTVR_OK
+
+
+def test_output_is_not_the_query():
+    from paper_2609_36757_gb300 import fastvr as FV
+    att = FV.StreamingAttention4(FV.make_config(1, 2, 64, 1, 1, 3))
+    t = torch.ones(1, 1, 2, 64, dtype=torch.bfloat16, device="cuda")
+    att.append(t, t)
+    with pytest.raises(ValueError):
+        att.forward(t, out=t)
+
+
 def test_peaked_and_flat_rows():
     """Large scores (the reference moves often) and Q = 0 (the mean of V)."""
     from paper_2609_36757_gb300 import fastvr as FV

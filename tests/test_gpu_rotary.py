@@ -129,6 +129,25 @@ def test_gradient_matches_differences():
         assert abs(diff - float(grad[idx])) <= 768 * 1e-6
 
 
+def test_strides_of_single_entries_and_broadcast_inputs():
+    """A dimension of one entry may have any stride, and an input may repeat
+    one token (stride 0)."""
+    from paper_2609_36757_gb300 import fastvr as FV
+    cfg = FV.make_rotary_config(64)
+    x = _inputs(1, 1, 2, 1, 64, torch.bfloat16, 9).cuda()
+    q = x[:, :, :2]
+    odd = torch.as_strided(q, q.shape, (13, 7, 64, 1))  # one batch, one token
+    pos = torch.tensor([[5]], dtype=torch.int32, device="cuda")
+    assert torch.equal(FV.rotary(cfg, odd, None, pos)[0],
+                       FV.rotary(cfg, q.contiguous(), None, pos)[0])
+    wide = q.expand(3, 4, 2, 64)
+    pos = torch.arange(12, dtype=torch.int32, device="cuda").view(3, 4, 1)
+    assert torch.equal(FV.rotary(cfg, wide, None, pos)[0],
+                       FV.rotary(cfg, wide.contiguous(), None, pos)[0])
+    with pytest.raises(FV.FastVRError):
+        FV.rotary(cfg, wide, None, pos, out=(wide, None))
+
+
 def test_other_stream_and_bad_tensors():
     from paper_2609_36757_gb300 import fastvr as FV
     cfg = FV.make_rotary_config(64)
