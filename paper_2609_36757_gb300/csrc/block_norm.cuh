@@ -109,6 +109,80 @@ __device__ __forceinline__ void store8(float* base, int64_t i, const F8& f) {
   p[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
 
+// Rows on their way: 16-byte pieces of each thread's columns, copied
+// asynchronously by the threads of its own warp, so that they need not meet the
+// others.  kDeep rows of kPieces pieces; a row is asked for kDeep - 1 rows ahead,
+// in the place of the one last worked on.
+template <int kDeep, int kPieces>
+struct Ring {
+  float4* base;  // [row][piece][thread]
+  int at = 0;    // the row that is worked on
+  // Piece i, half h of a vector of a thread: neighbours swap their second
+  // halves' places, so that neither the copies nor the reads meet in a bank.
+  __device__ __forceinline__ float4* piece(int row, int i, int h,
+                                           int thread) const {
+    return base + (row * kPieces + i + h) * blockDim.x + (thread ^ 4 * h);
+  }
+  // 8 elements per thread into the row `ahead` of the one that is worked on;
+  // index(thread): where a thread's elements are, negative if it has none.
+  // Float32: the 64 pieces of a warp in the order of memory.
+  template <typename T, typename F>
+  __device__ __forceinline__ void ask(int ahead, int i, const void* from,
+                                      F index) const {
+    int row = at + ahead;
+    if (row >= kDeep) row -= kDeep;
+    if constexpr (sizeof(T) == 2) {
+      const int64_t e = index(threadIdx.x);
+      if (e >= 0)
+        copy_async<16>(smem_u32(piece(row, i, 0, threadIdx.x)),
+                       static_cast<const T*>(from) + e, true);
+    } else {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        const int of =
+            (threadIdx.x & ~31) + (threadIdx.x & 31) / 2 + 16 * n;
+        const int64_t e = index(of);
+        const int h = threadIdx.x & 1;
+        if (e >= 0)
+          copy_async<16>(smem_u32(piece(row, i, h, of)),
+                         static_cast<const T*>(from) + e + 4 * h, true);
+      }
+    }
+  }
+  // until the row that is worked on is there
+  __device__ __forceinline__ void wait() const {
+    copy_wait<kDeep - 1>();
+    __syncwarp();
+  }
+  template <typename T>
+  __device__ __forceinline__ F8 get(int i) const {
+    if constexpr (sizeof(T) == 2) {
+      const Raw8<T> r = {*reinterpret_cast<const uint4*>(
+          piece(at, i, 0, threadIdx.x))};
+      return r.widen();
+    } else {
+      const Raw8<T> r = {*piece(at, i, 0, threadIdx.x),
+                         *piece(at, i, 1, threadIdx.x)};
+      return r.widen();
+    }
+  }
+  // done with it on every lane
+  __device__ __forceinline__ void next() {
+    __syncwarp();
+    at = at + 1 == kDeep ? 0 : at + 1;
+  }
+};
+
+// Its depth: what a CTA's share of an SM's 227 KB leaves beside `fixed` bytes of
+// each of its vectors (2 KB for the system and the static part); 0 where two
+// rows do not fit.
+constexpr int kSmBytes = 232448;
+constexpr int ring_depth(int ctas, int vectors, int fixed, int bytes,
+                         int most) {
+  const int fit = ((kSmBytes / ctas - 2048) / vectors - fixed) / bytes;
+  return fit < 2 ? 0 : fit > most ? most : fit;
+}
+
 // 8 floats of an optional vector, `absent` where there is none.
 __device__ __forceinline__ F8 load8_or(const float* base, int64_t i,
                                        float absent) {
@@ -145,19 +219,19 @@ struct Private {
   }
 };
 
-// N such vectors, in registers where kRegs.
-template <bool kRegs, int N>
+// N such vectors, the first kRegs in registers.
+template <int kRegs, int N>
 struct Kept {
-  F8 r[kRegs ? N : 1];
+  F8 r[kRegs ? kRegs : 1];
   Private m;
   __device__ __forceinline__ F8 get(int i) const {
-    return kRegs ? r[kRegs ? i : 0] : m.get(i);
+    return i < kRegs ? r[i < kRegs ? i : 0] : m.get(i - kRegs);
   }
   __device__ __forceinline__ void set(int i, const F8& f) {
-    if (kRegs)
-      r[kRegs ? i : 0] = f;
+    if (i < kRegs)
+      r[i < kRegs ? i : 0] = f;
     else
-      m.set(i, f);
+      m.set(i - kRegs, f);
   }
 };
 
@@ -182,6 +256,9 @@ __device__ __forceinline__ void both_sums(float& a, float& b) {
   a = hi ? o : v;
   b = hi ? v : o;
 }
+
+// Groups of fewer tokens than this: what happens once per group counts.
+constexpr int kFewTokens = 16;
 
 // A row's threads: TPR of them with NV vectors of 8 columns each, vector i at
 // column (i TPR + thread) 8.  Up to 32: 128 / TPR rows side by side in a CTA of
@@ -220,8 +297,33 @@ struct Cols {
       n[S::kMany ? threadIdx.x / 32 : 0] = (float)mine;
   }
   __device__ __forceinline__ int at(int i) const { return c + i * TPR * 8; }
+  // the same for another thread
+  __device__ __forceinline__ int at(int i, int thread) const {
+    return ((S::kRows > 1 ? thread % TPR : thread) + i * TPR) * 8;
+  }
   __device__ __forceinline__ bool on(int i) const { return at(i) < dim; }
 };
+
+// Sums of the N (4 or 8) values over the L lanes of a row within a warp: the
+// lanes trade halves, quarters and so on of what they hold, so lane i ends with
+// the sum of value i / (L / N).
+template <int L, int N>
+__device__ __forceinline__ float keep_sum(float (&v)[N]) {
+#pragma unroll
+  for (int n = N / 2, m = L / 2; n > 0; n /= 2, m /= 2) {
+    const bool hi = threadIdx.x & m;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float give = hi ? v[i] : v[n + i];
+      v[i] = (hi ? v[n + i] : v[i]) + __shfl_xor_sync(0xffffffffu, give, m);
+    }
+  }
+  float s = v[0];
+#pragma unroll
+  for (int m = L / N / 2; m > 0; m >>= 1)
+    s += __shfl_xor_sync(0xffffffffu, s, m);
+  return s;
+}
 
 // Sums over the row of a and of b, on every thread; `part` (kWarps entries)
 // is this exchange's own: two exchanges with another part between them need
@@ -259,6 +361,18 @@ __device__ __forceinline__ Stats row_stats(const F8 (&a)[NV], const F8 (&b)[NV],
   using S = Shape<TPR>;
   Stats st;
   st.mu_a = st.mu_b = 0.f;
+  if (S::kMany && !mean_a && !mean_b) {  // squares alone
+    F8 qa = mul(a[0], a[0]), qb = mul(b[0], b[0]);
+#pragma unroll
+    for (int i = 1; i < NV; ++i) {
+      qa = fma(a[i], a[i], qa);
+      qb = fma(b[i], b[i], qb);
+    }
+    st.sq_a = sum(qa);
+    st.sq_b = sum(qb);
+    row_sums<TPR>(st.sq_a, st.sq_b, reinterpret_cast<float2*>(part));
+    return st;
+  }
   if (mean_a || mean_b) {
     F8 x = a[0], y = b[0];
 #pragma unroll

@@ -8,12 +8,21 @@
 //   dscale = pre_weight A, dshift = C, dgate = post_weight E   per group,
 //   dpre_weight = sum_g (1 + scale) A,  dpost_weight = sum_g gate E.
 //
+// d is not needed for the sums that J_post takes over it: with s(.) a sum over
+// the row and w = gate post_weight n(y),
+//   s(d w) = s(dr w) + rho (s(dn w) + m0 s(w) + m1 s(n(r) w)),
+//   m0 = -mean(dn), m1 = -mean(dn n(r)),
+// so a row needs one exchange between its warps: of up to twelve sums and two
+// means, each taken about the warp's own mean and moved when they are put
+// together.
+//
 // Bound by memory: dr, dh, r, y are read once, dx, dy written once (18 bytes
 // per element with a float32 residual stream).  A thread owns the same columns
 // of all the rows that its CTA takes, so A, C and E are its own and every token
-// sum has a fixed order; the next row is loaded while a row's eight sums go
-// across the CTA in three exchanges, whose latency is what is left: 73.7 us
-// (4.6 TB/s) for 12288 rows of 1536 with a float32 residual.
+// sum has a fixed order.  The slices of a group take its rows in turn, so that
+// neighbours in memory are asked for together.  72.0 us (4.7 TB/s) for 12288 rows
+// of 1536 with a float32 residual; three exchanges, one after the other, took
+// 73.7, and 88.6 instead of 80.9 for 3600 rows of 5120.
 #include "block_norm.cuh"
 
 namespace fastvr {
@@ -61,7 +70,123 @@ __device__ __forceinline__ void end_group(const NormBwdParams& p, int64_t g,
   }
 }
 
-template <typename TR, typename TY, int TPR, int NV, bool kAhead, bool kRegs,
+// What a row's gradients need of all its columns, with r and y less their means
+// where the norm takes them off, dn = dh (1 + scale) pre_weight, gp = gate
+// post_weight and w = gp y: sums of r r, y y, dn r, dn, dr w, dn w, r w, w, and
+// for a post norm with a mean of dr gp, dn gp, r gp, gp.
+struct RowSums {
+  float mu_r, mu_y, rr, yy, dn_r, dn, dr_w, dn_w, r_w, w, dr_g, dn_g, r_g, g;
+};
+
+// Means over the row's columns in this warp.
+template <int TPR, int NV>
+__device__ __forceinline__ void warp_means(const F8 (&r)[NV], const F8 (&y)[NV],
+                                           const Cols<TPR, NV>& k, float& mu_r,
+                                           float& mu_y) {
+  F8 a = r[0], b = y[0];
+#pragma unroll
+  for (int i = 1; i < NV; ++i) {
+    a = add(a, r[i]);
+    b = add(b, y[i]);
+  }
+  mu_r = sum(a);
+  mu_y = sum(b);
+  both_sums<Shape<TPR>::kLanes>(mu_r, mu_y);
+  mu_r *= k.inv_warp;
+  mu_y *= k.inv_warp;
+}
+
+// The sums over the row from a thread's parts (v: rr to w, v4: dr_g to g), that
+// were taken about its warp's means.  One exchange: the warps' parts are moved to
+// the row's means when they are put together.  `part`: not written again before
+// the next exchange.
+template <int TPR, int NV>
+__device__ __forceinline__ RowSums row_part_sums(float (&v)[8], float (&v4)[4],
+                                                 float mu_r, float mu_y,
+                                                 bool mean_r, bool mean_y,
+                                                 const Cols<TPR, NV>& k,
+                                                 float4 (*part)[4]) {
+  using S = Shape<TPR>;
+  constexpr int L = S::kLanes;
+  const int lane = threadIdx.x % 32;
+  RowSums s = {};
+  const float mine = keep_sum<L>(v);
+  const float mine4 = mean_y ? keep_sum<L>(v4) : 0.f;
+  if constexpr (!S::kMany) {
+    const int first = lane & ~(L - 1);
+    auto of = [&](float x, int lanes, int i) {
+      return __shfl_sync(0xffffffffu, x, first + i * lanes);
+    };
+    s.mu_r = mu_r;
+    s.mu_y = mu_y;
+    s.rr = of(mine, L / 8, 0);
+    s.yy = of(mine, L / 8, 1);
+    s.dn_r = of(mine, L / 8, 2);
+    s.dn = of(mine, L / 8, 3);
+    s.dr_w = of(mine, L / 8, 4);
+    s.dn_w = of(mine, L / 8, 5);
+    s.r_w = of(mine, L / 8, 6);
+    s.w = of(mine, L / 8, 7);
+    if (mean_y) {
+      s.dr_g = of(mine4, L / 4, 0);
+      s.dn_g = of(mine4, L / 4, 1);
+      s.r_g = of(mine4, L / 4, 2);
+      s.g = of(mine4, L / 4, 3);
+    }
+  } else {
+    float4* to = part[threadIdx.x / 32];
+    if (lane == 0) to[0] = make_float4(mu_r, mu_y, 0.f, 0.f);
+    if (lane % 4 == 0) reinterpret_cast<float*>(to + 1)[lane / 4] = mine;
+    if (mean_y && lane % 8 == 0)
+      reinterpret_cast<float*>(to + 3)[lane / 8] = mine4;
+    __syncthreads();
+    if (mean_r || mean_y) {
+#pragma unroll(S::kUnroll)
+      for (int i = 0; i < S::kWarps; ++i) {
+        s.mu_r = fmaf(part[i][0].x, k.counts[i], s.mu_r);
+        s.mu_y = fmaf(part[i][0].y, k.counts[i], s.mu_y);
+      }
+      s.mu_r *= k.inv_dim;
+      s.mu_y *= k.inv_dim;
+    }
+#pragma unroll(S::kUnroll)
+    for (int i = 0; i < S::kWarps; ++i) {
+      const float4 a = part[i][1], b = part[i][2];
+      s.rr += a.x;
+      s.yy += a.y;
+      s.dn_r += a.z;
+      s.dn += a.w;
+      s.dr_w += b.x;
+      s.dn_w += b.y;
+      s.r_w += b.z;
+      s.w += b.w;
+      if (mean_r) {
+        const float by = part[i][0].x - s.mu_r;
+        s.rr = fmaf(by * by, k.counts[i], s.rr);
+        s.dn_r = fmaf(by, a.w, s.dn_r);
+        s.r_w = fmaf(by, b.w, s.r_w);
+      }
+      if (mean_y) {
+        const float4 c = part[i][3];
+        const float by = part[i][0].y - s.mu_y;
+        const float by_r = mean_r ? part[i][0].x - s.mu_r : 0.f;
+        const float r_g = fmaf(by_r, c.w, c.z);
+        s.yy = fmaf(by * by, k.counts[i], s.yy);
+        s.dr_w = fmaf(by, c.x, s.dr_w);
+        s.dn_w = fmaf(by, c.y, s.dn_w);
+        s.r_w = fmaf(by, r_g, s.r_w);
+        s.w = fmaf(by, c.w, s.w);
+        s.dr_g += c.x;
+        s.dn_g += c.y;
+        s.r_g += r_g;
+        s.g += c.w;
+      }
+    }
+  }
+  return s;
+}
+
+template <typename TR, typename TY, int TPR, int NV, bool kAhead, int kRegs,
           int kMinCtas>
 __global__ void __launch_bounds__(Shape<TPR>::kThreads, kMinCtas)
 norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
@@ -70,13 +195,12 @@ norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
   // mine: gate post_weight (j), (1 + scale) pre_weight (NV + j), and the sums
   // over tokens A, C, E ((2, 3, 4) NV + j); then [2][dim] weight sums
   extern __shared__ float4 dyn4[];
-  Kept<kRegs, 5 * NV> mine;
+  Kept<kRegs * NV, 5 * NV> mine;
   mine.m = Private{dyn4};
-  static_assert(!kRegs || S::kRows == 1, "rows side by side are added there");
-  float* dyn = reinterpret_cast<float*>(
-      dyn4 + (kRegs ? 0 : 10 * NV * S::kThreads));
-  __shared__ float4 s_stat[S::kWarps];
-  __shared__ float2 s_dn[S::kWarps], s_du[S::kWarps];
+  static_assert(kRegs <= 2 || S::kRows == 1, "rows side by side are added there");
+  float* dyn =
+      reinterpret_cast<float*>(dyn4 + 2 * (5 - kRegs) * NV * S::kThreads);
+  __shared__ float4 s_part[2][S::kWarps][4];
   __shared__ float s_n[S::kWarps];
   pdl_trigger();
   const Cols<TPR, NV> k(p.dim, s_n);
@@ -103,25 +227,34 @@ norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
   const int64_t g1 =
       p.slices > 1 ? g0 + 1 : min(g0 + p.cta_groups, p.all_groups);
   const int slice = p.slices > 1 ? (int)(blockIdx.x % p.slices) : 0;
-  const int64_t t0 = slice * p.group_tokens / p.slices;
-  const int64_t t1 = (slice + 1) * p.group_tokens / p.slices;
+  const int64_t t0 = (int64_t)slice * kRows, step = (int64_t)p.slices * kRows;
+  const int64_t t1 = p.group_tokens;
 
   RowIn<TR, TY> in[NV];
-  auto fetch = [&](int64_t g, int64_t t) {
-    if (t >= t1) return;
+  // (fg, ft): the pass to load next
+  int64_t fg = g0, ft = t0;
+  auto fetch = [&] {
+    const int64_t t = ft + slot;
+    if (fg < g1 && t < t1)
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (k.on(j)) {
-        const int64_t at = (g * p.group_tokens + t) * p.dim + k.at(j);
-        if (has_dr) in[j].dr.load(p.dr, at);
-        if (has_h) {
-          in[j].dh.load(p.dh, at);
-          in[j].r.load(p.r, at);
+      for (int j = 0; j < NV; ++j)
+        if (k.on(j)) {
+          const int64_t at = (fg * p.group_tokens + t) * p.dim + k.at(j);
+          if (has_dr) in[j].dr.load(p.dr, at);
+          if (has_h) {
+            in[j].dh.load(p.dh, at);
+            in[j].r.load(p.r, at);
+          }
+          if (has_y) in[j].y.load(p.y, at);
         }
-        if (has_y) in[j].y.load(p.y, at);
-      }
+    ft += step;
+    if (ft >= t1) {
+      ft = t0;
+      ++fg;
+    }
   };
-  if (kAhead) fetch(g0, t0 + slot);
+  if (kAhead) fetch();
+  int turn = 0;
   for (int64_t g = g0; g < g1; ++g) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
@@ -141,82 +274,107 @@ norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
     }
     // Every thread makes every pass (barriers and shuffles inside); a slot
     // past the last row works on zeros.
-    for (int64_t tb = t0; tb < t1; tb += kRows) {
+    for (int64_t tb = t0; tb < t1; tb += step) {
       const int64_t t = tb + slot;
-      if (!kAhead) fetch(g, t);
+      if (!kAhead) fetch();
+      const bool on = t < t1;
       F8 d[NV], dh[NV], n[NV], u[NV];
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const bool on = t < t1 && k.on(j);
-        d[j] = on && has_dr ? in[j].dr.widen() : splat(0.f);
-        dh[j] = on && has_h ? in[j].dh.widen() : splat(0.f);
-        n[j] = on && has_h ? in[j].r.widen() : splat(0.f);
-        u[j] = on && has_y ? in[j].y.widen() : splat(0.f);
+        const bool here = on && k.on(j);
+        d[j] = here && has_dr ? in[j].dr.widen() : splat(0.f);
+        dh[j] = here && has_h ? in[j].dh.widen() : splat(0.f);
+        n[j] = here && has_h ? in[j].r.widen() : splat(0.f);
+        u[j] = here && has_y ? in[j].y.widen() : splat(0.f);
       }
       // the next row is on its way while this one is worked on
-      if (kAhead && tb + kRows < t1)
-        fetch(g, t + kRows);
-      else if (kAhead && g + 1 < g1)
-        fetch(g + 1, t0 + slot);
+      if (kAhead) fetch();
 
-      float rho = 1.f, rho_y = 1.f;
+      RowSums s = {};
       if (has_h || post) {
-        const Stats st = row_stats<TPR, NV>(n, u, mean_r, mean_y, k, s_stat);
-        rho = rsqrtf(st.sq_a * inv_dim + p.eps);
-        if (post) rho_y = rsqrtf(st.sq_b * inv_dim + p.eps);
+        float mu_r = 0.f, mu_y = 0.f;  // of this warp's columns
+        if (mean_r || mean_y) warp_means<TPR, NV>(n, u, k, mu_r, mu_y);
+        if (!mean_r) mu_r = 0.f;
+        if (!mean_y) mu_y = 0.f;
+        F2 q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = f2(0.f);
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-          if (t < t1 && k.on(j)) {
-            n[j] = fma(n[j], rho, -st.mu_a * rho);
-            u[j] = fma(u[j], rho_y, -st.mu_b * rho_y);
+          if (on && k.on(j)) {
+            const F8 r = add(n[j], splat(-mu_r)), y = add(u[j], splat(-mu_y));
+            const F8 dn = mul(dh[j], mine.get(NV + j));
+            const F8 w = mul(y, mine.get(j));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              q[0] = fma(r.v[e], r.v[e], q[0]);
+              q[1] = fma(y.v[e], y.v[e], q[1]);
+              q[2] = fma(dn.v[e], r.v[e], q[2]);
+              q[3] = add(dn.v[e], q[3]);
+              q[4] = fma(d[j].v[e], w.v[e], q[4]);
+              q[5] = fma(dn.v[e], w.v[e], q[5]);
+              q[6] = fma(r.v[e], w.v[e], q[6]);
+              q[7] = add(w.v[e], q[7]);
+            }
           }
-      }
-      if (has_h) {
-        F8 s0 = splat(0.f), s1 = s0;
+        float v[8], v4[4];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          mine.set(2 * NV + j, fma(dh[j], n[j], mine.get(2 * NV + j)));
-          mine.set(3 * NV + j, add(dh[j], mine.get(3 * NV + j)));
-          dh[j] = mul(dh[j], mine.get(NV + j));
-          s0 = add(s0, dh[j]);
-          s1 = fma(dh[j], n[j], s1);
-        }
-        float m0 = sum(s0), m1 = sum(s1);
-        row_sums<TPR>(m0, m1, s_dn);
-        m0 = p.pre == kNormLayer ? -m0 * inv_dim : 0.f;
-        m1 *= -inv_dim;
+        for (int i = 0; i < 8; ++i) v[i] = sum(q[i]);
+        if (mean_y) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-          d[j] = fma(fma(n[j], m1, add(dh[j], splat(m0))), rho, d[j]);
-      }
-      const int64_t at = (g * p.group_tokens + t) * p.dim;
-#pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (t < t1 && k.on(j))
-          store8(static_cast<TR*>(p.dx), at + k.at(j),
-                 mul(d[j], p.residual_scale));
-      if (has_y) {
-        F8 s0 = splat(0.f), s1 = s0;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-          mine.set(4 * NV + j, fma(d[j], u[j], mine.get(4 * NV + j)));
-          d[j] = mul(d[j], mine.get(j));
-          s0 = add(s0, d[j]);
-          s1 = fma(d[j], u[j], s1);
-        }
-        if (post) {
-          float m0 = sum(s0), m1 = sum(s1);
-          row_sums<TPR>(m0, m1, s_du);
-          m0 = p.post == kNormLayer ? -m0 * inv_dim : 0.f;
-          m1 *= -inv_dim;
+          for (int i = 0; i < 4; ++i) q[i] = f2(0.f);
 #pragma unroll
           for (int j = 0; j < NV; ++j)
-            d[j] = mul(fma(u[j], m1, add(d[j], splat(m0))), rho_y);
-        }
+            if (on && k.on(j)) {
+              const F8 gp = mine.get(j), r = add(n[j], splat(-mu_r));
+              const F8 dn = mul(dh[j], mine.get(NV + j));
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-          if (t < t1 && k.on(j))
-            store8(static_cast<TY*>(p.dy), at + k.at(j), d[j]);
+              for (int e = 0; e < 4; ++e) {
+                q[0] = fma(d[j].v[e], gp.v[e], q[0]);
+                q[1] = fma(dn.v[e], gp.v[e], q[1]);
+                q[2] = fma(r.v[e], gp.v[e], q[2]);
+                q[3] = add(gp.v[e], q[3]);
+              }
+            }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v4[i] = sum(q[i]);
+        }
+        s = row_part_sums<TPR, NV>(v, v4, mu_r, mu_y, mean_r, mean_y, k,
+                                   s_part[turn]);
+        turn ^= 1;
+      }
+      // d = dr + rho (dn + m0 + m1 n(r)), dy = rho_y (d gp + m2 + m3 n(y))
+      const float rho = rsqrtf(s.rr * inv_dim + p.eps);
+      const float rho_y = post ? rsqrtf(s.yy * inv_dim + p.eps) : 1.f;
+      const float m0 = mean_r ? -s.dn * inv_dim : 0.f;
+      const float m1 = -s.dn_r * rho * inv_dim;
+      const float m2 =
+          mean_y ? -(s.dr_g + rho * (s.dn_g + m0 * s.g + m1 * rho * s.r_g)) *
+                       inv_dim
+                 : 0.f;
+      const float m3 =
+          -(s.dr_w + rho * (s.dn_w + m0 * s.w + m1 * rho * s.r_w)) * rho_y *
+          inv_dim;
+      const int64_t at = (g * p.group_tokens + t) * p.dim;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        if (has_h) {
+          const F8 unit = fma(n[j], rho, -s.mu_r * rho);
+          mine.set(2 * NV + j, fma(dh[j], unit, mine.get(2 * NV + j)));
+          mine.set(3 * NV + j, add(dh[j], mine.get(3 * NV + j)));
+          d[j] = fma(fma(unit, m1, fma(dh[j], mine.get(NV + j), splat(m0))),
+                     rho, d[j]);
+        }
+        if (on && k.on(j))
+          store8(static_cast<TR*>(p.dx), at + k.at(j),
+                 mul(d[j], p.residual_scale));
+        if (!has_y) continue;
+        if (post) u[j] = fma(u[j], rho_y, -s.mu_y * rho_y);
+        mine.set(4 * NV + j, fma(d[j], u[j], mine.get(4 * NV + j)));
+        d[j] = mul(d[j], mine.get(j));
+        if (post) d[j] = mul(fma(u[j], m3, add(d[j], splat(m2))), rho_y);
+        if (on && k.on(j))
+          store8(static_cast<TY*>(p.dy), at + k.at(j), d[j]);
       }
     }
 
@@ -233,7 +391,7 @@ norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
 #pragma unroll
             for (int r = 1; r < kRows; ++r)
               sums[q] = add(sums[q], Private{dyn4 + r * TPR}.get(
-                                         (2 + q) * NV + j));
+                                         (2 + q - kRegs) * NV + j));
           }
           end_group(p, g, k.at(j), sums[0], sums[1], sums[2], dyn);
         }
@@ -306,16 +464,22 @@ norm_bwd_sum_kernel(const __grid_constant__ NormBwdParams p) {
   }
 }
 
-// CTAs per SM of the kernel that dim selects, see launch_t.
-int ctas_per_sm(int dim) {
-  return dim <= 256 ? 4 : dim <= 512 ? 5 : dim <= 1024 ? 3 : dim <= 2048 ? 2 : 1;
+// CTAs per SM of the kernel that is selected, see launch_t.
+int ctas_per_sm(int dim, int64_t group_tokens) {
+  if (dim > 1024 && dim <= 1536 && group_tokens < kFewTokens) return 3;
+  return dim <= 256    ? 4
+         : dim <= 512  ? 5
+         : dim <= 768  ? 4
+         : dim <= 1024 ? 3
+         : dim <= 2048 ? 2
+                       : 1;
 }
 
-template <typename TR, typename TY, int TPR, int NV, bool kAhead, bool kRegs,
+template <typename TR, typename TY, int TPR, int NV, bool kAhead, int kRegs,
           int kMinCtas>
 cudaError_t launch_v(const NormBwdParams& p, cudaStream_t stream) {
   const size_t smem =
-      (kRegs ? 0 : (size_t)10 * NV * Shape<TPR>::kThreads * sizeof(float4)) +
+      (size_t)2 * (5 - kRegs) * NV * Shape<TPR>::kThreads * sizeof(float4) +
       (p.weight_partial != nullptr ? (size_t)2 * p.dim * sizeof(float) : 0);
   auto kernel = norm_bwd_kernel<TR, TY, TPR, NV, kAhead, kRegs, kMinCtas>;
   if (smem > 32768) {  // up to 224 KB at dim 8192
@@ -327,26 +491,30 @@ cudaError_t launch_v(const NormBwdParams& p, cudaStream_t stream) {
                     dim3(Shape<TPR>::kThreads), smem, stream, p);
 }
 
-// Threads and vectors of a row, whether its sums stay in registers, and CTAs
-// per SM: what was fastest of those that do not spill (12288 rows of 1536 with
-// a float32 residual: 96 threads of 16 columns 73.7 us, 192 of 8 76.1, the
-// same with the sums in shared memory 82; one more CTA per SM at the price of
-// spills 115 and more).  With groups of a few rows, whose ends then count, 192
-// threads of 8 columns: 84.8 us for 8160 groups of one row, against 120.9.
+// Threads and vectors of a row, whether the next row is loaded ahead, how many of
+// a thread's five vectors stay in registers, CTAs per SM: what was fastest of
+// those that do not spill (12288 rows of 1536 with a float32 residual: 96 threads
+// of 16 columns 72.0 us, the same with all five in shared memory and four CTAs
+// 73.5, 192 of 8 and three CTAs 81.8; rows ahead in shared memory 92 and more;
+// 9000 rows of 2048: 61.7 us, 128 threads of 16 columns 68.8).  With groups of a
+// few rows, whose ends then count, 192 threads of 8 columns: 78.5 us for 8160
+// groups of one row, against 98.  Rows above 5120 do not leave the registers to
+// load ahead (128.7 us for 3000 rows of 8192).
 template <typename TR, typename TY>
 cudaError_t launch_t(const NormBwdParams& p, cudaStream_t stream) {
-  if (p.dim <= 64) return launch_v<TR, TY, 8, 1, true, false, 4>(p, stream);
-  if (p.dim <= 128) return launch_v<TR, TY, 16, 1, true, false, 4>(p, stream);
-  if (p.dim <= 256) return launch_v<TR, TY, 32, 1, true, false, 4>(p, stream);
-  if (p.dim <= 512) return launch_v<TR, TY, 64, 1, true, true, 5>(p, stream);
-  if (p.dim <= 1024) return launch_v<TR, TY, 128, 1, true, true, 3>(p, stream);
-  if (p.dim <= 1536 && p.group_tokens < 16)
-    return launch_v<TR, TY, 192, 1, true, true, 2>(p, stream);
-  if (p.dim <= 1536) return launch_v<TR, TY, 96, 2, true, true, 2>(p, stream);
-  if (p.dim <= 2048) return launch_v<TR, TY, 256, 1, true, false, 2>(p, stream);
-  if (p.dim <= 4096) return launch_v<TR, TY, 256, 2, true, false, 1>(p, stream);
-  if (p.dim <= 5120) return launch_v<TR, TY, 320, 2, true, false, 1>(p, stream);
-  return launch_v<TR, TY, 1024, 1, false, false, 1>(p, stream);
+  if (p.dim <= 64) return launch_v<TR, TY, 8, 1, true, 0, 4>(p, stream);
+  if (p.dim <= 128) return launch_v<TR, TY, 16, 1, true, 0, 4>(p, stream);
+  if (p.dim <= 256) return launch_v<TR, TY, 32, 1, true, 0, 4>(p, stream);
+  if (p.dim <= 512) return launch_v<TR, TY, 64, 1, true, 5, 5>(p, stream);
+  if (p.dim <= 768) return launch_v<TR, TY, 96, 1, true, 5, 4>(p, stream);
+  if (p.dim <= 1024) return launch_v<TR, TY, 128, 1, true, 5, 3>(p, stream);
+  if (p.dim <= 1536 && p.group_tokens < kFewTokens)
+    return launch_v<TR, TY, 192, 1, true, 0, 3>(p, stream);
+  if (p.dim <= 1536) return launch_v<TR, TY, 96, 2, true, 5, 2>(p, stream);
+  if (p.dim <= 2048) return launch_v<TR, TY, 256, 1, true, 3, 2>(p, stream);
+  if (p.dim <= 4096) return launch_v<TR, TY, 256, 2, true, 0, 1>(p, stream);
+  if (p.dim <= 5120) return launch_v<TR, TY, 320, 2, true, 0, 1>(p, stream);
+  return launch_v<TR, TY, 512, 2, false, 0, 1>(p, stream);
 }
 
 }  // namespace
@@ -356,7 +524,7 @@ cudaError_t launch_t(const NormBwdParams& p, cudaStream_t stream) {
 NormBwdSplit norm_bwd_split(int64_t all_groups, int64_t group_tokens, int dim,
                             int sms) {
   NormBwdSplit s;
-  const int64_t want = (int64_t)sms * ctas_per_sm(dim);
+  const int64_t want = (int64_t)sms * ctas_per_sm(dim, group_tokens);
   s.slices = 1;
   s.cta_groups = 1;
   if (all_groups < want) {

@@ -48,6 +48,7 @@
 #include <algorithm>
 
 #include "fastvr_internal.h"
+#include "vec_math.cuh"
 
 namespace fastvr {
 namespace {
@@ -59,30 +60,6 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
-}
-__device__ __forceinline__ uint32_t smem_u32(const void* p) {
-  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
-}
-// Asynchronous copy of N bytes to shared memory, zeros when !valid.
-template <int N>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src,
-                                           bool valid) {
-  const int n = valid ? N : 0;
-  if constexpr (N == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst),
-                 "l"(src), "r"(n)
-                 : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst),
-                 "l"(src), "n"(N), "r"(n)
-                 : "memory");
-}
-__device__ __forceinline__ void copy_commit() {
-  asm volatile("cp.async.commit_group;" ::: "memory");
-}
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ void mma_half(float (&c)[4], const uint32_t (&a)[4],
                                          uint32_t b0, uint32_t b1) {

@@ -1,6 +1,6 @@
 // Small device helpers shared by the elementwise kernels: packed float32 pairs
-// (one instruction for two values on sm_103a) and divisions by a number fixed
-// at launch.
+// (one instruction for two values on sm_103a), divisions by a number fixed at
+// launch and asynchronous copies to shared memory.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -77,6 +77,31 @@ __device__ __forceinline__ uint32_t bf16_pack(F2 a) {
   float lo, hi;
   split(a, lo, hi);
   return bf16_pack(lo, hi);
+}
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+// Asynchronous copy of N bytes to shared memory, zeros when !valid.
+template <int N>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src,
+                                           bool valid) {
+  const int n = valid ? N : 0;
+  if constexpr (N == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst),
+                 "l"(src), "r"(n)
+                 : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst),
+                 "l"(src), "n"(N), "r"(n)
+                 : "memory");
+}
+__device__ __forceinline__ void copy_commit() {
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 #endif
 
