@@ -280,14 +280,17 @@ cudaError_t launch_q4_read(const Q4ReadParams& p, bool head_major, int sms,
 
 // Whether a call goes straight over the codes (q4_attn.cu) or first writes the
 // visible keys and values in bfloat16 to the workspace and runs the tile
-// kernel over them.  Per key and key head the former takes about 0.17 ns for
-// every 32 query rows (tokens times query heads per key head), the latter 0.10
-// to expand and 0.12 for every query head and 256 tokens (measured on 12 heads
-// and 32768 keys, and on 8 streams of 32 over 8 heads and 8192 keys; the two
-// meet at 32 rows and at 112).
+// kernel over them.  Per key and key head the former takes about 0.06 ns and
+// 0.07 for every 32 query rows (tokens times query heads per key head), the
+// latter 0.17 to expand and 0.04 for every query head and 256 tokens: 12 heads
+// over 32768 keys take 50.9 us directly with 32 rows, 75.6 with 64 and 84 the
+// other way, 8 streams of 32 heads over 8 and 8192 keys 144 us with 96 rows, 182
+// with 128 and 178.  The few keys of a short window leave the direct way's
+// shares too small for its second block to pay (4096 keys: 26.8 us with 64 rows
+// against 19.4), hence the 8.
 inline bool q4_direct(int64_t q_tokens, int64_t group) {
   const int64_t blocks = (q_tokens * group + 31) / 32;
-  return blocks * 17 < 10 + 12 * group * ((q_tokens + 255) / 256);
+  return 8 + 7 * blocks < 17 + 4 * group * ((q_tokens + 255) / 256);
 }
 constexpr int kQ4MaxCtas = 512;               // of a launch
 constexpr int kQ4MaxParts = 2 * kQ4MaxCtas;   // partial results, two per CTA
