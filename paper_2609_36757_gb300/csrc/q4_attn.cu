@@ -139,9 +139,10 @@ __device__ __forceinline__ int v_offset(int r, int byte) {
 // slowest) are cut into even shares, one to a CTA, however different the
 // entries' lengths are.  Every unit counts kUnitCost tiles more than it has,
 // about what starting and ending it costs, so that a CTA with many short
-// units is not the last one; an entry that sees no key still has units, whose
+// units is not the last one (eight streams of 6000 to 66000 keys: 64.7 us with 12,
+// 57.0 with 24, 58.1 with 32); an entry that sees no key still has units, whose
 // zeros someone writes.
-constexpr int kUnitCost = 12;
+constexpr int kUnitCost = 24;
 
 // A CTA's part of a unit.
 struct Piece {
