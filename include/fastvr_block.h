@@ -213,8 +213,9 @@ FASTVR_API fastvr_status_t fastvr_gated_norm_bwd(
 /* Bytes of cache and of workspace for cfg with kv_heads key/value heads
  * (cfg->heads query heads, a multiple of kv_heads: consecutive query heads
  * share one).  A head's cache holds fewer than 2^30 tokens, S*k*N, and a
- * chunk has fewer than 2^30 query rows per key head.  A workspace may serve any number of plans whose calls do not
- * overlap on the GPU; nothing is kept in it between calls.
+ * chunk has fewer than 2^30 query rows per key head.  A workspace may serve
+ * any number of plans whose calls do not overlap on the GPU; nothing is kept
+ * in it between calls.
  * Host only.  Errors: INVALID_ARG, UNSUPPORTED (head_dim not 64 or 128). */
 FASTVR_API fastvr_status_t fastvr_q4_cache_bytes(
     const fastvr_attn_config_t* cfg, int32_t kv_heads, size_t* bytes);

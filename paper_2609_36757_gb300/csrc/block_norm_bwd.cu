@@ -468,7 +468,7 @@ norm_bwd_sum_kernel(const __grid_constant__ NormBwdParams p) {
 int ctas_per_sm(int dim, int64_t group_tokens) {
   if (dim > 1024 && dim <= 1536 && group_tokens < kFewTokens) return 3;
   return dim <= 256    ? 4
-         : dim <= 512  ? 5
+         : dim <= 512  ? 6
          : dim <= 768  ? 4
          : dim <= 1024 ? 3
          : dim <= 2048 ? 2
@@ -493,19 +493,19 @@ cudaError_t launch_v(const NormBwdParams& p, cudaStream_t stream) {
 
 // Threads and vectors of a row, whether the next row is loaded ahead, how many of
 // a thread's five vectors stay in registers, CTAs per SM: what was fastest of
-// those that do not spill (12288 rows of 1536 with a float32 residual: 96 threads
+// those that spill nothing, or next to nothing in float32 throughout (12288 rows of 1536 with a float32 residual: 96 threads
 // of 16 columns 72.0 us, the same with all five in shared memory and four CTAs
 // 73.5, 192 of 8 and three CTAs 81.8; rows ahead in shared memory 92 and more;
 // 9000 rows of 2048: 61.7 us, 128 threads of 16 columns 68.8).  With groups of a
 // few rows, whose ends then count, 192 threads of 8 columns: 78.5 us for 8160
-// groups of one row, against 98.  Rows above 5120 do not leave the registers to
-// load ahead (128.7 us for 3000 rows of 8192).
+// groups of one row, against 98.  Rows above 5120 leave no registers to load
+// ahead and spill some (128.7 us for 3000 rows of 8192; 1024 threads took 181).
 template <typename TR, typename TY>
 cudaError_t launch_t(const NormBwdParams& p, cudaStream_t stream) {
   if (p.dim <= 64) return launch_v<TR, TY, 8, 1, true, 0, 4>(p, stream);
   if (p.dim <= 128) return launch_v<TR, TY, 16, 1, true, 0, 4>(p, stream);
   if (p.dim <= 256) return launch_v<TR, TY, 32, 1, true, 0, 4>(p, stream);
-  if (p.dim <= 512) return launch_v<TR, TY, 64, 1, true, 5, 5>(p, stream);
+  if (p.dim <= 512) return launch_v<TR, TY, 64, 1, true, 5, 6>(p, stream);
   if (p.dim <= 768) return launch_v<TR, TY, 96, 1, true, 5, 4>(p, stream);
   if (p.dim <= 1024) return launch_v<TR, TY, 128, 1, true, 5, 3>(p, stream);
   if (p.dim <= 1536 && p.group_tokens < kFewTokens)

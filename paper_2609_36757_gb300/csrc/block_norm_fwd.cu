@@ -210,9 +210,10 @@ cudaError_t launch_v(const NormFwdParams& p, int sms, cudaStream_t stream) {
 
 // Threads, vectors and rows of a pass, passes ahead in shared memory (0: one in
 // registers), CTAs per SM.  Rows of up to 256 columns lie side by side in a CTA
-// (in shared memory ahead: 49.5 us against 40 for 277236 rows of 64).  From there
-// to 512 eight columns to a thread and the next row in registers (36000 rows of
-// 512: 27.4 us, 30.2 through shared memory), above that through shared memory
+// (277236 rows of 64: 35.3 us with one row to a thread and 6 CTAs, 40.2 with two
+// and 4, 49.5 with rows ahead in shared memory).  From there to 512 eight columns
+// to a thread and the next row in registers as well (36000 rows of
+// 512: 25.7 us, 30.2 through shared memory), above that through shared memory
 // (against registers: 36.4 us and 52.6 for 36000 rows of 520, 27.4 and 30.4 for
 // 18000 of 1024, 36.1 and 38.6 for 16320 of 1536 by twos), from 2048 on with 16
 // columns to a thread, which leaves fewer warps to exchange with (29.1 and 38.6
@@ -221,10 +222,10 @@ cudaError_t launch_v(const NormFwdParams& p, int sms, cudaStream_t stream) {
 // one row at a time and in registers then (8160 rows of 1536: 43.0 us and 45.3).
 template <typename TR, typename TY>
 cudaError_t launch_t(const NormFwdParams& p, int sms, cudaStream_t stream) {
-  if (p.dim <= 64) return launch_v<TR, TY, 8, 1, 2, 0, 4>(p, sms, stream);
-  if (p.dim <= 128) return launch_v<TR, TY, 16, 1, 2, 0, 4>(p, sms, stream);
-  if (p.dim <= 256) return launch_v<TR, TY, 32, 1, 2, 0, 4>(p, sms, stream);
-  if (p.dim <= 512) return launch_v<TR, TY, 64, 1, 1, 0, 12>(p, sms, stream);
+  if (p.dim <= 64) return launch_v<TR, TY, 8, 1, 1, 0, 6>(p, sms, stream);
+  if (p.dim <= 128) return launch_v<TR, TY, 16, 1, 1, 0, 6>(p, sms, stream);
+  if (p.dim <= 256) return launch_v<TR, TY, 32, 1, 1, 0, 6>(p, sms, stream);
+  if (p.dim <= 512) return launch_v<TR, TY, 64, 1, 1, 0, 16>(p, sms, stream);
   if (p.dim <= 768) return launch_v<TR, TY, 96, 1, 1, 2, 9>(p, sms, stream);
   if (p.dim <= 1024) return launch_v<TR, TY, 128, 1, 1, 2, 8>(p, sms, stream);
   if (p.dim <= 1536 && p.group_tokens < kFewTokens)
