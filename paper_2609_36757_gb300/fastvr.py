@@ -17,6 +17,7 @@ attention in a block.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple, Optional, Tuple
 
@@ -553,18 +554,18 @@ class StreamingAttention:
 # directly (torch.cuda.current_stream() builds a stream object, 2.9 us on the
 # measured host against 0.1).
 _CODES: dict = {}
-_raw_stream = None
+_torch = _raw_stream = None
 
 
 def _setup():
     """torch, with the tables that need it filled in."""
-    global _raw_stream
+    global _raw_stream, _torch
     import torch
-    if not _CODES:
-        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-            lambda i: torch.cuda.current_stream(i).cuda_stream)
-        _CODES[torch.bfloat16] = FASTVR_BF16
-        _CODES[torch.float32] = FASTVR_F32
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+        lambda i: torch.cuda.current_stream(i).cuda_stream)
+    _CODES[torch.bfloat16] = FASTVR_BF16
+    _CODES[torch.float32] = FASTVR_F32
+    _torch = torch
     return torch
 
 
@@ -580,17 +581,22 @@ def _dtype_code(t) -> int:
     return code
 
 
+@functools.lru_cache(maxsize=64)
+def _strides_ref(batch: int, token: int, head: int):
+    return ctypes.byref(fastvr_strides_t(batch, token, head))
+
+
 def _head_strides(t, name: str):
     """fastvr_strides_t of a [B, L, H, d] tensor whose heads are contiguous,
     None when the whole tensor is."""
-    if not t.is_cuda or t.dim() != 4:
+    strides = t.stride()
+    if not t.is_cuda or len(strides) != 4:
         raise ValueError(f"{name} must be a CUDA tensor [B, L, H, d]")
     if t.is_contiguous():
         return None
-    b, l, h, e = t.stride()
-    if e != 1:
+    if strides[3] != 1:
         raise ValueError(f"the elements of a head of {name} must be contiguous")
-    return fastvr_strides_t(b, l, h)
+    return _strides_ref(*strides[:3])
 
 
 def make_rotary_config(head_dim: int, rotary_dim: Optional[int] = None,
@@ -624,7 +630,7 @@ def rotary(cfg: fastvr_rotary_config_t, q, k, positions, out=None,
     (slices of a fused projection); positions int32 [L, axes] or [B or 1, L,
     axes].  Returns (q', k'), contiguous unless `out` gives the two outputs
     (out=(q, k) works in place)."""
-    torch = _setup()
+    torch = _torch or _setup()
     code = _dtype_code(q)
     q_str = _head_strides(q, "q")
     B, L, H, d = q.shape
@@ -633,18 +639,18 @@ def rotary(cfg: fastvr_rotary_config_t, q, k, positions, out=None,
         raise ValueError(f"q has shape {tuple(q.shape)}")
     if k is not None:
         k_str = _head_strides(k, "k")
-        Hk = k.shape[2]
-        if k.shape != (B, L, Hk, d) or k.dtype != q.dtype:
+        shape = k.shape
+        Hk = shape[2]
+        if shape != (B, L, Hk, d) or k.dtype != q.dtype:
             raise ValueError("q and k differ in type or shape")
     if positions.dtype != torch.int32 or not positions.is_cuda or \
             not positions.is_contiguous():
         raise ValueError("positions must be a contiguous int32 CUDA tensor")
-    if positions.dim() == 2:
-        rows = 1
-    else:
-        rows = positions.shape[0] if positions.dim() == 3 else -1
-    if positions.shape[-2:] != (L, cfg.axes) or rows not in (1, B):
-        raise ValueError(f"positions have shape {tuple(positions.shape)}")
+    axes, shape = cfg.axes, positions.shape
+    rows = shape[0] if len(shape) == 3 else 1
+    if shape != ((rows, L, axes) if len(shape) == 3 else (L, axes)) or \
+            rows != 1 and rows != B:
+        raise ValueError(f"positions have shape {tuple(shape)}")
     if out is None:
         q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         k_out = None if k is None else torch.empty_like(
@@ -661,7 +667,7 @@ def rotary(cfg: fastvr_rotary_config_t, q, k, positions, out=None,
             k_out, "the output for k")
     fastvr_rotary(cfg, B, L, H, Hk, code, q.data_ptr(), q_str,
                   0 if k is None else k.data_ptr(), k_str,
-                  positions.data_ptr(), L * cfg.axes if rows > 1 else 0,
+                  positions.data_ptr(), L * axes if rows > 1 else 0,
                   q_out.data_ptr(), q_out_str,
                   0 if k is None else k_out.data_ptr(), k_out_str,
                   int(transpose), _stream_of(q))
@@ -682,7 +688,7 @@ def make_norm_config(pre: str = "rms", post: str = "none", eps: float = 1e-6,
 
 def _norm_call(cfg, x, y, mods, weights):
     """cfg for the tensors of a call, after their checks."""
-    torch = _setup()
+    torch = _torch or _setup()
     shape = x.shape
     if len(shape) != 3 or not x.is_cuda or not x.is_contiguous():
         raise ValueError("x must be a contiguous CUDA tensor [B, L, D]")
@@ -726,7 +732,7 @@ def gated_norm(cfg: fastvr_norm_config_t, x, y, gate=None, scale=None,
     float32) and y the same shape (or None: no block output), gate, scale and
     shift float32 [B, G, D], weights float32 [D].  Returns (r, h), None for
     the one not wanted; h has y's type (block_dtype without y)."""
-    torch = _setup()
+    torch = _torch or _setup()
     c = _norm_call(cfg, x, (y,), (gate, scale, shift),
                    (pre_weight, post_weight))
     block = (block_dtype or torch.bfloat16) if y is None else y.dtype
@@ -759,7 +765,7 @@ def gated_norm_bwd(cfg: fastvr_norm_config_t, dr, dh, r, y, gate=None,
     and h (either may be None), r the forward's r.  dshift is formed when
     scale is given, or as want_dshift says (the groups are then gate's or
     scale's, or one)."""
-    torch = _setup()
+    torch = _torch or _setup()
     if dr is not None and (dr.shape != r.shape or dr.dtype != r.dtype or
                            not dr.is_contiguous()):
         raise ValueError("dr must be contiguous and of r's type and shape")
@@ -797,7 +803,7 @@ class StreamingAttention4:
 
     def __init__(self, cfg: fastvr_attn_config_t,
                  kv_heads: Optional[int] = None, device=None, workspace=None):
-        torch = _setup()
+        torch = _torch or _setup()
         self.cfg = cfg
         self.kv_heads = cfg.heads if kv_heads is None else kv_heads
         device = device or "cuda"
@@ -821,7 +827,7 @@ class StreamingAttention4:
             self.plan = None
 
     def append(self, k, v) -> None:
-        torch = _setup()
+        torch = _torch or _setup()
         c = self.cfg
         if k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
             raise ValueError("k and v must be bfloat16")
@@ -840,7 +846,7 @@ class StreamingAttention4:
                 want_lse: bool = False):
         """Attention of the newest chunk's queries; first_chunk, int32 [B]:
         the first chunk that each batch entry sees."""
-        torch = _setup()
+        torch = _torch or _setup()
         c = self.cfg
         if q.dtype != torch.bfloat16 or not q.is_cuda or \
                 not q.is_contiguous() or q.dim() != 4:
@@ -875,7 +881,7 @@ class StreamingAttention4:
     def read(self, chunk: Optional[int] = None):
         """(k, v) bfloat16 [B, f*N, kv_heads, d]: the values held for a chunk
         (default: the newest)."""
-        torch = _setup()
+        torch = _torch or _setup()
         c = self.cfg
         chunks, frames = self.state()
         chunk = chunks - 1 if chunk is None else chunk
