@@ -347,98 +347,137 @@ __device__ __forceinline__ void end_piece(const Q4AttnParams& p, S* sh,
   if (threadIdx.x == 0 && piece.parts > 1) sh->shared[piece.mine] = piece;
 }
 
-// The last CTA of a unit to arrive joins its parts, in their order: the weight
-// of every (row, part) first, then sums of weighted rows with many loads in
-// flight.
+// The last CTA of a unit to arrive joins its parts, in their order: m and l of
+// all of them first, the weight of every (part, row) from these, then sums of
+// weighted rows.  Each step has its loads in flight together: what a join costs
+// is their latency (32 rows over 4096 keys of 12 heads: 25.5 us with a row and a
+// few loads at a time, 21.8 now).
 template <int D, int NT, int W, int kWarpBytes, class S>
 __device__ __forceinline__ void join_parts(const Q4AttnParams& p, S* sh,
                                            uint8_t* smem, const Piece& piece) {
-  constexpr int kRows = 8 * NT;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  constexpr int kRows = 8 * NT, kThreads = W * 32;
+  int tid;  // read anew: what follows from it is not kept across the tiles
+  asm volatile("mov.u32 %0, %%tid.x;" : "=r"(tid));
+  const int warp = tid / 32, lane = tid % 32;
   const int parts = piece.parts, cta0 = piece.cta0, slot0 = piece.slot0;
   const int rows = min(kRows, p.rows - piece.rb * kRows);
   auto slot_of = [&](int cta) {
     return (cta * 2 + (cta == cta0 ? slot0 : 0)) * kRows;
   };
   const float2* all_ml = partial_ml<D>(p);
-  float* weight = reinterpret_cast<float*>(smem);  // [row][part]
-  for (int row = warp; row < rows; row += W) {
-    float* w = weight + row * parts;
-    float top = -INFINITY;
-    for (int i = lane; i < parts; i += 32) {
-      const float2 ml = __ldcg(all_ml + slot_of(cta0 + i) + row);
-      w[i] = ml.x;
-      top = fmaxf(top, ml.x);
-    }
+  constexpr int kPitch = kRows + 1;
+  float2* ml = reinterpret_cast<float2*>(smem);  // [part][row]
+  constexpr int kAtOnce = 32 / kRows;            // parts to a warp
+  const int r = lane % kRows;
+#pragma unroll 4
+  for (int i = warp * kAtOnce + lane / kRows; i < parts; i += W * kAtOnce)
+    if (r < rows) ml[i * kPitch + r] = __ldcg(all_ml + slot_of(cta0 + i) + r);
+  __syncthreads();
+  // Rows warp, warp + W, ... of a warp, side by side.
+  constexpr int kOwn = (kRows + W - 1) / W;
+  float top[kOwn], sum[kOwn];
 #pragma unroll
-    for (int y = 16; y > 0; y /= 2)
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, y));
-    float sum = 0.f;
-    for (int i = lane; i < parts; i += 32) {
-      const float l = __ldcg(all_ml + slot_of(cta0 + i) + row).y;
-      // a part without keys has m = -inf and l = 0
-      const float f = w[i] == -INFINITY && l == 0.f ? 0.f : ex2(w[i] - top);
-      w[i] = f;
-      sum = fmaf(f, l, sum);
-    }
+  for (int k = 0; k < kOwn; ++k) {
+    top[k] = -INFINITY;
+    sum[k] = 0.f;
+  }
+  for (int i = lane; i < parts; i += 32)
 #pragma unroll
-    for (int y = 16; y > 0; y /= 2)
-      sum += __shfl_xor_sync(0xffffffffu, sum, y);
-    if (lane == 0) {
-      sh->m[0][row] = top;
-      sh->l[0][row] = sum;
-    }
+    for (int k = 0; k < kOwn; ++k)
+      if (warp + k * W < rows)
+        top[k] = fmaxf(top[k], ml[i * kPitch + warp + k * W].x);
+#pragma unroll
+  for (int y = 16; y > 0; y /= 2)
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+      top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], y));
+  for (int i = lane; i < parts; i += 32)
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+      if (warp + k * W < rows) {
+        float2& v = ml[i * kPitch + warp + k * W];
+        // a part without keys has m = -inf and l = 0
+        const float f =
+            v.x == -INFINITY && v.y == 0.f ? 0.f : ex2(v.x - top[k]);
+        v.x = f;
+        sum[k] = fmaf(f, v.y, sum[k]);
+      }
+#pragma unroll
+  for (int y = 16; y > 0; y /= 2)
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+      sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], y);
+  if (lane < kOwn && warp + lane * W < rows) {
+    // lane k: row warp + k W
+    float m = top[0], l = sum[0];
+#pragma unroll
+    for (int k = 1; k < kOwn; ++k)
+      if (lane == k) m = top[k], l = sum[k];
+    const int row = warp + lane * W;
+    sh->m[0][row] = m;
+    sh->l[0][row] = l;
   }
   __syncthreads();
+  // A thread takes up to kPer pieces of 4 columns; with few rows the parts are
+  // shared out over `share` threads, whose sums are added in their order.
   constexpr int kSlots = D / 4;
+  constexpr int kPer = (kRows * kSlots + kThreads - 1) / kThreads;
+  constexpr int kBatch = NT == 1 ? 8 : 16 / kPer;
   const int slots = rows * kSlots;
-  // With few rows the parts are shared out over `share` threads, whose sums
-  // are added in their order.
-  static_assert(kQ4MaxCtas * kRows * 4 + W * 32 * 16 <= W * kWarpBytes,
+  static_assert(kQ4MaxCtas * kPitch * 8 + kThreads * 16 <= W * kWarpBytes,
                 "weights and sums do not fit");
-  float4* sums = reinterpret_cast<float4*>(weight + kQ4MaxCtas * kRows);
-  const int share = max(1, W * 32 / slots);
-  const int who = share > 1 ? threadIdx.x / slots : 0;
-  for (int x0 = 0; x0 < slots; x0 += W * 32) {
-    const int x = x0 + threadIdx.x - who * slots;
-    const bool on = x < slots && who < share;
-    const int row = x / kSlots, d = x % kSlots * 4;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (on) {
-      const float* src = p.partial + row * D + d;
-      const float* w = weight + row * parts;
-      constexpr int kBatch = 8;
-      for (int i0 = who; i0 < parts; i0 += kBatch * share) {
-        float4 v[kBatch];
+  float4* sums = reinterpret_cast<float4*>(ml + kQ4MaxCtas * kPitch);
+  const int share = max(1, kThreads / slots);
+  const int who = share > 1 ? tid / slots : 0;
+  const int x0 = tid - who * slots;
+  float4 acc[kPer];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u)
-          if (i0 + u * share < parts)
-            v[u] = __ldcg(reinterpret_cast<const float4*>(
-                src + slot_of(cta0 + i0 + u * share) * D));
+  for (int k = 0; k < kPer; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (who < share)
+    for (int i0 = who; i0 < parts; i0 += kBatch * share) {
+      float4 v[kPer][kBatch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u)
-          if (i0 + u * share < parts) {
-            const float f = w[i0 + u * share];
-            acc.x = fmaf(f, v[u].x, acc.x);
-            acc.y = fmaf(f, v[u].y, acc.y);
-            acc.z = fmaf(f, v[u].z, acc.z);
-            acc.w = fmaf(f, v[u].w, acc.w);
-          }
-      }
-    }
-    if (share > 1) {
-      sums[threadIdx.x] = acc;
-      __syncthreads();
-      if (who == 0)
-        for (int i = 1; i < share; ++i) {
-          if (x >= slots) break;
-          const float4 v = sums[i * slots + x];
-          acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
+      for (int u = 0; u < kBatch; ++u)
+        if (i0 + u * share < parts) {
+          const float* src = p.partial + slot_of(cta0 + i0 + u * share) * D;
+#pragma unroll
+          for (int k = 0; k < kPer; ++k)
+            if (x0 + k * kThreads < slots)
+              v[k][u] = __ldcg(
+                  reinterpret_cast<const float4*>(src) + x0 + k * kThreads);
         }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (i0 + u * share < parts)
+#pragma unroll
+          for (int k = 0; k < kPer; ++k)
+            if (x0 + k * kThreads < slots) {
+              const float f = ml[(i0 + u * share) * kPitch +
+                                 (x0 + k * kThreads) / kSlots].x;
+              acc[k].x = fmaf(f, v[k][u].x, acc[k].x);
+              acc[k].y = fmaf(f, v[k][u].y, acc[k].y);
+              acc[k].z = fmaf(f, v[k][u].z, acc[k].z);
+              acc[k].w = fmaf(f, v[k][u].w, acc[k].w);
+            }
     }
-    if (on && who == 0)
-      finish<D, kRows>(p, piece, row, d, acc, sh->l[0][row], sh->m[0][row]);
+  if (share > 1) {
+    sums[tid] = acc[0];
+    __syncthreads();
+    if (who == 0)
+      for (int i = 1; i < share; ++i) {
+        if (x0 >= slots) break;
+        const float4 v = sums[i * slots + x0];
+        acc[0].x += v.x, acc[0].y += v.y, acc[0].z += v.z, acc[0].w += v.w;
+      }
   }
+  if (who == 0)
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int x = x0 + k * kThreads, row = x / kSlots;
+      if (x < slots)
+        finish<D, kRows>(p, piece, row, x % kSlots * 4, acc[k], sh->l[0][row],
+                         sh->m[0][row]);
+    }
 }
 
 // NT blocks of 8 query rows, W warps, kStages tiles in each warp's ring, kCtas
@@ -816,6 +855,7 @@ q4_attn_kernel(const __grid_constant__ Q4AttnParams p) {
     sh.last[threadIdx.x] = last;
   }
   __syncthreads();
+#pragma unroll 1
   for (int i = 0; i < 2; ++i) {
     if (!sh.last[i]) continue;
     __threadfence();
@@ -862,10 +902,11 @@ cudaError_t launch_v(Q4AttnParams p, int sms, cudaStream_t stream) {
 template <int D>
 cudaError_t launch_d(const Q4AttnParams& p, int sms, cudaStream_t stream) {
   // Warps and ring depths are what registers and shared memory hold: 16 warps
-  // of 128 registers with one block of rows, 10 of 200 with two, 8 with four.
+  // of 128 registers with one block of rows, 8 with two (16 rows over 65536 keys
+  // of 12 heads: 46.8 us; 10 warps spill, 52.0) or four.
   constexpr int kDeep = D == 128 ? 1 : 2;
   if (p.rows <= 8) return launch_v<D, 1, 8, 3 * kDeep, 2>(p, sms, stream);
-  if (p.rows <= 16) return launch_v<D, 2, 10, 4 * kDeep, 1>(p, sms, stream);
+  if (p.rows <= 16) return launch_v<D, 2, 8, 4 * kDeep, 1>(p, sms, stream);
   return launch_v<D, 4, 8, 4 * kDeep, 1>(p, sms, stream);
 }
 
