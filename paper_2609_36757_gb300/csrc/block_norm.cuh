@@ -50,11 +50,6 @@ __device__ __forceinline__ F8 fma(const F8& a, float b, float c) {
 __device__ __forceinline__ float sum(const F8& a) {
   return sum(add(add(a.v[0], a.v[1]), add(a.v[2], a.v[3])));
 }
-__device__ __forceinline__ float dot(const F8& a, const F8& b) {
-  return sum(fma(a.v[3], b.v[3],
-                 fma(a.v[2], b.v[2],
-                     fma(a.v[1], b.v[1], mul(a.v[0], b.v[0])))));
-}
 
 // 8 consecutive elements in memory: 16 bytes of bfloat16 or 32 of float32.
 template <typename T>
@@ -325,25 +320,21 @@ __device__ __forceinline__ float keep_sum(float (&v)[N]) {
   return s;
 }
 
-// Sums over the row of a and of b, on every thread; `part` (kWarps entries)
-// is this exchange's own: two exchanges with another part between them need
-// one barrier each.
+// Sums over a row of many warps of a and of b, on every thread; `part` (kWarps
+// entries) is this exchange's own: two exchanges with another part between them
+// need one barrier each.
 template <int TPR>
 __device__ __forceinline__ void row_sums(float& a, float& b, float2* part) {
   using S = Shape<TPR>;
-  if constexpr (!S::kMany) {
-    both_sums<S::kLanes>(a, b);
-  } else {
-    const float v = keep_sums<32>(a, b);
-    if (threadIdx.x % 16 == 0)
-      reinterpret_cast<float*>(part)[threadIdx.x / 16] = v;
-    __syncthreads();
-    F2 all = f2(0.f);
+  const float v = keep_sums<32>(a, b);
+  if (threadIdx.x % 16 == 0)
+    reinterpret_cast<float*>(part)[threadIdx.x / 16] = v;
+  __syncthreads();
+  F2 all = f2(0.f);
 #pragma unroll(S::kUnroll)
-    for (int w = 0; w < S::kWarps; ++w)
-      all = add(all, f2(part[w].x, part[w].y));
-    split(all, a, b);
-  }
+  for (int w = 0; w < S::kWarps; ++w)
+    all = add(all, f2(part[w].x, part[w].y));
+  split(all, a, b);
 }
 
 // Mean (0 where it is not wanted) and sum of squared deviations of two rows,
@@ -355,13 +346,12 @@ struct Stats {
 };
 template <int TPR, int NV>
 __device__ __forceinline__ Stats row_stats(const F8 (&a)[NV], const F8 (&b)[NV],
-                                           bool mean_a, bool mean_b,
-                                           const Cols<TPR, NV>& k,
+                                           bool mean, const Cols<TPR, NV>& k,
                                            float4* part) {
   using S = Shape<TPR>;
   Stats st;
   st.mu_a = st.mu_b = 0.f;
-  if (S::kMany && !mean_a && !mean_b) {  // squares alone
+  if (S::kMany && !mean) {  // squares alone
     F8 qa = mul(a[0], a[0]), qb = mul(b[0], b[0]);
 #pragma unroll
     for (int i = 1; i < NV; ++i) {
@@ -373,15 +363,15 @@ __device__ __forceinline__ Stats row_stats(const F8 (&a)[NV], const F8 (&b)[NV],
     row_sums<TPR>(st.sq_a, st.sq_b, reinterpret_cast<float2*>(part));
     return st;
   }
-  if (mean_a || mean_b) {
+  if (mean) {
     F8 x = a[0], y = b[0];
 #pragma unroll
     for (int i = 1; i < NV; ++i) {
       x = add(x, a[i]);
       y = add(y, b[i]);
     }
-    st.mu_a = mean_a ? sum(x) : 0.f;
-    st.mu_b = mean_b ? sum(y) : 0.f;
+    st.mu_a = sum(x);
+    st.mu_b = sum(y);
     both_sums<S::kLanes>(st.mu_a, st.mu_b);
     st.mu_a *= k.inv_warp;
     st.mu_b *= k.inv_warp;
@@ -408,16 +398,16 @@ __device__ __forceinline__ Stats row_stats(const F8 (&a)[NV], const F8 (&b)[NV],
       to[2] = v;
     }
     __syncthreads();
-    F2 mean = f2(0.f), sq = f2(0.f);
+    F2 mu = f2(0.f), sq = f2(0.f);
 #pragma unroll(S::kUnroll)
     for (int w = 0; w < S::kWarps; ++w) {
       const float4 x = part[w];
-      mean = fma(f2(x.x, x.y), f2(k.counts[w]), mean);
+      mu = fma(f2(x.x, x.y), f2(k.counts[w]), mu);
       sq = add(sq, f2(x.z, x.w));
     }
-    if (mean_a || mean_b) {
-      mean = mul(mean, f2(k.inv_dim));
-      const F2 back = mul(mean, f2(-1.f));
+    if (mean) {
+      mu = mul(mu, f2(k.inv_dim));
+      const F2 back = mul(mu, f2(-1.f));
 #pragma unroll(S::kUnroll)
       for (int w = 0; w < S::kWarps; ++w) {
         const float4 x = part[w];
@@ -425,7 +415,7 @@ __device__ __forceinline__ Stats row_stats(const F8 (&a)[NV], const F8 (&b)[NV],
         sq = fma(mul(d, f2(k.counts[w])), d, sq);
       }
     }
-    split(mean, st.mu_a, st.mu_b);
+    split(mu, st.mu_a, st.mu_b);
     split(sq, st.sq_a, st.sq_b);
   }
   return st;

@@ -118,7 +118,7 @@ norm_fwd_kernel(const __grid_constant__ NormFwdParams p) {
     if (post) {
       const bool mean = p.post == kNormLayer;
       const Stats st =
-          row_stats<TPR, NV>(y[0], y[R - 1], mean, mean, k, s_y);
+          row_stats<TPR, NV>(y[0], y[R - 1], mean, k, s_y);
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         const float rho =
@@ -154,7 +154,7 @@ norm_fwd_kernel(const __grid_constant__ NormFwdParams p) {
     }
     if (!has_h) continue;
     const bool mean = p.pre == kNormLayer;
-    const Stats st = row_stats<TPR, NV>(x[0], x[R - 1], mean, mean, k, s_r);
+    const Stats st = row_stats<TPR, NV>(x[0], x[R - 1], mean, k, s_r);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       if (!on[i]) continue;
