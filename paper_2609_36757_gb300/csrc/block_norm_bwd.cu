@@ -197,7 +197,9 @@ norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
   extern __shared__ float4 dyn4[];
   Kept<kRegs * NV, 5 * NV> mine;
   mine.m = Private{dyn4};
-  static_assert(kRegs <= 2 || S::kRows == 1, "rows side by side are added there");
+  static_assert(kRegs <= 2 || S::kRows == 1,
+                "rows side by side are added there");
+  static_assert(kAhead || S::kRows == 1, "");
   float* dyn =
       reinterpret_cast<float*>(dyn4 + 2 * (5 - kRegs) * NV * S::kThreads);
   __shared__ float4 s_part[2][S::kWarps][4];
@@ -247,6 +249,18 @@ norm_bwd_kernel(const __grid_constant__ NormBwdParams p) {
           }
           if (has_y) in[j].y.load(p.y, at);
         }
+    // without registers to load the next row ahead, at least to L2
+    if (!kAhead && threadIdx.x == 0 && fg < g1 && ft + step < t1) {
+      const int64_t at = (fg * p.group_tokens + ft + step) * p.dim;
+      if (has_dr)
+        prefetch_l2(static_cast<const TR*>(p.dr) + at, p.dim * sizeof(TR));
+      if (has_h) {
+        prefetch_l2(static_cast<const TR*>(p.r) + at, p.dim * sizeof(TR));
+        prefetch_l2(static_cast<const TY*>(p.dh) + at, p.dim * sizeof(TY));
+      }
+      if (has_y)
+        prefetch_l2(static_cast<const TY*>(p.y) + at, p.dim * sizeof(TY));
+    }
     ft += step;
     if (ft >= t1) {
       ft = t0;
@@ -499,7 +513,8 @@ cudaError_t launch_v(const NormBwdParams& p, cudaStream_t stream) {
 // 9000 rows of 2048: 61.7 us, 128 threads of 16 columns 68.8).  With groups of a
 // few rows, whose ends then count, 192 threads of 8 columns: 78.5 us for 8160
 // groups of one row, against 98.  Rows above 5120 leave no registers to load
-// ahead and spill some (128.7 us for 3000 rows of 8192; 1024 threads took 181).
+// ahead and spill some (3000 rows of 8192: 105.8 us; without asking for the next
+// row in L2 128.7).  Asked for in L2 as well, narrower rows gain nothing.
 template <typename TR, typename TY>
 cudaError_t launch_t(const NormBwdParams& p, cudaStream_t stream) {
   if (p.dim <= 64) return launch_v<TR, TY, 8, 1, true, 0, 4>(p, stream);

@@ -96,6 +96,12 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src,
                  "l"(src), "n"(N), "r"(n)
                  : "memory");
 }
+// Asks for bytes (place and number multiples of 16) to be brought to L2.
+__device__ __forceinline__ void prefetch_l2(const void* from, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from),
+               "r"(bytes)
+               : "memory");
+}
 __device__ __forceinline__ void copy_commit() {
   asm volatile("cp.async.commit_group;" ::: "memory");
 }
