@@ -106,8 +106,8 @@ __device__ __forceinline__ void store8(float* base, int64_t i, const F8& f) {
 
 // Rows on their way: 16-byte pieces of each thread's columns, copied
 // asynchronously by the threads of its own warp, so that they need not meet the
-// others.  kDeep rows of kPieces pieces; a row is asked for kDeep - 1 rows ahead,
-// in the place of the one last worked on.
+// others.  kDeep rows of kPieces pieces; a row is asked for kDeep - 1 rows
+// ahead, in the place of the one last worked on.
 template <int kDeep, int kPieces>
 struct Ring {
   float4* base;  // [row][piece][thread]
@@ -168,8 +168,8 @@ struct Ring {
   }
 };
 
-// Its depth: what a CTA's share of an SM's 227 KB leaves beside `fixed` bytes of
-// each of its vectors (2 KB for the system and the static part); 0 where two
+// Its depth: what a CTA's share of an SM's 227 KB leaves beside `fixed` bytes
+// of each of its vectors (2 KB for the system and the static part); 0 where two
 // rows do not fit.
 constexpr int kSmBytes = 232448;
 constexpr int ring_depth(int ctas, int vectors, int fixed, int bytes,

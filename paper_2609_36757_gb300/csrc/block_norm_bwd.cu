@@ -20,9 +20,9 @@
 // per element with a float32 residual stream).  A thread owns the same columns
 // of all the rows that its CTA takes, so A, C and E are its own and every token
 // sum has a fixed order.  The slices of a group take its rows in turn, so that
-// neighbours in memory are asked for together.  72.0 us (4.7 TB/s) for 12288 rows
-// of 1536 with a float32 residual; three exchanges, one after the other, took
-// 73.7, and 88.6 instead of 80.9 for 3600 rows of 5120.
+// neighbours in memory are asked for together.  72.0 us (4.7 TB/s) for 12288
+// rows of 1536 with a float32 residual; three exchanges, one after the other,
+// took 73.7, and 88.6 instead of 80.9 for 3600 rows of 5120.
 #include "block_norm.cuh"
 
 namespace fastvr {
@@ -97,9 +97,9 @@ __device__ __forceinline__ void warp_means(const F8 (&r)[NV], const F8 (&y)[NV],
 }
 
 // The sums over the row from a thread's parts (v: rr to w, v4: dr_g to g), that
-// were taken about its warp's means.  One exchange: the warps' parts are moved to
-// the row's means when they are put together.  `part`: not written again before
-// the next exchange.
+// were taken about its warp's means.  One exchange: the warps' parts are moved
+// to the row's means when they are put together.  `part`: not written again
+// before the next exchange.
 template <int TPR, int NV>
 __device__ __forceinline__ RowSums row_part_sums(float (&v)[8], float (&v4)[4],
                                                  float mu_r, float mu_y,
@@ -505,16 +505,17 @@ cudaError_t launch_v(const NormBwdParams& p, cudaStream_t stream) {
                     dim3(Shape<TPR>::kThreads), smem, stream, p);
 }
 
-// Threads and vectors of a row, whether the next row is loaded ahead, how many of
-// a thread's five vectors stay in registers, CTAs per SM: what was fastest of
-// those that spill nothing, or next to nothing in float32 throughout (12288 rows of 1536 with a float32 residual: 96 threads
-// of 16 columns 72.0 us, the same with all five in shared memory and four CTAs
-// 73.5, 192 of 8 and three CTAs 81.8; rows ahead in shared memory 92 and more;
-// 9000 rows of 2048: 61.7 us, 128 threads of 16 columns 68.8).  With groups of a
-// few rows, whose ends then count, 192 threads of 8 columns: 78.5 us for 8160
-// groups of one row, against 98.  Rows above 5120 leave no registers to load
-// ahead and spill some (3000 rows of 8192: 105.8 us; without asking for the next
-// row in L2 128.7).  Asked for in L2 as well, narrower rows gain nothing.
+// Threads and vectors of a row, whether the next row is loaded ahead, how many
+// of a thread's five vectors stay in registers, CTAs per SM: what was fastest
+// of those that spill nothing, or next to nothing in float32 throughout (12288
+// rows of 1536 with a float32 residual: 96 threads of 16 columns 72.0 us, the
+// same with all five in shared memory and four CTAs 73.5, 192 of 8 and three
+// CTAs 81.8; rows ahead in shared memory 92 and more; 9000 rows of 2048: 61.7
+// us, 128 threads of 16 columns 68.8).  With groups of a few rows, whose ends
+// then count, 192 threads of 8 columns: 78.5 us for 8160 groups of one row,
+// against 98.  Rows above 5120 leave no registers to load ahead and spill some
+// (3000 rows of 8192: 105.8 us; without asking for the next row in L2 128.7).
+// Asked for in L2 as well, narrower rows gain nothing.
 template <typename TR, typename TY>
 cudaError_t launch_t(const NormBwdParams& p, cudaStream_t stream) {
   if (p.dim <= 64) return launch_v<TR, TY, 8, 1, true, 0, 4>(p, stream);

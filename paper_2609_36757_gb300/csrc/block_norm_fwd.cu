@@ -3,13 +3,13 @@
 //
 // Bound by memory: x and y are read once, r and h written once (8 bytes per
 // element in bfloat16).  A thread owns the same columns of all the rows that
-// its CTA takes, so the modulation vectors of a group are read and combined once
-// (with a warp to a row they were read again for every row, which kept L1
+// its CTA takes, so the modulation vectors of a group are read and combined
+// once (with a warp to a row they were read again for every row, which kept L1
 // busier than memory) and kept in shared memory.  What is left is the exchange
-// of a row's sums and the instructions around it, so as many CTAs as fit without
-// spilling share an SM; where the rows ahead wait in shared memory instead of
-// registers, more of them do.  36.1 us (5.6 TB/s) for 16320 rows of 1536 in
-// bfloat16.
+// of a row's sums and the instructions around it, so as many CTAs as fit
+// without spilling share an SM; where the rows ahead wait in shared memory
+// instead of registers, more of them do.  36.1 us (5.6 TB/s) for 16320 rows of
+// 1536 in bfloat16.
 #include <algorithm>
 
 #include "block_norm.cuh"
@@ -210,16 +210,17 @@ cudaError_t launch_v(const NormFwdParams& p, int sms, cudaStream_t stream) {
 
 // Threads, vectors and rows of a pass, passes ahead in shared memory (0: one in
 // registers), CTAs per SM.  Rows of up to 256 columns lie side by side in a CTA
-// (277236 rows of 64: 35.3 us with one row to a thread and 6 CTAs, 40.2 with two
-// and 4, 49.5 with rows ahead in shared memory).  From there to 512 eight columns
-// to a thread and the next row in registers as well (36000 rows of
-// 512: 25.7 us, 30.2 through shared memory), above that through shared memory
+// (277236 rows of 64: 35.3 us with one row to a thread and 6 CTAs, 40.2 with
+// two and 4, 49.5 with rows ahead in shared memory).  From there to 512 eight
+// columns to a thread and the next row in registers as well (36000 rows of 512:
+// 25.7 us, 30.2 through shared memory), above that through shared memory
 // (against registers: 36.4 us and 52.6 for 36000 rows of 520, 27.4 and 30.4 for
 // 18000 of 1024, 36.1 and 38.6 for 16320 of 1536 by twos), from 2048 on with 16
 // columns to a thread, which leaves fewer warps to exchange with (29.1 and 38.6
 // for 9000 rows of 2048, 30.9 and 40.9 for 3600 of 5120, 46.3 and 66.5 for 3000
-// of 8192).  A modulation of its own for every row makes the ends of groups count:
-// one row at a time and in registers then (8160 rows of 1536: 43.0 us and 45.3).
+// of 8192).  A modulation of its own for every row makes the ends of groups
+// count: one row at a time and in registers then (8160 rows of 1536: 43.0 us
+// and 45.3).
 template <typename TR, typename TY>
 cudaError_t launch_t(const NormFwdParams& p, int sms, cudaStream_t stream) {
   if (p.dim <= 64) return launch_v<TR, TY, 8, 1, 1, 0, 6>(p, sms, stream);

@@ -284,8 +284,8 @@ cudaError_t launch_q4_read(const Q4ReadParams& p, bool head_major, int sms,
 // 0.07 for every 32 query rows (tokens times query heads per key head), the
 // latter 0.17 to expand and 0.04 for every query head and 256 tokens: 12 heads
 // over 32768 keys take 50.9 us directly with 32 rows, 75.6 with 64 and 84 the
-// other way, 8 streams of 32 heads over 8 and 8192 keys 144 us with 96 rows, 182
-// with 128 and 178.  The few keys of a short window leave the direct way's
+// other way, 8 streams of 32 heads over 8 and 8192 keys 144 us with 96 rows,
+// 182 with 128 and 178.  The few keys of a short window leave the direct way's
 // shares too small for its second block to pay (4096 keys: 26.8 us with 64 rows
 // against 19.4), hence the 8.
 inline bool q4_direct(int64_t q_tokens, int64_t group) {

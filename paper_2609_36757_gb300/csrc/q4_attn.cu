@@ -35,13 +35,13 @@
 // MMA row r of a block of 8 keys is key r / 2 + 4 (r % 2), so that the four
 // token pairs that a V load touches lie in different banks.
 //
-// Measured: 604 MB of cache (8 streams of 65536 keys, 12 heads of 128) in 124 us,
-// 4.9 TB/s.  In the steady state the integer pipe is busy for about 80 % of the
-// cycles (logic, byte selection and moves of the expansion), on average for 58 %;
-// shifting V's nibbles by multiplication instead, on the other pipe, took 130 us,
-// eight warps to an SM instead of sixteen 132.  One head and 4096 keys take 9.6 us,
-// of which the stages that only one warp or CTA can do (its share, the first
-// tile's way from memory, the join) are most.
+// Measured: 604 MB of cache (8 streams of 65536 keys, 12 heads of 128) in 124
+// us, 4.9 TB/s.  In the steady state the integer pipe is busy for about 80 % of
+// the cycles (logic, byte selection and moves of the expansion), on average for
+// 58 %; shifting V's nibbles by multiplication instead, on the other pipe, took
+// 130 us, eight warps to an SM instead of sixteen 132.  One head and 4096 keys
+// take 9.6 us, of which the stages that only one warp or CTA can do (its share,
+// the first tile's way from memory, the join) are most.
 //
 // A warp streams its own key tiles (32 keys) through a ring in shared memory
 // filled by cp.async, and keeps its own softmax state; the warps of a CTA and
@@ -139,9 +139,9 @@ __device__ __forceinline__ int v_offset(int r, int byte) {
 // slowest) are cut into even shares, one to a CTA, however different the
 // entries' lengths are.  Every unit counts kUnitCost tiles more than it has,
 // about what starting and ending it costs, so that a CTA with many short
-// units is not the last one (eight streams of 6000 to 66000 keys: 64.7 us with 12,
-// 57.0 with 24, 58.1 with 32); an entry that sees no key still has units, whose
-// zeros someone writes.
+// units is not the last one (eight streams of 6000 to 66000 keys: 64.7 us with
+// 12, 57.0 with 24, 58.1 with 32); an entry that sees no key still has units,
+// whose zeros someone writes.
 constexpr int kUnitCost = 24;
 
 // A CTA's part of a unit.
@@ -350,8 +350,8 @@ __device__ __forceinline__ void end_piece(const Q4AttnParams& p, S* sh,
 // The last CTA of a unit to arrive joins its parts, in their order: m and l of
 // all of them first, the weight of every (part, row) from these, then sums of
 // weighted rows.  Each step has its loads in flight together: what a join costs
-// is their latency (32 rows over 4096 keys of 12 heads: 25.5 us with a row and a
-// few loads at a time, 21.8 now).
+// is their latency (32 rows over 4096 keys of 12 heads: 25.5 us with a row and
+// a few loads at a time, 21.8 now).
 template <int D, int NT, int W, int kWarpBytes, class S>
 __device__ __forceinline__ void join_parts(const Q4AttnParams& p, S* sh,
                                            uint8_t* smem, const Piece& piece) {
@@ -902,8 +902,8 @@ cudaError_t launch_v(Q4AttnParams p, int sms, cudaStream_t stream) {
 template <int D>
 cudaError_t launch_d(const Q4AttnParams& p, int sms, cudaStream_t stream) {
   // Warps and ring depths are what registers and shared memory hold: 16 warps
-  // of 128 registers with one block of rows, 8 with two (16 rows over 65536 keys
-  // of 12 heads: 46.8 us; 10 warps spill, 52.0) or four.
+  // of 128 registers with one block of rows, 8 with two (16 rows over 65536
+  // keys of 12 heads: 46.8 us; 10 warps spill, 52.0) or four.
   constexpr int kDeep = D == 128 ? 1 : 2;
   if (p.rows <= 8) return launch_v<D, 1, 8, 3 * kDeep, 2>(p, sms, stream);
   if (p.rows <= 16) return launch_v<D, 2, 8, 4 * kDeep, 1>(p, sms, stream);
