@@ -880,7 +880,14 @@ combine_kernel(const __grid_constant__ TcParams p) {
     float mg = m;
 #pragma unroll
     for (int u = 0; u < kPartUnroll; ++u) mg = fmaxf(mg, w8[u]);
-    if (mg == -INFINITY) continue;  // nothing finite yet
+    if (mg == -INFINITY) {  // nothing finite yet
+      // fmaxf passes over a NaN: a part with one makes the row NaN, a row
+      // without a visible key has none
+#pragma unroll
+      for (int u = 0; u < kPartUnroll; ++u)
+        if (w8[u] != w8[u]) wsum = w8[u];
+      continue;
+    }
     // 0 on the first finite group (nothing accumulated), else <= 1
     const float sc = m == -INFINITY ? 0.f : ex2(m - mg);
     wsum *= sc;
