@@ -132,7 +132,8 @@ FASTVR_API fastvr_status_t fastvr_rotary(
  *   r = residual_scale x + gate_g o post(y)
  *   h = pre(r) o (1 + scale_g) + shift_g
  * post and pre are the norms above, each followed by an optional weight
- * vector.  Tensors are contiguous [batch, tokens, dim]. */
+ * vector (with post NONE post_weight is not used).  Tensors are contiguous
+ * [batch, tokens, dim]. */
 typedef struct {
   int32_t batch, tokens, dim; /* dim: a multiple of 8, 8 .. 8192;
                                  batch * tokens below 2^30                  */
@@ -174,10 +175,10 @@ FASTVR_API fastvr_status_t fastvr_gated_norm_bwd_scratch_bytes(
  *   dgate = sum d o post(y),  dscale = sum dh o pre(r),  dshift = sum dh,
  *   dpre_weight = sum dh o (1 + scale) o n(r),
  *   dpost_weight = sum du o n(y)       (n: the norm before its weight)
- * A gradient of the absent: dgate and dpost_weight need y; dscale, dshift and
- * dpre_weight need dh; they are zero otherwise.  Token sums are float32 in a
- * fixed order (no atomics): repeated calls agree bit for bit.  dx may be dr
- * and dy may be dh (in place, equal types).
+ * A gradient of the absent: dgate and dpost_weight need y, the latter a post
+ * norm; dscale, dshift and dpre_weight need dh; they are zero otherwise.
+ * Token sums are float32 in a fixed order (no atomics): repeated calls agree
+ * bit for bit.  dx may be dr and dy may be dh (in place, equal types).
  * Errors: INVALID_ARG, CAPACITY (scratch), UNSUPPORTED (device), CUDA. */
 FASTVR_API fastvr_status_t fastvr_gated_norm_bwd(
     const fastvr_norm_config_t* cfg, const void* dr, const void* dh,

@@ -78,5 +78,7 @@ def backward(dr, dh, r, y, gate=None, scale=None, pre_weight=None,
         yn, ry = unit(np.asarray(y, np.float64), post, eps)
         out["dy"] = unit_bwd(d * g * pw, yn, ry, post)
         add("dgate", d * yn * pw, fold)
-        add("dpost_weight", d * g * yn, everything)
+        # without a post norm its weight is not used
+        add("dpost_weight", d * g * yn if post != "none" else 0.0 * d,
+            everything)
     return out

@@ -451,7 +451,8 @@ norm_bwd_sum_kernel(const __grid_constant__ NormBwdParams p) {
   } else {
     float* out = job == group_jobs ? p.dpre_weight : p.dpost_weight;
     if (out == nullptr) return;
-    if (on)
+    // without a post norm its weight is not used: a gradient of zeros
+    if (on && (job == group_jobs || p.post != kNormNone))
       for (int64_t i = warp; i < p.ctas; i += 8)
         s[0] += p.weight_partial[(i * 2 + (job - group_jobs)) * p.dim + c];
   }
