@@ -60,7 +60,8 @@ typedef enum {
   FASTVR_ERR_CAPACITY = 3,     /* frames > k, more chunks than max_chunks,
                                   cache buffer too small                      */
   FASTVR_ERR_SEQUENCE = 4,     /* fwd before any append; append after a
-                                  ragged (final) chunk                        */
+                                  ragged (final) chunk; first call of a
+                                  4-bit plan under stream capture             */
   FASTVR_ERR_CUDA = 5,         /* a CUDA runtime/driver call failed           */
   FASTVR_ERR_TIMEOUT = 6,      /* a bounded device-side wait gave up          */
   FASTVR_ERR_BOUNDS = 7        /* a device-side index or layout check failed

@@ -229,6 +229,10 @@ FASTVR_API fastvr_status_t fastvr_q4_workspace_bytes(
  * _destroy and fastvr_get_status take it; fastvr_kv_append and
  * fastvr_chunk_attn_fwd do not (INVALID_ARG), nor do the calls below take a
  * bfloat16 plan.
+ * Stream capture: the plan's first call that launches work clears the control
+ * block and cannot be a captured one (SEQUENCE, nothing is enqueued).  A
+ * captured call keeps the chunk counter of its capture: replays append to, read
+ * or attend to the same chunks, and do not move the plan's counter.
  * Errors: INVALID_ARG, UNSUPPORTED, CAPACITY (a buffer is too small). */
 FASTVR_API fastvr_status_t fastvr_q4_plan(const fastvr_attn_config_t* cfg,
                                           int32_t kv_heads, void* cache,

@@ -108,6 +108,17 @@ int fastvr::device_sms() {
 fastvr_status_t fastvr::ensure_device(fastvr_plan_s* p, size_t control_bytes,
                                       struct CUstream_st* stream) {
   if (p->device_ready) return FASTVR_OK;
+  if (p->q4) {
+    // Captured, the control block would be cleared by the graph's replays and
+    // not by now, and calls in between would join on counters of any value.
+    cudaStreamCaptureStatus capture;
+    if (cudaStreamIsCapturing(reinterpret_cast<cudaStream_t>(stream),
+                              &capture) != cudaSuccess) {
+      cudaGetLastError();
+      return FASTVR_ERR_CUDA;
+    }
+    if (capture != cudaStreamCaptureStatusNone) return FASTVR_ERR_SEQUENCE;
+  }
   const fastvr_status_t st = check_device();
   if (st != FASTVR_OK) return st;
   int dev = 0;

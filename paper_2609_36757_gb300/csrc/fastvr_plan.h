@@ -45,7 +45,8 @@ inline int* control_word(const fastvr_plan_s* p) {
 }
 
 // First device call of a plan: checks the device and the buffer, clears the
-// control block (control_bytes of it) on the stream.
+// control block (control_bytes of it) on the stream.  A 4-bit plan's first call
+// cannot be captured (SEQUENCE).
 fastvr_status_t ensure_device(fastvr_plan_s* p, size_t control_bytes,
                               struct CUstream_st* stream);
 
