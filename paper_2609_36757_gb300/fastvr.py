@@ -574,8 +574,8 @@ def _stream_of(t) -> int:
     return _raw_stream(t.device.index)
 
 
-def _dtype_code(t) -> int:
-    code = _CODES.get(t.dtype)
+def _dtype_code(dtype) -> int:
+    code = _CODES.get(dtype)
     if code is None:
         raise ValueError("tensors must be bfloat16 or float32")
     return code
@@ -631,7 +631,7 @@ def rotary(cfg: fastvr_rotary_config_t, q, k, positions, out=None,
     axes].  Returns (q', k'), contiguous unless `out` gives the two outputs
     (out=(q, k) works in place)."""
     torch = _torch or _setup()
-    code = _dtype_code(q)
+    code = _dtype_code(q.dtype)
     q_str = _head_strides(q, "q")
     B, L, H, d = q.shape
     Hk, k_str = 0, None
@@ -693,14 +693,14 @@ def _norm_call(cfg, x, y, mods, weights):
     if len(shape) != 3 or not x.is_cuda or not x.is_contiguous():
         raise ValueError("x must be a contiguous CUDA tensor [B, L, D]")
     B, L, D = shape
-    code = _dtype_code(x)
+    code = _dtype_code(x.dtype)
     block = FASTVR_BF16
     for t in y:
         if t is not None:
             if t.shape != shape or not t.is_cuda or not t.is_contiguous():
                 raise ValueError(
                     "block tensors must be contiguous and of x's shape")
-            block = _dtype_code(t)
+            block = _dtype_code(t.dtype)
     f32, groups = torch.float32, 0
     for t in mods:
         if t is not None:
@@ -737,7 +737,7 @@ def gated_norm(cfg: fastvr_norm_config_t, x, y, gate=None, scale=None,
                    (pre_weight, post_weight))
     block = (block_dtype or torch.bfloat16) if y is None else y.dtype
     if y is None:
-        c.block_dtype = FASTVR_F32 if block == torch.float32 else FASTVR_BF16
+        c.block_dtype = _dtype_code(block)
     r = torch.empty_like(x) if want_r else None
     h = torch.empty_like(x, dtype=block) if want_h else None
     fastvr_gated_norm_fwd(c, x.data_ptr(), _ptr(y), _ptr(gate), _ptr(scale),
