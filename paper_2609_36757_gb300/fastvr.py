@@ -554,24 +554,32 @@ class StreamingAttention:
 # directly (torch.cuda.current_stream() builds a stream object, 2.9 us on the
 # measured host against 0.1).
 _CODES: dict = {}
-_torch = _raw_stream = None
+_torch = _raw_stream = _current_device = None
 
 
 def _setup():
     """torch, with the tables that need it filled in."""
-    global _raw_stream, _torch
+    global _current_device, _raw_stream, _torch
     import torch
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
         lambda i: torch.cuda.current_stream(i).cuda_stream)
+    _current_device = getattr(torch._C, "_cuda_getDevice",
+                              torch.cuda.current_device)
     _CODES[torch.bfloat16] = FASTVR_BF16
     _CODES[torch.float32] = FASTVR_F32
     _torch = torch
     return torch
 
 
-def _stream_of(t) -> int:
-    """Handle of the current stream of t's device."""
-    return _raw_stream(t.device.index)
+def _stream_of(*tensors) -> int:
+    """Handle of the current device's current stream, where all tensors of a
+    call lie (None: absent)."""
+    device = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("a call's tensors must lie on the current CUDA "
+                             "device")
+    return _raw_stream(device)
 
 
 def _dtype_code(dtype) -> int:
@@ -670,7 +678,7 @@ def rotary(cfg: fastvr_rotary_config_t, q, k, positions, out=None,
                   positions.data_ptr(), L * axes if rows > 1 else 0,
                   q_out.data_ptr(), q_out_str,
                   0 if k is None else k_out.data_ptr(), k_out_str,
-                  int(transpose), _stream_of(q))
+                  int(transpose), _stream_of(q, k, positions, q_out, k_out))
     return q_out, k_out
 
 
@@ -743,7 +751,8 @@ def gated_norm(cfg: fastvr_norm_config_t, x, y, gate=None, scale=None,
     fastvr_gated_norm_fwd(c, x.data_ptr(), _ptr(y), _ptr(gate), _ptr(scale),
                           _ptr(shift), _ptr(pre_weight), _ptr(post_weight),
                           _ptr(r), _ptr(h),
-                          _stream_of(x))
+                          _stream_of(x, y, gate, scale, shift, pre_weight,
+                                     post_weight))
     return r, h
 
 
@@ -787,7 +796,8 @@ def gated_norm_bwd(cfg: fastvr_norm_config_t, dr, dh, r, y, gate=None,
                           _ptr(gate), _ptr(scale), _ptr(pre_weight),
                           _ptr(post_weight), *(_ptr(t) for t in g),
                           scratch.data_ptr(), nbytes,
-                          _stream_of(r))
+                          _stream_of(r, y, dr, dh, gate, scale, pre_weight,
+                                     post_weight))
     return g
 
 
@@ -842,7 +852,7 @@ class StreamingAttention4:
             raise ValueError(f"k has shape {tuple(k.shape)}")
         fastvr_q4_append(self.plan, k.data_ptr(), k_str, v.data_ptr(), v_str,
                          L // c.tokens_per_frame,
-                         _stream_of(k))
+                         _stream_of(k, v, self.cache))
 
     def forward(self, q, first_chunk=None, out=None, lse=None,
                 want_lse: bool = False):
@@ -877,7 +887,7 @@ class StreamingAttention4:
             raise ValueError("lse must be contiguous float32 [B, H, L]")
         fastvr_q4_attn_fwd(self.plan, q.data_ptr(), _ptr(first_chunk),
                            out.data_ptr(), _ptr(lse),
-                           _stream_of(q))
+                           _stream_of(q, first_chunk, out, lse, self.cache))
         return (out, lse) if lse is not None else out
 
     def read(self, chunk: Optional[int] = None):
