@@ -823,6 +823,8 @@ class StreamingAttention4:
         need = fastvr_q4_workspace_bytes(cfg, self.kv_heads)
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        elif not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous CUDA tensor")
         self.workspace = workspace
         self.cache = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
         self.plan = fastvr_q4_plan(cfg, self.kv_heads, self.cache.data_ptr(),
