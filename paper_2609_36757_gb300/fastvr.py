@@ -598,7 +598,7 @@ def _head_strides(t, name: str):
     """fastvr_strides_t of a [B, L, H, d] tensor whose heads are contiguous,
     None when the whole tensor is."""
     strides = t.stride()
-    if not t.is_cuda or len(strides) != 4:
+    if len(strides) != 4:
         raise ValueError(f"{name} must be a CUDA tensor [B, L, H, d]")
     if t.is_contiguous():
         return None
@@ -651,8 +651,7 @@ def rotary(cfg: fastvr_rotary_config_t, q, k, positions, out=None,
         Hk = shape[2]
         if shape != (B, L, Hk, d) or k.dtype != q.dtype:
             raise ValueError("q and k differ in type or shape")
-    if positions.dtype != torch.int32 or not positions.is_cuda or \
-            not positions.is_contiguous():
+    if positions.dtype != torch.int32 or not positions.is_contiguous():
         raise ValueError("positions must be a contiguous int32 CUDA tensor")
     axes, shape = cfg.axes, positions.shape
     rows = shape[0] if len(shape) == 3 else 1
@@ -678,7 +677,7 @@ def rotary(cfg: fastvr_rotary_config_t, q, k, positions, out=None,
                   positions.data_ptr(), L * axes if rows > 1 else 0,
                   q_out.data_ptr(), q_out_str,
                   0 if k is None else k_out.data_ptr(), k_out_str,
-                  int(transpose), _stream_of(q, k, positions, q_out, k_out))
+                  int(transpose), _stream_of(q, k, positions, *(out or ())))
     return q_out, k_out
 
 
@@ -695,17 +694,18 @@ def make_norm_config(pre: str = "rms", post: str = "none", eps: float = 1e-6,
 
 
 def _norm_call(cfg, x, y, mods, weights):
-    """cfg for the tensors of a call, after their checks."""
+    """cfg for the tensors of a call, after the checks of their types and
+    shapes."""
     torch = _torch or _setup()
     shape = x.shape
-    if len(shape) != 3 or not x.is_cuda or not x.is_contiguous():
+    if len(shape) != 3 or not x.is_contiguous():
         raise ValueError("x must be a contiguous CUDA tensor [B, L, D]")
     B, L, D = shape
     code = _dtype_code(x.dtype)
     block = FASTVR_BF16
     for t in y:
         if t is not None:
-            if t.shape != shape or not t.is_cuda or not t.is_contiguous():
+            if t.shape != shape or not t.is_contiguous():
                 raise ValueError(
                     "block tensors must be contiguous and of x's shape")
             block = _dtype_code(t.dtype)
@@ -713,7 +713,7 @@ def _norm_call(cfg, x, y, mods, weights):
     for t in mods:
         if t is not None:
             s = t.shape
-            if t.dtype != f32 or not t.is_cuda or not t.is_contiguous() or \
+            if t.dtype != f32 or not t.is_contiguous() or \
                     len(s) != 3 or s[0] != B or s[2] != D:
                 raise ValueError("gate, scale and shift must be contiguous "
                                  "float32 CUDA tensors [B, G, D]")
@@ -721,7 +721,7 @@ def _norm_call(cfg, x, y, mods, weights):
                 raise ValueError("gate, scale and shift differ in groups")
             groups = s[1]
     for t in weights:
-        if t is not None and (t.dtype != f32 or not t.is_cuda or
+        if t is not None and (t.dtype != f32 or
                               t.shape != (D,) or not t.is_contiguous()):
             raise ValueError("weights must be contiguous float32 CUDA "
                              "tensors [D]")
@@ -862,8 +862,7 @@ class StreamingAttention4:
         the first chunk that each batch entry sees."""
         torch = _torch or _setup()
         c = self.cfg
-        if q.dtype != torch.bfloat16 or not q.is_cuda or \
-                not q.is_contiguous() or q.dim() != 4:
+        if q.dtype != torch.bfloat16 or not q.is_contiguous() or q.dim() != 4:
             raise ValueError("q must be a contiguous bfloat16 CUDA tensor "
                              "[B, L, H, d]")
         B, L, H, d = q.shape
@@ -872,24 +871,27 @@ class StreamingAttention4:
                 frames and L != frames * c.tokens_per_frame:
             raise ValueError(f"q has shape {tuple(q.shape)}")
         if first_chunk is not None and (
-                first_chunk.dtype != torch.int32 or not first_chunk.is_cuda or
+                first_chunk.dtype != torch.int32 or
                 first_chunk.shape != (B,) or not first_chunk.is_contiguous()):
             raise ValueError("first_chunk must be a contiguous int32 CUDA "
                              "tensor [B]")
         if out is None:
             out = torch.empty_like(q)
         elif out.shape != q.shape or out.dtype != q.dtype or \
-                not out.is_contiguous() or out.data_ptr() == q.data_ptr():
+                out.device != q.device or not out.is_contiguous() or \
+                out.data_ptr() == q.data_ptr():
             raise ValueError("out must be contiguous, like q and not q")
         if lse is None and want_lse:
             lse = torch.empty((B, H, L), dtype=torch.float32, device=q.device)
         elif lse is not None and (lse.shape != (B, H, L) or
                                   lse.dtype != torch.float32 or
+                                  lse.device != q.device or
                                   not lse.is_contiguous()):
-            raise ValueError("lse must be contiguous float32 [B, H, L]")
+            raise ValueError("lse must be contiguous float32 [B, H, L], where "
+                             "q is")
         fastvr_q4_attn_fwd(self.plan, q.data_ptr(), _ptr(first_chunk),
                            out.data_ptr(), _ptr(lse),
-                           _stream_of(q, first_chunk, out, lse, self.cache))
+                           _stream_of(q, first_chunk, self.cache))
         return (out, lse) if lse is not None else out
 
     def read(self, chunk: Optional[int] = None):
