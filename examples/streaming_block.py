@@ -3,8 +3,9 @@
     python examples/streaming_block.py [--chunks N] [--heads H] [--rows R --cols C]
 
 streams synthetic chunks through one block (random weights) twice, over a
-bfloat16 cache and over a 4-bit one, and prints both caches' bytes, the time
-per chunk and how far the outputs are apart.  Per chunk the block runs
+bfloat16 cache and over a 4-bit one, and prints both caches' bytes, those of
+the 4-bit cache's workspace, the time per chunk and how far the outputs are
+apart.  Per chunk the block runs
 
     gated_norm            modulated norm of the residual stream
     (QKV projection)      a plain matrix product
@@ -174,8 +175,10 @@ def main() -> None:
         stream(block, cache, xs[:2], a.frames)  # warm-up
         cache.reset()
         outs[name], ms = stream(block, cache, xs, a.frames)
-        print(f"{name:8s} cache {cache.nbytes / 2**20:8.1f} MiB, "
-              f"{ms[-1]:.3f} ms for the last chunk")
+        work = getattr(cache, "workspace", None)  # can serve many streams
+        work = 0 if work is None else work.numel()
+        print(f"{name:8s} cache {cache.nbytes / 2**20:8.1f} MiB, workspace "
+              f"{work / 2**20:8.1f} MiB, {ms[-1]:.3f} ms for the last chunk")
     a16, a4 = (outs[n][-1][0].float() for n in caches)
     print(f"residual streams differ by {float((a4 - a16).norm() / a16.norm()):.2e}"
           " (relative L2)")

@@ -68,7 +68,9 @@ typedef struct {
  *           g = clamp((C theta_i / 2 pi - beta_slow) / (beta_fast -
  *           beta_slow), 0, 1), C = original_context[axis]: pairs that turn
  *           often within the original context keep their frequency, slow
- *           ones are interpolated.
+ *           ones are interpolated.  The ramp g is linear in the turns, as in
+ *           the method's paper; models trained with a ramp that is linear in
+ *           the pair's index have other frequencies in between.
  * Every rotated element is multiplied by `magnitude`; 0 stands for
  * 0.1 ln(max s) + 1 with YARN and for 1 otherwise. */
 typedef struct {
@@ -191,10 +193,12 @@ FASTVR_API fastvr_status_t fastvr_gated_norm_bwd(
 /* ----------------------------------------------------- a KV cache in 4 bits
  *
  * The streaming cache of fastvr_attn.h with its keys and values in 4 bits:
- * a quarter of the memory, and of the bytes that a call with few queries has
- * to read.  The values of a head are cut into groups of 32 along d; a group
- * stores one scale s and 32 codes c in 1 .. 15 and stands for the values
- * (c - 8) s:
+ * 4.5 / 16 of the cache's memory, and of the bytes that a call with few queries
+ * has to read.  Calls with many queries need a workspace that holds the visible
+ * window in bfloat16, as large as the bfloat16 cache: memory is saved where
+ * several caches (the layers of a model, streams in turn) share one.  The
+ * values of a head are cut into groups of 32 along d; a group stores one scale
+ * s and 32 codes c in 1 .. 15 and stands for the values (c - 8) s:
  *   s = max |v| / 7, rounded to 5 significant bits (ties to even),
  *   c = 8 + v / s rounded to the nearest whole number, ties toward zero,
  *       within -7 .. 7.
@@ -264,7 +268,9 @@ FASTVR_API fastvr_status_t fastvr_q4_append(fastvr_plan_t plan, const void* k,
  * Calls with few query rows (frames * N * heads / kv_heads) read the codes
  * directly; longer ones first write the visible keys and values in bfloat16
  * to the workspace.  A plan whose chunks are all short needs a workspace of
- * a few MB only.
+ * a few MB only.  Either way the probabilities are rounded to bfloat16 before
+ * their product with the values, and sums and log-sum-exp are float32.  A row
+ * with a NaN score is NaN.
  * Errors: INVALID_ARG, SEQUENCE, UNSUPPORTED, CUDA. */
 FASTVR_API fastvr_status_t fastvr_q4_attn_fwd(fastvr_plan_t plan,
                                               const void* q,

@@ -21,8 +21,13 @@
 // of all the rows that its CTA takes, so A, C and E are its own and every token
 // sum has a fixed order.  The slices of a group take its rows in turn, so that
 // neighbours in memory are asked for together.  72.0 us (4.7 TB/s) for 12288
-// rows of 1536 with a float32 residual; three exchanges, one after the other,
-// took 73.7, and 88.6 instead of 80.9 for 3600 rows of 5120.
+// rows of 1536 with a float32 residual, layer norm and RMS post norm; three
+// exchanges, one after the other, took 73.7, and 88.6 instead of 80.9 for 3600
+// rows of 5120.  With a bfloat16 residual, a third of the bytes less, it gains
+// 2 to 12 % up to 2048 columns and loses at 1536 and 5120 (93.6 and 93.5 us
+// against 74.5 and 81.5 in the same run; the cause is not known).  These and
+// the times below are of calls replayed from a graph, a few per cent below a
+// call's own.
 #include "block_norm.cuh"
 
 namespace fastvr {
@@ -512,11 +517,12 @@ cudaError_t launch_v(const NormBwdParams& p, cudaStream_t stream) {
 // rows of 1536 with a float32 residual: 96 threads of 16 columns 72.0 us, the
 // same with all five in shared memory and four CTAs 73.5, 192 of 8 and three
 // CTAs 81.8; rows ahead in shared memory 92 and more; 9000 rows of 2048: 61.7
-// us, 128 threads of 16 columns 68.8).  With groups of a few rows, whose ends
-// then count, 192 threads of 8 columns: 78.5 us for 8160 groups of one row,
-// against 98.  Rows above 5120 leave no registers to load ahead and spill some
-// (3000 rows of 8192: 105.8 us; without asking for the next row in L2 128.7).
-// Asked for in L2 as well, narrower rows gain nothing.
+// us, 128 threads of 16 columns 68.8, bfloat16 and RMS norms).  With groups of
+// a few rows, whose ends then count, 192 threads of 8 columns: 78.5 us for 8160
+// groups of one row, against 98 (bfloat16, layer norm alone).  Rows above 5120
+// leave no registers to load ahead and spill some (3000 rows of 8192, bfloat16,
+// RMS norms: 105.8 us; without asking for the next row in L2 128.7).  Asked for
+// in L2 as well, narrower rows gain nothing.
 template <typename TR, typename TY>
 cudaError_t launch_t(const NormBwdParams& p, cudaStream_t stream) {
   if (p.dim <= 64) return launch_v<TR, TY, 8, 1, true, 0, 4>(p, stream);

@@ -9,7 +9,8 @@
 // of a row's sums and the instructions around it, so as many CTAs as fit
 // without spilling share an SM; where the rows ahead wait in shared memory
 // instead of registers, more of them do.  36.1 us (5.6 TB/s) for 16320 rows of
-// 1536 in bfloat16.
+// 1536 in bfloat16 with a layer norm and no post norm.  This and the times
+// below are of calls replayed from a graph, a few per cent below a call's own.
 #include <algorithm>
 
 #include "block_norm.cuh"
@@ -209,18 +210,20 @@ cudaError_t launch_v(const NormFwdParams& p, int sms, cudaStream_t stream) {
 }
 
 // Threads, vectors and rows of a pass, passes ahead in shared memory (0: one in
-// registers), CTAs per SM.  Rows of up to 256 columns lie side by side in a CTA
-// (277236 rows of 64: 35.3 us with one row to a thread and 6 CTAs, 40.2 with
-// two and 4, 49.5 with rows ahead in shared memory).  From there to 512 eight
-// columns to a thread and the next row in registers as well (36000 rows of 512:
-// 25.7 us, 30.2 through shared memory), above that through shared memory
-// (against registers: 36.4 us and 52.6 for 36000 rows of 520, 27.4 and 30.4 for
-// 18000 of 1024, 36.1 and 38.6 for 16320 of 1536 by twos), from 2048 on with 16
-// columns to a thread, which leaves fewer warps to exchange with (29.1 and 38.6
-// for 9000 rows of 2048, 30.9 and 40.9 for 3600 of 5120, 46.3 and 66.5 for 3000
-// of 8192).  A modulation of its own for every row makes the ends of groups
-// count: one row at a time and in registers then (8160 rows of 1536: 43.0 us
-// and 45.3).
+// registers), CTAs per SM.  Times in bfloat16 with RMS norms before and after,
+// but for 64 columns (float32 residual, layer norm after) and 1536 (a layer
+// norm alone).  Rows of up to 256 columns lie side by side in a CTA (277236
+// rows of 64: 35.3 us with one row to a thread and 6 CTAs, 40.2 with two and 4,
+// 49.5 with rows ahead in shared memory).  From there to 512 eight columns to a
+// thread and the next row in registers as well (36000 rows of 512: 25.7 us,
+// 30.2 through shared memory), above that through shared memory (against
+// registers: 36.4 us and 52.6 for 36000 rows of 520, 27.4 and 30.4 for 18000 of
+// 1024, 36.1 and 38.6 for 16320 of 1536 by twos), from 2048 on with 16 columns
+// to a thread, which leaves fewer warps to exchange with (29.1 and 38.6 for
+// 9000 rows of 2048, 30.9 and 40.9 for 3600 of 5120, 46.3 and 66.5 for 3000 of
+// 8192).  A modulation of its own for every row makes the ends of groups count:
+// one row at a time and in registers then (8160 rows of 1536: 43.0 us and
+// 45.3).
 template <typename TR, typename TY>
 cudaError_t launch_t(const NormFwdParams& p, int sms, cudaStream_t stream) {
   if (p.dim <= 64) return launch_v<TR, TY, 8, 1, 1, 0, 6>(p, sms, stream);

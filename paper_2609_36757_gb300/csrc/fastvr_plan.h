@@ -53,7 +53,7 @@ fastvr_status_t ensure_device(fastvr_plan_s* p, size_t control_bytes,
 // FASTVR_OK when the current device is sm_103.
 fastvr_status_t check_device();
 
-// SM count of the current device, looked up once per device.
+// SM count of the current device, asked from the runtime on every call.
 int device_sms();
 
 }  // namespace fastvr

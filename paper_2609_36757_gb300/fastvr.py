@@ -809,9 +809,11 @@ class StreamingAttention4:
     once), forward(q) contiguous [B, f*N, heads, d]; both enqueue on the
     current CUDA stream.  `workspace` (a uint8 CUDA tensor of at least
     fastvr_q4_workspace_bytes) may be shared by streams whose calls do not
-    overlap on the GPU; by default one is allocated.  A stream's first call that
-    launches work cannot be captured into a CUDA graph (FASTVR_ERR_SEQUENCE);
-    a captured call is replayed on the chunks of its capture."""
+    overlap on the GPU, as the layers of a model should: with long chunks it is
+    as large as a bfloat16 cache.  By default one is allocated for the stream.
+    A stream's first call that launches work cannot be captured into a CUDA
+    graph (FASTVR_ERR_SEQUENCE); a captured call is replayed on the chunks of
+    its capture."""
 
     def __init__(self, cfg: fastvr_attn_config_t,
                  kv_heads: Optional[int] = None, device=None, workspace=None):
