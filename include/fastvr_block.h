@@ -1,8 +1,9 @@
 /*
  * fastvr_block.h -- C ABI of the operators around the attention of a
  * streaming DiT block on GB300 (sm_103a): rotary positions, the gated
- * residual update fused with the norms before and after a block, and a KV
- * cache held in 4 bits with the attention that reads it.
+ * residual update fused with the norms before and after a block, a KV
+ * cache held in 4 bits with the attention that reads it, cross attention to
+ * an encoder's states, and the gated feed-forward.
  *
  * One block of a streaming model runs, per chunk,
  *   fastvr_gated_norm_fwd      residual update of the previous block and this
@@ -12,8 +13,12 @@
  *   fastvr_q4_append           keys and values into the 4-bit cache
  *   fastvr_q4_attn_fwd         the chunk's queries over the cache
  *   (the caller's output projection)
- * and training runs fastvr_gated_norm_bwd and fastvr_rotary (transpose = 1)
- * next to fastvr_blockcausal_attn_bwd.
+ *   fastvr_cross_attn_fwd      the chunk's queries over the prompt's states
+ *   fastvr_gated_ffn_fwd       gate and up projections with the activation
+ *   (the caller's down projection)
+ * each with its own residual and norm, and training runs
+ * fastvr_gated_norm_bwd, fastvr_rotary (transpose = 1), fastvr_cross_attn_bwd
+ * and fastvr_gated_ffn_bwd next to fastvr_blockcausal_attn_bwd.
  *
  * The conventions of fastvr_attn.h hold: the caller owns all device memory,
  * pointers are device addresses on the current device, 16-byte aligned unless
@@ -285,6 +290,125 @@ FASTVR_API fastvr_status_t fastvr_q4_attn_fwd(fastvr_plan_t plan,
 FASTVR_API fastvr_status_t fastvr_q4_read(fastvr_plan_t plan, int64_t chunk,
                                           void* k, void* v,
                                           struct CUstream_st* stream);
+
+/* ------------------------------- cross attention to an encoder's states */
+
+/* Queries of one sequence attend to the keys and values of another: the
+ * states of a text or image encoder, of another length, without a causal
+ * order.  Query head h reads key head h / (heads / kv_heads).  With
+ * T_b = min(max(kv_len[b], 0), kv_tokens), or kv_tokens without kv_len:
+ *   S = softmax_scale q k^T over the keys t < T_b,  P = softmax(S),  out = P v
+ * and lse = ln sum exp S.  An entry with T_b = 0 sees nothing: its out is 0 and
+ * its lse -infinity.  What k and v hold at t >= T_b (padding, NaN and
+ * infinities included) does not matter. */
+typedef struct {
+  int32_t batch, q_tokens, kv_tokens; /* >= 1; a sequence's tokens below 2^30 */
+  int32_t heads, kv_heads;            /* heads a multiple of kv_heads         */
+  int32_t head_dim;                   /* 64 or 128                            */
+  float softmax_scale;                /* >= 0; 0 = 1 / sqrt(head_dim)         */
+} fastvr_cross_config_t;
+
+/* The forward.
+ *   q, out  bfloat16 [batch, q_tokens, heads, d], strides q_str, out_str
+ *   k, v    bfloat16 [batch, kv_tokens, kv_heads, d], strides k_str, v_str
+ *           (the halves of a fused projection); strides are >= 0 and below
+ *           2^39; null: contiguous.  An input's batch stride may be 0 (one
+ *           prompt for the whole batch).
+ *   kv_len  nullable, device int32 [batch] (4-byte aligned); any values
+ *   lse     nullable, float32 [batch, heads, q_tokens]
+ * out overlaps no input.  Probabilities are rounded to bfloat16 before their
+ * product with the values; sums and log-sum-exp are float32.  No scratch; a
+ * bounded-wait timeout leaves out undefined and is reported by
+ * fastvr_get_device_status.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim, device), CUDA. */
+FASTVR_API fastvr_status_t fastvr_cross_attn_fwd(
+    const fastvr_cross_config_t* cfg, const void* q,
+    const fastvr_strides_t* q_str, const void* k,
+    const fastvr_strides_t* k_str, const void* v,
+    const fastvr_strides_t* v_str, const int32_t* kv_len, void* out,
+    const fastvr_strides_t* out_str, float* lse, struct CUstream_st* stream);
+
+/* Scratch bytes of fastvr_cross_attn_bwd: the rows' log-sum-exp and
+ * <dout, out>, and partial sums of dk and dv where the queries are split.
+ * Host only.  Errors: INVALID_ARG, UNSUPPORTED (head_dim). */
+FASTVR_API fastvr_status_t fastvr_cross_attn_bwd_scratch_bytes(
+    const fastvr_cross_config_t* cfg, size_t* bytes);
+
+/* Gradients.  out and lse are the forward's, dout out's gradient (strides
+ * dout_str); out_str as in the forward.  Outputs, bfloat16 with their own
+ * strides: dq as q; dk, dv as k and v for every batch entry (with a shared
+ * prompt the caller sums them), zero at t >= T_b.
+ *   D = rowsum(dout o out),  dP = dout v^T,  dS = P o (dP - D)
+ *   dq = scale dS k,  dk = scale dS^T q,  dv = P^T dout
+ * dk and dv sum over the query heads that share a key head.  P and dS enter
+ * the products in bfloat16, sums are float32 in a fixed order (no atomics):
+ * repeated calls agree bit for bit.  Outputs overlap no input and no other
+ * output.  A bounded-wait timeout is reported by fastvr_get_device_status.
+ * Errors: INVALID_ARG, CAPACITY (scratch), UNSUPPORTED (head_dim, device),
+ * CUDA. */
+FASTVR_API fastvr_status_t fastvr_cross_attn_bwd(
+    const fastvr_cross_config_t* cfg, const void* q,
+    const fastvr_strides_t* q_str, const void* k,
+    const fastvr_strides_t* k_str, const void* v,
+    const fastvr_strides_t* v_str, const int32_t* kv_len, const void* out,
+    const fastvr_strides_t* out_str, const void* dout,
+    const fastvr_strides_t* dout_str, const float* lse, void* dq,
+    const fastvr_strides_t* dq_str, void* dk, const fastvr_strides_t* dk_str,
+    void* dv, const fastvr_strides_t* dv_str, void* scratch,
+    size_t scratch_bytes, struct CUstream_st* stream);
+
+/* ------------------------------------------------- the gated feed-forward */
+
+#define FASTVR_ACT_SILU 0      /* g / (1 + exp(-g))                          */
+#define FASTVR_ACT_GELU 1      /* g Phi(g), Phi the normal distribution      */
+#define FASTVR_ACT_GELU_TANH 2 /* g/2 (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) */
+
+/* The first half of a gated feed-forward block, for every token:
+ *   g = x w_gate^T,  u = x w_up^T,  h = act(g) o u
+ * (the down projection of h is a plain product and the caller's). */
+typedef struct {
+  int32_t tokens;     /* >= 1, below 2^30                                     */
+  int32_t dim;        /* a multiple of 8, 8 .. 65536                          */
+  int32_t hidden;     /* a multiple of 8, 8 .. 262144                         */
+  int32_t activation; /* FASTVR_ACT_*                                         */
+} fastvr_ffn_config_t;
+
+/* The forward.
+ *   x       bfloat16 [tokens, dim], x_row elements from row to row (a multiple
+ *           of 8, at least dim; 0: dim)
+ *   w_gate, w_up  bfloat16 [hidden, dim] contiguous
+ *   h       bfloat16 [tokens, hidden] contiguous
+ *   g, u    both or neither null: [tokens, hidden] contiguous, the projections
+ *           rounded to bfloat16, kept for the gradient
+ * Products accumulate in float32, activation and product are float32, h is
+ * rounded once.  Outputs overlap no input and no other output.  A
+ * bounded-wait timeout leaves h undefined and is reported by
+ * fastvr_get_device_status.
+ * Errors: INVALID_ARG, UNSUPPORTED (device), CUDA. */
+FASTVR_API fastvr_status_t fastvr_gated_ffn_fwd(
+    const fastvr_ffn_config_t* cfg, const void* x, int64_t x_row,
+    const void* w_gate, const void* w_up, void* h, void* g, void* u,
+    struct CUstream_st* stream);
+
+/* Scratch bytes of fastvr_gated_ffn_bwd: dg and du.
+ * Host only.  Errors: INVALID_ARG. */
+FASTVR_API fastvr_status_t fastvr_gated_ffn_bwd_scratch_bytes(
+    const fastvr_ffn_config_t* cfg, size_t* bytes);
+
+/* Gradients from dh, with the forward's x, weights, g and u:
+ *   dg = dh o u o act'(g),  du = dh o act(g)
+ *   dx = dg w_gate + du w_up,  dw_gate = dg^T x,  dw_up = du^T x
+ * dx bfloat16 [tokens, dim] contiguous; dw_gate, dw_up bfloat16 [hidden, dim],
+ * both or neither null (frozen weights).  dg and du are rounded to bfloat16
+ * for their products, which accumulate in float32 in a fixed order: repeated
+ * calls agree bit for bit.  Outputs and scratch overlap no input.  A
+ * bounded-wait timeout is reported by fastvr_get_device_status.
+ * Errors: INVALID_ARG, CAPACITY (scratch), UNSUPPORTED (device), CUDA. */
+FASTVR_API fastvr_status_t fastvr_gated_ffn_bwd(
+    const fastvr_ffn_config_t* cfg, const void* dh, const void* x,
+    int64_t x_row, const void* w_gate, const void* w_up, const void* g,
+    const void* u, void* dx, void* dw_gate, void* dw_up, void* scratch,
+    size_t scratch_bytes, struct CUstream_st* stream);
 
 #ifdef __cplusplus
 }

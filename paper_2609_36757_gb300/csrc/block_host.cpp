@@ -17,18 +17,10 @@
 namespace {
 
 using fastvr::aligned16;
-
-bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
-
-cudaStream_t to_stream(struct CUstream_st* s) {
-  return reinterpret_cast<cudaStream_t>(s);
-}
-
-// a * b, or -1 when it does not fit (or a factor already did not).
-int64_t mul(int64_t a, int64_t b) {
-  int64_t r;
-  return a < 0 || b < 0 || __builtin_mul_overflow(a, b, &r) ? -1 : r;
-}
+using fastvr::aligned4;
+using fastvr::get_strides;
+using fastvr::mul;
+using fastvr::to_stream;
 
 // ------------------------------------------------------------------ rotary
 constexpr double kTwoPi = 6.283185307179586476925286766559;
@@ -113,29 +105,6 @@ const RotaryTurns& rotary_turns(const fastvr_rotary_config_t& c) {
       last.turn[i] = (uint64_t)(theta[i] / kTwoPi * 18446744073709551616.0);
   }
   return last;
-}
-
-// Strides in elements that keep every head 16-byte aligned; those of a
-// dimension of one entry do not matter.  A tensor that is written may not have
-// several entries in one place.
-bool get_strides(const fastvr_strides_t* s, int64_t batch, int64_t tokens,
-                 int64_t heads, int64_t d, int elem_bytes, bool written,
-                 fastvr::Strides* out) {
-  if (s == nullptr) {
-    out->head = d;
-    out->token = heads * d;
-    out->batch = tokens * heads * d;
-    return true;
-  }
-  const int64_t size[] = {batch, tokens, heads};
-  const int64_t given[] = {s->batch, s->token, s->head};
-  int64_t* to[] = {&out->batch, &out->token, &out->head};
-  for (int i = 0; i < 3; ++i) {
-    *to[i] = size[i] > 1 ? given[i] : 0;
-    if (*to[i] % (16 / elem_bytes) != 0) return false;
-    if (written && size[i] > 1 && given[i] == 0) return false;
-  }
-  return true;
 }
 
 // ------------------------------------------------------------------- norms

@@ -98,6 +98,11 @@ fastvr_status_t fastvr::check_device() {
   return major == 10 && minor == 3 ? FASTVR_OK : FASTVR_ERR_UNSUPPORTED;
 }
 
+void fastvr::noplan_debug(int32_t* stall, uint64_t* wait_limit_ns) {
+  *stall = g_noplan_stall.load();
+  *wait_limit_ns = g_noplan_wait_ns.load();
+}
+
 int fastvr::device_sms() {
   int dev = 0, sms = 0;
   cudaGetDevice(&dev);

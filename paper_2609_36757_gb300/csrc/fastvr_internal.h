@@ -318,6 +318,57 @@ struct Q4AttnParams {
 cudaError_t launch_q4_attn(const Q4AttnParams& p, int sms,
                            cudaStream_t stream);
 
+// ------------------------------------------- cross attention, feed-forward
+
+struct CrossArgs {
+  const uint16_t *q, *k, *v;  // bfloat16, strides in elements
+  uint16_t* o;
+  float* lse;                 // [batch, heads, q_tokens] or null
+  Strides q_str, k_str, v_str, o_str;
+  const int32_t* kv_len;      // [batch] or null
+  int32_t batch, heads, kv_heads, head_dim, q_tokens, kv_tokens;
+  float scale;
+  int* status;                // device status word or null (not reported)
+  int32_t inject_stall;       // failure-detection test hook
+  uint64_t wait_limit_ns;     // 0 = kernel default
+  int sms;
+};
+cudaError_t launch_cross_attn(const CrossArgs& a, cudaStream_t stream);
+
+struct CrossBwdArgs {
+  CrossArgs f;                // the forward's arguments (o and lse: results)
+  const uint16_t* dout;
+  uint16_t *dq, *dk, *dv;
+  Strides dout_str, dq_str, dk_str, dv_str;
+  float* scratch;             // cross_bwd_scratch_floats of them
+};
+size_t cross_bwd_scratch_floats(int32_t batch, int32_t heads, int32_t kv_heads,
+                                int32_t head_dim, int32_t q_tokens,
+                                int32_t kv_tokens);
+cudaError_t launch_cross_attn_bwd(const CrossBwdArgs& a, cudaStream_t stream);
+
+constexpr int kActSilu = 0, kActGelu = 1, kActGeluTanh = 2;
+
+struct FfnArgs {
+  const uint16_t *x, *w_gate, *w_up;  // [tokens, dim], [hidden, dim] twice
+  int64_t x_row;                      // elements from row to row of x
+  uint16_t *h, *g, *u;                // [tokens, hidden]; g, u nullable
+  int32_t tokens, dim, hidden, act;
+  int* status;
+  int32_t inject_stall;
+  uint64_t wait_limit_ns;
+  int sms;
+};
+cudaError_t launch_ffn_fwd(const FfnArgs& a, cudaStream_t stream);
+
+struct FfnBwdArgs {
+  FfnArgs f;                    // the forward's arguments (h is not used)
+  const uint16_t* dh;           // [tokens, hidden]
+  uint16_t *dx, *dw_gate, *dw_up;
+  uint16_t *dg, *du;            // scratch: [tokens, hidden] each
+};
+cudaError_t launch_ffn_bwd(const FfnBwdArgs& a, cudaStream_t stream);
+
 #ifdef __CUDACC__
 // The first of `keys` tokens (counted from the start of chunk lo_chunk) that
 // a batch entry sees when nothing before chunk first_chunk is visible to it.

@@ -5,7 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
-#include "../../include/fastvr_attn.h"
+#include "../../include/fastvr_block.h"
+#include "fastvr_internal.h"
 
 struct fastvr_plan_s {
   fastvr_attn_config_t cfg;
@@ -55,5 +56,26 @@ fastvr_status_t check_device();
 
 // SM count of the current device, asked from the runtime on every call.
 int device_sms();
+
+// The failure-detection hook of the calls without a plan.
+void noplan_debug(int32_t* stall, uint64_t* wait_limit_ns);
+
+inline bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+inline cudaStream_t to_stream(struct CUstream_st* s) {
+  return reinterpret_cast<cudaStream_t>(s);
+}
+
+// a * b, or -1 when it does not fit (or a factor already did not).
+inline int64_t mul(int64_t a, int64_t b) {
+  int64_t r;
+  return a < 0 || b < 0 || __builtin_mul_overflow(a, b, &r) ? -1 : r;
+}
+
+// Strides in elements that keep every head 16-byte aligned; those of a
+// dimension of one entry do not matter.  A tensor that is written may not have
+// several entries in one place.
+bool get_strides(const fastvr_strides_t* s, int64_t batch, int64_t tokens,
+                 int64_t heads, int64_t d, int elem_bytes, bool written,
+                 Strides* out);
 
 }  // namespace fastvr

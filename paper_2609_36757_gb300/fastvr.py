@@ -12,7 +12,9 @@ the KV cache with torch (device memory is the caller's in the C ABI) and
 passes data pointers and the current CUDA stream through;
 `StreamingAttention4` is the same over a cache held in 4 bits.  `rotary`,
 `gated_norm` and their gradients cover what runs before and after the
-attention in a block.
+attention in a block, `cross_attention` (queries over an encoder's states) and
+`gated_ffn` (the feed-forward's projections and activation) with their
+gradients the block's other operators.
 """
 from __future__ import annotations
 
@@ -51,6 +53,7 @@ FASTVR_BF16, FASTVR_F32 = 0, 1
 ROTARY_LAYOUTS = {"interleaved": 0, "half": 1}
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 NORMS = {"none": 0, "rms": 1, "layer": 2}
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 
 class fastvr_strides_t(ctypes.Structure):
@@ -78,6 +81,18 @@ class fastvr_norm_config_t(ctypes.Structure):
                 ("residual_scale", ctypes.c_float)]
 
 
+class fastvr_cross_config_t(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("q_tokens", ctypes.c_int32),
+                ("kv_tokens", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float)]
+
+
+class fastvr_ffn_config_t(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("hidden", ctypes.c_int32), ("activation", ctypes.c_int32)]
+
+
 # Every symbol the headers declare, with (restype, argtypes).
 _VP, _I32, _I64, _SZ = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                         ctypes.c_size_t)
@@ -85,6 +100,8 @@ _CFGP = ctypes.POINTER(fastvr_attn_config_t)
 _STRP = ctypes.POINTER(fastvr_strides_t)
 _ROTP = ctypes.POINTER(fastvr_rotary_config_t)
 _NRMP = ctypes.POINTER(fastvr_norm_config_t)
+_CRSP = ctypes.POINTER(fastvr_cross_config_t)
+_FFNP = ctypes.POINTER(fastvr_ffn_config_t)
 SIGNATURES = {
     "fastvr_kv_cache_bytes": (_I32, [_CFGP, ctypes.POINTER(_SZ)]),
     "fastvr_attn_plan": (_I32, [_CFGP, _VP, _SZ, ctypes.POINTER(_VP)]),
@@ -135,6 +152,18 @@ SIGNATURES = {
     "fastvr_q4_append": (_I32, [_VP, _VP, _STRP, _VP, _STRP, _I32, _VP]),
     "fastvr_q4_attn_fwd": (_I32, [_VP] * 6),
     "fastvr_q4_read": (_I32, [_VP, _I64, _VP, _VP, _VP]),
+    "fastvr_cross_attn_fwd": (_I32, [_CRSP] + [_VP, _STRP] * 3 +
+                              [_VP, _VP, _STRP, _VP, _VP]),
+    "fastvr_cross_attn_bwd_scratch_bytes": (_I32, [_CRSP,
+                                                   ctypes.POINTER(_SZ)]),
+    "fastvr_cross_attn_bwd": (_I32, [_CRSP] + [_VP, _STRP] * 3 + [_VP] +
+                              [_VP, _STRP] * 2 + [_VP] + [_VP, _STRP] * 3 +
+                              [_VP, _SZ, _VP]),
+    "fastvr_gated_ffn_fwd": (_I32, [_FFNP, _VP, _I64] + [_VP] * 6),
+    "fastvr_gated_ffn_bwd_scratch_bytes": (_I32, [_FFNP,
+                                                  ctypes.POINTER(_SZ)]),
+    "fastvr_gated_ffn_bwd": (_I32, [_FFNP, _VP, _VP, _I64] + [_VP] * 8 +
+                             [_SZ, _VP]),
 }
 
 
@@ -461,6 +490,51 @@ def fastvr_q4_attn_fwd(plan: int, q: int, first_chunk: int, out: int,
 def fastvr_q4_read(plan: int, chunk: int, k: int, v: int,
                    stream: int) -> None:
     _check(lib.fastvr_q4_read(plan, chunk, k, v, stream), "fastvr_q4_read")
+
+
+def fastvr_cross_attn_fwd(cfg, q, q_str, k, k_str, v, v_str, kv_len, out,
+                          out_str, lse, stream) -> None:
+    """Strides are fastvr_strides_t or None (contiguous)."""
+    _check(lib.fastvr_cross_attn_fwd(cfg, q, q_str, k, k_str, v, v_str, kv_len,
+                                     out, out_str, lse, stream),
+           "fastvr_cross_attn_fwd")
+
+
+def fastvr_cross_attn_bwd_scratch_bytes(cfg: fastvr_cross_config_t) -> int:
+    n = _SZ(0)
+    _check(lib.fastvr_cross_attn_bwd_scratch_bytes(cfg, ctypes.byref(n)),
+           "fastvr_cross_attn_bwd_scratch_bytes")
+    return n.value
+
+
+def fastvr_cross_attn_bwd(cfg, q, q_str, k, k_str, v, v_str, kv_len, out,
+                          out_str, dout, dout_str, lse, dq, dq_str, dk, dk_str,
+                          dv, dv_str, scratch, scratch_bytes, stream) -> None:
+    """Strides are fastvr_strides_t or None (contiguous)."""
+    _check(lib.fastvr_cross_attn_bwd(
+        cfg, q, q_str, k, k_str, v, v_str, kv_len, out, out_str, dout,
+        dout_str, lse, dq, dq_str, dk, dk_str, dv, dv_str, scratch,
+        scratch_bytes, stream), "fastvr_cross_attn_bwd")
+
+
+def fastvr_gated_ffn_fwd(cfg, x, x_row, w_gate, w_up, h, g, u,
+                         stream) -> None:
+    _check(lib.fastvr_gated_ffn_fwd(cfg, x, x_row, w_gate, w_up, h, g, u,
+                                    stream), "fastvr_gated_ffn_fwd")
+
+
+def fastvr_gated_ffn_bwd_scratch_bytes(cfg: fastvr_ffn_config_t) -> int:
+    n = _SZ(0)
+    _check(lib.fastvr_gated_ffn_bwd_scratch_bytes(cfg, ctypes.byref(n)),
+           "fastvr_gated_ffn_bwd_scratch_bytes")
+    return n.value
+
+
+def fastvr_gated_ffn_bwd(cfg, dh, x, x_row, w_gate, w_up, g, u, dx, dw_gate,
+                         dw_up, scratch, scratch_bytes, stream) -> None:
+    _check(lib.fastvr_gated_ffn_bwd(cfg, dh, x, x_row, w_gate, w_up, g, u, dx,
+                                    dw_gate, dw_up, scratch, scratch_bytes,
+                                    stream), "fastvr_gated_ffn_bwd")
 
 
 def make_config(batch: int, heads: int, head_dim: int, tokens_per_frame: int,
@@ -799,6 +873,168 @@ def gated_norm_bwd(cfg: fastvr_norm_config_t, dr, dh, r, y, gate=None,
                           _stream_of(r, y, dr, dh, gate, scale, pre_weight,
                                      post_weight))
     return g
+
+
+def make_cross_config(softmax_scale: float = 0.0) -> fastvr_cross_config_t:
+    """Cross attention with a softmax scale (0: 1 / sqrt(d)); the shapes are
+    taken from its tensors."""
+    return fastvr_cross_config_t(0, 0, 0, 0, 0, 0, softmax_scale)
+
+
+def _cross_call(cfg, q, k, v, kv_len):
+    """cfg for the tensors of a call and the strides of q, k and v, after the
+    checks of their types and shapes."""
+    torch = _torch or _setup()
+    bf16 = torch.bfloat16
+    if q.dtype != bf16 or k.dtype != bf16 or v.dtype != bf16:
+        raise ValueError("q, k and v must be bfloat16")
+    q_str = _head_strides(q, "q")
+    k_str, v_str = _head_strides(k, "k"), _head_strides(v, "v")
+    B, L, H, d = q.shape
+    _, T, K, _ = shape = k.shape
+    if shape != (B, T, K, d) or v.shape != shape:
+        raise ValueError("q, k and v differ in batch or head size, or k and v "
+                         "in shape")
+    if kv_len is not None and (kv_len.dtype != torch.int32 or
+                               kv_len.shape != (B,) or
+                               not kv_len.is_contiguous()):
+        raise ValueError("kv_len must be a contiguous int32 CUDA tensor [B]")
+    return (fastvr_cross_config_t(B, L, T, H, K, d, cfg.softmax_scale), q_str,
+            k_str, v_str)
+
+
+def cross_attention(cfg: fastvr_cross_config_t, q, k, v, kv_len=None,
+                    want_lse: bool = False):
+    """Torch convenience for fastvr_cross_attn_fwd: q [B, L, H, d] and k, v
+    [B, T, Hkv, d] bfloat16, heads contiguous, any other strides (halves of a
+    fused projection; one prompt expanded over the batch); kv_len int32 [B]:
+    the keys that each batch entry sees (none: all).  Returns out [B, L, H, d],
+    or (out, lse) with the float32 log-sum-exp [B, H, L]."""
+    c, q_str, k_str, v_str = _cross_call(cfg, q, k, v, kv_len)
+    torch = _torch
+    out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    lse = (torch.empty((c.batch, c.heads, c.q_tokens), dtype=torch.float32,
+                       device=q.device) if want_lse else None)
+    fastvr_cross_attn_fwd(c, q.data_ptr(), q_str, k.data_ptr(), k_str,
+                          v.data_ptr(), v_str, _ptr(kv_len), out.data_ptr(),
+                          None, _ptr(lse), _stream_of(q, k, v, kv_len))
+    return (out, lse) if want_lse else out
+
+
+class CrossGrads(NamedTuple):
+    """Gradients of cross_attention."""
+    dq: object
+    dk: object
+    dv: object
+
+
+def cross_attention_bwd(cfg: fastvr_cross_config_t, q, k, v, out, dout, lse,
+                        kv_len=None) -> CrossGrads:
+    """Torch convenience for fastvr_cross_attn_bwd: out and lse are
+    cross_attention's, dout out's gradient (heads contiguous, any other
+    strides).  The gradients are contiguous, with q's, k's and v's shapes: of
+    a prompt expanded over the batch, a gradient for each entry."""
+    c, q_str, k_str, v_str = _cross_call(cfg, q, k, v, kv_len)
+    torch = _torch
+    for t, name in ((out, "out"), (dout, "dout")):
+        if t.dtype != torch.bfloat16 or t.shape != q.shape:
+            raise ValueError(f"{name} must be bfloat16 and of q's shape")
+    if lse.dtype != torch.float32 or not lse.is_contiguous() or \
+            lse.shape != (c.batch, c.heads, c.q_tokens):
+        raise ValueError("lse must be contiguous float32 [B, H, L]")
+    like = lambda t: torch.empty_like(t, memory_format=torch.contiguous_format)
+    g = CrossGrads(like(q), like(k), like(v))
+    nbytes = fastvr_cross_attn_bwd_scratch_bytes(c)
+    scratch = torch.empty((nbytes + 3) // 4, dtype=torch.float32,
+                          device=q.device)
+    fastvr_cross_attn_bwd(
+        c, q.data_ptr(), q_str, k.data_ptr(), k_str, v.data_ptr(), v_str,
+        _ptr(kv_len), out.data_ptr(), _head_strides(out, "out"),
+        dout.data_ptr(), _head_strides(dout, "dout"), lse.data_ptr(),
+        g.dq.data_ptr(), None, g.dk.data_ptr(), None, g.dv.data_ptr(), None,
+        scratch.data_ptr(), nbytes,
+        _stream_of(q, k, v, kv_len, out, dout, lse))
+    return g
+
+
+def make_ffn_config(activation: str = "silu") -> fastvr_ffn_config_t:
+    """A gated feed-forward with the activation "silu", "gelu" or "gelu_tanh";
+    the shapes are taken from its tensors."""
+    return fastvr_ffn_config_t(0, 0, 0, ACTIVATIONS[activation])
+
+
+def _ffn_call(cfg, x, w_gate, w_up, hidden):
+    """cfg for the tensors of a call and x's row stride, after the checks of
+    their types and shapes; hidden: tensors [..., hidden]."""
+    torch = _torch or _setup()
+    bf16 = torch.bfloat16
+    if x.dtype != bf16 or w_gate.dtype != bf16 or w_up.dtype != bf16:
+        raise ValueError("x and the weights must be bfloat16")
+    shape = w_gate.shape
+    if len(shape) != 2 or w_up.shape != shape or \
+            not w_gate.is_contiguous() or not w_up.is_contiguous():
+        raise ValueError("w_gate and w_up must be contiguous [F, D]")
+    F, D = shape
+    lead = x.shape[:-1]
+    if not lead or x.shape[-1] != D:
+        raise ValueError("x must be [..., D]")
+    row = D
+    if not x.is_contiguous():
+        try:
+            row = x.view(-1, D).stride(0)
+        except RuntimeError:
+            row = 0
+        if row < D or x.stride(-1) != 1:
+            raise ValueError("x's rows must be contiguous and evenly spaced")
+    for t in hidden:
+        if t.dtype != bf16 or t.shape != lead + (F,) or not t.is_contiguous():
+            raise ValueError("dh and the saved projections must be contiguous "
+                             "bfloat16 [..., F]")
+    tokens = x.numel() // D if D else 0
+    return fastvr_ffn_config_t(tokens, D, F, cfg.activation), row
+
+
+def gated_ffn(cfg: fastvr_ffn_config_t, x, w_gate, w_up,
+              want_saved: bool = False):
+    """Torch convenience for fastvr_gated_ffn_fwd: x [..., D] (rows evenly
+    spaced), w_gate and w_up [F, D], bfloat16.  Returns h [..., F], or
+    (h, (g, u)) with the projections that gated_ffn_bwd takes."""
+    c, row = _ffn_call(cfg, x, w_gate, w_up, ())
+    shape = x.shape[:-1] + (c.hidden,)
+    h = x.new_empty(shape)
+    g = u = None
+    if want_saved:
+        g, u = x.new_empty(shape), x.new_empty(shape)
+    fastvr_gated_ffn_fwd(c, x.data_ptr(), row, w_gate.data_ptr(),
+                         w_up.data_ptr(), h.data_ptr(), _ptr(g), _ptr(u),
+                         _stream_of(x, w_gate, w_up))
+    return (h, (g, u)) if want_saved else h
+
+
+class FfnGrads(NamedTuple):
+    """Gradients of gated_ffn; None for frozen weights."""
+    dx: object
+    dw_gate: object
+    dw_up: object
+
+
+def gated_ffn_bwd(cfg: fastvr_ffn_config_t, dh, x, w_gate, w_up, saved,
+                  want_dw: bool = True) -> FfnGrads:
+    """Torch convenience for fastvr_gated_ffn_bwd: dh [..., F] the gradient of
+    h, saved the forward's (g, u).  The scratch is allocated with torch."""
+    g, u = saved
+    c, row = _ffn_call(cfg, x, w_gate, w_up, (dh, g, u))
+    torch = _torch
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+    dw = [torch.empty_like(w) if want_dw else None for w in (w_gate, w_up)]
+    nbytes = fastvr_gated_ffn_bwd_scratch_bytes(c)
+    scratch = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    fastvr_gated_ffn_bwd(c, dh.data_ptr(), x.data_ptr(), row,
+                         w_gate.data_ptr(), w_up.data_ptr(), g.data_ptr(),
+                         u.data_ptr(), dx.data_ptr(), _ptr(dw[0]),
+                         _ptr(dw[1]), scratch.data_ptr(), nbytes,
+                         _stream_of(x, dh, w_gate, w_up, g, u))
+    return FfnGrads(dx, *dw)
 
 
 class StreamingAttention4:
