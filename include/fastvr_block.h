@@ -367,7 +367,8 @@ FASTVR_API fastvr_status_t fastvr_cross_attn_bwd(
  *   g = x w_gate^T,  u = x w_up^T,  h = act(g) o u
  * (the down projection of h is a plain product and the caller's). */
 typedef struct {
-  int32_t tokens;     /* >= 1, below 2^30                                     */
+  int32_t tokens;     /* >= 1, below 2^30; tokens times dim and times hidden
+                         at most 2^44                                        */
   int32_t dim;        /* a multiple of 8, 8 .. 65536                          */
   int32_t hidden;     /* a multiple of 8, 8 .. 262144                         */
   int32_t activation; /* FASTVR_ACT_*                                         */

@@ -91,6 +91,9 @@ bool valid_ffn(const fastvr_ffn_config_t* c) {
   return c != nullptr && c->tokens >= 1 && c->tokens <= INT32_MAX / 2 &&
          c->dim >= 8 && c->dim <= 65536 && c->dim % 8 == 0 && c->hidden >= 8 &&
          c->hidden <= 262144 && c->hidden % 8 == 0 &&
+         // tiles are counted in 32 bits
+         mul(c->tokens, c->dim > c->hidden ? c->dim : c->hidden) <=
+             (int64_t)1 << 44 &&
          c->activation >= FASTVR_ACT_SILU &&
          c->activation <= FASTVR_ACT_GELU_TANH;
 }

@@ -1,153 +1,557 @@
-// Gated feed-forward: h = act(x Wg^T) o (x Wu^T) and its gradients, as 64 x 64
-// tiles in float32.
+// Gated feed-forward, h = act(x Wg^T) o (x Wu^T), and its gradients, on
+// tcgen05 tensor cores with CTA pairs.
+//
+// With dg = dh o u o act'(g) and du = dh o act(g) (slope_kernel), every product
+// is a sum over an axis that either operand has as its rows or its columns:
+//   forward  g, u [tokens, hidden]  = x W^T        x and W by rows
+//   dx       [tokens, dim] = dg Wg + du Wu         dg by rows, W by columns
+//   dW       [hidden, dim] = dg^T x, du^T x        dg and x by columns
+// so one kernel serves all: TMA brings 128-byte-swizzled boxes of 64 columns,
+// which the MMA's descriptors read as K-major (rows) or MN-major (columns)
+// operands, and nothing is transposed in memory.
+//
+// A pair of CTAs owns a 256 x 256 tile of results (a forward tile: 128 columns
+// of g and the same 128 of u, whose product is formed in the epilogue, so g and
+// u need not leave the SM).  Each CTA loads 128 rows of A and 128 of B's 256,
+// 32 KB for 64 steps of the sum: half of what a CTA alone would load for the
+// same products, which L2 could not deliver.  Persistent: warp 0 loads (six
+// stages), warp 1 of the even CTA issues the MMAs of both, warps 4-11 form and
+// store the results from one half of TMEM while the next tile accumulates in
+// the other.  Every wait is bounded, as in chunk_attn_fwd.cu.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <math.h>
+#include <string.h>
+
+#include <algorithm>
 
 #include "fastvr_internal.h"
+#include "sm100_ptx.cuh"
 
 namespace fastvr {
 namespace {
 
-// act(g) and its derivative in float32.
+using namespace sm100;
+
+constexpr int kThreads = 384;
+constexpr int kStages = 6;
+constexpr int kHalf = 128;              // rows of A and of B in one CTA
+constexpr int kStep = 64;               // of the summed axis in one stage
+constexpr int kOperand = kHalf * kStep * 2;  // bytes of one operand's stage
+constexpr uint32_t kTmemCols = 512;     // two tiles' results
+constexpr uint64_t kDefaultWaitLimitNs = 4000000000ull;
+constexpr uint64_t kAbortGraceNs = 1000000;
+constexpr int kGroupTiles = 8;  // row tiles that share their columns' tiles
+
+// act(g) and its derivative in float32.  tanh's form is written with the
+// logistic function, (1 + tanh y) / 2 = 1 / (1 + exp(-2 y)), which keeps its
+// relative accuracy where g is far below 0.
+__device__ __forceinline__ float logistic(float y) {
+  return 1.f / (1.f + __expf(-y));
+}
 __device__ __forceinline__ float activation(float g, int act, float* slope) {
   if (act == kActSilu) {
-    const float s = 1.f / (1.f + expf(-g));
+    const float s = logistic(g);
     *slope = s * (1.f + g * (1.f - s));
     return g * s;
   }
   if (act == kActGelu) {
     const float c = 0.5f * (1.f + erff(g * 0.70710678f));
-    *slope = c + g * 0.39894228f * expf(-0.5f * g * g);
+    *slope = c + g * 0.39894228f * __expf(-0.5f * g * g);
     return g * c;
   }
-  const float t = tanhf(0.79788456f * (g + 0.044715f * g * g * g));
-  *slope = 0.5f * (1.f + t) + 0.5f * g * (1.f - t * t) * 0.79788456f *
-                                  (1.f + 3.f * 0.044715f * g * g);
-  return 0.5f * g * (1.f + t);
+  // 2 sqrt(2 / pi) and its product with 0.044715; s (1 - s) is 0 past +-30,
+  // where the other factor could overflow
+  const float s = logistic(g * (1.5957691f + 0.071354816f * g * g));
+  const float b = fminf(fmaxf(g, -30.f), 30.f);
+  *slope = s + b * s * (1.f - s) * (1.5957691f + 0.21406445f * b * b);
+  return g * s;
 }
 
-// c[m, n] = sum_k a[m, k] b[n, k] over two operand pairs one after the other
-// (join) or side by side (h = act(c0) o c1); element strides for both axes.
-struct Mat {
-  const uint16_t* p;
-  int64_t row, k;
-};
-struct Product {
-  Mat a[2], b[2];
-  int m, n, k, act;
-  bool gated;
-  uint16_t *c, *g, *u;  // [m, n]
+enum Kind { kFwd, kDx, kDw };
+
+// Tiles of one kind: results [rows, cols], rows of tiles by tiles across.
+struct Tiles {
+  int32_t rows, cols, mt, nt, count, steps;
 };
 
-__global__ void __launch_bounds__(256) product_kernel(Product p) {
-  __shared__ float sa[16][65], sb[16][65];
-  const int m0 = blockIdx.y * 64, n0 = blockIdx.x * 64;
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  float acc[2][4][4] = {};
-  for (int pass = 0; pass < 2 && p.a[pass].p; ++pass)
-    for (int k0 = 0; k0 < p.k; k0 += 16) {
-      for (int i = threadIdx.x; i < 1024; i += 256) {
-        const int r = i / 16, k = i % 16;
-        const bool in = k0 + k < p.k;
-        sa[k][r] = in && m0 + r < p.m
-                       ? bf16_lo(p.a[pass].p[(m0 + r) * p.a[pass].row +
-                                             (k0 + k) * p.a[pass].k])
-                       : 0.f;
-        sb[k][r] = in && n0 + r < p.n
-                       ? bf16_lo(p.b[pass].p[(n0 + r) * p.b[pass].row +
-                                             (k0 + k) * p.b[pass].k])
-                       : 0.f;
-      }
-      __syncthreads();
-      for (int k = 0; k < 16; ++k)
-        for (int i = 0; i < 4; ++i)
-          for (int j = 0; j < 4; ++j) {
-            const float t = sa[k][ty + 16 * i] * sb[k][tx + 16 * j];
-            if (p.gated && pass)
-              acc[1][i][j] += t;
-            else
-              acc[0][i][j] += t;
-          }
-      __syncthreads();
-    }
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-      if (m >= p.m || n >= p.n) continue;
-      const int64_t x = (int64_t)m * p.n + n;
-      float v = acc[0][i][j], slope;
-      if (p.gated) {
-        if (p.g) {
-          p.g[x] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-          p.u[x] = __bfloat16_as_ushort(__float2bfloat16_rn(acc[1][i][j]));
-        }
-        v = activation(v, p.act, &slope) * acc[1][i][j];
-      }
-      p.c[x] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-    }
+struct PairParams {
+  CUtensorMap x, w[2], d[2];  // x; gate and up weights; dg and du
+  Tiles tile[2];              // forward: [0]; backward: those listed first, and
+  int32_t kind[2];            // the others
+  // Backward: pairs from `heavy` on (0: none) have one tile fewer of the first
+  // list and take `extra` of the second list before its common rounds.
+  int32_t heavy, extra;
+  uint16_t *out, *out2, *g, *u;  // forward: h, g, u; backward: dx, dWg, dWu
+  uint16_t* dw[2];
+  int32_t act, half_steps;  // dx: steps of dg Wg
+  int32_t wide;             // rows of results start on 32-byte boundaries
+  int* status;
+  int32_t inject_stall;
+  uint64_t wait_limit_ns;
+};
+
+struct Shared {
+  uint64_t full[kStages], empty[kStages];
+  uint64_t acc_full[2], acc_empty[2], drain;
+  uint32_t tmem_base;
+  int abort;
+  uint64_t wait_limit_ns;
+};
+constexpr int kSharedBytes = kStages * 2 * kOperand;
+constexpr int kSmem = kSharedBytes + (int)sizeof(Shared) + 1024;
+
+__device__ __forceinline__ bool give_up(Shared* S, uint64_t t0, int* status) {
+  if (*reinterpret_cast<volatile int*>(&S->abort)) return true;
+  if (global_timer_ns() - t0 <= S->wait_limit_ns) return false;
+  *reinterpret_cast<volatile int*>(&S->abort) = 1;
+  if (status != nullptr) atomicExch(status, kDevTimeout);
+  return true;
+}
+// Bounded waits: one thread's, and a whole warp's that stays converged.  The
+// barriers are arrived at from both CTAs of the pair.
+__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity,
+                                         Shared* S, int* status) {
+  if (mbar_try_wait_cluster(bar, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+  while (!mbar_try_wait_cluster(bar, parity))
+    if (give_up(S, t0, status)) return false;
+  return true;
+}
+__device__ __forceinline__ bool wait_bar_warp(uint64_t* bar, uint32_t parity,
+                                              Shared* S, int* status) {
+  if (__all_sync(~0u, mbar_try_wait_cluster(bar, parity))) return true;
+  const uint64_t t0 = global_timer_ns();
+  while (!__all_sync(~0u, mbar_try_wait_cluster(bar, parity)))
+    if (__any_sync(~0u, give_up(S, t0, status))) return false;
+  return true;
+}
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity,
+                                           const Shared* S) {
+  const uint64_t t0 = global_timer_ns();
+  while (!mbar_try_wait_cluster(bar, parity))
+    if (global_timer_ns() - t0 > S->wait_limit_ns) return;
 }
 
-__global__ void __launch_bounds__(256) slope_kernel(FfnBwdArgs a) {
-  const int64_t n = (int64_t)a.f.tokens * a.f.hidden;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n;
-       i += (int64_t)gridDim.x * 256) {
-    float slope;
-    const float g = bf16_lo(a.f.g[i]), u = bf16_lo(a.f.u[i]),
-                d = bf16_lo(a.dh[i]);
-    const float y = activation(g, a.f.act, &slope);
-    a.dg[i] = __bfloat16_as_ushort(__float2bfloat16_rn(d * u * slope));
-    a.du[i] = __bfloat16_as_ushort(__float2bfloat16_rn(d * y));
+// The i-th tile of a pair of CTAs; false behind its last.
+struct Work {
+  int kind, m0, n0, steps, which;  // which: dWg or dWu
+};
+__host__ __device__ inline bool nth_tile(const PairParams& p, int pair,
+                                         int pairs, int i, Work* w) {
+  int list = 0, t = pair + i * pairs;
+  if (t >= p.tile[0].count) {
+    list = 1;
+    i -= (p.tile[0].count + pairs - 1 - pair) / pairs;  // had of the first
+    const int light = pairs - p.heavy;
+    const int ahead = min(p.tile[1].count, p.extra * light);
+    if (p.extra > 0 && pair >= p.heavy && i < p.extra) {
+      t = pair - p.heavy + i * light;
+      if (t >= ahead) return false;
+    } else {
+      if (p.extra > 0 && pair >= p.heavy) i -= p.extra;
+      t = ahead + pair + i * pairs;
+    }
+    if (t >= p.tile[1].count) return false;
+  }
+  const Tiles& a = p.tile[list];
+  w->kind = p.kind[list];
+  w->steps = a.steps;
+  w->which = 0;
+  if (w->kind == kDw) {
+    const int one = a.mt * a.nt;
+    w->which = t >= one;
+    t -= w->which * one;
+  }
+  const int across = kGroupTiles * a.nt;
+  const int first = t / across * kGroupTiles;
+  const int gm = min(kGroupTiles, a.mt - first), r = t % across;
+  w->m0 = (first + r % gm) * 2 * kHalf;
+  w->n0 = r / gm * (w->kind == kFwd ? kHalf : 2 * kHalf);
+  return true;
+}
+
+// 32 results of a row as bfloat16 from column c on.
+__device__ __forceinline__ void store_row32(uint16_t* row, int c, int cols,
+                                            const uint32_t (&pk)[16],
+                                            bool wide) {
+  if (wide) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (c + 16 * i < cols) store_32b(row + c + 16 * i, pk + 8 * i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + 8 * i < cols)
+        *reinterpret_cast<uint4*>(row + c + 8 * i) =
+            make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
   }
 }
 
-cudaError_t launch_product(const Product& p, cudaStream_t stream) {
-  const dim3 grid((p.n + 63) / 64, (p.m + 63) / 64);
-  product_kernel<<<grid, 256, 0, stream>>>(p);
-  return cudaGetLastError();
+__device__ __forceinline__ void pack_row32(const uint32_t (&v)[32],
+                                           uint32_t (&pk)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    pk[i] = bf16_pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+}
+
+template <bool kBackward>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+pair_kernel(const __grid_constant__ PairParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  Shared* S = reinterpret_cast<Shared*>(smem + kSharedBytes);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int rank = (int)cluster_rank();
+  const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
+
+  if (warp == 1) tmem_alloc_pair(&S->tmem_base, kTmemCols);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&S->full[s], 1);
+      mbar_init(&S->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&S->acc_full[b], 1);
+      mbar_init(&S->acc_empty[b], 16);  // the storing warps of both CTAs
+    }
+    mbar_init(&S->drain, 1);
+    S->abort = 0;
+    S->wait_limit_ns = p.wait_limit_ns ? p.wait_limit_ns : kDefaultWaitLimitNs;
+    fence_barrier_init();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = S->tmem_base;
+  pdl_trigger();
+  pdl_wait();
+  Work w;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int it = 0;
+      bool ok = true;
+      for (int i = 0; ok && nth_tile(p, pair, pairs, i, &w); ++i) {
+        for (int s = 0; s < w.steps; ++s, ++it) {
+          const int st = it % kStages;
+          if (!(ok = wait_bar(&S->empty[st], ((it / kStages) & 1) ^ 1, S,
+                              p.status)))
+            break;
+          uint8_t* a = smem + st * 2 * kOperand;
+          uint8_t* b = a + kOperand;
+          // both CTAs' bytes count on the even CTA's barrier
+          const uint32_t bar = cluster_addr(&S->full[st], 0);
+          if (rank == 0) mbar_arrive_expect_tx(&S->full[st], 4 * kOperand);
+          if (!kBackward) {
+            tma_load_2d_pair(&p.x, a, bar, s * kStep, w.m0 + rank * kHalf);
+            tma_load_2d_pair(&p.w[rank], b, bar, s * kStep, w.n0);
+          } else if (w.kind == kDx) {
+            const int up = s >= p.half_steps;
+            const int k = (s - up * p.half_steps) * kStep;
+            for (int x = 0; x < 2; ++x) {
+              tma_load_2d_pair(&p.d[up], a + x * (kOperand / 2), bar, k,
+                               w.m0 + rank * kHalf + x * 64);
+              tma_load_2d_pair(&p.w[up], b + x * (kOperand / 2), bar,
+                               w.n0 + rank * kHalf + x * 64, k);
+            }
+          } else {
+            for (int x = 0; x < 2; ++x) {
+              tma_load_2d_pair(&p.d[w.which], a + x * (kOperand / 2),
+                               bar, w.m0 + rank * kHalf + x * 64, s * kStep);
+              tma_load_2d_pair(&p.x, b + x * (kOperand / 2), bar,
+                               w.n0 + rank * kHalf + x * 64, s * kStep);
+            }
+          }
+        }
+      }
+      // every load has landed before the pair exits
+      if (rank == 0)
+        for (int i = max(0, it - kStages); i < it; ++i)
+          drain_wait(&S->full[i % kStages], (i / kStages) & 1, S);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0) {
+      const uint32_t base = smem_addr(smem);
+      // Test hook: `drain` receives no arrival before the end, so this wait
+      // runs out and exercises the abort path.
+      bool ok = !p.inject_stall || wait_bar_warp(&S->drain, 0, S, p.status);
+      int it = 0;
+      for (int i = 0; ok && nth_tile(p, pair, pairs, i, &w); ++i) {
+        const int buf = i & 1;
+        if (!(ok = wait_bar_warp(&S->acc_empty[buf], ((i >> 1) & 1) ^ 1, S,
+                                 p.status)))
+          break;
+        tc_fence_after();
+        // K-major: 16 elements are 32 bytes of a row, 8 rows 1024 bytes apart.
+        // MN-major: 16 elements are 16 rows of 128 bytes, 64 of the other axis
+        // a box of 64 rows.
+        const bool a_mn = kBackward && w.kind == kDw, b_mn = kBackward;
+        const uint32_t idesc = idesc_bf16_f32(256, 256, b_mn, a_mn);
+        const uint32_t hi = desc_hi_sw128(1024);
+        const uint32_t a_lbo = a_mn ? kOperand / 2 : 16;
+        const uint32_t b_lbo = b_mn ? kOperand / 2 : 16;
+        const uint32_t a_step = (a_mn ? 2048 : 32) >> 4;
+        const uint32_t b_step = (b_mn ? 2048 : 32) >> 4;
+        for (int s = 0; s < w.steps; ++s, ++it) {
+          const int st = it % kStages;
+          if (!(ok = wait_bar_warp(&S->full[st], (it / kStages) & 1, S,
+                                   p.status)))
+            break;
+          tc_fence_after();
+          const uint32_t a_lo = desc_lo(base + st * 2 * kOperand, a_lbo);
+          const uint32_t b_lo =
+              desc_lo(base + st * 2 * kOperand + kOperand, b_lbo);
+#pragma unroll
+          for (int k = 0; k < kStep / 16; ++k)
+            mma_ss_pair_warp(tmem + buf * 256, a_lo + k * a_step, hi,
+                             b_lo + k * b_step, hi, idesc, (s | k) != 0);
+          mma_commit_pair_warp(&S->empty[st]);
+        }
+        if (ok) mma_commit_pair_warp(&S->acc_full[buf]);
+      }
+      mma_commit_pair_warp(&S->drain);
+      if (lane == 0) drain_wait(&S->drain, 0, S);
+      __syncwarp();
+    }
+  } else if (warp >= 4) {
+    const int quarter = warp % 4, hf = (warp - 4) / 4;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    for (int i = 0; nth_tile(p, pair, pairs, i, &w); ++i) {
+      const int buf = i & 1;
+      if (!wait_bar_warp(&S->acc_full[buf], (i >> 1) & 1, S, p.status)) break;
+      tc_fence_after();
+      const Tiles& shape = p.tile[kBackward && w.kind != p.kind[0]];
+      const int row = w.m0 + rank * kHalf + quarter * 32 + lane;
+      const bool in = row < shape.rows;
+      const uint32_t acc = tmem + buf * 256 + lanes;
+      const uint32_t freed = cluster_addr(&S->acc_empty[buf], 0);
+      const int64_t at = (int64_t)row * shape.cols;
+      if (!kBackward) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int col = hf * 64 + c * 32;
+          __syncwarp();
+          uint32_t g[32], u[32], pk[16];
+          tmem_ld32(acc + col, g);
+          tmem_ld32(acc + 128 + col, u);
+          tmem_wait_ld();
+          if (c == 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(freed);
+          }
+          if (p.g != nullptr && in) {
+            pack_row32(g, pk);
+            store_row32(p.g + at, w.n0 + col, shape.cols, pk, p.wide);
+            pack_row32(u, pk);
+            store_row32(p.u + at, w.n0 + col, shape.cols, pk, p.wide);
+          }
+          if (in) {
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              float s;
+              const float h0 =
+                  activation(__uint_as_float(g[2 * x]), p.act, &s) *
+                  __uint_as_float(u[2 * x]);
+              const float h1 =
+                  activation(__uint_as_float(g[2 * x + 1]), p.act, &s) *
+                  __uint_as_float(u[2 * x + 1]);
+              pk[x] = bf16_pack(h0, h1);
+            }
+            store_row32(p.out + at, w.n0 + col, shape.cols, pk, p.wide);
+          }
+        }
+      } else {
+        uint16_t* out = w.kind == kDx ? p.out : p.dw[w.which];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int col = hf * 128 + c * 32;
+          __syncwarp();
+          uint32_t v[32], pk[16];
+          tmem_ld32(acc + col, v);
+          tmem_wait_ld();
+          if (c == 3) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(freed);
+          }
+          pack_row32(v, pk);
+          if (in) store_row32(out + at, w.n0 + col, shape.cols, pk, p.wide);
+        }
+      }
+      __syncwarp();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  // The odd CTA's barriers have had their last arrivals once its `drain` has;
+  // after a failed wait its last loads get the time to land.
+  if (warp == 1 && lane == 0) {
+    if (rank == 1) drain_wait(&S->drain, 0, S);
+    if (S->abort) {
+      const uint64_t t0 = global_timer_ns();
+      while (global_timer_ns() - t0 < kAbortGraceNs) {
+      }
+    }
+  }
+  __syncwarp();
+  cluster_sync();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, kTmemCols);
+  }
+}
+
+// dg = dh o u o act'(g), du = dh o act(g): memory-bound, five bfloat16 tensors
+// once each, 16 bytes of each to a thread.  Float32 inside; dg and du are
+// rounded to bfloat16 because the tensor cores take them so.
+__global__ void __launch_bounds__(256) slope_kernel(FfnBwdArgs a) {
+  pdl_trigger();
+  pdl_wait();
+  const int64_t n = (int64_t)a.f.tokens * a.f.hidden / 8;
+  const int64_t step = (int64_t)gridDim.x * 256;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += step) {
+    const uint4 g = reinterpret_cast<const uint4*>(a.f.g)[i];
+    const uint4 u = reinterpret_cast<const uint4*>(a.f.u)[i];
+    const uint4 d = reinterpret_cast<const uint4*>(a.dh)[i];
+    const uint32_t gw[4] = {g.x, g.y, g.z, g.w}, uw[4] = {u.x, u.y, u.z, u.w},
+                   dw[4] = {d.x, d.y, d.z, d.w};
+    uint32_t og[4], ou[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float s0, s1;
+      const float a0 = activation(bf16_lo(gw[e]), a.f.act, &s0);
+      const float a1 = activation(bf16_hi(gw[e]), a.f.act, &s1);
+      og[e] = bf16_pack(bf16_lo(dw[e]) * bf16_lo(uw[e]) * s0,
+                        bf16_hi(dw[e]) * bf16_hi(uw[e]) * s1);
+      ou[e] = bf16_pack(bf16_lo(dw[e]) * a0, bf16_hi(dw[e]) * a1);
+    }
+    reinterpret_cast<uint4*>(a.dg)[i] = make_uint4(og[0], og[1], og[2], og[3]);
+    reinterpret_cast<uint4*>(a.du)[i] = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+  }
+}
+
+// ------------------------------------------------------------------ host
+
+// [rows, cols] bfloat16, boxes of 64 columns by `box_rows` rows.
+bool make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols,
+              int64_t row_elems, int box_rows) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (enc == nullptr) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)row_elems * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base),
+             dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+bool wide_rows(const void* p, int64_t cols) {
+  return ((uintptr_t)p & 31) == 0 && cols % 16 == 0;
+}
+
+Tiles make_tiles(int64_t rows, int64_t cols, int col_tile, int copies,
+                 int steps) {
+  Tiles t;
+  t.rows = (int32_t)rows;
+  t.cols = (int32_t)cols;
+  t.mt = up(rows, 2 * kHalf);
+  t.nt = up(cols, col_tile);
+  t.count = t.mt * t.nt * copies;
+  t.steps = steps;
+  return t;
+}
+
+template <bool kBackward>
+cudaError_t launch_pairs(PairParams& p, const FfnArgs& a, cudaStream_t stream) {
+  const int pairs = std::min(a.sms / 2, p.tile[0].count + p.tile[1].count);
+  if (kBackward) {
+    const int rest = p.tile[0].count % pairs;
+    if (rest > 0 && p.tile[0].count > 0) {
+      p.heavy = rest;
+      p.extra = p.tile[0].steps / p.tile[1].steps;
+    }
+  }
+  p.act = a.act;
+  p.status = a.status;
+  p.inject_stall = a.inject_stall;
+  p.wait_limit_ns = a.wait_limit_ns;
+  const cudaError_t e = cudaFuncSetAttribute(
+      pair_kernel<kBackward>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      kSmem);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(pair_kernel<kBackward>, dim3(2 * pairs), dim3(kThreads),
+                    kSmem, stream, p);
 }
 
 }  // namespace
 
 cudaError_t launch_ffn_fwd(const FfnArgs& a, cudaStream_t stream) {
-  Product p = {};
-  p.a[0] = p.a[1] = {a.x, a.x_row, 1};
-  p.b[0] = {a.w_gate, a.dim, 1};
-  p.b[1] = {a.w_up, a.dim, 1};
-  p.m = a.tokens;
-  p.n = a.hidden;
-  p.k = a.dim;
-  p.act = a.act;
-  p.gated = true;
-  p.c = a.h;
+  PairParams p;
+  memset(&p, 0, sizeof(p));
+  if (!make_map(&p.x, a.x, a.tokens, a.dim, a.x_row, kHalf) ||
+      !make_map(&p.w[0], a.w_gate, a.hidden, a.dim, a.dim, kHalf) ||
+      !make_map(&p.w[1], a.w_up, a.hidden, a.dim, a.dim, kHalf))
+    return cudaErrorInvalidValue;
+  p.kind[0] = p.kind[1] = kFwd;
+  p.tile[0] = make_tiles(a.tokens, a.hidden, kHalf, 1, up(a.dim, kStep));
+  p.out = a.h;
   p.g = a.g;
   p.u = a.u;
-  return launch_product(p, stream);
+  p.wide = wide_rows(a.h, a.hidden) && wide_rows(a.g, a.hidden) &&
+           wide_rows(a.u, a.hidden);
+  return launch_pairs<false>(p, a, stream);
 }
 
-cudaError_t launch_ffn_bwd(const FfnBwdArgs& a, cudaStream_t stream) {
-  slope_kernel<<<a.f.sms * 8, 256, 0, stream>>>(a);
-  Product p = {};
-  const int64_t F = a.f.hidden, D = a.f.dim;
-  p.a[0] = {a.dg, F, 1};
-  p.a[1] = {a.du, F, 1};
-  p.b[0] = {a.f.w_gate, 1, D};
-  p.b[1] = {a.f.w_up, 1, D};
-  p.m = a.f.tokens;
-  p.n = a.f.dim;
-  p.k = a.f.hidden;
-  p.c = a.dx;
-  cudaError_t e = launch_product(p, stream);
-  for (int i = 0; e == cudaSuccess && a.dw_gate && i < 2; ++i) {
-    Product w = {};
-    w.a[0] = {i ? a.du : a.dg, 1, F};
-    w.b[0] = {a.f.x, 1, a.f.x_row};
-    w.m = a.f.hidden;
-    w.n = a.f.dim;
-    w.k = a.f.tokens;
-    w.c = i ? a.dw_up : a.dw_gate;
-    e = launch_product(w, stream);
+cudaError_t launch_ffn_bwd(const FfnBwdArgs& b, cudaStream_t stream) {
+  const FfnArgs& a = b.f;
+  const int64_t n = (int64_t)a.tokens * a.hidden / 8;
+  const cudaError_t e = launch_pdl(
+      slope_kernel, dim3((unsigned)std::min<int64_t>(up(n, 256), a.sms * 8)),
+      dim3(256), 0, stream, b);
+  if (e != cudaSuccess) return e;
+  PairParams p;
+  memset(&p, 0, sizeof(p));
+  // dx reads dg and du in boxes of 128 rows, dW in boxes of 64: 64 rows twice
+  // where either could be read
+  const int kinds = b.dw_gate != nullptr ? 2 : 1;
+  if (!make_map(&p.x, a.x, a.tokens, a.dim, a.x_row, kStep) ||
+      !make_map(&p.w[0], a.w_gate, a.hidden, a.dim, a.dim, kStep) ||
+      !make_map(&p.w[1], a.w_up, a.hidden, a.dim, a.dim, kStep) ||
+      !make_map(&p.d[0], b.dg, a.tokens, a.hidden, a.hidden, kStep) ||
+      !make_map(&p.d[1], b.du, a.tokens, a.hidden, a.hidden, kStep))
+    return cudaErrorInvalidValue;
+  p.half_steps = up(a.hidden, kStep);
+  const Tiles dx =
+      make_tiles(a.tokens, a.dim, 2 * kHalf, 1, 2 * p.half_steps);
+  const Tiles dw =
+      make_tiles(a.hidden, a.dim, 2 * kHalf, 2, up(a.tokens, kStep));
+  // the tiles with the longer sums first
+  const int first = kinds == 2 && dw.steps > dx.steps ? 1 : 0;
+  p.tile[first] = dx;
+  p.kind[first] = kDx;
+  if (kinds == 2) {
+    p.tile[1 - first] = dw;
+    p.kind[1 - first] = kDw;
+  } else {
+    p.tile[1] = dx;
+    p.tile[1].count = 0;
+    p.kind[1] = kDw;
   }
-  return e;
+  p.out = b.dx;
+  p.dw[0] = b.dw_gate;
+  p.dw[1] = b.dw_up;
+  p.wide = wide_rows(b.dx, a.dim) && wide_rows(b.dw_gate, a.dim) &&
+           wide_rows(b.dw_up, a.dim);
+  return launch_pairs<true>(p, a, stream);
 }
 
 }  // namespace fastvr
