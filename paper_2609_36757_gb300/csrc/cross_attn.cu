@@ -1,65 +1,714 @@
-// Cross attention forward: one warp per query row, online softmax over the
-// keys (lanes hold the head's elements).
+// Cross attention forward on tcgen05 tensor cores: out = softmax(scale q k^T) v
+// over the first kv_len[b] of kv_tokens keys, heads in groups that share a key
+// head.
+//
+// Few keys (a prompt) and many queries: at 512 keys the tensor pipe and HBM
+// (q in, out back) bound it about alike, below that HBM does, and a unit of
+// work (two tiles of 128 queries over all keys) is short.  So the kernel is
+// persistent and its units follow one another without a gap: the schedule is
+// chunk_attn_fwd.cu's (QK_0(j), PV_0(j-1), QK_1(j), PV_1(j-1), one S tile shared
+// by both query tiles, PV one key tile behind), taken across the units' ends,
+// where the queries of the next unit come from a ring of tiles and a tile's
+// output leaves between its last PV and the next unit's first:
+//   warp 8      TMA producer of the query and the K tiles (rings)
+//   warp 10     TMA producer of the V tiles (ring)
+//   warp 11     relay: hands landed tiles to the MMA warp through named barriers
+//               and zeroes V rows past the last key (their contents, which may
+//               be NaN, would meet P = 0)
+//   warp 9      MMA issuer
+//   warps 0-3, 4-7  softmax and output of the first and second query tile
+// TMEM (512 columns): S | P_0 | P_1 | O_0 | O_1.
+//
+// Rows leave from registers in pieces of 32 bytes (whole sectors); staging them
+// for TMA stores would take the shared memory of two ring stages.
+//
+// Waits on mbarriers are bounded; past the limit every role stops.  The MMA
+// warp waits on named barriers, which have no limit: after a failure the relay
+// keeps arriving on all of them until the MMA warp has left.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <math.h>
+#include <string.h>
 
+#include <algorithm>
+
+#include "attn_softmax.cuh"
+#include "cross_attn.cuh"
 #include "fastvr_internal.h"
+#include "sm100_ptx.cuh"
 
 namespace fastvr {
 namespace {
 
+using namespace sm100;
+
+constexpr int kBM = 128;         // query rows per tile (one TMEM lane each)
+constexpr int kBN = 128;         // keys per tile
+constexpr int kThreads = 384;
+constexpr int kBox = 128 * 128;  // one TMA box: 128 rows x 64 bf16 (bytes)
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kTmemS = 0, kTmemP = 128, kTmemO = 256;
+constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr uint64_t kDefaultWaitLimitNs = 4000000000ull;
+// Named barriers of the hand-offs to the MMA warp.
+constexpr int kBarSFree = 1;
+constexpr int kBarP = 2;   // + query tile
+constexpr int kBarK = 4;   // + stage (at most 3)
+constexpr int kBarV = 7;   // + stage (at most 3)
+constexpr int kBarQ = 10;  // + stage (at most 4)
+constexpr int kBars = 14;
+constexpr int kHandoff = 5 * 32;  // four softmax warps and the MMA warp
+constexpr int kRelay = 2 * 32;
+
 template <int D>
-__global__ void __launch_bounds__(256) cross_rows_kernel(CrossArgs p) {
-  constexpr int E = D / 32;
-  const int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) / 32;
-  const int lane = threadIdx.x % 32;
-  const int64_t rows = (int64_t)p.batch * p.heads * p.q_tokens;
-  if (i >= rows) return;
-  const int t = (int)(i % p.q_tokens);
-  const int h = (int)(i / p.q_tokens % p.heads);
-  const int b = (int)(i / p.q_tokens / p.heads);
-  const int hk = h / (p.heads / p.kv_heads);
-  const int n = p.kv_len ? min(max(p.kv_len[b], 0), p.kv_tokens) : p.kv_tokens;
-  const uint16_t* q = p.q + b * p.q_str.batch + t * p.q_str.token + h * p.q_str.head;
-  const uint16_t* k = p.k + b * p.k_str.batch + hk * p.k_str.head;
-  const uint16_t* v = p.v + b * p.v_str.batch + hk * p.v_str.head;
-  float qf[E], acc[E];
-  for (int e = 0; e < E; ++e) {
-    qf[e] = bf16_lo(q[lane * E + e]);
-    acc[e] = 0.f;
+struct Layout {
+  static constexpr int kNB = D / 64;  // boxes per tile
+  static constexpr int kTile = kNB * kBox;
+  static constexpr int kQ = D == 64 ? 4 : 3;  // ring stages
+  static constexpr int kK = D == 64 ? 3 : 2;
+  static constexpr int kV = D == 64 ? 3 : 2;
+  static constexpr int k_off = kQ * kTile;
+  static constexpr int v_off = k_off + kK * kTile;
+  static constexpr int shared_off = v_off + kV * kTile;
+  static constexpr int bytes = shared_off + 1024 /*Shared*/ + 1024 /*align*/;
+};
+
+struct CrossParams {
+  CUtensorMap q_map, k_map, v_map;  // {d, tokens, heads, batch}
+  uint16_t* o;
+  float* lse;
+  Strides o_str;
+  const int32_t* kv_len;
+  int32_t batch, heads, group, q_tokens, kv_tokens;
+  int32_t q_pairs, units;
+  FastDiv by_pairs, by_heads, by_group;
+  int32_t q_batch, k_batch, v_batch;  // 0: one entry for the whole batch
+  int32_t wide;                       // output rows on 32-byte boundaries
+  float scale_log2;
+  int* status;
+  int32_t inject_stall;
+  uint64_t wait_limit_ns;
+};
+
+struct Shared {
+  uint64_t q_full[4], q_empty[4], k_full[3], k_empty[3], v_full[3], v_empty[3];
+  uint64_t s_full[2], p_free[2], drain;
+  uint32_t tmem_base;
+  int abort, mma_done;
+  uint64_t wait_limit_ns;
+};
+static_assert(sizeof(Shared) <= 1024, "Shared fits its place");
+
+// A unit: two tiles of one (b, h)'s queries (or one, at the end) over its keys.
+struct Unit {
+  int b, h, q0, len, n;  // n: key tiles
+  bool two;
+};
+__device__ __forceinline__ void get_unit(const CrossParams& p, int x, Unit* u) {
+  const uint32_t bh = fast_div(x, p.by_pairs);
+  u->q0 = (int)(x - bh * p.q_pairs) * 2 * kBM;
+  u->b = (int)fast_div(bh, p.by_heads);
+  u->h = (int)(bh - (uint32_t)u->b * p.heads);
+  u->two = p.q_tokens - u->q0 > kBM;
+  u->len = cross_keys(p.kv_len, u->b, p.kv_tokens);
+  u->n = (u->len + kBN - 1) / kBN;
+}
+// The CTA's next unit that has keys, from unit x on; false when there is none.
+__device__ __forceinline__ bool next_unit(const CrossParams& p, int& x,
+                                          Unit* u) {
+  for (; x < p.units; x += gridDim.x) {
+    get_unit(p, x, u);
+    if (u->n > 0) {
+      x += gridDim.x;
+      return true;
+    }
   }
-  float m = -INFINITY, l = 0.f;
-  for (int j = 0; j < n; ++j) {
-    float s = 0.f;
-    for (int e = 0; e < E; ++e)
-      s += qf[e] * bf16_lo(k[j * p.k_str.token + lane * E + e]);
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
-    s *= p.scale;
-    const float mn = fmaxf(m, s), a = expf(m - mn), w = expf(s - mn);
-    l = l * a + w;
-    for (int e = 0; e < E; ++e)
-      acc[e] = acc[e] * a + w * bf16_lo(v[j * p.v_str.token + lane * E + e]);
-    m = mn;
+  return false;
+}
+
+__device__ __forceinline__ bool give_up(Shared* S, uint64_t t0, int* status) {
+  if (*reinterpret_cast<volatile int*>(&S->abort)) return true;
+  if (global_timer_ns() - t0 <= S->wait_limit_ns) return false;
+  *reinterpret_cast<volatile int*>(&S->abort) = 1;
+  if (status != nullptr) atomicExch(status, kDevTimeout);
+  return true;
+}
+__device__ __forceinline__ bool wait_bar(uint64_t* bar, uint32_t parity,
+                                         Shared* S, int* status) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+  while (!mbar_try_wait(bar, parity))
+    if (give_up(S, t0, status)) return false;
+  return true;
+}
+// The whole warp's, which stays converged.
+__device__ __forceinline__ bool wait_bar_warp(uint64_t* bar, uint32_t parity,
+                                              Shared* S, int* status) {
+  if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
+  const uint64_t t0 = global_timer_ns();
+  while (!__all_sync(~0u, mbar_try_wait(bar, parity)))
+    if (__any_sync(~0u, give_up(S, t0, status))) return false;
+  return true;
+}
+// Ignores the abort flag (draining what is in flight).
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity,
+                                           const Shared* S) {
+  const uint64_t t0 = global_timer_ns();
+  while (!mbar_try_wait(bar, parity))
+    if (global_timer_ns() - t0 > S->wait_limit_ns) return;
+}
+
+__device__ __forceinline__ void handoff_arrive(int id) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kHandoff) : "memory");
+}
+__device__ __forceinline__ void handoff_sync(int id) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kHandoff) : "memory");
+}
+__device__ __forceinline__ void relay_arrive(int id) {
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kRelay) : "memory");
+}
+__device__ __forceinline__ void relay_sync(int id) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kRelay) : "memory");
+}
+
+// The first query tile, K_0, the second query tile, K_1, ...: the order in which
+// the MMA warp takes them.
+template <int D>
+__device__ void qk_producer(const CrossParams& p, uint8_t* smem, Shared* S) {
+  using L = Layout<D>;
+  // a query tile is read once, the keys of a head by every unit of it
+  const uint64_t once = l2_policy_evict_first(), keep = l2_policy_evict_last();
+  int x = blockIdx.x, qc = 0, kc = 0;
+  Unit u;
+  bool ok = true;
+  while (ok && next_unit(p, x, &u)) {
+    const int hk = (int)fast_div(u.h, p.by_group);
+    auto query = [&](int t) {
+      const int st = qc % L::kQ;
+      if (!(ok = wait_bar(&S->q_empty[st], ((qc / L::kQ) & 1) ^ 1, S,
+                          p.status)))
+        return;
+      mbar_arrive_expect_tx(&S->q_full[st], L::kTile);
+      for (int bx = 0; bx < L::kNB; ++bx)
+        tma_load_4d_hint(&p.q_map, smem + st * L::kTile + bx * kBox,
+                         &S->q_full[st], bx * 64, u.q0 + t * kBM, u.h,
+                         u.b * p.q_batch, once);
+      ++qc;
+    };
+    query(0);
+    for (int j = 0; ok && j < u.n; ++j) {
+      const int st = kc % L::kK;
+      if (!(ok = wait_bar(&S->k_empty[st], ((kc / L::kK) & 1) ^ 1, S,
+                          p.status)))
+        break;
+      mbar_arrive_expect_tx(&S->k_full[st], L::kTile);
+      for (int bx = 0; bx < L::kNB; ++bx)
+        tma_load_4d_hint(&p.k_map, smem + L::k_off + st * L::kTile + bx * kBox,
+                         &S->k_full[st], bx * 64, j * kBN, hk,
+                         u.b * p.k_batch, keep);
+      ++kc;
+      if (j == 0 && u.two) query(1);
+    }
   }
-  uint16_t* o = p.o + b * p.o_str.batch + t * p.o_str.token + h * p.o_str.head;
-  for (int e = 0; e < E; ++e)
-    o[lane * E + e] =
-        __bfloat16_as_ushort(__float2bfloat16_rn(n ? acc[e] / l : 0.f));
-  if (p.lse && lane == 0)
-    p.lse[((int64_t)b * p.heads + h) * p.q_tokens + t] =
-        n ? m + logf(l) : -INFINITY;
+  // every load has landed before the CTA exits
+  for (int i = max(0, qc - L::kQ); i < qc; ++i)
+    drain_wait(&S->q_full[i % L::kQ], (i / L::kQ) & 1, S);
+  for (int i = max(0, kc - L::kK); i < kc; ++i)
+    drain_wait(&S->k_full[i % L::kK], (i / L::kK) & 1, S);
+}
+
+template <int D>
+__device__ void v_producer(const CrossParams& p, uint8_t* smem, Shared* S) {
+  using L = Layout<D>;
+  const uint64_t keep = l2_policy_evict_last();
+  int x = blockIdx.x, vc = 0;
+  Unit u;
+  bool ok = true;
+  while (ok && next_unit(p, x, &u)) {
+    const int hk = (int)fast_div(u.h, p.by_group);
+    for (int j = 0; j < u.n; ++j) {
+      const int st = vc % L::kV;
+      if (!(ok = wait_bar(&S->v_empty[st], ((vc / L::kV) & 1) ^ 1, S,
+                          p.status)))
+        break;
+      mbar_arrive_expect_tx(&S->v_full[st], L::kTile);
+      for (int bx = 0; bx < L::kNB; ++bx)
+        tma_load_4d_hint(&p.v_map, smem + L::v_off + st * L::kTile + bx * kBox,
+                         &S->v_full[st], bx * 64, j * kBN, hk,
+                         u.b * p.v_batch, keep);
+      ++vc;
+    }
+  }
+  for (int i = max(0, vc - L::kV); i < vc; ++i)
+    drain_wait(&S->v_full[i % L::kV], (i / L::kV) & 1, S);
+}
+
+// Observes the landed tiles in the order in which the MMA warp takes them.
+template <int D>
+__device__ void relay_role(const CrossParams& p, uint8_t* smem, Shared* S,
+                           int lane) {
+  using L = Layout<D>;
+  int x = blockIdx.x, qc = 0, kc = 0, vc = 0;
+  Unit u;
+  bool ok = true, pend = false, have = next_unit(p, x, &u);
+  int j = 0, pvalid = 0;
+  auto query = [&]() {
+    const int st = qc % L::kQ;
+    if ((ok = ok && wait_bar_warp(&S->q_full[st], (qc / L::kQ) & 1, S,
+                                  p.status)))
+      relay_arrive(kBarQ + st);
+    ++qc;
+  };
+  while (ok && (have || pend)) {
+    if (have) {
+      if (j == 0) query();
+      const int st = kc % L::kK;
+      if ((ok = ok && wait_bar_warp(&S->k_full[st], (kc / L::kK) & 1, S,
+                                    p.status)))
+        relay_arrive(kBarK + st);
+      ++kc;
+    }
+    if (ok && pend) {
+      const int st = vc % L::kV;
+      if ((ok = wait_bar_warp(&S->v_full[st], (vc / L::kV) & 1, S,
+                              p.status))) {
+        // A row is 128 bytes of each box; the swizzle stays within rows.
+        if (pvalid < kBN) {
+          for (int bx = 0; bx < L::kNB; ++bx) {
+            uint4* rows = reinterpret_cast<uint4*>(smem + L::v_off +
+                                                   st * L::kTile + bx * kBox);
+            for (int i = pvalid * 8 + lane; i < kBN * 8; i += 32)
+              rows[i] = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        relay_arrive(kBarV + st);
+      }
+      ++vc;
+    }
+    if (ok && have && j == 0 && u.two) query();
+    pend = have;
+    if (have) {
+      pvalid = min(kBN, u.len - j * kBN);
+      if (++j == u.n) {
+        j = 0;
+        have = next_unit(p, x, &u);
+      }
+    }
+  }
+  // The MMA warp may still wait for arrivals that a failed role will not make.
+  volatile int* done = &S->mma_done;
+  volatile int* abort = &S->abort;
+  const uint64_t t0 = global_timer_ns();
+  while (!__any_sync(~0u, *done != 0)) {
+    if (__any_sync(~0u, *abort != 0)) {
+      for (int id = kBarSFree; id < kBarK; ++id) handoff_arrive(id);
+      for (int id = kBarK; id < kBars; ++id) relay_arrive(id);
+    }
+    if (__any_sync(~0u, global_timer_ns() - t0 > 3 * S->wait_limit_ns)) break;
+    __nanosleep(200);
+  }
+}
+
+template <int D>
+__device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
+                           uint32_t tmem) {
+  using L = Layout<D>;
+  constexpr uint32_t kIdescQK = idesc_bf16_f32(kBM, kBN, 0);
+  constexpr uint32_t kIdescPV = idesc_bf16_f32(kBM, D, 1);
+  const uint32_t sbase = smem_addr(smem);
+  const uint32_t hi = desc_hi_sw128(1024);
+  const uint32_t q_lo = desc_lo(sbase, 16);
+  const uint32_t k_lo = desc_lo(sbase + L::k_off, 16);
+  const uint32_t v_lo = desc_lo(sbase + L::v_off, kBox);
+  constexpr uint32_t kStage16 = (uint32_t)L::kTile >> 4;
+  auto qk = [&](uint32_t a0, uint32_t b0) {
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      const uint32_t off = (uint32_t)((ks / 4) * kBox + (ks % 4) * 32) >> 4;
+      mma_ss_warp(tmem + kTmemS, a0 + off, b0 + off, hi, kIdescQK, ks > 0);
+    }
+  };
+  auto pv = [&](int t, uint32_t b0, int acc) {
+#pragma unroll
+    for (int kk = 0; kk < kBN / 16; ++kk)
+      mma_ts_warp(tmem + kTmemO + t * 128, tmem + kTmemP + t * 64 + kk * 8,
+                  b0 + (uint32_t)(kk * 2048 >> 4), hi, kIdescPV,
+                  (acc | kk) != 0);
+  };
+  int s_uses = 0;
+  auto take_s = [&]() {
+    if (s_uses > 0) handoff_sync(kBarSFree);
+    ++s_uses;
+    tc_fence_after();
+  };
+  // Test hook: `drain` receives no arrival before the end, so this wait runs
+  // out and exercises the abort path.
+  bool ok = !p.inject_stall || wait_bar_warp(&S->drain, 0, S, p.status);
+  int x = blockIdx.x, qs = 0, ks = 0, vs = 0;  // ring stages
+  Unit u, nu;
+  bool have = next_unit(p, x, &u);
+  bool have_next = have && next_unit(p, x, &nu);
+  bool pend = false, ptwo = false;
+  int j = 0, q1 = 0, pacc = 0;
+  while (ok && (have || pend)) {
+    // read now, looked at when the step's MMAs have been issued
+    uint32_t aborted;
+    asm volatile("ld.volatile.shared.u32 %0, [%1];"
+                 : "=r"(aborted)
+                 : "r"(smem_addr(&S->abort)));
+    const bool last = have && j == u.n - 1;
+    if (have) {
+      if (j == 0) relay_sync(kBarQ + qs);
+      relay_sync(kBarK + ks);
+      take_s();
+      qk(q_lo + qs * kStage16, k_lo + ks * kStage16);
+      mma_commit_warp(&S->s_full[0]);
+      if (last) mma_commit_warp(&S->q_empty[qs]);
+      if (!u.two) mma_commit_warp(&S->k_empty[ks]);
+    }
+    if (pend) {
+      relay_sync(kBarV + vs);
+      handoff_sync(kBarP);
+      tc_fence_after();
+      pv(0, v_lo + vs * kStage16, pacc);
+      mma_commit_warp(&S->p_free[0]);
+      if (!ptwo) mma_commit_warp(&S->v_empty[vs]);
+    }
+    if (have && u.two) {
+      if (j == 0) {
+        q1 = qs + 1 == L::kQ ? 0 : qs + 1;
+        relay_sync(kBarQ + q1);
+      }
+      take_s();
+      qk(q_lo + q1 * kStage16, k_lo + ks * kStage16);
+      mma_commit_warp(&S->s_full[1]);
+      if (last) mma_commit_warp(&S->q_empty[q1]);
+      mma_commit_warp(&S->k_empty[ks]);
+    }
+    if (pend) {
+      if (ptwo) {
+        handoff_sync(kBarP + 1);
+        tc_fence_after();
+        pv(1, v_lo + vs * kStage16, pacc);
+        mma_commit_warp(&S->p_free[1]);
+        mma_commit_warp(&S->v_empty[vs]);
+      }
+      vs = vs + 1 == L::kV ? 0 : vs + 1;
+    }
+    pend = have;
+    if (have) {
+      ptwo = u.two;
+      pacc = j > 0;
+      ks = ks + 1 == L::kK ? 0 : ks + 1;
+      ++j;
+      if (last) {
+        const int last_q = u.two ? q1 : qs;
+        qs = last_q + 1 == L::kQ ? 0 : last_q + 1;
+        j = 0;
+        u = nu;
+        have = have_next;
+        have_next = have && next_unit(p, x, &nu);
+      }
+    }
+    if (__any_sync(~0u, aborted != 0)) ok = false;
+  }
+  mma_commit_warp(&S->drain);
+  if ((threadIdx.x & 31) == 0) {
+    drain_wait(&S->drain, 0, S);
+    *reinterpret_cast<volatile int*>(&S->mma_done) = 1;
+  }
+  __syncwarp();
+}
+
+// Row `row` of (b, h): out = O / l from TMEM (zeros without keys) and lse.
+template <int D>
+__device__ __forceinline__ void write_row(const CrossParams& p, uint32_t tO,
+                                          int b, int h, int row, float m,
+                                          float l, bool none) {
+  const bool in = row < p.q_tokens;
+  const float inv = 1.f / l;
+  uint16_t* o = p.o + (int64_t)b * p.o_str.batch +
+                (int64_t)row * p.o_str.token + (int64_t)h * p.o_str.head;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t r[32], pk[16];
+    if (!none) {
+      __syncwarp();
+      tmem_ld32(tO + c * 32, r);
+      tmem_wait_ld();
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      pk[i] = none ? 0u
+                   : pack_bf16(__uint_as_float(r[2 * i]) * inv,
+                               __uint_as_float(r[2 * i + 1]) * inv);
+    if (in) {
+      if (p.wide) {
+        store_32b(o + c * 32, pk);
+        store_32b(o + c * 32 + 16, pk + 8);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<uint4*>(o + c * 32 + 8 * i) = make_uint4(
+              pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
+      }
+    }
+  }
+  if (in && p.lse != nullptr)
+    p.lse[((int64_t)b * p.heads + h) * p.q_tokens + row] =
+        none ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
+  __syncwarp();
+}
+
+template <int D>
+__device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
+                             int t, int wq, int lane) {
+  const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+  const uint32_t tS = tmem + kTmemS + lane_off;
+  const uint32_t tP = tmem + kTmemP + t * 64 + lane_off;
+  const uint32_t tO = tmem + kTmemO + t * 128 + lane_off;
+  const float sl2 = p.scale_log2;
+  const uint64_t sl2x2 = f2_pack(sl2, sl2);
+  int tiles = 0;  // key tiles of this query tile so far: barrier phases
+  // the unit whose output is still to be written
+  bool owed = false;
+  int ob = 0, oh = 0, orow = 0;
+  float om = 0.f, ol = 0.f;
+  bool ok = true;
+  int x = blockIdx.x;
+  // last unit with keys of this CTA
+  int last_x = -1;
+  {
+    Unit u;
+    for (int y = x; y < p.units; y += gridDim.x) {
+      get_unit(p, y, &u);
+      if (u.n > 0) last_x = y;
+      if (p.kv_len == nullptr) {
+        last_x = x + (p.units - 1 - x) / (int)gridDim.x * (int)gridDim.x;
+        break;
+      }
+    }
+  }
+  for (; ok && x < p.units; x += gridDim.x) {
+    Unit u;
+    get_unit(p, x, &u);
+    if (t == 1 && !u.two) continue;
+    const int row = u.q0 + t * kBM + wq * 32 + lane;
+    if (u.n == 0) {
+      write_row<D>(p, tO, u.b, u.h, row, 0.f, 1.f, true);
+      continue;
+    }
+    float m_ref = -INFINITY, l = 0.f;
+    for (int j = 0; j < u.n; ++j) {
+      if (!(ok = wait_bar_warp(&S->s_full[t], tiles & 1, S, p.status))) break;
+      tc_fence_after();
+      uint32_t s[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, s[c]);
+      tmem_wait_ld();
+      tc_fence_before();
+      // no QK^T follows the CTA's last S
+      if (!(x == last_x && j == u.n - 1 && t == (u.two ? 1 : 0)))
+        handoff_arrive(kBarSFree);
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      const int valid = u.len - j * kBN;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) mask_max32(s[c], c, valid, mx);
+      const float mrow = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2;
+      const bool rescale =
+          __any_sync(~0u, mrow > m_ref + kRescaleThreshold);
+      float alpha = 1.f;
+      if (rescale) {
+        const float m_new = fmaxf(m_ref, mrow);
+        alpha = ex2(m_ref - m_new);
+        l *= alpha;
+        m_ref = m_new;
+      }
+      const uint64_t neg2 = f2_pack(-m_ref, -m_ref);
+      uint64_t acc[4] = {0, 0, 0, 0};
+      uint32_t pk[2][16];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) exp_pack32(s[c], sl2x2, neg2, pk[c], acc);
+      // this query tile's previous PV is done: P may be written, O is current
+      if (tiles > 0 && !(ok = wait_bar_warp(&S->p_free[t], (tiles - 1) & 1, S,
+                                            p.status)))
+        break;
+      tc_fence_after();
+      if (j == 0) {
+        if (owed) write_row<D>(p, tO, ob, oh, orow, om, ol, false);
+      } else if (rescale) {
+#pragma unroll 1
+        for (int c = 0; c < D / 8; ++c) {
+          uint32_t r[8];
+          tmem_ld8(tO + c * 8, r);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+          tmem_st8(tO + c * 8, r);
+        }
+      }
+      tmem_st16(tP, pk[0]);
+      tmem_st16(tP + 16, pk[1]);
+#pragma unroll
+      for (int c = 2; c < 4; ++c) {
+        exp_pack32(s[c], sl2x2, neg2, pk[c - 2], acc);
+        tmem_st16(tP + 16 * c, pk[c - 2]);
+      }
+      l += acc_total(acc);
+      tmem_wait_st();
+      tc_fence_before();
+      handoff_arrive(kBarP + t);
+      ++tiles;
+    }
+    owed = ok;
+    ob = u.b;
+    oh = u.h;
+    orow = row;
+    om = m_ref;
+    ol = l;
+  }
+  if (ok && owed &&
+      wait_bar_warp(&S->p_free[t], (tiles - 1) & 1, S, p.status)) {
+    tc_fence_after();
+    write_row<D>(p, tO, ob, oh, orow, om, ol, false);
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+cross_tile_kernel(const __grid_constant__ CrossParams p) {
+  using L = Layout<D>;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  Shared* S = reinterpret_cast<Shared*>(smem + L::shared_off);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (warp == 9) {
+    tmem_alloc(&S->tmem_base, kTmemCols);
+    tmem_relinquish();
+  }
+  if (threadIdx.x == 256) {
+    for (int s = 0; s < L::kQ; ++s) {
+      mbar_init(&S->q_full[s], 1);
+      mbar_init(&S->q_empty[s], 1);
+    }
+    for (int s = 0; s < L::kK; ++s) {
+      mbar_init(&S->k_full[s], 1);
+      mbar_init(&S->k_empty[s], 1);
+    }
+    for (int s = 0; s < L::kV; ++s) {
+      mbar_init(&S->v_full[s], 1);
+      mbar_init(&S->v_empty[s], 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&S->s_full[t], 1);
+      mbar_init(&S->p_free[t], 1);
+    }
+    mbar_init(&S->drain, 1);
+    S->abort = 0;
+    S->mma_done = 0;
+    S->wait_limit_ns = p.wait_limit_ns ? p.wait_limit_ns : kDefaultWaitLimitNs;
+    fence_barrier_init();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = S->tmem_base;
+  pdl_trigger();
+  pdl_wait();
+
+  if (warp == 8) {
+    if (lane == 0) qk_producer<D>(p, smem, S);
+    __syncwarp();
+  } else if (warp == 10) {
+    if (lane == 0) v_producer<D>(p, smem, S);
+    __syncwarp();
+  } else if (warp == 9) {
+    mma_issuer<D>(p, smem, S, tmem);
+  } else if (warp == 11) {
+    relay_role<D>(p, smem, S, lane);
+  } else {
+    softmax_role<D>(p, S, tmem, warp / 4, warp % 4, lane);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+template <int D>
+cudaError_t launch_tiles(const CrossArgs& a, cudaStream_t stream) {
+  CrossParams p;
+  memset(&p, 0, sizeof(p));
+  if (!cross_map(&p.q_map, a.q, D, a.q_tokens, a.heads, a.batch, a.q_str,
+                 &p.q_batch) ||
+      !cross_map(&p.k_map, a.k, D, a.kv_tokens, a.kv_heads, a.batch, a.k_str,
+                 &p.k_batch) ||
+      !cross_map(&p.v_map, a.v, D, a.kv_tokens, a.kv_heads, a.batch, a.v_str,
+                 &p.v_batch))
+    return cudaErrorInvalidValue;
+  p.o = a.o;
+  p.lse = a.lse;
+  p.o_str = a.o_str;
+  p.kv_len = a.kv_len;
+  p.batch = a.batch;
+  p.heads = a.heads;
+  p.group = a.heads / a.kv_heads;
+  p.q_tokens = a.q_tokens;
+  p.kv_tokens = a.kv_tokens;
+  p.q_pairs = (a.q_tokens + 2 * kBM - 1) / (2 * kBM);
+  p.units = p.q_pairs * a.heads * a.batch;
+  p.by_pairs = make_div((uint32_t)p.q_pairs);
+  p.by_heads = make_div((uint32_t)a.heads);
+  p.by_group = make_div((uint32_t)p.group);
+  p.wide = ((uintptr_t)a.o & 31) == 0 && a.o_str.batch % 16 == 0 &&
+           a.o_str.token % 16 == 0 && a.o_str.head % 16 == 0;
+  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.status = a.status;
+  p.inject_stall = a.inject_stall;
+  p.wait_limit_ns = a.wait_limit_ns;
+  const int smem = Layout<D>::bytes;
+  static_assert(Layout<D>::bytes <= 227 * 1024, "shared memory");
+  const cudaError_t e = cudaFuncSetAttribute(
+      cross_tile_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(cross_tile_kernel<D>, dim3(std::min(p.units, a.sms)),
+                    dim3(kThreads), smem, stream, p);
 }
 
 }  // namespace
 
+// A [batch, tokens, heads, d] tensor as a map over (d, token, head, batch), box
+// 64 x 128.  The stride of a dimension of one entry does not matter; a batch
+// stride of 0 becomes a batch of one, *batch_step 0.
+bool cross_map(CUtensorMap* m, const void* base, int d, int tokens, int heads,
+               int batch, const Strides& str, int32_t* batch_step) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (enc == nullptr) return false;
+  *batch_step = batch > 1 && str.batch > 0;
+  const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)tokens,
+                              (cuuint64_t)heads,
+                              (cuuint64_t)(*batch_step ? batch : 1)};
+  const int64_t given[3] = {str.token, str.head, str.batch};
+  cuuint64_t strides[3];
+  for (int i = 0; i < 3; ++i)
+    strides[i] = (cuuint64_t)(dims[i + 1] > 1 ? given[i] : d) * 2;
+  const cuuint32_t box[4] = {64, 128, 1, 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base),
+             dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 cudaError_t launch_cross_attn(const CrossArgs& a, cudaStream_t stream) {
-  const int64_t rows = (int64_t)a.batch * a.heads * a.q_tokens;
-  const unsigned grid = (unsigned)((rows + 7) / 8);
-  if (a.head_dim == 64)
-    cross_rows_kernel<64><<<grid, 256, 0, stream>>>(a);
-  else
-    cross_rows_kernel<128><<<grid, 256, 0, stream>>>(a);
-  return cudaGetLastError();
+  return a.head_dim == 64 ? launch_tiles<64>(a, stream)
+                          : launch_tiles<128>(a, stream);
 }
 
 }  // namespace fastvr

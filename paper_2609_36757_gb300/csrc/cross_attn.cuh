@@ -1,0 +1,22 @@
+// What the cross attention kernels share.
+#pragma once
+
+#include <cuda.h>
+#include <stdint.h>
+
+#include "fastvr_internal.h"
+
+namespace fastvr {
+
+bool cross_map(CUtensorMap* m, const void* base, int d, int tokens, int heads,
+               int batch, const Strides& str, int32_t* batch_step);
+
+#ifdef __CUDACC__
+// Keys that batch entry b sees.
+__device__ __forceinline__ int cross_keys(const int32_t* kv_len, int b,
+                                          int kv_tokens) {
+  return kv_len == nullptr ? kv_tokens : min(max(kv_len[b], 0), kv_tokens);
+}
+#endif
+
+}  // namespace fastvr
