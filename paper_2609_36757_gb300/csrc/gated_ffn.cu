@@ -45,23 +45,32 @@ constexpr int kGroupTiles = 8;  // row tiles that share their columns' tiles
 
 // act(g) and its derivative in float32.  tanh's form is written with the
 // logistic function, (1 + tanh y) / 2 = 1 / (1 + exp(-2 y)), which keeps its
-// relative accuracy where g is far below 0.
+// relative accuracy where g is far below 0.  The approximate exponential and
+// reciprocal are off by a few units of 2^-24 (more for an exponential's large
+// argument, where the logistic function is 0 or 1), far below bfloat16's 2^-9.
 __device__ __forceinline__ float logistic(float y) {
-  return 1.f / (1.f + __expf(-y));
+  return __fdividef(1.f, 1.f + __expf(-y));
 }
-__device__ __forceinline__ float activation(float g, int act, float* slope) {
-  if (act == kActSilu) {
+template <int kAct>
+__device__ __forceinline__ float activation(float g) {
+  if (kAct == kActSilu) return g * logistic(g);
+  if (kAct == kActGelu) return 0.5f * g * (1.f + erff(g * 0.70710678f));
+  // 2 sqrt(2 / pi) and its product with 0.044715
+  return g * logistic(g * (1.5957691f + 0.071354816f * g * g));
+}
+template <int kAct>
+__device__ __forceinline__ float activation(float g, float* slope) {
+  if (kAct == kActSilu) {
     const float s = logistic(g);
     *slope = s * (1.f + g * (1.f - s));
     return g * s;
   }
-  if (act == kActGelu) {
+  if (kAct == kActGelu) {
     const float c = 0.5f * (1.f + erff(g * 0.70710678f));
     *slope = c + g * 0.39894228f * __expf(-0.5f * g * g);
     return g * c;
   }
-  // 2 sqrt(2 / pi) and its product with 0.044715; s (1 - s) is 0 past +-30,
-  // where the other factor could overflow
+  // s (1 - s) is 0 past +-30, where the other factor could overflow
   const float s = logistic(g * (1.5957691f + 0.071354816f * g * g));
   const float b = fminf(fmaxf(g, -30.f), 30.f);
   *slope = s + b * s * (1.f - s) * (1.5957691f + 0.21406445f * b * b);
@@ -77,15 +86,15 @@ struct Tiles {
 
 struct PairParams {
   CUtensorMap x, w[2], d[2];  // x; gate and up weights; dg and du
+  // results: forward h, g, u; backward dx, dWg, dWu
+  CUtensorMap out[3];
   Tiles tile[2];              // forward: [0]; backward: those listed first, and
   int32_t kind[2];            // the others
   // Backward: pairs from `heavy` on (0: none) have one tile fewer of the first
   // list and take `extra` of the second list before its common rounds.
   int32_t heavy, extra;
-  uint16_t *out, *out2, *g, *u;  // forward: h, g, u; backward: dx, dWg, dWu
-  uint16_t* dw[2];
-  int32_t act, half_steps;  // dx: steps of dg Wg
-  int32_t wide;             // rows of results start on 32-byte boundaries
+  int32_t half_steps;       // dx: steps of dg Wg
+  int32_t save;             // forward: g and u are wanted
   int* status;
   int32_t inject_stall;
   uint64_t wait_limit_ns;
@@ -98,7 +107,11 @@ struct Shared {
   int abort;
   uint64_t wait_limit_ns;
 };
-constexpr int kSharedBytes = kStages * 2 * kOperand;
+// Results on their way out: a box of 128 rows by 64 columns for each half of the
+// storing warps.
+constexpr int kBoxBytes = kHalf * 128;
+constexpr int kStaging = kStages * 2 * kOperand;
+constexpr int kSharedBytes = kStaging + 2 * kBoxBytes;
 constexpr int kSmem = kSharedBytes + (int)sizeof(Shared) + 1024;
 
 __device__ __forceinline__ bool give_up(Shared* S, uint64_t t0, int* status) {
@@ -171,20 +184,32 @@ __host__ __device__ inline bool nth_tile(const PairParams& p, int pair,
   return true;
 }
 
-// 32 results of a row as bfloat16 from column c on.
-__device__ __forceinline__ void store_row32(uint16_t* row, int c, int cols,
-                                            const uint32_t (&pk)[16],
-                                            bool wide) {
-  if (wide) {
+// 32 results of row r, from column c of its box on, as bfloat16 into the box
+// (128-byte rows, 16-byte piece k at k ^ (r % 8)).
+__device__ __forceinline__ void stage_row32(uint8_t* box, int r, int c,
+                                            const uint32_t (&pk)[16]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (c + 16 * i < cols) store_32b(row + c + 16 * i, pk + 8 * i);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (c + 8 * i < cols)
-        *reinterpret_cast<uint4*>(row + c + 8 * i) =
-            make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
+  for (int q = 0; q < 4; ++q)
+    *reinterpret_cast<uint4*>(box + r * 128 + (((c / 8 + q) ^ (r & 7)) << 4)) =
+        make_uint4(pk[4 * q], pk[4 * q + 1], pk[4 * q + 2], pk[4 * q + 3]);
+}
+// The four warps that share a box (named barrier 1 + half).
+__device__ __forceinline__ void box_sync(int hf) {
+  asm volatile("bar.sync %0, 128;" ::"r"(1 + hf) : "memory");
+}
+// The box may be written again / goes out to (col, row) of a map.
+__device__ __forceinline__ void box_begin(int hf, bool leader) {
+  if (leader) bulk_wait_read0();
+  box_sync(hf);
+}
+__device__ __forceinline__ void box_end(const CUtensorMap* map, uint8_t* box,
+                                        int hf, bool leader, int col, int row,
+                                        const Tiles& shape) {
+  fence_proxy_async_smem();
+  box_sync(hf);
+  if (leader && col < shape.cols && row < shape.rows) {
+    tma_store_2d(map, box, col, row);
+    bulk_commit_group();
   }
 }
 
@@ -195,9 +220,11 @@ __device__ __forceinline__ void pack_row32(const uint32_t (&v)[32],
     pk[i] = bf16_pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
 }
 
-template <bool kBackward>
+// kAct: the forward's activation; -1: backward.
+template <int kAct>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 pair_kernel(const __grid_constant__ PairParams p) {
+  constexpr bool kBackward = kAct < 0;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -280,7 +307,10 @@ pair_kernel(const __grid_constant__ PairParams p) {
       // runs out and exercises the abort path.
       bool ok = !p.inject_stall || wait_bar_warp(&S->drain, 0, S, p.status);
       int it = 0;
-      for (int i = 0; ok && nth_tile(p, pair, pairs, i, &w); ++i) {
+      Work next;
+      bool have = nth_tile(p, pair, pairs, 0, &next);
+      for (int i = 0; ok && have; ++i) {
+        w = next;
         const int buf = i & 1;
         if (!(ok = wait_bar_warp(&S->acc_empty[buf], ((i >> 1) & 1) ^ 1, S,
                                  p.status)))
@@ -310,6 +340,8 @@ pair_kernel(const __grid_constant__ PairParams p) {
             mma_ss_pair_warp(tmem + buf * 256, a_lo + k * a_step, hi,
                              b_lo + k * b_step, hi, idesc, (s | k) != 0);
           mma_commit_pair_warp(&S->empty[st]);
+          // found while the first step's products run
+          if (s == 0) have = nth_tile(p, pair, pairs, i + 1, &next);
         }
         if (ok) mma_commit_pair_warp(&S->acc_full[buf]);
       }
@@ -319,72 +351,78 @@ pair_kernel(const __grid_constant__ PairParams p) {
     }
   } else if (warp >= 4) {
     const int quarter = warp % 4, hf = (warp - 4) / 4;
+    const int r = quarter * 32 + lane;
+    const bool leader = r == 0;
+    uint8_t* box = smem + kStaging + hf * kBoxBytes;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     for (int i = 0; nth_tile(p, pair, pairs, i, &w); ++i) {
       const int buf = i & 1;
       if (!wait_bar_warp(&S->acc_full[buf], (i >> 1) & 1, S, p.status)) break;
       tc_fence_after();
       const Tiles& shape = p.tile[kBackward && w.kind != p.kind[0]];
-      const int row = w.m0 + rank * kHalf + quarter * 32 + lane;
-      const bool in = row < shape.rows;
+      const int row = w.m0 + rank * kHalf;
       const uint32_t acc = tmem + buf * 256 + lanes;
       const uint32_t freed = cluster_addr(&S->acc_empty[buf], 0);
-      const int64_t at = (int64_t)row * shape.cols;
+      uint32_t pk[16];
       if (!kBackward) {
+        // h, then g and u where they are kept
+        const int rounds = p.save ? 3 : 1;
+        const int col = w.n0 + hf * 64;
+        for (int x = 0; x < rounds; ++x) {
+          box_begin(hf, leader);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int col = hf * 64 + c * 32;
-          __syncwarp();
-          uint32_t g[32], u[32], pk[16];
-          tmem_ld32(acc + col, g);
-          tmem_ld32(acc + 128 + col, u);
-          tmem_wait_ld();
-          if (c == 1) {
+          for (int c = 0; c < 64; c += 32) {
+            uint32_t g[32], u[32];
+            if (x != 2) tmem_ld32(acc + hf * 64 + c, g);
+            if (x != 1) tmem_ld32(acc + 128 + hf * 64 + c, u);
+            tmem_wait_ld();
+            if (x == 0) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                pk[e] = bf16_pack(activation<kAct>(__uint_as_float(g[2 * e])) *
+                                      __uint_as_float(u[2 * e]),
+                                  activation<kAct>(__uint_as_float(g[2 * e + 1])) *
+                                      __uint_as_float(u[2 * e + 1]));
+              }
+            } else if (x == 1) {
+              pack_row32(g, pk);
+            } else {
+              pack_row32(u, pk);
+            }
+            stage_row32(box, r, c, pk);
+          }
+          if (x == rounds - 1) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(freed);
           }
-          if (p.g != nullptr && in) {
-            pack_row32(g, pk);
-            store_row32(p.g + at, w.n0 + col, shape.cols, pk, p.wide);
-            pack_row32(u, pk);
-            store_row32(p.u + at, w.n0 + col, shape.cols, pk, p.wide);
-          }
-          if (in) {
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              float s;
-              const float h0 =
-                  activation(__uint_as_float(g[2 * x]), p.act, &s) *
-                  __uint_as_float(u[2 * x]);
-              const float h1 =
-                  activation(__uint_as_float(g[2 * x + 1]), p.act, &s) *
-                  __uint_as_float(u[2 * x + 1]);
-              pk[x] = bf16_pack(h0, h1);
-            }
-            store_row32(p.out + at, w.n0 + col, shape.cols, pk, p.wide);
-          }
+          box_end(&p.out[x], box, hf, leader, col, row, shape);
         }
       } else {
-        uint16_t* out = w.kind == kDx ? p.out : p.dw[w.which];
+        const CUtensorMap* map = &p.out[w.kind == kDx ? 0 : 1 + w.which];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int col = hf * 128 + c * 32;
-          __syncwarp();
-          uint32_t v[32], pk[16];
-          tmem_ld32(acc + col, v);
-          tmem_wait_ld();
-          if (c == 3) {
+        for (int x = 0; x < 2; ++x) {
+          const int col = hf * 128 + x * 64;
+          box_begin(hf, leader);
+#pragma unroll
+          for (int c = 0; c < 64; c += 32) {
+            uint32_t v[32];
+            tmem_ld32(acc + col + c, v);
+            tmem_wait_ld();
+            pack_row32(v, pk);
+            stage_row32(box, r, c, pk);
+          }
+          if (x == 1) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(freed);
           }
-          pack_row32(v, pk);
-          if (in) store_row32(out + at, w.n0 + col, shape.cols, pk, p.wide);
+          box_end(map, box, hf, leader, w.n0 + col, row, shape);
         }
       }
-      __syncwarp();
     }
+    if (leader) bulk_wait_group0();
+    __syncwarp();
   }
   tc_fence_before();
   __syncthreads();
@@ -409,6 +447,7 @@ pair_kernel(const __grid_constant__ PairParams p) {
 // dg = dh o u o act'(g), du = dh o act(g): memory-bound, five bfloat16 tensors
 // once each, 16 bytes of each to a thread.  Float32 inside; dg and du are
 // rounded to bfloat16 because the tensor cores take them so.
+template <int kAct>
 __global__ void __launch_bounds__(256) slope_kernel(FfnBwdArgs a) {
   pdl_trigger();
   pdl_wait();
@@ -424,8 +463,8 @@ __global__ void __launch_bounds__(256) slope_kernel(FfnBwdArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float s0, s1;
-      const float a0 = activation(bf16_lo(gw[e]), a.f.act, &s0);
-      const float a1 = activation(bf16_hi(gw[e]), a.f.act, &s1);
+      const float a0 = activation<kAct>(bf16_lo(gw[e]), &s0);
+      const float a1 = activation<kAct>(bf16_hi(gw[e]), &s1);
       og[e] = bf16_pack(bf16_lo(dw[e]) * bf16_lo(uw[e]) * s0,
                         bf16_hi(dw[e]) * bf16_hi(uw[e]) * s1);
       ou[e] = bf16_pack(bf16_lo(dw[e]) * a0, bf16_hi(dw[e]) * a1);
@@ -454,10 +493,6 @@ bool make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols,
 
 int up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-bool wide_rows(const void* p, int64_t cols) {
-  return ((uintptr_t)p & 31) == 0 && cols % 16 == 0;
-}
-
 Tiles make_tiles(int64_t rows, int64_t cols, int col_tile, int copies,
                  int steps) {
   Tiles t;
@@ -470,25 +505,24 @@ Tiles make_tiles(int64_t rows, int64_t cols, int col_tile, int copies,
   return t;
 }
 
-template <bool kBackward>
+template <int kAct>
 cudaError_t launch_pairs(PairParams& p, const FfnArgs& a, cudaStream_t stream) {
   const int pairs = std::min(a.sms / 2, p.tile[0].count + p.tile[1].count);
-  if (kBackward) {
+  if (kAct < 0) {
     const int rest = p.tile[0].count % pairs;
     if (rest > 0 && p.tile[0].count > 0) {
       p.heavy = rest;
       p.extra = p.tile[0].steps / p.tile[1].steps;
     }
   }
-  p.act = a.act;
   p.status = a.status;
   p.inject_stall = a.inject_stall;
   p.wait_limit_ns = a.wait_limit_ns;
   const cudaError_t e = cudaFuncSetAttribute(
-      pair_kernel<kBackward>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      pair_kernel<kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize,
       kSmem);
   if (e != cudaSuccess) return e;
-  return launch_pdl(pair_kernel<kBackward>, dim3(2 * pairs), dim3(kThreads),
+  return launch_pdl(pair_kernel<kAct>, dim3(2 * pairs), dim3(kThreads),
                     kSmem, stream, p);
 }
 
@@ -503,19 +537,24 @@ cudaError_t launch_ffn_fwd(const FfnArgs& a, cudaStream_t stream) {
     return cudaErrorInvalidValue;
   p.kind[0] = p.kind[1] = kFwd;
   p.tile[0] = make_tiles(a.tokens, a.hidden, kHalf, 1, up(a.dim, kStep));
-  p.out = a.h;
-  p.g = a.g;
-  p.u = a.u;
-  p.wide = wide_rows(a.h, a.hidden) && wide_rows(a.g, a.hidden) &&
-           wide_rows(a.u, a.hidden);
-  return launch_pairs<false>(p, a, stream);
+  uint16_t* out[3] = {a.h, a.g, a.u};
+  p.save = a.g != nullptr;
+  for (int i = 0; i < (p.save ? 3 : 1); ++i)
+    if (!make_map(&p.out[i], out[i], a.tokens, a.hidden, a.hidden, kHalf))
+      return cudaErrorInvalidValue;
+  return a.act == kActSilu   ? launch_pairs<kActSilu>(p, a, stream)
+         : a.act == kActGelu ? launch_pairs<kActGelu>(p, a, stream)
+                             : launch_pairs<kActGeluTanh>(p, a, stream);
 }
 
 cudaError_t launch_ffn_bwd(const FfnBwdArgs& b, cudaStream_t stream) {
   const FfnArgs& a = b.f;
   const int64_t n = (int64_t)a.tokens * a.hidden / 8;
+  const auto slope = a.act == kActSilu   ? slope_kernel<kActSilu>
+                     : a.act == kActGelu ? slope_kernel<kActGelu>
+                                         : slope_kernel<kActGeluTanh>;
   const cudaError_t e = launch_pdl(
-      slope_kernel, dim3((unsigned)std::min<int64_t>(up(n, 256), a.sms * 8)),
+      slope, dim3((unsigned)std::min<int64_t>(up(n, 256), a.sms * 8)),
       dim3(256), 0, stream, b);
   if (e != cudaSuccess) return e;
   PairParams p;
@@ -546,12 +585,12 @@ cudaError_t launch_ffn_bwd(const FfnBwdArgs& b, cudaStream_t stream) {
     p.tile[1].count = 0;
     p.kind[1] = kDw;
   }
-  p.out = b.dx;
-  p.dw[0] = b.dw_gate;
-  p.dw[1] = b.dw_up;
-  p.wide = wide_rows(b.dx, a.dim) && wide_rows(b.dw_gate, a.dim) &&
-           wide_rows(b.dw_up, a.dim);
-  return launch_pairs<true>(p, a, stream);
+  if (!make_map(&p.out[0], b.dx, a.tokens, a.dim, a.dim, kHalf) ||
+      (kinds == 2 &&
+       (!make_map(&p.out[1], b.dw_gate, a.hidden, a.dim, a.dim, kHalf) ||
+        !make_map(&p.out[2], b.dw_up, a.hidden, a.dim, a.dim, kHalf))))
+    return cudaErrorInvalidValue;
+  return launch_pairs<-1>(p, a, stream);
 }
 
 }  // namespace fastvr
