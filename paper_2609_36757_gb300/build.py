@@ -30,7 +30,8 @@ SOURCES = ["fastvr_host.cpp", "block_host.cpp", "kv_append.cu",
            "chunk_attn_static.cu", "one_step.cu", "chunk_attn_bwd.cu",
            "rotary.cu", "block_norm_fwd.cu", "block_norm_bwd.cu",
            "q4_cache.cu", "q4_attn.cu", "cond_host.cpp", "cross_attn.cu",
-           "cross_attn_bwd.cu", "gated_ffn.cu"]
+           "cross_attn_rows.cu", "cross_attn_bwd.cu", "gated_ffn.cu",
+           "gated_ffn_rows.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC",
          "-Xcompiler", "-fvisibility=hidden", "-I", INCLUDE, "-I", CSRC]

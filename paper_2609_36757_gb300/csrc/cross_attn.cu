@@ -522,11 +522,13 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
       float alpha = 1.f;
       if (rescale) {
         const float m_new = fmaxf(m_ref, mrow);
-        alpha = ex2(m_ref - m_new);
+        alpha = m_ref == -INFINITY ? 0.f : ex2(m_ref - m_new);
         l *= alpha;
         m_ref = m_new;
       }
-      const uint64_t neg2 = f2_pack(-m_ref, -m_ref);
+      // a row whose scores are all -infinity so far exponentiates against 0
+      const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
+      const uint64_t neg2 = f2_pack(neg, neg);
       uint64_t acc[4] = {0, 0, 0, 0};
       uint32_t pk[2][16];
 #pragma unroll
@@ -707,6 +709,8 @@ bool cross_map(CUtensorMap* m, const void* base, int d, int tokens, int heads,
 }
 
 cudaError_t launch_cross_attn(const CrossArgs& a, cudaStream_t stream) {
+  if (cross_few_rows((int64_t)a.q_tokens * (a.heads / a.kv_heads)))
+    return launch_cross_rows(a, stream);
   return a.head_dim == 64 ? launch_tiles<64>(a, stream)
                           : launch_tiles<128>(a, stream);
 }

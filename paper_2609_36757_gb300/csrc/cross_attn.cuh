@@ -11,6 +11,11 @@ namespace fastvr {
 bool cross_map(CUtensorMap* m, const void* base, int d, int tokens, int heads,
                int batch, const Strides& str, int32_t* batch_step);
 
+// The kernel for few query rows (cross_attn_rows.cu).
+constexpr int kCrossRows = 16;  // rows of a block: tokens times shared heads
+inline bool cross_few_rows(int64_t rows) { return rows <= 2 * kCrossRows; }
+cudaError_t launch_cross_rows(const CrossArgs& a, cudaStream_t stream);
+
 #ifdef __CUDACC__
 // Keys that batch entry b sees.
 __device__ __forceinline__ int cross_keys(const int32_t* kv_len, int b,

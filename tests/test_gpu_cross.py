@@ -34,6 +34,10 @@ CASES = [
     (16, 1, 513, 4, 1, 64, list(range(0, 528, 33))),
     (1, 5, 1030, 16, 2, 128, None),
     (2, 4, 129, 6, 3, 64, [128, 129]),
+    (1, 2, 1030, 16, 2, 128, None),
+    (1, 1, 2000, 2, 1, 64, None),
+    (2, 3, 700, 12, 2, 128, [700, 5]),
+    (1, 32, 260, 1, 1, 64, None),
     (1, 17, 40, 2, 1, 128, None),
     (2, 127, 128, 3, 3, 128, [1, 128]),
     (1, 128, 129, 2, 2, 64, None),
