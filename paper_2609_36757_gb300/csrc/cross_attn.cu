@@ -19,8 +19,10 @@
 //   warps 0-3, 4-7  softmax and output of the first and second query tile
 // TMEM (512 columns): S | P_0 | P_1 | O_0 | O_1.
 //
-// Rows leave from registers in pieces of 32 bytes (whole sectors); staging them
-// for TMA stores would take the shared memory of two ring stages.
+// What bounds a step is the data path of shared memory: the operands of the MMAs
+// and the tiles' way in take 128 bytes of it per clock, all that there is, and
+// every poll of a barrier or piece of an output row waits its turn.  With entries
+// of different lengths CTAs take ranges of query tiles of about equal work.
 //
 // Waits on mbarriers are bounded; past the limit every role stops.  The MMA
 // warp waits on named barriers, which have no limit: after a failure the relay
@@ -80,8 +82,10 @@ struct CrossParams {
   Strides o_str;
   const int32_t* kv_len;
   int32_t batch, heads, group, q_tokens, kv_tokens;
-  int32_t q_pairs, units;
-  FastDiv by_pairs, by_heads, by_group;
+  int32_t q_tiles;          // of a head
+  int32_t per_slot, slots;  // query tiles of a slot (1 or 2), slots of a head
+  int32_t all, step;        // slots of all heads; from a CTA's slot to its next
+  FastDiv by_slots, by_heads, by_group;
   int32_t q_batch, k_batch, v_batch;  // 0: one entry for the whole batch
   int32_t wide;                       // output rows on 32-byte boundaries
   float scale_log2;
@@ -95,35 +99,76 @@ struct Shared {
   uint64_t s_full[2], p_free[2], drain;
   uint32_t tmem_base;
   int abort, mma_done;
+  int first, last;  // the CTA's slots: first, first + step, ... below last
   uint64_t wait_limit_ns;
 };
 static_assert(sizeof(Shared) <= 1024, "Shared fits its place");
 
-// A unit: two tiles of one (b, h)'s queries (or one, at the end) over its keys.
+// A unit: two tiles of one (b, h)'s queries (or one, at an end) over its keys.
 struct Unit {
   int b, h, q0, len, n;  // n: key tiles
   bool two;
 };
-__device__ __forceinline__ void get_unit(const CrossParams& p, int x, Unit* u) {
-  const uint32_t bh = fast_div(x, p.by_pairs);
-  u->q0 = (int)(x - bh * p.q_pairs) * 2 * kBM;
+// The unit at slot x; returns the slot behind it.  Slots are pairs of query
+// tiles, or single ones, two neighbours of a CTA then making a unit.
+__device__ __forceinline__ int get_unit(const CrossParams& p, int x, int last,
+                                        Unit* u) {
+  const uint32_t bh = fast_div(x, p.by_slots);
+  const int t = (int)(x - bh * p.slots) * p.per_slot;
+  u->q0 = t * kBM;
   u->b = (int)fast_div(bh, p.by_heads);
   u->h = (int)(bh - (uint32_t)u->b * p.heads);
-  u->two = p.q_tokens - u->q0 > kBM;
+  u->two = t + 1 < p.q_tiles && (p.per_slot == 2 || x + 1 < last);
   u->len = cross_keys(p.kv_len, u->b, p.kv_tokens);
   u->n = (u->len + kBN - 1) / kBN;
+  return x + (p.per_slot == 1 ? 1 + (int)u->two : p.step);
 }
-// The CTA's next unit that has keys, from unit x on; false when there is none.
-__device__ __forceinline__ bool next_unit(const CrossParams& p, int& x,
+// The CTA's next unit that has keys, from x on; false when there is none.
+__device__ __forceinline__ bool next_unit(const CrossParams& p, int& x, int last,
                                           Unit* u) {
-  for (; x < p.units; x += gridDim.x) {
-    get_unit(p, x, u);
-    if (u->n > 0) {
-      x += gridDim.x;
-      return true;
-    }
+  while (x < last) {
+    x = get_unit(p, x, last, u);
+    if (u->n > 0) return true;
   }
   return false;
+}
+// First slot of CTA c: of about equal work to each, a slot weighing its key tiles
+// and one more for its way in and out.  A whole warp's.
+__device__ __forceinline__ int first_slot(const CrossParams& p, int c,
+                                          int lane) {
+  if (p.step > 1) return c;
+  if (p.kv_len == nullptr || c == (int)gridDim.x)
+    return (int)((int64_t)p.all * c / gridDim.x);
+  const int per = p.heads * p.slots;  // of a batch entry
+  const int chunk = (p.batch + 31) / 32;
+  const int b0 = min(lane * chunk, p.batch), b1 = min(b0 + chunk, p.batch);
+  auto weight = [&](int b) {
+    return 1 + (cross_keys(p.kv_len, b, p.kv_tokens) + kBN - 1) / kBN;
+  };
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += weight(b);
+  int64_t before = mine;  // of the lanes before this one, and of all
+  for (int d = 1; d < 32; d *= 2) {
+    const int64_t x = __shfl_up_sync(~0u, before, d);
+    if (lane >= d) before += x;
+  }
+  const int64_t total = __shfl_sync(~0u, before, 31);
+  before -= mine;
+  // in units of a batch entry's tiles: position total * c / grid
+  const int64_t num = total * c;  // / gridDim.x
+  int found = -1;
+  int64_t at = before * gridDim.x;
+  for (int b = b0; b < b1 && found < 0; ++b) {
+    const int64_t w = (int64_t)weight(b) * gridDim.x;
+    if (num < at + w)
+      found = num >= at ? b * per + (int)((double)(num - at) / (double)w * per)
+                        : -2;
+    at += w;
+  }
+  found = max(found, 0);
+  for (int d = 16; d > 0; d /= 2)
+    found = max(found, __shfl_xor_sync(~0u, found, d));
+  return min(found, p.all);
 }
 
 __device__ __forceinline__ bool give_up(Shared* S, uint64_t t0, int* status) {
@@ -178,10 +223,11 @@ __device__ void qk_producer(const CrossParams& p, uint8_t* smem, Shared* S) {
   using L = Layout<D>;
   // a query tile is read once, the keys of a head by every unit of it
   const uint64_t once = l2_policy_evict_first(), keep = l2_policy_evict_last();
-  int x = blockIdx.x, qc = 0, kc = 0;
+  const int end = S->last;
+  int x = S->first, qc = 0, kc = 0;
   Unit u;
   bool ok = true;
-  while (ok && next_unit(p, x, &u)) {
+  while (ok && next_unit(p, x, end, &u)) {
     const int hk = (int)fast_div(u.h, p.by_group);
     auto query = [&](int t) {
       const int st = qc % L::kQ;
@@ -195,6 +241,17 @@ __device__ void qk_producer(const CrossParams& p, uint8_t* smem, Shared* S) {
                          u.b * p.q_batch, once);
       ++qc;
     };
+    // The ring holds no more than the unit at hand: the queries of the next one
+    // are asked for in L2 now.
+    {
+      int y = x;
+      Unit v;
+      if (next_unit(p, y, end, &v))
+        for (int t = 0; t <= (int)v.two; ++t)
+          for (int bx = 0; bx < L::kNB; ++bx)
+            tma_prefetch_4d(&p.q_map, bx * 64, v.q0 + t * kBM, v.h,
+                            v.b * p.q_batch);
+    }
     query(0);
     for (int j = 0; ok && j < u.n; ++j) {
       const int st = kc % L::kK;
@@ -221,10 +278,11 @@ template <int D>
 __device__ void v_producer(const CrossParams& p, uint8_t* smem, Shared* S) {
   using L = Layout<D>;
   const uint64_t keep = l2_policy_evict_last();
-  int x = blockIdx.x, vc = 0;
+  const int end = S->last;
+  int x = S->first, vc = 0;
   Unit u;
   bool ok = true;
-  while (ok && next_unit(p, x, &u)) {
+  while (ok && next_unit(p, x, end, &u)) {
     const int hk = (int)fast_div(u.h, p.by_group);
     for (int j = 0; j < u.n; ++j) {
       const int st = vc % L::kV;
@@ -248,9 +306,10 @@ template <int D>
 __device__ void relay_role(const CrossParams& p, uint8_t* smem, Shared* S,
                            int lane) {
   using L = Layout<D>;
-  int x = blockIdx.x, qc = 0, kc = 0, vc = 0;
+  const int end = S->last;
+  int x = S->first, qc = 0, kc = 0, vc = 0;
   Unit u;
-  bool ok = true, pend = false, have = next_unit(p, x, &u);
+  bool ok = true, pend = false, have = next_unit(p, x, end, &u);
   int j = 0, pvalid = 0;
   auto query = [&]() {
     const int st = qc % L::kQ;
@@ -293,7 +352,7 @@ __device__ void relay_role(const CrossParams& p, uint8_t* smem, Shared* S,
       pvalid = min(kBN, u.len - j * kBN);
       if (++j == u.n) {
         j = 0;
-        have = next_unit(p, x, &u);
+        have = next_unit(p, x, end, &u);
       }
     }
   }
@@ -309,6 +368,14 @@ __device__ void relay_role(const CrossParams& p, uint8_t* smem, Shared* S,
     if (__any_sync(~0u, global_timer_ns() - t0 > 3 * S->wait_limit_ns)) break;
     __nanosleep(200);
   }
+}
+
+__device__ __forceinline__ uint32_t read_abort(const Shared* S) {
+  uint32_t a;
+  asm volatile("ld.volatile.shared.u32 %0, [%1];"
+               : "=r"(a)
+               : "r"(smem_addr(&S->abort)));
+  return a;
 }
 
 template <int D>
@@ -330,89 +397,72 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
       mma_ss_warp(tmem + kTmemS, a0 + off, b0 + off, hi, kIdescQK, ks > 0);
     }
   };
-  auto pv = [&](int t, uint32_t b0, int acc) {
+  auto pv = [&](int t, uint32_t b0, bool acc) {
 #pragma unroll
     for (int kk = 0; kk < kBN / 16; ++kk)
       mma_ts_warp(tmem + kTmemO + t * 128, tmem + kTmemP + t * 64 + kk * 8,
                   b0 + (uint32_t)(kk * 2048 >> 4), hi, kIdescPV,
-                  (acc | kk) != 0);
+                  acc || kk > 0);
   };
-  int s_uses = 0;
-  auto take_s = [&]() {
-    if (s_uses > 0) handoff_sync(kBarSFree);
-    ++s_uses;
+  auto take_s = [&](bool wait) {
+    if (wait) handoff_sync(kBarSFree);
     tc_fence_after();
   };
+  // The loop's numbers as the warp's own: a warp-uniform value that the compiler
+  // knows to be one keeps descriptors in uniform registers.
+  auto same = [](int v) { return __shfl_sync(~0u, v, 0); };
   // Test hook: `drain` receives no arrival before the end, so this wait runs
   // out and exercises the abort path.
   bool ok = !p.inject_stall || wait_bar_warp(&S->drain, 0, S, p.status);
-  int x = blockIdx.x, qs = 0, ks = 0, vs = 0;  // ring stages
-  Unit u, nu;
-  bool have = next_unit(p, x, &u);
-  bool have_next = have && next_unit(p, x, &nu);
-  bool pend = false, ptwo = false;
-  int j = 0, q1 = 0, pacc = 0;
-  while (ok && (have || pend)) {
-    // read now, looked at when the step's MMAs have been issued
-    uint32_t aborted;
-    asm volatile("ld.volatile.shared.u32 %0, [%1];"
-                 : "=r"(aborted)
-                 : "r"(smem_addr(&S->abort)));
-    const bool last = have && j == u.n - 1;
-    if (have) {
-      if (j == 0) relay_sync(kBarQ + qs);
+  const int end = same(S->last);
+  int x = same(S->first);
+  int s = 0, qc = 0;  // steps and query tiles so far
+  bool ptwo = false, pacc = false;  // of the step whose PV is owed
+  // PV_t of step i.
+  auto owed = [&](int t, int i, bool two) {
+    const int vs = i % L::kV;
+    if (t == 0) relay_sync(kBarV + vs);
+    handoff_sync(kBarP + t);
+    tc_fence_after();
+    pv(t, v_lo + vs * kStage16, pacc);
+    mma_commit_warp(&S->p_free[t]);
+    if (t == (int)two) mma_commit_warp(&S->v_empty[vs]);
+  };
+  Unit u;
+  while (ok && next_unit(p, x, end, &u)) {
+    const int n = same(u.n);
+    const bool two = same(u.two);
+    x = same(x);
+    const int q0 = qc % L::kQ, q1 = (qc + 1) % L::kQ;
+    qc += 1 + (int)two;
+    const uint32_t aborted = read_abort(S);  // looked at after the unit
+    for (int j = 0; j < n; ++j, ++s) {
+      const int ks = s % L::kK;
+      if (j == 0) relay_sync(kBarQ + q0);
       relay_sync(kBarK + ks);
-      take_s();
-      qk(q_lo + qs * kStage16, k_lo + ks * kStage16);
+      take_s(s > 0);
+      qk(q_lo + q0 * kStage16, k_lo + ks * kStage16);
       mma_commit_warp(&S->s_full[0]);
-      if (last) mma_commit_warp(&S->q_empty[qs]);
-      if (!u.two) mma_commit_warp(&S->k_empty[ks]);
-    }
-    if (pend) {
-      relay_sync(kBarV + vs);
-      handoff_sync(kBarP);
-      tc_fence_after();
-      pv(0, v_lo + vs * kStage16, pacc);
-      mma_commit_warp(&S->p_free[0]);
-      if (!ptwo) mma_commit_warp(&S->v_empty[vs]);
-    }
-    if (have && u.two) {
-      if (j == 0) {
-        q1 = qs + 1 == L::kQ ? 0 : qs + 1;
-        relay_sync(kBarQ + q1);
+      if (j == n - 1) mma_commit_warp(&S->q_empty[q0]);
+      if (!two) mma_commit_warp(&S->k_empty[ks]);
+      if (s > 0) owed(0, s - 1, ptwo);
+      if (two) {
+        if (j == 0) relay_sync(kBarQ + q1);
+        take_s(true);
+        qk(q_lo + q1 * kStage16, k_lo + ks * kStage16);
+        mma_commit_warp(&S->s_full[1]);
+        if (j == n - 1) mma_commit_warp(&S->q_empty[q1]);
+        mma_commit_warp(&S->k_empty[ks]);
       }
-      take_s();
-      qk(q_lo + q1 * kStage16, k_lo + ks * kStage16);
-      mma_commit_warp(&S->s_full[1]);
-      if (last) mma_commit_warp(&S->q_empty[q1]);
-      mma_commit_warp(&S->k_empty[ks]);
-    }
-    if (pend) {
-      if (ptwo) {
-        handoff_sync(kBarP + 1);
-        tc_fence_after();
-        pv(1, v_lo + vs * kStage16, pacc);
-        mma_commit_warp(&S->p_free[1]);
-        mma_commit_warp(&S->v_empty[vs]);
-      }
-      vs = vs + 1 == L::kV ? 0 : vs + 1;
-    }
-    pend = have;
-    if (have) {
-      ptwo = u.two;
+      if (s > 0 && ptwo) owed(1, s - 1, true);
+      ptwo = two;
       pacc = j > 0;
-      ks = ks + 1 == L::kK ? 0 : ks + 1;
-      ++j;
-      if (last) {
-        const int last_q = u.two ? q1 : qs;
-        qs = last_q + 1 == L::kQ ? 0 : last_q + 1;
-        j = 0;
-        u = nu;
-        have = have_next;
-        have_next = have && next_unit(p, x, &nu);
-      }
     }
     if (__any_sync(~0u, aborted != 0)) ok = false;
+  }
+  if (ok && s > 0) {
+    owed(0, s - 1, ptwo);
+    if (ptwo) owed(1, s - 1, true);
   }
   mma_commit_warp(&S->drain);
   if ((threadIdx.x & 31) == 0) {
@@ -422,30 +472,23 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
   __syncwarp();
 }
 
-// Row `row` of (b, h): out = O / l from TMEM (zeros without keys) and lse.
+// out = O / l from TMEM, a row of a thread in pieces of 32 bytes (whole sectors).
 template <int D>
-__device__ __forceinline__ void write_row(const CrossParams& p, uint32_t tO,
-                                          int b, int h, int row, float m,
-                                          float l, bool none) {
-  const bool in = row < p.q_tokens;
+__device__ __forceinline__ void write_row(uint16_t* o, uint32_t tO, float l,
+                                          bool wide) {
   const float inv = 1.f / l;
-  uint16_t* o = p.o + (int64_t)b * p.o_str.batch +
-                (int64_t)row * p.o_str.token + (int64_t)h * p.o_str.head;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
-    uint32_t r[32], pk[16];
-    if (!none) {
-      __syncwarp();
-      tmem_ld32(tO + c * 32, r);
-      tmem_wait_ld();
-    }
+    uint32_t v[32], pk[16];
+    __syncwarp();
+    tmem_ld32(tO + c * 32, v);
+    tmem_wait_ld();
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      pk[i] = none ? 0u
-                   : pack_bf16(__uint_as_float(r[2 * i]) * inv,
-                               __uint_as_float(r[2 * i + 1]) * inv);
-    if (in) {
-      if (p.wide) {
+      pk[i] = pack_bf16(__uint_as_float(v[2 * i]) * inv,
+                        __uint_as_float(v[2 * i + 1]) * inv);
+    if (o != nullptr) {
+      if (wide) {
         store_32b(o + c * 32, pk);
         store_32b(o + c * 32 + 16, pk + 8);
       } else {
@@ -456,9 +499,6 @@ __device__ __forceinline__ void write_row(const CrossParams& p, uint32_t tO,
       }
     }
   }
-  if (in && p.lse != nullptr)
-    p.lse[((int64_t)b * p.heads + h) * p.q_tokens + row] =
-        none ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
   __syncwarp();
 }
 
@@ -469,40 +509,58 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
   const uint32_t tS = tmem + kTmemS + lane_off;
   const uint32_t tP = tmem + kTmemP + t * 64 + lane_off;
   const uint32_t tO = tmem + kTmemO + t * 128 + lane_off;
+  const int r = wq * 32 + lane;  // row within the tile
   const float sl2 = p.scale_log2;
   const uint64_t sl2x2 = f2_pack(sl2, sl2);
+  const int end = S->last;
   int tiles = 0;  // key tiles of this query tile so far: barrier phases
-  // the unit whose output is still to be written
-  bool owed = false;
-  int ob = 0, oh = 0, orow = 0;
-  float om = 0.f, ol = 0.f;
+  // the slot of the unit whose output is owed (-1: none), the row's sum
+  int owed = -1;
+  float owed_l = 0.f;
   bool ok = true;
-  int x = blockIdx.x;
-  // last unit with keys of this CTA
-  int last_x = -1;
-  {
+  // A row's places in out and lse; computed anew where they are needed, since
+  // the loop over the keys has no registers to hold them.
+  auto out_row = [&](const Unit& u) {
+    return p.o + (int64_t)u.b * p.o_str.batch +
+           (int64_t)(u.q0 + t * kBM + r) * p.o_str.token +
+           (int64_t)u.h * p.o_str.head;
+  };
+  auto lse_row = [&](const Unit& u) {
+    return p.lse + ((int64_t)u.b * p.heads + u.h) * p.q_tokens + u.q0 +
+           t * kBM + r;
+  };
+  auto exists = [&](const Unit& u) {
+    return u.q0 + t * kBM + r < p.q_tokens && (t == 0 || u.two);
+  };
+  auto write_owed = [&]() {
     Unit u;
-    for (int y = x; y < p.units; y += gridDim.x) {
-      get_unit(p, y, &u);
-      if (u.n > 0) last_x = y;
-      if (p.kv_len == nullptr) {
-        last_x = x + (p.units - 1 - x) / (int)gridDim.x * (int)gridDim.x;
-        break;
+    get_unit(p, owed, end, &u);
+    write_row<D>(exists(u) ? out_row(u) : nullptr, tO, owed_l, p.wide);
+  };
+  for (int slot = S->first, next; ok && slot < end; slot = next) {
+    int n, len;
+    bool unfollowed;  // no QK^T follows this unit's last S of this tile
+    {
+      Unit u, v;
+      next = get_unit(p, slot, end, &u);
+      n = u.n;
+      len = u.len;
+      if (n == 0) {  // sees no key
+        if (exists(u)) {
+          for (int c = 0; c < D; c += 8)
+            *reinterpret_cast<uint4*>(out_row(u) + c) = make_uint4(0, 0, 0, 0);
+          if (p.lse != nullptr) *lse_row(u) = -INFINITY;
+        }
+        __syncwarp();
+        continue;
       }
-    }
-  }
-  for (; ok && x < p.units; x += gridDim.x) {
-    Unit u;
-    get_unit(p, x, &u);
-    if (t == 1 && !u.two) continue;
-    const int row = u.q0 + t * kBM + wq * 32 + lane;
-    if (u.n == 0) {
-      write_row<D>(p, tO, u.b, u.h, row, 0.f, 1.f, true);
-      continue;
+      if (t == 1 && !u.two) continue;
+      int y = next;
+      unfollowed = t == (int)u.two && !next_unit(p, y, end, &v);
     }
     float m_ref = -INFINITY, l = 0.f;
-    for (int j = 0; j < u.n; ++j) {
-      if (!(ok = wait_bar_warp(&S->s_full[t], tiles & 1, S, p.status))) break;
+    for (int j = 0; j < n; ++j) {
+      if (!(ok = wait_bar(&S->s_full[t], tiles & 1, S, p.status))) break;
       tc_fence_after();
       uint32_t s[4][32];
 #pragma unroll
@@ -510,10 +568,9 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
       tmem_wait_ld();
       tc_fence_before();
       // no QK^T follows the CTA's last S
-      if (!(x == last_x && j == u.n - 1 && t == (u.two ? 1 : 0)))
-        handoff_arrive(kBarSFree);
+      if (!unfollowed || j < n - 1) handoff_arrive(kBarSFree);
       float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      const int valid = u.len - j * kBN;
+      const int valid = len - j * kBN;
 #pragma unroll
       for (int c = 0; c < 4; ++c) mask_max32(s[c], c, valid, mx);
       const float mrow = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2;
@@ -534,22 +591,22 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
 #pragma unroll
       for (int c = 0; c < 2; ++c) exp_pack32(s[c], sl2x2, neg2, pk[c], acc);
       // this query tile's previous PV is done: P may be written, O is current
-      if (tiles > 0 && !(ok = wait_bar_warp(&S->p_free[t], (tiles - 1) & 1, S,
-                                            p.status)))
+      if (tiles > 0 && !(ok = wait_bar(&S->p_free[t], (tiles - 1) & 1, S,
+                                       p.status)))
         break;
       tc_fence_after();
       if (j == 0) {
-        if (owed) write_row<D>(p, tO, ob, oh, orow, om, ol, false);
+        if (owed >= 0) write_owed();
       } else if (rescale) {
 #pragma unroll 1
         for (int c = 0; c < D / 8; ++c) {
-          uint32_t r[8];
-          tmem_ld8(tO + c * 8, r);
+          uint32_t v[8];
+          tmem_ld8(tO + c * 8, v);
           tmem_wait_ld();
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-          tmem_st8(tO + c * 8, r);
+            v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+          tmem_st8(tO + c * 8, v);
         }
       }
       tmem_st16(tP, pk[0]);
@@ -565,17 +622,18 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
       handoff_arrive(kBarP + t);
       ++tiles;
     }
-    owed = ok;
-    ob = u.b;
-    oh = u.h;
-    orow = row;
-    om = m_ref;
-    ol = l;
+    if (!ok) break;
+    Unit u;
+    get_unit(p, slot, end, &u);
+    if (exists(u) && p.lse != nullptr)
+      *lse_row(u) = (m_ref + __log2f(l)) * 0.6931471805599453f;
+    owed = slot;
+    owed_l = l;
   }
-  if (ok && owed &&
+  if (ok && owed >= 0 &&
       wait_bar_warp(&S->p_free[t], (tiles - 1) & 1, S, p.status)) {
     tc_fence_after();
-    write_row<D>(p, tO, ob, oh, orow, om, ol, false);
+    write_owed();
   }
 }
 
@@ -591,6 +649,11 @@ cross_tile_kernel(const __grid_constant__ CrossParams p) {
   if (warp == 9) {
     tmem_alloc(&S->tmem_base, kTmemCols);
     tmem_relinquish();
+  }
+  if (threadIdx.x == 320) {
+    tma_prefetch_desc(&p.q_map);
+    tma_prefetch_desc(&p.k_map);
+    tma_prefetch_desc(&p.v_map);
   }
   if (threadIdx.x == 256) {
     for (int s = 0; s < L::kQ; ++s) {
@@ -621,6 +684,13 @@ cross_tile_kernel(const __grid_constant__ CrossParams p) {
   const uint32_t tmem = S->tmem_base;
   pdl_trigger();
   pdl_wait();
+  if (warp < 2) {
+    const int at = warp == 1 && p.step > 1
+                       ? p.all
+                       : first_slot(p, blockIdx.x + warp, lane);
+    if (lane == 0) (warp == 0 ? S->first : S->last) = at;
+  }
+  __syncthreads();
 
   if (warp == 8) {
     if (lane == 0) qk_producer<D>(p, smem, S);
@@ -663,9 +733,22 @@ cudaError_t launch_tiles(const CrossArgs& a, cudaStream_t stream) {
   p.group = a.heads / a.kv_heads;
   p.q_tokens = a.q_tokens;
   p.kv_tokens = a.kv_tokens;
-  p.q_pairs = (a.q_tokens + 2 * kBM - 1) / (2 * kBM);
-  p.units = p.q_pairs * a.heads * a.batch;
-  p.by_pairs = make_div((uint32_t)p.q_pairs);
+  p.q_tiles = (a.q_tokens + kBM - 1) / kBM;
+  // Pairs unless they leave some CTA more units than single tiles would (25 tiles
+  // of each of 12 heads over 152 CTAs: 156 pairs, but two tiles to each).
+  const int heads = a.batch * a.heads;
+  const int pairs = (p.q_tiles + 1) / 2;
+  auto each = [&](int n) { return (n * heads + a.sms - 1) / a.sms; };
+  const bool paired = each(pairs) <= (each(p.q_tiles) + 1) / 2 &&
+                      p.q_tiles * heads > a.sms;
+  p.per_slot = paired ? 2 : 1;
+  p.slots = paired ? pairs : p.q_tiles;
+  p.all = p.slots * heads;
+  p.by_slots = make_div((uint32_t)p.slots);
+  const int grid = std::min(p.all, a.sms);
+  // Pairs of equal work are dealt out in turn, so that the last ones run with the
+  // GPU to themselves; others are taken in ranges of equal work.
+  p.step = paired && a.kv_len == nullptr ? grid : 1;
   p.by_heads = make_div((uint32_t)a.heads);
   p.by_group = make_div((uint32_t)p.group);
   p.wide = ((uintptr_t)a.o & 31) == 0 && a.o_str.batch % 16 == 0 &&
@@ -679,7 +762,7 @@ cudaError_t launch_tiles(const CrossArgs& a, cudaStream_t stream) {
   const cudaError_t e = cudaFuncSetAttribute(
       cross_tile_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  return launch_pdl(cross_tile_kernel<D>, dim3(std::min(p.units, a.sms)),
+  return launch_pdl(cross_tile_kernel<D>, dim3(grid),
                     dim3(kThreads), smem, stream, p);
 }
 

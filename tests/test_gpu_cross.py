@@ -48,6 +48,11 @@ CASES = [
     (5, 130, 333, 4, 1, 64, [-3, 333, 1000, 200, 127]),
     (1, 700, 640, 3, 3, 128, None),
     (2, 1100, 97, 2, 1, 64, [97, 96]),
+    # many units to a CTA: one key tile each, and lengths of all kinds
+    (3, 1500, 100, 40, 20, 128, None),
+    (40, 300, 60, 10, 5, 64, [0, 60, 7, 60] * 10),
+    (3, 900, 260, 50, 25, 128, [260, 0, 1]),
+    (33, 280, 300, 8, 8, 64, [300, 1, 129] * 11),
 ]
 
 
