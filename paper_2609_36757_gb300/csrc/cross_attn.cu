@@ -241,17 +241,6 @@ __device__ void qk_producer(const CrossParams& p, uint8_t* smem, Shared* S) {
                          u.b * p.q_batch, once);
       ++qc;
     };
-    // The ring holds no more than the unit at hand: the queries of the next one
-    // are asked for in L2 now.
-    {
-      int y = x;
-      Unit v;
-      if (next_unit(p, y, end, &v))
-        for (int t = 0; t <= (int)v.two; ++t)
-          for (int bx = 0; bx < L::kNB; ++bx)
-            tma_prefetch_4d(&p.q_map, bx * 64, v.q0 + t * kBM, v.h,
-                            v.b * p.q_batch);
-    }
     query(0);
     for (int j = 0; ok && j < u.n; ++j) {
       const int st = kc % L::kK;

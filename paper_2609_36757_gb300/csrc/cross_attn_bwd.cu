@@ -9,18 +9,20 @@
 // TMEM:
 //   rows_kernel   D_i and the log-sum-exp in log2 units, both negated, one
 //                 padded row of scratch per (b, h);
-//   dkdv_kernel   one CTA per tile of 128 keys and range of query tiles (of all
+//   grads_kernel  both of these at once, so that each fills the SMs that the other's
+//                 last CTAs leave idle:
+//   dkdv_cta      one CTA per tile of 128 keys and range of query tiles (of all
 //                 heads of the group): S^T = K Q^T, dP^T = V dO^T, dV += P^T dO,
 //                 dK += dS^T Q.  Keys are few and queries many, so a key tile's
 //                 queries are cut into as many ranges as fill the GPU, whose
 //                 float32 sums join_kernel adds up in order;
-//   dq_kernel     persistent, a unit being a tile of 128 queries over all keys of
+//   dq_cta        a CTA takes a few units, a unit being a tile of 128 queries over all keys of
 //                 its head: S = Q K^T, dP = dO V^T, dQ += dS K.  With few keys a
 //                 unit is short, so units follow one another without a gap: the
 //                 next unit's S and dP run before this one's last dQ, whose
 //                 result leaves between the next unit's P and dS.
 // Lanes of TMEM are independent, so key rows past an entry's last need no mask
-// in dkdv_kernel (their results are replaced by zeros); in dq_kernel their
+// in dkdv_cta (their results are replaced by zeros); in dq_cta their
 // columns are masked and the K and V rows zeroed in shared memory, where NaN
 // would meet P = 0.  Waits are bounded as in cross_attn.cu.
 #include <cuda.h>
@@ -70,6 +72,7 @@ struct BwdParams {
   int32_t q_batch, k_batch, v_batch, do_batch;
   int32_t wide_q, wide_k, wide_v;
   int32_t parts;     // ranges of a key tile's query tiles
+  int32_t dkdv_ctas, dq_ctas;
   float *dk_part, *dv_part;  // [parts][batch kv_heads][k_tiles * 128][d]
   float scale, scale_log2;
   int* status;
@@ -94,27 +97,27 @@ struct Shared {
   uint64_t wait_limit_ns;
 };
 
+// A front region with the barriers (and, for dK and dV, two slots of row vectors),
+// then the tiles: 227 KB exactly at d = 128.
+constexpr int kFront = 3 * 1024;
+
 template <int D>
 struct DqLayout {
   static constexpr int kNB = D / 64, kTile = kNB * kBox;
   // d = 128: seven tiles of 32 KB.  K needs three (K_j lives until dQ_j, two
   // products after S_{j+1}), V two.
   static constexpr int kPrev = D == 64 ? 2 : 1;
-  using Q = Ring<0, kPrev, 0>;
-  using O = Ring<2, kPrev, kPrev * kTile>;
-  using K = Ring<4, 3, 2 * kPrev * kTile>;
-  using V = Ring<7, 2, (2 * kPrev + 3) * kTile>;
-  static constexpr int shared_off = (2 * kPrev + 5) * kTile;
-  static constexpr int bytes = shared_off + 1024 + 1024;
+  using Q = Ring<0, kPrev, kFront>;
+  using O = Ring<2, kPrev, kFront + kPrev * kTile>;
+  using K = Ring<4, 3, kFront + 2 * kPrev * kTile>;
+  using V = Ring<7, 2, kFront + (2 * kPrev + 3) * kTile>;
+  static constexpr int bytes = kFront + (2 * kPrev + 5) * kTile;
 };
 
-// As chunk_attn_bwd.cu's: a front region with the barriers and two slots of row
-// vectors, the resident K and V tiles, then the rings; 227 KB exactly at d = 128,
-// so the kernel checks that its shared memory starts on a 1024-byte boundary.
+// The resident K and V tiles, then the rings of Q and dO.
 template <int D>
 struct DkdvLayout {
   static constexpr int kNB = D / 64, kTile = kNB * kBox;
-  static constexpr int kFront = 3072;
   __host__ __device__ static constexpr int vec(int slot, int which) {
     return 1024 + (slot * 2 + which) * kT * (int)sizeof(float);
   }
@@ -254,6 +257,12 @@ __device__ __forceinline__ uint32_t setup(Shared* S, const BwdParams& p) {
     tmem_alloc(&S->tmem_base, kTmemCols);
     tmem_relinquish();
   }
+  if (threadIdx.x == kWarpB * 32) {
+    tma_prefetch_desc(&p.q_map);
+    tma_prefetch_desc(&p.k_map);
+    tma_prefetch_desc(&p.v_map);
+    tma_prefetch_desc(&p.do_map);
+  }
   if (threadIdx.x == kWarpA * 32) {
     for (int i = 0; i < kRingSlots; ++i) {
       mbar_init(&S->full[i], 1);
@@ -345,13 +354,11 @@ __device__ __forceinline__ void store_cols32(uint32_t taddr, float mul,
 // [384,384+d) dK.  Step x: query tile x % q_tiles of head x / q_tiles of the
 // group.
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
-dkdv_kernel(const __grid_constant__ BwdParams p) {
+__device__ __forceinline__ void dkdv_cta(const BwdParams& p, uint8_t* smem,
+                                         Shared* S, uint32_t tmem) {
   using L = DkdvLayout<D>;
   using RQ = typename L::Q;
   using RO = typename L::O;
-  extern __shared__ __align__(1024) uint8_t smem[];
-  Shared* S = reinterpret_cast<Shared*>(smem);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   // parts of a key tile and key tiles of a head side by side: their CTAs share
   // query tiles in L2
@@ -361,13 +368,6 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
   const int k0 = x % p.k_tiles * kT;
   const int bh = x / p.k_tiles;
   const int hk = bh % p.kv_heads, b = bh / p.kv_heads;
-  pdl_trigger();
-  pdl_wait();
-  if ((smem_addr(smem) & 1023u) != 0) {
-    if (threadIdx.x == 0 && p.status != nullptr)
-      atomicExch(p.status, kDevBounds);
-    return;
-  }
   const int len = cross_keys(p.kv_len, b, p.kv_tokens);
   if (k0 >= len) {  // no key of the tile is seen; parts are not read then
     if (p.parts == 1) {
@@ -390,7 +390,6 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
   const int x0 = (int)((int64_t)part * steps / p.parts);
   const int n = (int)((int64_t)(part + 1) * steps / p.parts) - x0;
   const int h0 = hk * p.group;
-  const uint32_t tmem = setup(S, p);
 
   if (warp == kWarpA) {
     if (lane == 0) {
@@ -586,7 +585,6 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
       }
     }
   }
-  teardown(tmem);
 }
 
 // dk and dv as the sums of their parts, in order; zeros past the last key.  A
@@ -652,10 +650,10 @@ __device__ __forceinline__ void get_unit(const BwdParams& p, int x, Unit* u) {
   u->n = (u->len + kT - 1) / kT;
 }
 __device__ __forceinline__ bool next_unit(const BwdParams& p, int& x, Unit* u) {
-  for (; x < p.units; x += gridDim.x) {
+  for (; x < p.units; x += p.dq_ctas) {
     get_unit(p, x, u);
     if (u->n > 0) {
-      x += gridDim.x;
+      x += p.dq_ctas;
       return true;
     }
   }
@@ -676,21 +674,14 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, int valid, int lane) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
-dq_kernel(const __grid_constant__ BwdParams p) {
+__device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
+                                       Shared* S, uint32_t tmem, int cta) {
   using L = DqLayout<D>;
   using RQ = typename L::Q;
   using RO = typename L::O;
   using RK = typename L::K;
   using RV = typename L::V;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>(
-      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  Shared* S = reinterpret_cast<Shared*>(smem + L::shared_off);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const uint32_t tmem = setup(S, p);
-  pdl_trigger();
-  pdl_wait();
 
   if (warp == kWarpA || warp == kWarpB) {
     // K_0, Q, K_1, ... and V_0, dO, V_1, ...: a unit's first K and V can be on
@@ -699,7 +690,7 @@ dq_kernel(const __grid_constant__ BwdParams p) {
       const bool a = warp == kWarpA;
       const uint64_t once = l2_policy_evict_first(),
                      keep = l2_policy_evict_last();
-      int x = blockIdx.x, c = 0, r = 0;
+      int x = cta, c = 0, r = 0;
       Unit u;
       bool ok = true;
       while (ok && next_unit(p, x, &u)) {
@@ -726,7 +717,7 @@ dq_kernel(const __grid_constant__ BwdParams p) {
     }
     __syncwarp();
   } else if (warp == kRelayWarp) {
-    int x = blockIdx.x, c = 0, r = 0;
+    int x = cta, c = 0, r = 0;
     Unit u;
     bool ok = true;
     while (ok && next_unit(p, x, &u)) {
@@ -759,7 +750,7 @@ dq_kernel(const __grid_constant__ BwdParams p) {
     };
     // Test hook: `drain` receives no arrival before the end.
     bool ok = !p.inject_stall || wait_bar_warp(&S->drain, 0, S, p.status);
-    int x = blockIdx.x;
+    int x = cta;
     Unit u, nu;
     bool have = next_unit(p, x, &u);
     bool have_next = have && next_unit(p, x, &nu);
@@ -830,9 +821,9 @@ dq_kernel(const __grid_constant__ BwdParams p) {
     };
     // A unit's row values lie at kT times its number; the next one's are asked
     // for a unit ahead.
-    float nl_next = p.lse2[(int64_t)blockIdx.x * kT + t];
-    float nd_next = p.delta[(int64_t)blockIdx.x * kT + t];
-    for (int x = blockIdx.x; ok && x < p.units; x += gridDim.x) {
+    float nl_next = p.lse2[(int64_t)cta * kT + t];
+    float nd_next = p.delta[(int64_t)cta * kT + t];
+    for (int x = cta; ok && x < p.units; x += p.dq_ctas) {
       Unit u;
       get_unit(p, x, &u);
       const int row = u.q0 + t;
@@ -840,9 +831,9 @@ dq_kernel(const __grid_constant__ BwdParams p) {
                       (int64_t)row * p.dq_str.token +
                       (int64_t)u.h * p.dq_str.head;
       const float nl_row = nl_next, nd_row = nd_next;
-      if (x + (int)gridDim.x < p.units) {
-        nl_next = p.lse2[(int64_t)(x + gridDim.x) * kT + t];
-        nd_next = p.delta[(int64_t)(x + gridDim.x) * kT + t];
+      if (x + p.dq_ctas < p.units) {
+        nl_next = p.lse2[(int64_t)(x + p.dq_ctas) * kT + t];
+        nd_next = p.delta[(int64_t)(x + p.dq_ctas) * kT + t];
       }
       if (u.n == 0) {  // sees no key
         if (row < p.q_tokens)
@@ -899,6 +890,26 @@ dq_kernel(const __grid_constant__ BwdParams p) {
     }
     if (ok && owed != nullptr) write_out();
   }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+grads_kernel(const __grid_constant__ BwdParams p) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  // The layouts leave no room to round the base up.
+  if ((smem_addr(smem) & 1023u) != 0) {
+    if (threadIdx.x == 0 && p.status != nullptr)
+      atomicExch(p.status, kDevBounds);
+    return;
+  }
+  Shared* S = reinterpret_cast<Shared*>(smem);
+  const uint32_t tmem = setup(S, p);
+  pdl_trigger();
+  pdl_wait();
+  if ((int)blockIdx.x < p.dkdv_ctas)
+    dkdv_cta<D>(p, smem, S, tmem);
+  else
+    dq_cta<D>(p, smem, S, tmem, (int)blockIdx.x - p.dkdv_ctas);
   teardown(tmem);
 }
 
@@ -970,12 +981,13 @@ constexpr int kSms = 152;
 
 // Ranges of a key tile's `steps` query tiles: the number that ends first, a CTA
 // taking about two steps' time to start and to end and a part's results about
-// a quarter of one to join.
+// a quarter of one to join, over entries that see all keys and half of them.
 int key_parts(int64_t ctas, int64_t steps) {
   int best = 1;
   double least = 1e300;
   for (int s = 1; s <= 32 && s <= steps; ++s) {
-    const double waves = (double)((ctas * s + kSms - 1) / kSms);
+    const double waves = (double)((ctas * s + kSms - 1) / kSms) +
+                         (double)((ctas * s / 2 + kSms - 1) / kSms);
     const double cost = waves * ((double)((steps + s - 1) / s) + 2.0) +
                         (s > 1 ? 2.0 + 0.25 * (double)ctas * s / kSms : 0.0);
     if (cost < least) {
@@ -985,6 +997,9 @@ int key_parts(int64_t ctas, int64_t steps) {
   }
   return best;
 }
+
+// CTAs of dq to an SM: few enough units in each to fill the end of a launch.
+constexpr int kDqWaves = 2;
 
 struct ScratchLayout {
   int64_t rows, part;  // floats of one row vector, of dk's (dv's) parts
@@ -1065,25 +1080,20 @@ cudaError_t launch_d(const CrossBwdArgs& a, cudaStream_t stream) {
       rows_kernel<D>, dim3((unsigned)(f.batch * f.heads * row_tiles)),
       dim3(256), 0, stream, a, lse2, delta, p.padded,
       make_div((uint32_t)row_tiles), p.by_heads);
+  constexpr int smem = std::max(DkdvLayout<D>::bytes, DqLayout<D>::bytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(dkdv_kernel<D>,
-                             cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             DkdvLayout<D>::bytes);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(dq_kernel<D>,
-                             cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             DqLayout<D>::bytes);
+    e = cudaFuncSetAttribute(
+        grads_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   const int tiles = f.batch * f.kv_heads * p.k_tiles;
-  e = launch_pdl(dkdv_kernel<D>, dim3(tiles * p.parts), dim3(kThreads),
-                 DkdvLayout<D>::bytes, stream, p);
-  if (e == cudaSuccess && p.parts > 1)
-    e = launch_pdl(join_kernel<D>,
-                   dim3((unsigned)((int64_t)tiles * kT * (D / 8) / 256)),
-                   dim3(256), 0, stream, p);
-  if (e != cudaSuccess) return e;
-  return launch_pdl(dq_kernel<D>, dim3(std::min(p.units, f.sms)),
-                    dim3(kThreads), DqLayout<D>::bytes, stream, p);
+  p.dkdv_ctas = tiles * p.parts;
+  p.dq_ctas = std::min(p.units, kDqWaves * f.sms);
+  e = launch_pdl(grads_kernel<D>, dim3((unsigned)(p.dkdv_ctas + p.dq_ctas)),
+                 dim3(kThreads), smem, stream, p);
+  if (e != cudaSuccess || p.parts == 1) return e;
+  return launch_pdl(join_kernel<D>,
+                    dim3((unsigned)((int64_t)tiles * kT * (D / 8) / 256)),
+                    dim3(256), 0, stream, p);
 }
 
 }  // namespace

@@ -109,16 +109,6 @@ __device__ __forceinline__ void tma_load_4d_hint(const CUtensorMap* map,
       : "memory");
 }
 
-// Asks for a box to be brought to L2.
-__device__ __forceinline__ void tma_prefetch_4d(const CUtensorMap* map,
-                                                int32_t c0, int32_t c1,
-                                                int32_t c2, int32_t c3) {
-  asm volatile(
-      "cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];"
-      ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-      : "memory");
-}
-
 // 4-D tiled store of one box from shared memory (the map's box and swizzle;
 // elements outside the tensor are not written), tracked by bulk groups.
 __device__ __forceinline__ void tma_store_4d(const CUtensorMap* map,
@@ -423,17 +413,6 @@ __device__ __forceinline__ void mma_commit_pair_warp(uint64_t* bar) {
       "multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(smem_addr(bar)),
       "h"((uint16_t)3)
       : "memory");
-}
-
-// Registers of a thread from here on, for a whole warpgroup; all warpgroups'
-// shares add up to what the block was launched with.
-template <int N>
-__device__ __forceinline__ void regs_inc() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-template <int N>
-__device__ __forceinline__ void regs_dec() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
 }
 
 // 32 bytes to a 32-byte aligned place.
