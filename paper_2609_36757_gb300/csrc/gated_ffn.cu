@@ -8,16 +8,18 @@
 //   dW       [hidden, dim] = dg^T x, du^T x        dg and x by columns
 // so one kernel serves all: TMA brings 128-byte-swizzled boxes of 64 columns,
 // which the MMA's descriptors read as K-major (rows) or MN-major (columns)
-// operands, and nothing is transposed in memory.
+// operands, and nothing is transposed in memory.  A copy brings 16 KB where it
+// can: with two copies of 8 KB for one operand the 1080p chunk took 242 us
+// instead of 228.
 //
 // A pair of CTAs owns a 256 x 256 tile of results (a forward tile: 128 columns
 // of g and the same 128 of u, whose product is formed in the epilogue, so g and
 // u need not leave the SM).  Each CTA loads 128 rows of A and 128 of B's 256,
 // 32 KB for 64 steps of the sum: half of what a CTA alone would load for the
-// same products, which L2 could not deliver.  Persistent: warp 0 loads (six
-// stages), warp 1 of the even CTA issues the MMAs of both, warps 4-11 form and
+// same products, which L2 could not deliver.  Persistent: warps 0 and 2 load A and B
+// (six stages), warp 1 of the even CTA issues the MMAs of both, warps 4-11 form and
 // store the results from one half of TMEM while the next tile accumulates in
-// the other.  Every wait is bounded, as in chunk_attn_fwd.cu.
+// the other.  Where there are too few tiles for all pairs they are half as wide.  Every wait is bounded, as in chunk_attn_fwd.cu.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <math.h>
@@ -49,10 +51,12 @@ enum Kind { kFwd, kDx, kDw };
 // Tiles of one kind: results [rows, cols], rows of tiles by tiles across.
 struct Tiles {
   int32_t rows, cols, mt, nt, count, steps;
+  int32_t narrow;  // 128 columns of results instead of 256
 };
 
 struct PairParams {
-  CUtensorMap x, w[2], d[2];  // x; gate and up weights; dg and du
+  // x; gate and up weights; dg and du, by rows (dx) and by columns (dW)
+  CUtensorMap x, w[2], d[2], dt[2];
   // results: forward h, g, u; backward dx, dWg, dWu
   CUtensorMap out[3];
   Tiles tile[2];              // forward: [0]; backward: those listed first, and
@@ -62,6 +66,9 @@ struct PairParams {
   int32_t heavy, extra;
   int32_t half_steps;       // dx: steps of dg Wg
   int32_t save;             // forward: g and u are wanted
+  // by columns, a copy takes all the columns that a CTA needs: dim, hidden are
+  // whole boxes
+  int32_t dim_boxes, hidden_boxes;
   int* status;
   int32_t inject_stall;
   uint64_t wait_limit_ns;
@@ -115,7 +122,7 @@ __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity,
 
 // The i-th tile of a pair of CTAs; false behind its last.
 struct Work {
-  int kind, m0, n0, steps, which;  // which: dWg or dWu
+  int kind, m0, n0, steps, which, narrow;  // which: dWg or dWu
 };
 __host__ __device__ inline bool nth_tile(const PairParams& p, int pair,
                                          int pairs, int i, Work* w) {
@@ -137,6 +144,7 @@ __host__ __device__ inline bool nth_tile(const PairParams& p, int pair,
   const Tiles& a = p.tile[list];
   w->kind = p.kind[list];
   w->steps = a.steps;
+  w->narrow = a.narrow;
   w->which = 0;
   if (w->kind == kDw) {
     const int one = a.mt * a.nt;
@@ -147,8 +155,22 @@ __host__ __device__ inline bool nth_tile(const PairParams& p, int pair,
   const int first = t / across * kGroupTiles;
   const int gm = min(kGroupTiles, a.mt - first), r = t % across;
   w->m0 = (first + r % gm) * 2 * kHalf;
-  w->n0 = r / gm * (w->kind == kFwd ? kHalf : 2 * kHalf);
+  w->n0 = r / gm * ((w->kind == kFwd ? kHalf : 2 * kHalf) >> w->narrow);
   return true;
+}
+
+// An operand by columns: `boxes` of 64 columns from col on, 64 rows from row on.
+__device__ __forceinline__ void load_columns(const CUtensorMap* map,
+                                             uint8_t* dst, uint32_t bar,
+                                             int col, int row, int boxes,
+                                             bool whole) {
+  if (whole) {
+    tma_load_3d_pair(map, dst, bar, 0, row, col / 64);
+  } else {
+    for (int x = 0; x < boxes; ++x)
+      tma_load_3d_pair(map, dst + x * (kOperand / 2), bar, col + 64 * x, row,
+                       0);
+  }
 }
 
 // 32 results of row r, from column c of its box on, as bfloat16 into the box
@@ -224,11 +246,15 @@ pair_kernel(const __grid_constant__ PairParams p) {
   pdl_wait();
   Work w;
 
-  if (warp == 0) {
+  if (warp == 0 || warp == 2) {
+    // A's and B's tiles: one thread for both would need longer than a step's
+    // products (229 us against 259 for the 1080p chunk with three copies a step)
+    const bool first = warp == 0;
     if (lane == 0) {
       int it = 0;
       bool ok = true;
       for (int i = 0; ok && nth_tile(p, pair, pairs, i, &w); ++i) {
+        const int b_boxes = 2 - w.narrow;
         for (int s = 0; s < w.steps; ++s, ++it) {
           const int st = it % kStages;
           if (!(ok = wait_bar(&S->empty[st], ((it / kStages) & 1) ^ 1, S,
@@ -238,31 +264,32 @@ pair_kernel(const __grid_constant__ PairParams p) {
           uint8_t* b = a + kOperand;
           // both CTAs' bytes count on the even CTA's barrier
           const uint32_t bar = cluster_addr(&S->full[st], 0);
-          if (rank == 0) mbar_arrive_expect_tx(&S->full[st], 4 * kOperand);
+          if (first && rank == 0)
+            mbar_arrive_expect_tx(&S->full[st], (2 + b_boxes) * kOperand);
           if (!kBackward) {
-            tma_load_2d_pair(&p.x, a, bar, s * kStep, w.m0 + rank * kHalf);
-            tma_load_2d_pair(&p.w[rank], b, bar, s * kStep, w.n0);
+            if (first)
+              tma_load_2d_pair(&p.x, a, bar, s * kStep, w.m0 + rank * kHalf);
+            else
+              tma_load_2d_pair(&p.w[rank], b, bar, s * kStep, w.n0);
           } else if (w.kind == kDx) {
             const int up = s >= p.half_steps;
             const int k = (s - up * p.half_steps) * kStep;
-            for (int x = 0; x < 2; ++x) {
-              tma_load_2d_pair(&p.d[up], a + x * (kOperand / 2), bar, k,
-                               w.m0 + rank * kHalf + x * 64);
-              tma_load_2d_pair(&p.w[up], b + x * (kOperand / 2), bar,
-                               w.n0 + rank * kHalf + x * 64, k);
-            }
+            if (first)
+              tma_load_2d_pair(&p.d[up], a, bar, k, w.m0 + rank * kHalf);
+            else
+              load_columns(&p.w[up], b, bar, w.n0 + rank * b_boxes * 64, k,
+                           b_boxes, p.dim_boxes);
+          } else if (first) {
+            load_columns(&p.dt[w.which], a, bar, w.m0 + rank * kHalf,
+                         s * kStep, 2, p.hidden_boxes);
           } else {
-            for (int x = 0; x < 2; ++x) {
-              tma_load_2d_pair(&p.d[w.which], a + x * (kOperand / 2),
-                               bar, w.m0 + rank * kHalf + x * 64, s * kStep);
-              tma_load_2d_pair(&p.x, b + x * (kOperand / 2), bar,
-                               w.n0 + rank * kHalf + x * 64, s * kStep);
-            }
+            load_columns(&p.x, b, bar, w.n0 + rank * b_boxes * 64, s * kStep,
+                         b_boxes, p.dim_boxes);
           }
         }
       }
       // every load has landed before the pair exits
-      if (rank == 0)
+      if (first && rank == 0)
         for (int i = max(0, it - kStages); i < it; ++i)
           drain_wait(&S->full[i % kStages], (i / kStages) & 1, S);
     }
@@ -287,7 +314,8 @@ pair_kernel(const __grid_constant__ PairParams p) {
         // MN-major: 16 elements are 16 rows of 128 bytes, 64 of the other axis
         // a box of 64 rows.
         const bool a_mn = kBackward && w.kind == kDw, b_mn = kBackward;
-        const uint32_t idesc = idesc_bf16_f32(256, 256, b_mn, a_mn);
+        const uint32_t idesc =
+            idesc_bf16_f32(256, w.narrow ? 128 : 256, b_mn, a_mn);
         const uint32_t hi = desc_hi_sw128(1024);
         const uint32_t a_lbo = a_mn ? kOperand / 2 : 16;
         const uint32_t b_lbo = b_mn ? kOperand / 2 : 16;
@@ -331,17 +359,23 @@ pair_kernel(const __grid_constant__ PairParams p) {
       const uint32_t acc = tmem + buf * 256 + lanes;
       const uint32_t freed = cluster_addr(&S->acc_empty[buf], 0);
       uint32_t pk[16];
-      if (!kBackward) {
+      if (!kBackward && w.narrow && hf == 1) {
+        // one box of columns: the other half's
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(freed);
+      } else if (!kBackward) {
         // h, then g and u where they are kept
         const int rounds = p.save ? 3 : 1;
         const int col = w.n0 + hf * 64;
+        const int u_col = w.narrow ? 64 : 128;
         for (int x = 0; x < rounds; ++x) {
           box_begin(hf, leader);
 #pragma unroll
           for (int c = 0; c < 64; c += 32) {
             uint32_t g[32], u[32];
             if (x != 2) tmem_ld32(acc + hf * 64 + c, g);
-            if (x != 1) tmem_ld32(acc + 128 + hf * 64 + c, u);
+            if (x != 1) tmem_ld32(acc + u_col + hf * 64 + c, u);
             tmem_wait_ld();
             if (x == 0) {
 #pragma unroll
@@ -367,9 +401,9 @@ pair_kernel(const __grid_constant__ PairParams p) {
         }
       } else {
         const CUtensorMap* map = &p.out[w.kind == kDx ? 0 : 1 + w.which];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int col = hf * 128 + x * 64;
+        const int boxes = 2 - w.narrow;
+        for (int x = 0; x < boxes; ++x) {
+          const int col = (hf * boxes + x) * 64;
           box_begin(hf, leader);
 #pragma unroll
           for (int c = 0; c < 64; c += 32) {
@@ -379,7 +413,7 @@ pair_kernel(const __grid_constant__ PairParams p) {
             pack_row32(v, pk);
             stage_row32(box, r, c, pk);
           }
-          if (x == 1) {
+          if (x == boxes - 1) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(freed);
@@ -458,30 +492,75 @@ bool make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t cols,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same by columns, boxes of 64 rows: where the columns are whole boxes they
+// become an axis of boxes, `boxes` of which a copy takes.
+bool make_column_map(CUtensorMap* m, const void* base, int64_t rows,
+                     int64_t cols, int64_t row_elems, int boxes) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (enc == nullptr) return false;
+  const bool whole = cols % 64 == 0;
+  const cuuint64_t dims[3] = {(cuuint64_t)(whole ? 64 : cols), (cuuint64_t)rows,
+                              (cuuint64_t)(whole ? cols / 64 : 1)};
+  const cuuint64_t strides[2] = {(cuuint64_t)row_elems * 2, 128};
+  const cuuint32_t box[3] = {64, kStep, (cuuint32_t)(whole ? boxes : 1)};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base),
+             dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-Tiles make_tiles(int64_t rows, int64_t cols, int col_tile, int copies,
-                 int steps) {
+// `wide`: columns of a wide tile.
+Tiles make_tiles(int64_t rows, int64_t cols, int wide, int copies, int steps,
+                 int narrow) {
   Tiles t;
   t.rows = (int32_t)rows;
   t.cols = (int32_t)cols;
   t.mt = up(rows, 2 * kHalf);
-  t.nt = up(cols, col_tile);
+  t.nt = up(cols, wide >> narrow);
   t.count = t.mt * t.nt * copies;
   t.steps = steps;
+  t.narrow = narrow;
   return t;
+}
+
+// The pairs' shares of two lists of tiles, and the time of the pair that ends
+// last in steps of wide tiles.  A narrow tile has half of the products but three
+// quarters of the loads, which bound it.
+struct Shares {
+  int pairs, heavy, extra;
+  double time;
+};
+Shares share(const Tiles& a, const Tiles& b, int sms) {
+  Shares s = {std::min(sms / 2, a.count + b.count), 0, 0, 0.0};
+  const double ca = (a.steps + 8) * (a.narrow ? 0.75 : 1.0);
+  const double cb = (b.steps + 8) * (b.narrow ? 0.75 : 1.0);
+  const int rest = a.count % s.pairs;
+  if (b.count > 0 && rest > 0) {
+    s.heavy = rest;
+    s.extra = (int)(ca / cb);
+  }
+  const int light = s.pairs - s.heavy;
+  const int ahead = s.extra > 0 ? std::min<int64_t>(b.count, (int64_t)s.extra * light) : 0;
+  for (int p = 0; p < s.pairs; ++p) {
+    int64_t n = (b.count - ahead + s.pairs - 1 - p) / s.pairs;
+    if (s.extra > 0 && p >= s.heavy) {
+      const int own = p - s.heavy;
+      n += std::min(s.extra, (ahead - own + light - 1) / light);
+    }
+    s.time = std::max(
+        s.time, (a.count + s.pairs - 1 - p) / s.pairs * ca + (double)n * cb);
+  }
+  return s;
 }
 
 template <int kAct>
 cudaError_t launch_pairs(PairParams& p, const FfnArgs& a, cudaStream_t stream) {
-  const int pairs = std::min(a.sms / 2, p.tile[0].count + p.tile[1].count);
-  if (kAct < 0) {
-    const int rest = p.tile[0].count % pairs;
-    if (rest > 0 && p.tile[0].count > 0) {
-      p.heavy = rest;
-      p.extra = p.tile[0].steps / p.tile[1].steps;
-    }
-  }
+  const Shares s = share(p.tile[0], p.tile[1], a.sms);
+  p.heavy = s.heavy;
+  p.extra = s.extra;
   p.status = a.status;
   p.inject_stall = a.inject_stall;
   p.wait_limit_ns = a.wait_limit_ns;
@@ -489,7 +568,7 @@ cudaError_t launch_pairs(PairParams& p, const FfnArgs& a, cudaStream_t stream) {
       pair_kernel<kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize,
       kSmem);
   if (e != cudaSuccess) return e;
-  return launch_pdl(pair_kernel<kAct>, dim3(2 * pairs), dim3(kThreads),
+  return launch_pdl(pair_kernel<kAct>, dim3(2 * s.pairs), dim3(kThreads),
                     kSmem, stream, p);
 }
 
@@ -499,12 +578,22 @@ cudaError_t launch_ffn_fwd(const FfnArgs& a, cudaStream_t stream) {
   if (ffn_few_rows(a.tokens)) return launch_ffn_rows(a, stream);
   PairParams p;
   memset(&p, 0, sizeof(p));
-  if (!make_map(&p.x, a.x, a.tokens, a.dim, a.x_row, kHalf) ||
-      !make_map(&p.w[0], a.w_gate, a.hidden, a.dim, a.dim, kHalf) ||
-      !make_map(&p.w[1], a.w_up, a.hidden, a.dim, a.dim, kHalf))
-    return cudaErrorInvalidValue;
   p.kind[0] = p.kind[1] = kFwd;
-  p.tile[0] = make_tiles(a.tokens, a.hidden, kHalf, 1, up(a.dim, kStep));
+  double best = 0.0;
+  for (int narrow = 0; narrow < 2; ++narrow) {
+    const Tiles t = make_tiles(a.tokens, a.hidden, kHalf, 1, up(a.dim, kStep),
+                               narrow);
+    const double time = share(t, p.tile[1], a.sms).time;
+    if (narrow == 0 || time < best) {
+      best = time;
+      p.tile[0] = t;
+    }
+  }
+  const int w_rows = kHalf >> p.tile[0].narrow;
+  if (!make_map(&p.x, a.x, a.tokens, a.dim, a.x_row, kHalf) ||
+      !make_map(&p.w[0], a.w_gate, a.hidden, a.dim, a.dim, w_rows) ||
+      !make_map(&p.w[1], a.w_up, a.hidden, a.dim, a.dim, w_rows))
+    return cudaErrorInvalidValue;
   uint16_t* out[3] = {a.h, a.g, a.u};
   p.save = a.g != nullptr;
   for (int i = 0; i < (p.save ? 3 : 1); ++i)
@@ -527,32 +616,40 @@ cudaError_t launch_ffn_bwd(const FfnBwdArgs& b, cudaStream_t stream) {
   if (e != cudaSuccess) return e;
   PairParams p;
   memset(&p, 0, sizeof(p));
-  // dx reads dg and du in boxes of 128 rows, dW in boxes of 64: 64 rows twice
-  // where either could be read
   const int kinds = b.dw_gate != nullptr ? 2 : 1;
-  if (!make_map(&p.x, a.x, a.tokens, a.dim, a.x_row, kStep) ||
-      !make_map(&p.w[0], a.w_gate, a.hidden, a.dim, a.dim, kStep) ||
-      !make_map(&p.w[1], a.w_up, a.hidden, a.dim, a.dim, kStep) ||
-      !make_map(&p.d[0], b.dg, a.tokens, a.hidden, a.hidden, kStep) ||
-      !make_map(&p.d[1], b.du, a.tokens, a.hidden, a.hidden, kStep))
-    return cudaErrorInvalidValue;
   p.half_steps = up(a.hidden, kStep);
-  const Tiles dx =
-      make_tiles(a.tokens, a.dim, 2 * kHalf, 1, 2 * p.half_steps);
-  const Tiles dw =
-      make_tiles(a.hidden, a.dim, 2 * kHalf, 2, up(a.tokens, kStep));
-  // the tiles with the longer sums first
-  const int first = kinds == 2 && dw.steps > dx.steps ? 1 : 0;
-  p.tile[first] = dx;
-  p.kind[first] = kDx;
-  if (kinds == 2) {
-    p.tile[1 - first] = dw;
+  // the tiles with the longer sums first, each kind as wide as ends first
+  double best = 0.0;
+  for (int narrow = 0; narrow < 4; ++narrow) {
+    const Tiles dx = make_tiles(a.tokens, a.dim, 2 * kHalf, 1,
+                                2 * p.half_steps, narrow & 1);
+    Tiles dw = make_tiles(a.hidden, a.dim, 2 * kHalf, 2, up(a.tokens, kStep),
+                          narrow >> 1);
+    if (kinds == 1) dw.count = 0;
+    const int first = kinds == 2 && dw.steps > dx.steps ? 1 : 0;
+    const Tiles& a0 = first ? dw : dx;
+    const Tiles& a1 = first ? dx : dw;
+    const double time = share(a0, a1, a.sms).time;
+    if (narrow > 0 && time >= best) continue;
+    best = time;
+    p.tile[0] = a0;
+    p.tile[1] = a1;
+    p.kind[first] = kDx;
     p.kind[1 - first] = kDw;
-  } else {
-    p.tile[1] = dx;
-    p.tile[1].count = 0;
-    p.kind[1] = kDw;
   }
+  const Tiles& dx = p.tile[p.kind[1] == kDx];
+  const Tiles& dw = p.tile[p.kind[1] == kDw];
+  const int64_t M = a.tokens, F = a.hidden, D = a.dim;
+  p.dim_boxes = D % 64 == 0;
+  p.hidden_boxes = F % 64 == 0;
+  if (!make_column_map(&p.x, a.x, M, D, a.x_row, 2 - dw.narrow) ||
+      !make_column_map(&p.w[0], a.w_gate, F, D, D, 2 - dx.narrow) ||
+      !make_column_map(&p.w[1], a.w_up, F, D, D, 2 - dx.narrow) ||
+      !make_map(&p.d[0], b.dg, M, F, F, kHalf) ||
+      !make_map(&p.d[1], b.du, M, F, F, kHalf) ||
+      !make_column_map(&p.dt[0], b.dg, M, F, F, 2) ||
+      !make_column_map(&p.dt[1], b.du, M, F, F, 2))
+    return cudaErrorInvalidValue;
   if (!make_map(&p.out[0], b.dx, a.tokens, a.dim, a.dim, kHalf) ||
       (kinds == 2 &&
        (!make_map(&p.out[1], b.dw_gate, a.hidden, a.dim, a.dim, kHalf) ||

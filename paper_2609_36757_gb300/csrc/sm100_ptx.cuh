@@ -370,6 +370,18 @@ __device__ __forceinline__ void tma_load_2d_pair(const CUtensorMap* map,
       "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1)
       : "memory");
 }
+// The same for three axes.
+__device__ __forceinline__ void tma_load_3d_pair(const CUtensorMap* map,
+                                                 void* dst, uint32_t bar,
+                                                 int32_t c0, int32_t c1,
+                                                 int32_t c2) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile."
+      "mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
+          smem_addr(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+      : "memory");
+}
 // Allocation and release by one whole warp of each CTA of the pair.
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* dst_smem,
                                                 uint32_t ncols) {
