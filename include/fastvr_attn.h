@@ -284,8 +284,9 @@ FASTVR_API fastvr_status_t fastvr_debug_inject_stall(fastvr_plan_t plan,
                                                      uint64_t wait_limit_ns);
 
 /* Device-side failures of the calls without a plan (the one-shot forward
- * fastvr_blockcausal_attn_fwd, the backward fastvr_blockcausal_attn_bwd and
- * the allocation-free fastvr_chunk_attn_fwd_static):
+ * fastvr_blockcausal_attn_fwd, the backward fastvr_blockcausal_attn_bwd,
+ * the allocation-free fastvr_chunk_attn_fwd_static, and the cross attention
+ * and gated feed-forward of fastvr_block.h):
  * a bounded wait that gave up — or, in the debug library, a failed index
  * check — is recorded in a status word of the current device, shared by all
  * such calls on it.  This call waits for the device to finish (it
@@ -296,6 +297,7 @@ FASTVR_API fastvr_status_t fastvr_get_device_status(void);
 
 /* Failure-detection hook (tests) for the calls without a plan, process-wide:
  * stall != 0 makes every following one-shot forward and backward launch
+ * (and those of the cross attention's and gated feed-forward's tile kernels)
  * wait, in its MMA-issuing warp, on a barrier that nothing arrives on; the
  * bounded wait runs out after wait_limit_ns (0 = the 4 s default), every
  * role stops, in-flight copies and MMAs are drained, tensor memory is

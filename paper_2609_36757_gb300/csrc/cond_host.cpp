@@ -48,7 +48,7 @@ fastvr_status_t check_cross(const fastvr_cross_config_t* c) {
   const int64_t most = c->q_tokens > c->kv_tokens ? c->q_tokens : c->kv_tokens;
   if (c->q_tokens > INT32_MAX / 2 || c->kv_tokens > INT32_MAX / 2 ||
       heads < 0 || mul(heads, (most + 127) / 128) < 0 ||
-      mul(heads, (most + 127) / 128) > INT32_MAX / 2)
+      mul(heads, (most + 127) / 128) > INT32_MAX / 4)
     return FASTVR_ERR_INVALID_ARG;
   return FASTVR_OK;
 }

@@ -611,7 +611,7 @@ cudaError_t launch_ffn_bwd(const FfnBwdArgs& b, cudaStream_t stream) {
                      : a.act == kActGelu ? slope_kernel<kActGelu>
                                          : slope_kernel<kActGeluTanh>;
   const cudaError_t e = launch_pdl(
-      slope, dim3((unsigned)std::min<int64_t>(up(n, 256), a.sms * 8)),
+      slope, dim3((unsigned)std::min<int64_t>((n + 255) / 256, a.sms * 8)),
       dim3(256), 0, stream, b);
   if (e != cudaSuccess) return e;
   PairParams p;
