@@ -52,10 +52,13 @@ constexpr int kThreads = 384;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint64_t kDefaultWaitLimitNs = 4000000000ull;
 constexpr int kWarpA = 8, kMmaWarp = 9, kWarpB = 10, kRelayWarp = 11;
-// Named barriers of the hand-offs to the MMA warp.
+// Named barriers of the hand-offs to the MMA warp.  dq's dS has one for even and
+// one for odd steps: its next S and dP are issued before the MMA warp waits for
+// this dS, so a compute warp may hand over the next one while another still works
+// on this one, and two arrivals of one warp would stand for both.
 constexpr int kBarP = 1, kBarDS = 2;
-constexpr int kBarRing = 3;  // + ring's first + stage
-constexpr int kBars = 14;
+constexpr int kBarRing = 4;  // + ring's first + stage
+constexpr int kBars = 15;
 constexpr int kComputeHandoff = 9 * 32;
 constexpr int kRelayHandoff = 2 * 32;
 
@@ -227,6 +230,7 @@ __device__ __forceinline__ void relay_release(Shared* S) {
     if (__any_sync(~0u, *abort != 0)) {
       compute_arrive(kBarP);
       compute_arrive(kBarDS);
+      compute_arrive(kBarDS + 1);
       for (int id = kBarRing; id < kBars; ++id) relay_arrive(id);
     }
     if (__any_sync(~0u, global_timer_ns() - t0 > 3 * S->wait_limit_ns)) break;
@@ -782,7 +786,7 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
         scores(s + 1, qc, false, j + 1 == u.n - 1);
       else if (have_next)
         scores(s + 1, qc + 1, true, nu.n == 1);
-      compute_sync(kBarDS);
+      compute_sync(kBarDS + (s & 1));
       tc_fence_after();
       mma_tn<D>(base, tmem + 256, tmem + dp_col(s),
                 at(RK::off, RK::depth, s), j > 0);
@@ -883,7 +887,7 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
         tmem_st16(row_t + cp + 16, pk);
         tmem_wait_st();
         tc_fence_before();
-        compute_arrive(kBarDS);
+        compute_arrive(kBarDS + (s & 1));
       }
       owed = dst;
       owed_in = row < p.q_tokens;
@@ -979,17 +983,19 @@ int64_t pad_rows(int64_t n) { return (n + kT - 1) / kT * kT; }
 // asked for on the host, possibly without one.
 constexpr int kSms = 152;
 
-// Ranges of a key tile's `steps` query tiles: the number that ends first, a CTA
-// taking about two steps' time to start and to end and a part's results about
-// a quarter of one to join, over entries that see all keys and half of them.
-int key_parts(int64_t ctas, int64_t steps) {
+// Ranges of a key tile's `steps` query tiles, four at most: the number that ends
+// first, a CTA taking about two steps' time to start and to end and a part's
+// results about a quarter of one to join.  Three for 96 tiles of 96 steps (229 us
+// with dq, 238 without ranges, 259 with six), three for 48 of 52 (60, 83 and 67),
+// four for 16 of 52 (40, 69 and 39).
+int key_parts(int64_t tiles, int64_t steps) {
   int best = 1;
   double least = 1e300;
-  for (int s = 1; s <= 32 && s <= steps; ++s) {
-    const double waves = (double)((ctas * s + kSms - 1) / kSms) +
-                         (double)((ctas * s / 2 + kSms - 1) / kSms);
-    const double cost = waves * ((double)((steps + s - 1) / s) + 2.0) +
-                        (s > 1 ? 2.0 + 0.25 * (double)ctas * s / kSms : 0.0);
+  for (int s = 1; s <= 4 && s <= steps; ++s) {
+    const double waves = (double)((tiles * s + kSms - 1) / kSms);
+    const double cost =
+        waves * ((double)((steps + s - 1) / s) + 2.0) +
+        (s > 1 ? 2.0 + 0.25 * (double)(tiles * s) / kSms : 0.0);
     if (cost < least) {
       least = cost;
       best = s;
@@ -997,8 +1003,8 @@ int key_parts(int64_t ctas, int64_t steps) {
   }
   return best;
 }
-
-// CTAs of dq to an SM: few enough units in each to fill the end of a launch.
+// CTAs of dq to an SM: few enough units in each to fill the end of a launch, with
+// one 3 to 5 % more, with three no less.
 constexpr int kDqWaves = 2;
 
 struct ScratchLayout {
@@ -1009,8 +1015,10 @@ ScratchLayout layout(int64_t batch, int64_t heads, int64_t kv_heads, int64_t d,
                      int64_t q_tokens, int64_t kv_tokens) {
   ScratchLayout l;
   l.rows = batch * heads * pad_rows(q_tokens);
-  const int64_t tiles = batch * kv_heads * (pad_rows(kv_tokens) / kT);
-  l.parts = key_parts(tiles, heads / kv_heads * (pad_rows(q_tokens) / kT));
+  const int64_t k_tiles = pad_rows(kv_tokens) / kT;
+  const int64_t q_tiles = pad_rows(q_tokens) / kT;
+  const int64_t tiles = batch * kv_heads * k_tiles;
+  l.parts = key_parts(tiles, heads / kv_heads * q_tiles);
   l.part = l.parts > 1 ? l.parts * tiles * kT * d : 0;
   return l;
 }

@@ -287,3 +287,24 @@ def test_cross_rows_are_independent_of_the_path():
         torch.testing.assert_close(l1[..., 0], lse[..., i], atol=2e-4, rtol=0)
         torch.testing.assert_close(one[:, 0].float(), many[:, i].float(),
                                    atol=2 * (2 * R + 2 * E) * 4.5, rtol=0)
+
+
+@pytest.mark.parametrize("case", [(1, 2000, 512, 12, 12, 128, None),
+                                  (3, 1100, 130, 16, 4, 64, [130, 64, 2])],
+                         ids=str)
+def test_cross_bwd_many_times(case):
+    """dq's units follow one another without a gap, its warps at their own pace:
+    every one of many calls gives the first one's bits and no wait runs out."""
+    from paper_2609_36757_gb300 import fastvr as FV
+    q, k, v, do, lens = (t.cuda() if torch.is_tensor(t) else t
+                         for t in make(case, 14))
+    cfg, kv_len = FV.make_cross_config(), cuda_len(lens)
+    out, lse = FV.cross_attention(cfg, q, k, v, kv_len, want_lse=True)
+    first = FV.cross_attention_bwd(cfg, q, k, v, out, do, lse, kv_len)
+    differ = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(2000):
+        got = FV.cross_attention_bwd(cfg, q, k, v, out, do, lse, kv_len)
+        for a, b in zip(got, first):
+            differ += (a != b).sum()
+    assert int(differ) == 0
+    assert FV.fastvr_get_device_status() == FV.FASTVR_OK
