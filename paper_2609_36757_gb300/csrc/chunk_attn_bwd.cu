@@ -73,6 +73,13 @@ constexpr int kBarDS = 2;
 constexpr int kBarRing0 = 3;  // + stage, up to kMaxStages
 constexpr int kBarRing1 = 6;  // + stage, up to kStages1
 constexpr int kBarStaged = 8;  // the compute warps' output tiles are staged
+// dQ's dS of odd steps: its next S and dP are issued before the MMA warp waits
+// for this step's dS, so a compute warp may hand over the next one while another
+// still works on this one; on one barrier its two arrivals would stand for both.
+constexpr int kBarDSOdd = 9;
+__device__ __forceinline__ int dq_ds_bar(int j) {
+  return j & 1 ? kBarDSOdd : kBarDS;
+}
 constexpr int kComputeHandoff = 9 * 32;
 constexpr int kRelayHandoff = 2 * 32;
 constexpr uint32_t kTmemCols = 512;
@@ -733,7 +740,7 @@ dq_kernel(const __grid_constant__ BwdParams p) {
         mma_commit_warp(&S->dp_ready[(j + 1) & 1]);
         mma_commit_warp(&S->empty[1][v_stn]);  // V_{j+1} read for the last time
       }
-      compute_sync(kBarDS);
+      compute_sync(dq_ds_bar(j));
       tc_fence_after();
       mma_tn<D>(sbase, tmem, 256, dq_dp_col(j), L::ring(k_st, 0, 0), j > 0);  // dQ
       mma_commit_warp(&S->empty[0][k_st]);  // K_j read for the last time
@@ -805,14 +812,14 @@ dq_kernel(const __grid_constant__ BwdParams p) {
       tmem_st16(row_t + cp + 16, pk);
       tmem_wait_st();
       tc_fence_before();
-      compute_arrive(kBarDS);
+      compute_arrive(dq_ds_bar(j));
       ++ds_arr;
     }
     // After a failed wait the remaining hand-offs are still made (with
     // undefined contents), so that the MMA warp never waits for an arrival
     // that does not come.
     for (; p_arr < n; ++p_arr) compute_arrive(kBarP);
-    for (; ds_arr < n; ++ds_arr) compute_arrive(kBarDS);
+    for (; ds_arr < n; ++ds_arr) compute_arrive(dq_ds_bar(ds_arr));
     // dQ is staged in the first K stage (free once o_full has completed)
     // and leaves as TMA stores; rows past the sequence are not written.
     uint8_t* const tiles[1] = {smem + L::ring(0, 0, 0)};
