@@ -5,6 +5,9 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
+#include <mutex>
+
 #include "fastvr_internal.h"
 #include "fastvr_plan.h"
 
@@ -34,6 +37,40 @@ using fastvr::aligned16;
 using fastvr::aligned4;
 using fastvr::mul;
 using fastvr::to_stream;
+
+// The current device: what the calls ask of it, found once.
+constexpr int kMaxDevices = 64;
+struct Device {
+  std::atomic<bool> ready;
+  int sms;
+  int* word;
+};
+Device g_devices[kMaxDevices];
+std::mutex g_devices_mutex;
+
+template <class Args>
+fastvr_status_t use_device(Args* a) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return FASTVR_ERR_CUDA;
+  a->device = dev;
+  if (dev < 0 || dev >= kMaxDevices) {
+    a->sms = fastvr::device_sms();
+    a->status = nullptr;
+    return fastvr::check_device();
+  }
+  Device& d = g_devices[dev];
+  if (!d.ready.load(std::memory_order_acquire)) {
+    std::lock_guard<std::mutex> lock(g_devices_mutex);
+    const fastvr_status_t st = fastvr::check_device();
+    if (st != FASTVR_OK) return st;
+    d.sms = fastvr::device_sms();
+    d.word = fastvr::device_status_word();
+    d.ready.store(true, std::memory_order_release);
+  }
+  a->sms = d.sms;
+  a->status = d.word;
+  return FASTVR_OK;
+}
 
 fastvr_status_t check_cross(const fastvr_cross_config_t* c) {
   if (c == nullptr || c->batch < 1 || c->q_tokens < 1 || c->kv_tokens < 1 ||
@@ -143,7 +180,7 @@ fastvr_status_t fastvr_cross_attn_fwd(
       !check_tensor(*cfg, out, out_str, true, true, &a.o_str) ||
       !aligned4(kv_len) || !aligned4(lse) || out == q || out == k || out == v)
     return FASTVR_ERR_INVALID_ARG;
-  const fastvr_status_t st = fastvr::check_device();
+  const fastvr_status_t st = use_device(&a);
   if (st != FASTVR_OK) return st;
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);
@@ -151,8 +188,6 @@ fastvr_status_t fastvr_cross_attn_fwd(
   a.o = static_cast<uint16_t*>(out);
   a.lse = lse;
   a.kv_len = kv_len;
-  a.status = fastvr::device_status_word();
-  a.sms = fastvr::device_sms();
   return fastvr::launch_cross_attn(a, to_stream(stream)) == cudaSuccess
              ? FASTVR_OK
              : FASTVR_ERR_CUDA;
@@ -206,7 +241,7 @@ fastvr_status_t fastvr_cross_attn_bwd(
                                        cfg->head_dim, cfg->q_tokens,
                                        cfg->kv_tokens))
     return FASTVR_ERR_CAPACITY;
-  const fastvr_status_t st = fastvr::check_device();
+  const fastvr_status_t st = use_device(&a.f);
   if (st != FASTVR_OK) return st;
   a.f.q = static_cast<const uint16_t*>(q);
   a.f.k = static_cast<const uint16_t*>(k);
@@ -214,8 +249,6 @@ fastvr_status_t fastvr_cross_attn_bwd(
   a.f.o = static_cast<uint16_t*>(const_cast<void*>(out));
   a.f.lse = const_cast<float*>(lse);
   a.f.kv_len = kv_len;
-  a.f.status = fastvr::device_status_word();
-  a.f.sms = fastvr::device_sms();
   a.dout = static_cast<const uint16_t*>(dout);
   a.dq = static_cast<uint16_t*>(dq);
   a.dk = static_cast<uint16_t*>(dk);
@@ -241,13 +274,11 @@ fastvr_status_t fastvr_gated_ffn_fwd(const fastvr_ffn_config_t* cfg,
   const void* in[] = {x, w_gate, w_up};
   for (const void* p : in)
     if (p == h || p == g || p == u) return FASTVR_ERR_INVALID_ARG;
-  const fastvr_status_t st = fastvr::check_device();
+  const fastvr_status_t st = use_device(&a);
   if (st != FASTVR_OK) return st;
   a.h = static_cast<uint16_t*>(h);
   a.g = static_cast<uint16_t*>(g);
   a.u = static_cast<uint16_t*>(u);
-  a.status = fastvr::device_status_word();
-  a.sms = fastvr::device_sms();
   return fastvr::launch_ffn_fwd(a, to_stream(stream)) == cudaSuccess
              ? FASTVR_OK
              : FASTVR_ERR_CUDA;
@@ -281,12 +312,10 @@ fastvr_status_t fastvr_gated_ffn_bwd(
   for (const void* p : {dh, x, w_gate, w_up, g, u})
     if (p == scratch) return FASTVR_ERR_INVALID_ARG;
   if (scratch_bytes < 2 * ffn_region(*cfg)) return FASTVR_ERR_CAPACITY;
-  const fastvr_status_t st = fastvr::check_device();
+  const fastvr_status_t st = use_device(&a.f);
   if (st != FASTVR_OK) return st;
   a.f.g = static_cast<uint16_t*>(const_cast<void*>(g));
   a.f.u = static_cast<uint16_t*>(const_cast<void*>(u));
-  a.f.status = fastvr::device_status_word();
-  a.f.sms = fastvr::device_sms();
   a.dh = static_cast<const uint16_t*>(dh);
   a.dx = static_cast<uint16_t*>(dx);
   a.dw_gate = static_cast<uint16_t*>(dw_gate);

@@ -748,8 +748,7 @@ cudaError_t launch_tiles(const CrossArgs& a, cudaStream_t stream) {
   p.wait_limit_ns = a.wait_limit_ns;
   const int smem = Layout<D>::bytes;
   static_assert(Layout<D>::bytes <= 227 * 1024, "shared memory");
-  const cudaError_t e = cudaFuncSetAttribute(
-      cross_tile_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const cudaError_t e = allow_smem<cross_tile_kernel<D>>(smem, a.device);
   if (e != cudaSuccess) return e;
   return launch_pdl(cross_tile_kernel<D>, dim3(grid),
                     dim3(kThreads), smem, stream, p);

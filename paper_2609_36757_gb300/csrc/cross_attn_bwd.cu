@@ -1090,8 +1090,7 @@ cudaError_t launch_d(const CrossBwdArgs& a, cudaStream_t stream) {
       make_div((uint32_t)row_tiles), p.by_heads);
   constexpr int smem = std::max(DkdvLayout<D>::bytes, DqLayout<D>::bytes);
   if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(
-        grads_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    e = allow_smem<grads_kernel<D>>(smem, f.device);
   if (e != cudaSuccess) return e;
   const int tiles = f.batch * f.kv_heads * p.k_tiles;
   p.dkdv_ctas = tiles * p.parts;

@@ -299,8 +299,7 @@ cudaError_t launch_d(const CrossArgs& a, cudaStream_t stream) {
          ctas * kWarps * kKeys < a.kv_tokens)
     ctas *= 2;
   const int smem = (int)sizeof(RowsShared<D>);
-  const cudaError_t e = cudaFuncSetAttribute(
-      cross_rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const cudaError_t e = allow_smem<cross_rows_kernel<D>>(smem, a.device);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * ctas));

@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "vec_math.cuh"
 
 namespace fastvr {
@@ -320,6 +322,21 @@ cudaError_t launch_q4_attn(const Q4AttnParams& p, int sms,
 
 // ------------------------------------------- cross attention, feed-forward
 
+#ifdef __CUDACC__
+// Dynamic shared memory of a kernel past 48 KB, set once per device: a decode
+// step's host time counts, and the runtime call costs about a microsecond.
+template <auto kKernel>
+inline cudaError_t allow_smem(int bytes, int device) {
+  static std::atomic<uint64_t> done{0};
+  const uint64_t bit = device >= 0 && device < 64 ? 1ull << device : 0;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(
+      kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
+}
+#endif
+
 struct CrossArgs {
   const uint16_t *q, *k, *v;  // bfloat16, strides in elements
   uint16_t* o;
@@ -331,7 +348,7 @@ struct CrossArgs {
   int* status;                // device status word or null (not reported)
   int32_t inject_stall;       // failure-detection test hook
   uint64_t wait_limit_ns;     // 0 = kernel default
-  int sms;
+  int sms, device;
 };
 cudaError_t launch_cross_attn(const CrossArgs& a, cudaStream_t stream);
 
@@ -357,7 +374,7 @@ struct FfnArgs {
   int* status;
   int32_t inject_stall;
   uint64_t wait_limit_ns;
-  int sms;
+  int sms, device;
 };
 cudaError_t launch_ffn_fwd(const FfnArgs& a, cudaStream_t stream);
 

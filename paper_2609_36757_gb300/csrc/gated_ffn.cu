@@ -564,9 +564,7 @@ cudaError_t launch_pairs(PairParams& p, const FfnArgs& a, cudaStream_t stream) {
   p.status = a.status;
   p.inject_stall = a.inject_stall;
   p.wait_limit_ns = a.wait_limit_ns;
-  const cudaError_t e = cudaFuncSetAttribute(
-      pair_kernel<kAct>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-      kSmem);
+  const cudaError_t e = allow_smem<pair_kernel<kAct>>(kSmem, a.device);
   if (e != cudaSuccess) return e;
   return launch_pdl(pair_kernel<kAct>, dim3(2 * s.pairs), dim3(kThreads),
                     kSmem, stream, p);

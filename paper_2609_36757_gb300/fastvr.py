@@ -1000,11 +1000,11 @@ def gated_ffn(cfg: fastvr_ffn_config_t, x, w_gate, w_up,
     spaced), w_gate and w_up [F, D], bfloat16.  Returns h [..., F], or
     (h, (g, u)) with the projections that gated_ffn_bwd takes."""
     c, row = _ffn_call(cfg, x, w_gate, w_up, ())
-    shape = x.shape[:-1] + (c.hidden,)
-    h = x.new_empty(shape)
+    empty, shape, kind = _torch.empty, x.shape[:-1] + (c.hidden,), x.dtype
+    h = empty(shape, dtype=kind, device=x.device)
     g = u = None
     if want_saved:
-        g, u = x.new_empty(shape), x.new_empty(shape)
+        g, u = (empty(shape, dtype=kind, device=x.device) for _ in "gu")
     fastvr_gated_ffn_fwd(c, x.data_ptr(), row, w_gate.data_ptr(),
                          w_up.data_ptr(), h.data_ptr(), _ptr(g), _ptr(u),
                          _stream_of(x, w_gate, w_up))
