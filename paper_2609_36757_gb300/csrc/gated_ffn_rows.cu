@@ -1,11 +1,12 @@
 // Gated feed-forward of few tokens, h = act(x Wg^T) o (x Wu^T): bound by reading
 // the weights once.
 //
-// A CTA forms 8 columns of h for all tokens.  One warp-level product has 8 rows
+// A CTA forms 8 or 16 columns of h for all tokens.  One warp-level product has 8 rows
 // of Wg over the same 8 of Wu as its 16 rows and 8 tokens as its columns, so a
 // lane ends up with g and u of the same column and token.  The eight warps take
 // 128-byte pieces of the rows in turn (a row's pieces of one pass are 1 KB) and
-// their sums are added through shared memory in order.
+// their sums are added through shared memory in order.  One token of 1536 to 4096
+// takes 6.8 us (25 MB of weights: 3.8 us), 16 tokens 8.7: every CTA reads all of x.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -19,34 +20,45 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kPiece = 64;  // elements of a row that four lanes read
 
-// kTok: blocks of 8 tokens.
-template <int kTok, int kAct>
-__global__ void __launch_bounds__(kWarps * 32)
+// kTok: blocks of 8 tokens; kCols: blocks of 8 columns of a CTA.  With more tokens
+// a CTA takes two, or it would read more of x than of the weights (24 tokens of 1536
+// to 4096 10.4 us with one).  Three CTAs to an SM, for which the compiler spills a
+// little from 17 tokens on: 2048 to 5632 is 352 CTAs, 17.4 us with two to an SM.
+template <int kTok, int kCols, int kAct>
+__global__ void __launch_bounds__(kWarps * 32, 3)
 rows_kernel(const __grid_constant__ FfnArgs a) {
-  __shared__ float part[kWarps][kTok][32][4];
+  __shared__ float part[kWarps][kCols * kTok][32][4];
   pdl_trigger();
   pdl_wait();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int g = lane / 4, t = lane % 4;
-  const int f0 = blockIdx.x * 8;
-  const uint16_t* wg = a.w_gate + (int64_t)(f0 + g) * a.dim;
-  const uint16_t* wu = a.w_up + (int64_t)(f0 + g) * a.dim;
-  float c[kTok][4];
+  const int f0 = blockIdx.x * 8 * kCols;
+  float c[kCols][kTok][4];
 #pragma unroll
-  for (int n = 0; n < kTok; ++n)
+  for (int f = 0; f < kCols; ++f)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c[n][e] = 0.f;
+    for (int n = 0; n < kTok; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[f][n][e] = 0.f;
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  // two pieces of a row at a time: eight loads of weights in flight
-  for (int k0 = warp * kPiece; k0 < a.dim; k0 += 2 * kWarps * kPiece) {
-    uint4 vg[4], vu[4];
+  // eight loads of weights in flight: two pieces of a row, or one of two
+  constexpr int kLoads = 4 / kCols;
+  for (int k0 = warp * kPiece; k0 < a.dim;
+       k0 += kLoads / 2 * kWarps * kPiece) {
+    uint4 vg[kCols][kLoads], vu[kCols][kLoads];
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int k = k0 + (s / 2) * kWarps * kPiece + (s % 2) * 32 + 8 * t;
-      vg[s] = vu[s] = zero;
-      if (k < a.dim) {
-        vg[s] = load_once(wg + k);
-        vu[s] = load_once(wu + k);
+    for (int f = 0; f < kCols; ++f) {
+      const int row = f0 + 8 * f + g;
+      const uint16_t* wg = a.w_gate + (int64_t)row * a.dim;
+      const uint16_t* wu = a.w_up + (int64_t)row * a.dim;
+#pragma unroll
+      for (int s = 0; s < kLoads; ++s) {
+        const int k = k0 + (s / 2) * kWarps * kPiece + (s % 2) * 32 + 8 * t;
+        vg[f][s] = vu[f][s] = zero;
+        if (k < a.dim && row < a.hidden) {
+          vg[f][s] = load_once(wg + k);
+          vu[f][s] = load_once(wu + k);
+        }
       }
     }
 #pragma unroll
@@ -54,37 +66,45 @@ rows_kernel(const __grid_constant__ FfnArgs a) {
       const bool in = n * 8 + g < a.tokens;
       const uint16_t* x = a.x + (int64_t)(n * 8 + g) * a.x_row;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
+      for (int s = 0; s < kLoads; ++s) {
         const int k = k0 + (s / 2) * kWarps * kPiece + (s % 2) * 32 + 8 * t;
         uint4 v = zero;
         if (in && k < a.dim) v = __ldg(reinterpret_cast<const uint4*>(x + k));
-        mma_16x8x16(c[n], vg[s].x, vu[s].x, vg[s].y, vu[s].y, v.x, v.y);
-        mma_16x8x16(c[n], vg[s].z, vu[s].z, vg[s].w, vu[s].w, v.z, v.w);
+#pragma unroll
+        for (int f = 0; f < kCols; ++f) {
+          mma_16x8x16(c[f][n], vg[f][s].x, vu[f][s].x, vg[f][s].y, vu[f][s].y,
+                      v.x, v.y);
+          mma_16x8x16(c[f][n], vg[f][s].z, vu[f][s].z, vg[f][s].w, vu[f][s].w,
+                      v.z, v.w);
+        }
       }
     }
   }
 #pragma unroll
-  for (int n = 0; n < kTok; ++n)
-    *reinterpret_cast<float4*>(part[warp][n][lane]) =
-        make_float4(c[n][0], c[n][1], c[n][2], c[n][3]);
+  for (int f = 0; f < kCols; ++f)
+#pragma unroll
+    for (int n = 0; n < kTok; ++n)
+      *reinterpret_cast<float4*>(part[warp][f * kTok + n][lane]) =
+          make_float4(c[f][n][0], c[f][n][1], c[f][n][2], c[f][n][3]);
   __syncthreads();
-  // Warp n joins token block n: lane (g, t) holds g of column f0 + g for tokens
-  // 2t and 2t + 1, then u.
-  for (int n = warp; n < kTok; n += kWarps) {
+  // Warp i joins block i: lane (g, t) holds g of column 8 f + g for tokens 2t and
+  // 2t + 1 of block n, then u.
+  for (int i = warp; i < kCols * kTok; i += kWarps) {
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float4 v = *reinterpret_cast<const float4*>(part[w][n][lane]);
+      const float4 v = *reinterpret_cast<const float4*>(part[w][i][lane]);
       s[0] += v.x;
       s[1] += v.y;
       s[2] += v.z;
       s[3] += v.w;
     }
+    const int col = f0 + i / kTok * 8 + g;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int64_t tok = n * 8 + 2 * t + e;
-      if (tok >= a.tokens) continue;
-      const int64_t at = tok * a.hidden + f0 + g;
+      const int64_t tok = i % kTok * 8 + 2 * t + e;
+      if (tok >= a.tokens || col >= a.hidden) continue;
+      const int64_t at = tok * a.hidden + col;
       if (a.g != nullptr) {
         a.g[at] = __bfloat16_as_ushort(__float2bfloat16_rn(s[e]));
         a.u[at] = __bfloat16_as_ushort(__float2bfloat16_rn(s[2 + e]));
@@ -95,13 +115,13 @@ rows_kernel(const __grid_constant__ FfnArgs a) {
   }
 }
 
-template <int kTok>
+template <int kTok, int kCols>
 cudaError_t launch_act(const FfnArgs& a, cudaStream_t stream) {
-  const auto kernel = a.act == kActSilu   ? rows_kernel<kTok, kActSilu>
-                      : a.act == kActGelu ? rows_kernel<kTok, kActGelu>
-                                          : rows_kernel<kTok, kActGeluTanh>;
-  return launch_pdl(kernel, dim3(a.hidden / 8), dim3(kWarps * 32), 0, stream,
-                    a);
+  const auto kernel = a.act == kActSilu   ? rows_kernel<kTok, kCols, kActSilu>
+                      : a.act == kActGelu ? rows_kernel<kTok, kCols, kActGelu>
+                                          : rows_kernel<kTok, kCols, kActGeluTanh>;
+  return launch_pdl(kernel, dim3((a.hidden + 8 * kCols - 1) / (8 * kCols)),
+                    dim3(kWarps * 32), 0, stream, a);
 }
 
 }  // namespace
@@ -110,13 +130,13 @@ cudaError_t launch_ffn_rows(const FfnArgs& a, cudaStream_t stream) {
   static_assert(kFfnMaxRows == 32, "a kernel for every number of blocks");
   switch ((a.tokens + 7) / 8) {
     case 1:
-      return launch_act<1>(a, stream);
+      return launch_act<1, 1>(a, stream);
     case 2:
-      return launch_act<2>(a, stream);
+      return launch_act<2, 2>(a, stream);
     case 3:
-      return launch_act<3>(a, stream);
+      return launch_act<3, 2>(a, stream);
     default:
-      return launch_act<4>(a, stream);
+      return launch_act<4, 2>(a, stream);
   }
 }
 
