@@ -324,8 +324,9 @@ __device__ void relay_role(const CrossParams& p, uint8_t* smem, Shared* S,
       const int st = vc % L::kV;
       if ((ok = wait_bar_warp(&S->v_full[st], (vc / L::kV) & 1, S,
                               p.status))) {
-        // A row is 128 bytes of each box; the swizzle stays within rows.
-        if (pvalid < kBN) {
+        // A row is 128 bytes of each box; the swizzle stays within rows.  Without
+        // lengths the rows past the last key lie outside the map: zeros.
+        if (pvalid < kBN && p.kv_len != nullptr) {
           for (int bx = 0; bx < L::kNB; ++bx) {
             uint4* rows = reinterpret_cast<uint4*>(smem + L::v_off +
                                                    st * L::kTile + bx * kBox);

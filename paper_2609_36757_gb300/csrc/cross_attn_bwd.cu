@@ -731,7 +731,8 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
     bool ok = true;
     while (ok && next_unit(p, x, &u)) {
       for (int j = 0; ok && j < u.n; ++j, ++c) {
-        const int valid = u.len - j * kT;
+        // without lengths the rows past the last key lie outside the maps: zeros
+        const int valid = p.kv_len != nullptr ? u.len - j * kT : kT;
         if (j == 0) {
           if (!(ok = ring_landed<RQ>(p, S, r))) break;
           ring_hand<RQ>(r);
