@@ -64,8 +64,8 @@ struct PairParams {
   CUtensorMap out[3];
   Tiles tile[2];              // forward: [0]; backward: those listed first, and
   int32_t kind[2];            // the others
-  // Backward: pairs from `heavy` on (0: none) have one tile fewer of the first
-  // list and take `extra` of the second list before its common rounds.
+  // Pairs from `heavy` on (0: all) have one tile fewer of the first list than the
+  // others and take `extra` of the second list before its common rounds.
   int32_t heavy, extra;
   int32_t half_steps;       // dx: steps of dg Wg
   int32_t save;             // forward: g and u are wanted
@@ -140,7 +140,8 @@ __host__ __device__ inline bool nth_tile(const PairParams& p, int pair,
       if (t >= ahead) return false;
     } else {
       if (p.extra > 0 && pair >= p.heavy) i -= p.extra;
-      t = ahead + pair + i * pairs;
+      // common rounds, the pairs with fewer tiles of the first list first
+      t = ahead + (pair >= p.heavy ? pair - p.heavy : pair + light) + i * pairs;
     }
     if (t >= p.tile[1].count) return false;
   }
@@ -538,26 +539,30 @@ struct Shares {
   double time;
 };
 Shares share(const Tiles& a, const Tiles& b, int sms) {
-  Shares s = {std::min(sms / 2, a.count + b.count), 0, 0, 0.0};
+  const int pairs = std::min(sms / 2, a.count + b.count);
   const double ca = (a.steps + 8) * (a.narrow ? 0.75 : 1.0);
   const double cb = (b.steps + 8) * (b.narrow ? 0.75 : 1.0);
-  const int rest = a.count % s.pairs;
-  if (b.count > 0 && rest > 0) {
-    s.heavy = rest;
-    s.extra = (int)(ca / cb);
-  }
-  const int light = s.pairs - s.heavy;
-  const int ahead = s.extra > 0 ? std::min<int64_t>(b.count, (int64_t)s.extra * light) : 0;
-  for (int p = 0; p < s.pairs; ++p) {
-    int64_t n = (b.count - ahead + s.pairs - 1 - p) / s.pairs;
-    if (s.extra > 0 && p >= s.heavy) {
-      const int own = p - s.heavy;
-      n += std::min(s.extra, (ahead - own + light - 1) / light);
+  const int heavy = a.count % pairs, light = pairs - heavy;
+  Shares best = {pairs, heavy, 0, 0.0};
+  // extra rounds that make up for a tile of the first list, or one more
+  const int most = b.count > 0 && heavy > 0 ? (int)(ca / cb) + 1 : 0;
+  for (int extra = std::max(0, most - 1); extra <= most; ++extra) {
+    const int ahead = (int)std::min<int64_t>(b.count, (int64_t)extra * light);
+    double time = 0.0;
+    for (int p = 0; p < pairs; ++p) {
+      const int own = p >= heavy ? p - heavy : p + light;
+      int64_t n = (b.count - ahead + pairs - 1 - own) / pairs;
+      if (extra > 0 && p >= heavy)
+        n += std::min(extra, (ahead - own + light - 1) / light);
+      time = std::max(time,
+                      (a.count + pairs - 1 - p) / pairs * ca + (double)n * cb);
     }
-    s.time = std::max(
-        s.time, (a.count + s.pairs - 1 - p) / s.pairs * ca + (double)n * cb);
+    if (extra == std::max(0, most - 1) || time < best.time) {
+      best.extra = extra;
+      best.time = time;
+    }
   }
-  return s;
+  return best;
 }
 
 template <int kAct>
