@@ -302,7 +302,8 @@ FASTVR_API fastvr_status_t fastvr_q4_read(fastvr_plan_t plan, int64_t chunk,
  * its lse -infinity.  What k and v hold at t >= T_b (padding, NaN and
  * infinities included) does not matter. */
 typedef struct {
-  int32_t batch, q_tokens, kv_tokens; /* >= 1; a sequence's tokens below 2^30 */
+  int32_t batch, q_tokens, kv_tokens; /* >= 1; batch * heads * (tokens / 128,
+                                         rounded up) below 2^29 for either   */
   int32_t heads, kv_heads;            /* heads a multiple of kv_heads         */
   int32_t head_dim;                   /* 64 or 128                            */
   float softmax_scale;                /* >= 0; 0 = 1 / sqrt(head_dim)         */
@@ -367,8 +368,8 @@ FASTVR_API fastvr_status_t fastvr_cross_attn_bwd(
  *   g = x w_gate^T,  u = x w_up^T,  h = act(g) o u
  * (the down projection of h is a plain product and the caller's). */
 typedef struct {
-  int32_t tokens;     /* >= 1, below 2^30; tokens times dim and times hidden
-                         at most 2^44                                        */
+  int32_t tokens;     /* 1 .. 2^28; tokens times dim and times hidden at most
+                         2^44                                                */
   int32_t dim;        /* a multiple of 8, 8 .. 65536                          */
   int32_t hidden;     /* a multiple of 8, 8 .. 262144                         */
   int32_t activation; /* FASTVR_ACT_*                                         */

@@ -125,7 +125,8 @@ fastvr::CrossArgs cross_args(const fastvr_cross_config_t& c) {
 }
 
 bool valid_ffn(const fastvr_ffn_config_t* c) {
-  return c != nullptr && c->tokens >= 1 && c->tokens <= INT32_MAX / 2 &&
+  // A weight's sum runs over all tokens within one bounded wait.
+  return c != nullptr && c->tokens >= 1 && c->tokens <= 1 << 28 &&
          c->dim >= 8 && c->dim <= 65536 && c->dim % 8 == 0 && c->hidden >= 8 &&
          c->hidden <= 262144 && c->hidden % 8 == 0 &&
          // tiles are counted in 32 bits

@@ -137,11 +137,13 @@ __device__ __forceinline__ bool next_unit(const CrossParams& p, int& x, int last
   return false;
 }
 // First slot of CTA c: of about equal work to each, a slot weighing its key tiles
-// and one more for its way in and out.  A whole warp's.
+// and one more for its way in and out (of equal numbers, for batches so large that
+// the sums would take longer than they save).  A whole warp's.
+constexpr int kMaxWeighed = 4096;
 __device__ __forceinline__ int first_slot(const CrossParams& p, int c,
                                           int lane) {
   if (p.step > 1) return c;
-  if (p.kv_len == nullptr || c == (int)gridDim.x)
+  if (p.kv_len == nullptr || p.batch > kMaxWeighed || c == (int)gridDim.x)
     return (int)((int64_t)p.all * c / gridDim.x);
   const int per = p.heads * p.slots;  // of a batch entry
   const int chunk = (p.batch + 31) / 32;

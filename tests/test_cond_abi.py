@@ -49,6 +49,7 @@ BWD = dict(q=_at(0), q_str=None, k=_at(1), k_str=None, v=_at(2), v_str=None,
     dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")),
     dict(softmax_scale=float("inf")), dict(q_tokens=1 << 30),
     dict(kv_tokens=1 << 30), dict(batch=1 << 20, heads=1 << 12),
+    dict(batch=1 << 20, heads=1 << 8, q_tokens=257),
 ])
 def test_cross_config_refused(fv, kw):
     c = _cross(fv, **kw)
@@ -130,7 +131,8 @@ FFB = dict(dh=_at(6), x=_at(0), x_row=0, w_gate=_at(1), w_up=_at(2), g=_at(4),
 
 
 @pytest.mark.parametrize("kw", [
-    dict(tokens=0), dict(tokens=1 << 30), dict(dim=0), dict(dim=12),
+    dict(tokens=0), dict(tokens=(1 << 28) + 1), dict(tokens=1 << 30),
+    dict(tokens=1 << 28, dim=65536, hidden=131072), dict(dim=0), dict(dim=12),
     dict(dim=65544), dict(hidden=0), dict(hidden=20), dict(hidden=262152),
     dict(activation=-1), dict(activation=3),
 ])

@@ -53,6 +53,8 @@ CASES = [
     (40, 300, 60, 10, 5, 64, [0, 60, 7, 60] * 10),
     (3, 900, 260, 50, 25, 128, [260, 0, 1]),
     (33, 280, 300, 8, 8, 64, [300, 1, 129] * 11),
+    # more entries than lengths are weighed
+    (4500, 34, 9, 1, 1, 64, [9, 0, 4] * 1500),
 ]
 
 
