@@ -341,8 +341,8 @@ FASTVR_API fastvr_status_t fastvr_cross_attn_bwd_scratch_bytes(
  * prompt the caller sums them), zero at t >= T_b.
  *   D = rowsum(dout o out),  dP = dout v^T,  dS = P o (dP - D)
  *   dq = scale dS k,  dk = scale dS^T q,  dv = P^T dout
- * dk and dv sum over the query heads that share a key head.  P and dS enter
- * the products in bfloat16, sums are float32 in a fixed order (no atomics):
+ * dk and dv sum over the query heads that share a key head.  dS, and P in dv,
+ * enter the products in bfloat16, sums are float32 in a fixed order (no atomics):
  * repeated calls agree bit for bit.  Outputs overlap no input and no other
  * output.  A bounded-wait timeout is reported by fastvr_get_device_status.
  * Errors: INVALID_ARG, CAPACITY (scratch), UNSUPPORTED (head_dim, device),

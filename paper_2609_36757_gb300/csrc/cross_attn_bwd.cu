@@ -46,9 +46,12 @@ namespace fastvr {
 namespace {
 
 using namespace sm100;
-using grad::ds32;
+using grad::exp2_poly;
 using grad::f2;
-using grad::p32;
+using grad::f2_add;
+using grad::f2_fma;
+using grad::f2_mul;
+using grad::f2_split;
 using grad::pack_bf16;
 
 constexpr int kT = 128;          // tile rows (TMEM lanes) and columns
@@ -333,6 +336,65 @@ __device__ __forceinline__ void mma_tn(uint32_t sbase, uint32_t d, uint32_t a,
                 b_lo + (uint32_t)(kk * 2048 >> 4), hi, kIdesc, acc || kk > 0);
 }
 
+// P = 2^(s c2 + nl) for 32 columns, in place as float32 and packed to bfloat16
+// pairs; columns from `hi` on are masked where kMask.  One group of four in eight
+// takes its exponentials on the FMA pipe, as in the one-shot backward.
+template <bool kMask>
+__device__ __forceinline__ void probs32(uint32_t (&s)[32],
+                                        const float4 (&nl)[8], int c0, int hi,
+                                        uint64_t c2x2, uint32_t (&pp)[16]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const float4 a = nl[q];
+    float x[4];
+    f2_split(f2_fma(f2(__uint_as_float(s[4 * q]), __uint_as_float(s[4 * q + 1])),
+                    c2x2, f2(a.x, a.y)),
+             x[0], x[1]);
+    f2_split(f2_fma(f2(__uint_as_float(s[4 * q + 2]),
+                       __uint_as_float(s[4 * q + 3])),
+                    c2x2, f2(a.z, a.w)),
+             x[2], x[3]);
+    if (kMask) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (c0 + 4 * q + u >= hi) x[u] = -INFINITY;
+    }
+    if (!kMask && grad::poly_group(q)) {
+      exp2_poly(x[0], x[1]);
+      exp2_poly(x[2], x[3]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = grad::ex2(x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) s[4 * q + u] = __float_as_uint(x[u]);
+    pp[2 * q] = pack_bf16(x[0], x[1]);
+    pp[2 * q + 1] = pack_bf16(x[2], x[3]);
+  }
+}
+// dS = P (dP - D) for 32 columns: P as probs32 left it, unrounded, so that dS is
+// rounded once; nd holds -D.
+__device__ __forceinline__ void dscores32(const uint32_t (&p)[32],
+                                          const uint32_t (&dp)[32],
+                                          const float4 (&nd)[8],
+                                          uint32_t (&pd)[16]) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const float4 g = nd[q];
+    float r[4];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      f2_split(f2_mul(f2(__uint_as_float(p[4 * q + 2 * u]),
+                         __uint_as_float(p[4 * q + 2 * u + 1])),
+                      f2_add(f2(__uint_as_float(dp[4 * q + 2 * u]),
+                                __uint_as_float(dp[4 * q + 2 * u + 1])),
+                             u == 0 ? f2(g.x, g.y) : f2(g.z, g.w))),
+               r[2 * u], r[2 * u + 1]);
+    pd[2 * q] = pack_bf16(r[0], r[1]);
+    pd[2 * q + 1] = pack_bf16(r[2], r[3]);
+  }
+}
+
 // 32 scaled results of TMEM as bfloat16 to a row.
 __device__ __forceinline__ void store_cols32(uint32_t taddr, float mul,
                                              bool zero, uint16_t* to, bool in,
@@ -521,16 +583,16 @@ __device__ __forceinline__ void dkdv_cta(const BwdParams& p, uint8_t* smem,
       for (int q = 0; q < 8; ++q) la[q] = nl[q];
       if (!(ok = wait_bar_warp(&S->s_ready, j & 1, S, p.status))) break;
       tc_fence_after();
-      uint32_t x0r[32], x1r[32], pb0[16], pb1[16], pk[16];
+      uint32_t x0r[32], x1r[32], y[32], pk[16];
       tmem_ld32(row_t + cs, x0r);
       tmem_ld32(row_t + cs + 32, x1r);
 #pragma unroll
       for (int q = 0; q < 8; ++q) lb[q] = nl[8 + q];
       tmem_wait_ld();
-      p32<false>(x0r, la, 0, 0, 0, c2x2, pb0);
-      tmem_st16(row_t + cs, pb0);
-      p32<false>(x1r, lb, 0, 0, 0, c2x2, pb1);
-      tmem_st16(row_t + cs + 16, pb1);
+      probs32<false>(x0r, la, 0, 0, c2x2, pk);
+      tmem_st16(row_t + cs, pk);
+      probs32<false>(x1r, lb, 0, 0, c2x2, pk);
+      tmem_st16(row_t + cs + 16, pk);
       tmem_wait_st();
       tc_fence_before();
       compute_arrive(kBarP);
@@ -538,14 +600,16 @@ __device__ __forceinline__ void dkdv_cta(const BwdParams& p, uint8_t* smem,
       for (int q = 0; q < 8; ++q) la[q] = nd[q];
       if (!(ok = wait_bar_warp(&S->dp_ready[0], j & 1, S, p.status))) break;
       tc_fence_after();
-      tmem_ld32(row_t + cp, x0r);
-      tmem_ld32(row_t + cp + 32, x1r);
-#pragma unroll
-      for (int q = 0; q < 8; ++q) lb[q] = nd[8 + q];
+      // half by half: there are no registers for P, dP and -D of 64 columns
+      tmem_ld32(row_t + cp, y);
       tmem_wait_ld();
-      ds32(pb0, x0r, la, pk);
+      dscores32(x0r, y, la, pk);
+      tmem_ld32(row_t + cp + 32, y);
       tmem_st16(row_t + cp, pk);
-      ds32(pb1, x1r, lb, pk);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) la[q] = nd[8 + q];
+      tmem_wait_ld();
+      dscores32(x1r, y, la, pk);
       tmem_st16(row_t + cp + 16, pk);
       tmem_wait_st();
       tc_fence_before();
@@ -862,16 +926,16 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
         if (!(ok = wait_bar_warp(&S->s_ready, s & 1, S, p.status))) break;
         tc_fence_after();
         const int hi = u.len - j * kT - 64 * hf;  // visible columns
-        uint32_t x0[32], x1[32], pb0[16], pb1[16], pk[16];
+        uint32_t x0[32], x1[32], y0[32], y1[32], pk[16];
         tmem_ld32(row_t + 64 * hf, x0);
         tmem_ld32(row_t + 64 * hf + 32, x1);
         tmem_wait_ld();
         if (hi < 64) {
-          p32<true>(x0, nl_v, 0, 0, hi, c2x2, pb0);
-          p32<true>(x1, nl_v, 32, 0, hi, c2x2, pb1);
+          probs32<true>(x0, nl_v, 0, hi, c2x2, pk);
+          probs32<true>(x1, nl_v, 32, hi, c2x2, pk);
         } else {
-          p32<false>(x0, nl_v, 0, 0, hi, c2x2, pb0);
-          p32<false>(x1, nl_v, 32, 0, hi, c2x2, pb1);
+          probs32<false>(x0, nl_v, 0, hi, c2x2, pk);
+          probs32<false>(x1, nl_v, 32, hi, c2x2, pk);
         }
         tc_fence_before();
         compute_arrive(kBarP);
@@ -884,12 +948,12 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
           break;
         tc_fence_after();
         const uint32_t cp = dp_col(s) + 64 * hf;
-        tmem_ld32(row_t + cp, x0);
-        tmem_ld32(row_t + cp + 32, x1);
+        tmem_ld32(row_t + cp, y0);
+        tmem_ld32(row_t + cp + 32, y1);
         tmem_wait_ld();
-        ds32(pb0, x0, nd_v, pk);
+        dscores32(x0, y0, nd_v, pk);
         tmem_st16(row_t + cp, pk);
-        ds32(pb1, x1, nd_v, pk);
+        dscores32(x1, y1, nd_v, pk);
         tmem_st16(row_t + cp + 16, pk);
         tmem_wait_st();
         tc_fence_before();

@@ -11,8 +11,8 @@ Bounds, with u = 2^-24 (float32) and r = 2^-8 (bfloat16, half a step):
   out = sum p v / sum p: (r + 2 (ds + e)) sum p |v|, and r of itself;
   D = dout.out takes out as it was rounded: sum |dout| (bound of out);
   dP: d u of its absolute terms;
-  dS = p (dP - D): (2 r + 2 (ds + e)) of its absolute value (p and dS in
-      bfloat16) and p times the errors of dP and D;
+  dS = p (dP - D), p unrounded here: (r + 2 (ds + e)) of its absolute value
+      and p times the errors of dP and D;
   dq, dk, dv: these through their sums, n u of the absolute terms for a
       float32 sum of n terms, and r of the result."""
 import numpy as np
@@ -99,7 +99,7 @@ def bounds(q, k, v, do, lens, scale):
             dp = g @ vv.T
             D = (g * out[b, :, h]).sum(-1, keepdims=True)
             s = p * (dp - D)
-            es = (2 * R + 2 * (ds + E)) * np.abs(s) + p * (
+            es = (R + 2 * (ds + E)) * np.abs(s) + p * (
                 (d + 4) * U * (np.abs(g) @ np.abs(vv).T) +
                 (np.abs(g) * b_out[b, :, h]).sum(-1, keepdims=True))
             b_g[0][b, :, h] = scale * (es @ np.abs(kk) +
