@@ -1077,6 +1077,9 @@ int key_parts(int64_t tiles, int64_t steps) {
 // one 3 to 5 % more, with three no less.
 constexpr int kDqWaves = 2;
 
+// Parts are written in pieces of 32 bytes; the caller's scratch lies on 16.
+constexpr uintptr_t kPartAlign = 32;
+
 struct ScratchLayout {
   int64_t rows, part;  // floats of one row vector, of dk's (dv's) parts
   int parts;
@@ -1118,7 +1121,8 @@ cudaError_t launch_d(const CrossBwdArgs& a, cudaStream_t stream) {
   float* delta = lse2 + l.rows;
   p.lse2 = lse2;
   p.delta = delta;
-  p.dk_part = delta + l.rows;
+  p.dk_part = reinterpret_cast<float*>(
+      ((uintptr_t)(delta + l.rows) + kPartAlign - 1) & ~(kPartAlign - 1));
   p.dv_part = p.dk_part + l.part;
   p.parts = l.parts;
   p.dq = a.dq;
@@ -1180,7 +1184,8 @@ size_t cross_bwd_scratch_floats(int32_t batch, int32_t heads, int32_t kv_heads,
                                 int32_t kv_tokens) {
   const ScratchLayout l =
       layout(batch, heads, kv_heads, head_dim, q_tokens, kv_tokens);
-  return (size_t)(2 * l.rows + 2 * l.part);
+  const int64_t pad = l.part > 0 ? (kPartAlign - 16) / sizeof(float) : 0;
+  return (size_t)(2 * l.rows + 2 * l.part + pad);
 }
 
 cudaError_t launch_cross_attn_bwd(const CrossBwdArgs& a, cudaStream_t stream) {

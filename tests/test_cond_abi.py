@@ -116,6 +116,14 @@ def test_cross_scratch(fv):
              **{**BWD, "scratch_bytes": n - 1})
 
 
+def test_cross_scratch_on_16_bytes_has_room_for_parts_on_32(fv):
+    """Scratch lies on 16 bytes; partial sums are written 32 bytes at a time."""
+    c = fv.fastvr_cross_config_t(1, 700, 640, 3, 3, 128, 0.0)
+    rows = 2 * 3 * 768 * 4
+    n = fv.fastvr_cross_attn_bwd_scratch_bytes(c)
+    assert n > rows and (n - rows) % 32 == 16
+
+
 def _ffn(fv, **kw):
     c = fv.make_ffn_config("gelu")
     for n, x in {**dict(tokens=5, dim=16, hidden=24), **kw}.items():

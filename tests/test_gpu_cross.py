@@ -310,3 +310,31 @@ def test_cross_bwd_many_times(case):
             differ += (a != b).sum()
     assert int(differ) == 0
     assert FV.fastvr_get_device_status() == FV.FASTVR_OK
+
+
+@pytest.mark.parametrize("at", [0, 4, 8, 12])
+@pytest.mark.parametrize("d", [64, 128])
+def test_cross_bwd_scratch_on_any_16_bytes(d, at):
+    """Split sums in scratch that begins `at` floats past a boundary."""
+    from paper_2609_36757_gb300 import fastvr as FV
+    q, k, v, do, _ = (t.cuda() if torch.is_tensor(t) else t for t in
+                      make((1, 700, 640, 3, 3, d, None), 15))
+    k, v = k.contiguous(), v.contiguous()
+    cfg = FV.make_cross_config()
+    out, lse = FV.cross_attention(cfg, q, k, v, want_lse=True)
+    want = FV.cross_attention_bwd(cfg, q, k, v, out, do, lse)
+    c = FV._cross_call(cfg, q, k, v, None)[0]
+    n = FV.fastvr_cross_attn_bwd_scratch_bytes(c)
+    assert n > 2 * 3 * 768 * 4  # there are parts
+    back = torch.full((n // 4 + 32,), 7.0, device="cuda")
+    scratch = back[at:at + n // 4]
+    got = [torch.empty_like(t) for t in want]
+    FV.fastvr_cross_attn_bwd(
+        c, q.data_ptr(), None, k.data_ptr(), None, v.data_ptr(), None, 0,
+        out.data_ptr(), None, do.data_ptr(), None, lse.data_ptr(),
+        got[0].data_ptr(), None, got[1].data_ptr(), None, got[2].data_ptr(),
+        None, scratch.data_ptr(), n, torch.cuda.current_stream().cuda_stream)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    scratch.fill_(7.0)
+    assert bool((back == 7.0).all())
