@@ -190,10 +190,21 @@ __device__ __forceinline__ void stage_row32(uint8_t* box, int r, int c,
 __device__ __forceinline__ void box_sync(int hf) {
   asm volatile("bar.sync %0, 128;" ::"r"(1 + hf) : "memory");
 }
-// The box may be written again / goes out to (col, row) of a map.
-__device__ __forceinline__ void box_begin(int hf, bool leader) {
+// The box may be written again / goes out to (col, row) of a map.  The first
+// answers whether the four warps' waits have all ended well: where a wait ran out
+// for some of them, none goes on, or those would wait for the others here.
+__device__ __forceinline__ bool box_begin(int hf, bool leader, bool ok) {
   if (leader) bulk_wait_read0();
-  box_sync(hf);
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, 0;\n\t"
+      "bar.red.and.pred q, %2, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"((uint32_t)ok), "r"(1 + hf)
+      : "memory");
+  return all != 0;
 }
 __device__ __forceinline__ void box_end(const CUtensorMap* map, uint8_t* box,
                                         int hf, bool leader, int col, int row,
@@ -354,9 +365,10 @@ pair_kernel(const __grid_constant__ PairParams p) {
     const bool leader = r == 0;
     uint8_t* box = smem + kStaging + hf * kBoxBytes;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    for (int i = 0; nth_tile(p, pair, pairs, i, &w); ++i) {
+    bool ok = true;
+    for (int i = 0; ok && nth_tile(p, pair, pairs, i, &w); ++i) {
       const int buf = i & 1;
-      if (!wait_bar_warp(&S->acc_full[buf], (i >> 1) & 1, S, p.status)) break;
+      ok = wait_bar_warp(&S->acc_full[buf], (i >> 1) & 1, S, p.status);
       tc_fence_after();
       const Tiles& shape = p.tile[kBackward && w.kind != p.kind[0]];
       const int row = w.m0 + rank * kHalf;
@@ -365,6 +377,7 @@ pair_kernel(const __grid_constant__ PairParams p) {
       uint32_t pk[16];
       if (!kBackward && w.narrow && hf == 1) {
         // one box of columns: the other half's
+        if (!ok) break;
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(freed);
@@ -374,7 +387,7 @@ pair_kernel(const __grid_constant__ PairParams p) {
         const int col = w.n0 + hf * 64;
         const int u_col = w.narrow ? 64 : 128;
         for (int x = 0; x < rounds; ++x) {
-          box_begin(hf, leader);
+          if (!(ok = box_begin(hf, leader, ok))) break;
 #pragma unroll
           for (int c = 0; c < 64; c += 32) {
             uint32_t g[32], u[32];
@@ -408,7 +421,7 @@ pair_kernel(const __grid_constant__ PairParams p) {
         const int boxes = 2 - w.narrow;
         for (int x = 0; x < boxes; ++x) {
           const int col = (hf * boxes + x) * 64;
-          box_begin(hf, leader);
+          if (!(ok = box_begin(hf, leader, ok))) break;
 #pragma unroll
           for (int c = 0; c < 64; c += 32) {
             uint32_t v[32];
