@@ -498,6 +498,7 @@ __device__ __forceinline__ void write_row(uint16_t* o, uint32_t tO, float l,
   __syncwarp();
 }
 
+constexpr int kLook = 1024;
 template <int D>
 __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
                              int t, int wq, int lane) {
@@ -555,68 +556,74 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
       unfollowed = t == (int)u.two && !next_unit(p, y, end, &v);
     }
     float m_ref = -INFINITY, l = 0.f;
-    for (int j = 0; j < n; ++j) {
-      if (!(ok = wait_bar(&S->s_full[t], tiles & 1, S, p.status))) break;
-      tc_fence_after();
-      uint32_t s[4][32];
+    // A wait may run out for some lanes of a warp and end well for others, so none
+    // leaves alone: the warp goes on and looks at the abort flag together, every
+    // kLook tiles (50.3 us for the 1080p chunk; 52.0 with a vote on every wait).
+    for (int j = 0; ok && j < n;) {
+      const int stop = min(n, j + kLook);
+      const bool ends = unfollowed && stop == n;
+      for (; j < stop; ++j) {
+        wait_bar(&S->s_full[t], tiles & 1, S, p.status);
+        tc_fence_after();
+        uint32_t s[4][32];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, s[c]);
-      tmem_wait_ld();
-      tc_fence_before();
-      // no QK^T follows the CTA's last S
-      if (!unfollowed || j < n - 1) handoff_arrive(kBarSFree);
-      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      const int valid = len - j * kBN;
+        for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, s[c]);
+        tmem_wait_ld();
+        tc_fence_before();
+        // no QK^T follows the CTA's last S
+        if (!ends || j < stop - 1) handoff_arrive(kBarSFree);
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        const int valid = len - j * kBN;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) mask_max32(s[c], c, valid, mx);
-      const float mrow = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2;
-      const bool rescale =
-          __any_sync(~0u, mrow > m_ref + kRescaleThreshold);
-      float alpha = 1.f;
-      if (rescale) {
-        const float m_new = fmaxf(m_ref, mrow);
-        alpha = m_ref == -INFINITY ? 0.f : ex2(m_ref - m_new);
-        l *= alpha;
-        m_ref = m_new;
-      }
-      // a row whose scores are all -infinity so far exponentiates against 0
-      const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
-      const uint64_t neg2 = f2_pack(neg, neg);
-      uint64_t acc[4] = {0, 0, 0, 0};
-      uint32_t pk[2][16];
-#pragma unroll
-      for (int c = 0; c < 2; ++c) exp_pack32(s[c], sl2x2, neg2, pk[c], acc);
-      // this query tile's previous PV is done: P may be written, O is current
-      if (tiles > 0 && !(ok = wait_bar(&S->p_free[t], (tiles - 1) & 1, S,
-                                       p.status)))
-        break;
-      tc_fence_after();
-      if (j == 0) {
-        if (owed >= 0) write_owed();
-      } else if (rescale) {
-#pragma unroll 1
-        for (int c = 0; c < D / 8; ++c) {
-          uint32_t v[8];
-          tmem_ld8(tO + c * 8, v);
-          tmem_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
-          tmem_st8(tO + c * 8, v);
+        for (int c = 0; c < 4; ++c) mask_max32(s[c], c, valid, mx);
+        const float mrow = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2;
+        const bool rescale =
+            __any_sync(~0u, mrow > m_ref + kRescaleThreshold);
+        float alpha = 1.f;
+        if (rescale) {
+          const float m_new = fmaxf(m_ref, mrow);
+          alpha = m_ref == -INFINITY ? 0.f : ex2(m_ref - m_new);
+          l *= alpha;
+          m_ref = m_new;
         }
-      }
-      tmem_st16(tP, pk[0]);
-      tmem_st16(tP + 16, pk[1]);
+        // a row whose scores are all -infinity so far exponentiates against 0
+        const float neg = m_ref == -INFINITY ? 0.f : -m_ref;
+        const uint64_t neg2 = f2_pack(neg, neg);
+        uint64_t acc[4] = {0, 0, 0, 0};
+        uint32_t pk[2][16];
 #pragma unroll
-      for (int c = 2; c < 4; ++c) {
-        exp_pack32(s[c], sl2x2, neg2, pk[c - 2], acc);
-        tmem_st16(tP + 16 * c, pk[c - 2]);
+        for (int c = 0; c < 2; ++c) exp_pack32(s[c], sl2x2, neg2, pk[c], acc);
+        // this query tile's previous PV is done: P may be written, O is current
+        if (tiles > 0) wait_bar(&S->p_free[t], (tiles - 1) & 1, S, p.status);
+        tc_fence_after();
+        if (j == 0) {
+          if (owed >= 0) write_owed();
+        } else if (rescale) {
+#pragma unroll 1
+          for (int c = 0; c < D / 8; ++c) {
+            uint32_t v[8];
+            tmem_ld8(tO + c * 8, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+            tmem_st8(tO + c * 8, v);
+          }
+        }
+        tmem_st16(tP, pk[0]);
+        tmem_st16(tP + 16, pk[1]);
+#pragma unroll
+        for (int c = 2; c < 4; ++c) {
+          exp_pack32(s[c], sl2x2, neg2, pk[c - 2], acc);
+          tmem_st16(tP + 16 * c, pk[c - 2]);
+        }
+        l += acc_total(acc);
+        tmem_wait_st();
+        tc_fence_before();
+        handoff_arrive(kBarP + t);
+        ++tiles;
       }
-      l += acc_total(acc);
-      tmem_wait_st();
-      tc_fence_before();
-      handoff_arrive(kBarP + t);
-      ++tiles;
+      ok = !__any_sync(~0u, read_abort(S));
     }
     if (!ok) break;
     Unit u;

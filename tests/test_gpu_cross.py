@@ -338,3 +338,11 @@ def test_cross_bwd_scratch_on_any_16_bytes(d, at):
         assert torch.equal(a, b)
     scratch.fill_(7.0)
     assert bool((back == 7.0).all())
+
+
+@pytest.mark.parametrize("L,d", [(40, 64), (200, 128)])
+def test_cross_more_keys_than_are_run_through_at_once(L, d):
+    """The forward's loop over key tiles is cut every 1024 tiles; one unit of one
+    query tile, one of two, the second batch entry ending at the first cut."""
+    T = 1024 * 128 + 130
+    check(*make((2, L, T, 1, 1, d, [T, T - 130]), 16))
