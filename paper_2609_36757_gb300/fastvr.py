@@ -881,6 +881,12 @@ def make_cross_config(softmax_scale: float = 0.0) -> fastvr_cross_config_t:
     return fastvr_cross_config_t(0, 0, 0, 0, 0, 0, softmax_scale)
 
 
+def _check_32_bits(*sizes) -> None:
+    """ctypes keeps the low 32 bits of a size without a word."""
+    if max(sizes) >> 31:
+        raise ValueError("a call's sizes must be below 2^31")
+
+
 def _cross_call(cfg, q, k, v, kv_len):
     """cfg for the tensors of a call and the strides of q, k and v, after the
     checks of their types and shapes."""
@@ -899,6 +905,7 @@ def _cross_call(cfg, q, k, v, kv_len):
                                kv_len.shape != (B,) or
                                not kv_len.is_contiguous()):
         raise ValueError("kv_len must be a contiguous int32 CUDA tensor [B]")
+    _check_32_bits(B, L, T, H, K, d)
     return (fastvr_cross_config_t(B, L, T, H, K, d, cfg.softmax_scale), q_str,
             k_str, v_str)
 
@@ -991,6 +998,7 @@ def _ffn_call(cfg, x, w_gate, w_up, hidden):
             raise ValueError("dh and the saved projections must be contiguous "
                              "bfloat16 [..., F]")
     tokens = x.numel() // D if D else 0
+    _check_32_bits(tokens, F, D)
     return fastvr_ffn_config_t(tokens, D, F, cfg.activation), row
 
 

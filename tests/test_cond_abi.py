@@ -271,3 +271,23 @@ def test_ffn_activation_names(fv):
         fv.make_ffn_config("relu")
     assert [fv.make_ffn_config(n).activation
             for n in ("silu", "gelu", "gelu_tanh")] == [0, 1, 2]
+
+
+@pytest.mark.parametrize("at", ["B", "T", "L"])
+def test_cross_sizes_past_32_bits_are_refused(fv, at):
+    """ctypes would cut a size to its low 32 bits: 2^32 + 2 must not pass for 2."""
+    n = {"B": 1, "L": 2, "T": 3, at: 2 ** 32 + 2}
+    q = torch.empty(n["B"], n["L"], 1, 64, dtype=torch.bfloat16, device="meta")
+    k = torch.empty(n["B"], n["T"], 1, 64, dtype=torch.bfloat16, device="meta")
+    with pytest.raises(ValueError, match="2\\^31"):
+        fv._cross_call(fv.make_cross_config(), q, k, k, None)
+
+
+@pytest.mark.parametrize("tokens,hidden,dim", [
+    (2 ** 32 + 5, 8, 8), (5, 2 ** 32 + 8, 8), (5, 8, 2 ** 32 + 8),
+    (2 ** 31, 8, 8)])
+def test_ffn_sizes_past_32_bits_are_refused(fv, tokens, hidden, dim):
+    x = torch.empty(tokens, dim, dtype=torch.bfloat16, device="meta")
+    w = torch.empty(hidden, dim, dtype=torch.bfloat16, device="meta")
+    with pytest.raises(ValueError, match="2\\^31"):
+        fv._ffn_call(fv.make_ffn_config(), x, w, w, ())
