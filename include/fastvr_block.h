@@ -343,8 +343,8 @@ FASTVR_API fastvr_status_t fastvr_cross_attn_bwd_scratch_bytes(
  *   dq = scale dS k,  dk = scale dS^T q,  dv = P^T dout
  * dk and dv sum over the query heads that share a key head.  dS, and P in dv,
  * enter the products in bfloat16, sums are float32 in a fixed order (no atomics):
- * repeated calls agree bit for bit.  Outputs overlap no input and no other
- * output.  A bounded-wait timeout is reported by fastvr_get_device_status.
+ * repeated calls agree bit for bit.  Outputs and scratch overlap neither an input
+ * nor one another.  A bounded-wait timeout is reported by fastvr_get_device_status.
  * Errors: INVALID_ARG, CAPACITY (scratch), UNSUPPORTED (head_dim, device),
  * CUDA. */
 FASTVR_API fastvr_status_t fastvr_cross_attn_bwd(

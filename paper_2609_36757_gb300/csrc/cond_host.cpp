@@ -179,7 +179,8 @@ fastvr_status_t fastvr_cross_attn_fwd(
       !check_tensor(*cfg, k, k_str, false, false, &a.k_str) ||
       !check_tensor(*cfg, v, v_str, false, false, &a.v_str) ||
       !check_tensor(*cfg, out, out_str, true, true, &a.o_str) ||
-      !aligned4(kv_len) || !aligned4(lse) || out == q || out == k || out == v)
+      !aligned4(kv_len) || !aligned4(lse) || out == q || out == k ||
+      out == v || out == lse)
     return FASTVR_ERR_INVALID_ARG;
   const fastvr_status_t st = use_device(&a);
   if (st != FASTVR_OK) return st;
@@ -232,10 +233,11 @@ fastvr_status_t fastvr_cross_attn_bwd(
       !aligned4(kv_len) || lse == nullptr || !aligned4(lse) ||
       scratch == nullptr || !aligned16(scratch))
     return FASTVR_ERR_INVALID_ARG;
-  const void* in[] = {q, k, v, out, dout};
-  for (const void* p : in)
-    if (p == dq || p == dk || p == dv || p == scratch)
-      return FASTVR_ERR_INVALID_ARG;
+  for (const void* p : {q, k, v, out, dout, (const void*)lse})
+    if (p == scratch) return FASTVR_ERR_INVALID_ARG;
+  for (const void* p : {q, k, v, out, dout, (const void*)lse,
+                        (const void*)scratch})
+    if (p == dq || p == dk || p == dv) return FASTVR_ERR_INVALID_ARG;
   if (dq == dk || dq == dv || dk == dv) return FASTVR_ERR_INVALID_ARG;
   if (scratch_bytes / sizeof(float) <
       fastvr::cross_bwd_scratch_floats(cfg->batch, cfg->heads, cfg->kv_heads,

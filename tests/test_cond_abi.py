@@ -291,3 +291,16 @@ def test_ffn_sizes_past_32_bits_are_refused(fv, tokens, hidden, dim):
     w = torch.empty(hidden, dim, dtype=torch.bfloat16, device="meta")
     with pytest.raises(ValueError, match="2\\^31"):
         fv._ffn_call(fv.make_ffn_config(), x, w, w, ())
+
+
+@pytest.mark.parametrize("kw", [
+    dict(scratch=BWD["dq"]), dict(scratch=BWD["dk"]), dict(scratch=BWD["dv"]),
+    dict(scratch=BWD["lse"]), dict(scratch=BWD["dout"]), dict(lse=BWD["dk"])])
+def test_cross_bwd_refuses_shared_scratch_and_lse(fv, kw):
+    _refused(fv, fv.FASTVR_ERR_INVALID_ARG, fv.fastvr_cross_attn_bwd,
+             _cross(fv), **{**BWD, **kw})
+
+
+def test_cross_fwd_refuses_lse_in_out(fv):
+    _refused(fv, fv.FASTVR_ERR_INVALID_ARG, fv.fastvr_cross_attn_fwd,
+             _cross(fv), **{**FWD, "lse": FWD["out"]})
