@@ -380,6 +380,11 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
   using L = Layout<D>;
   constexpr uint32_t kIdescQK = idesc_bf16_f32(kBM, kBN, 0);
   constexpr uint32_t kIdescPV = idesc_bf16_f32(kBM, D, 1);
+  // Unrolled code is issued faster, but has to be fetched: with heads of 64, whose
+  // MMAs are half as long, one piece of code for both query tiles and four MMAs at
+  // a time take 82 us for 19456 tokens of 24 heads over 512 keys, the unrolled
+  // form 89; with 128 the unrolled one takes 49 us for 12 heads, the other 50.
+  constexpr int kSides = D == 64 ? 1 : 2, kMmas = D == 64 ? 4 : 8;
   const uint32_t sbase = smem_addr(smem);
   const uint32_t hi = desc_hi_sw128(1024);
   const uint32_t q_lo = desc_lo(sbase, 16);
@@ -394,7 +399,7 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
     }
   };
   auto pv = [&](int t, uint32_t b0, bool acc) {
-#pragma unroll
+#pragma unroll kMmas
     for (int kk = 0; kk < kBN / 16; ++kk)
       mma_ts_warp(tmem + kTmemO + t * 128, tmem + kTmemP + t * 64 + kk * 8,
                   b0 + (uint32_t)(kk * 2048 >> 4), hi, kIdescPV,
@@ -404,14 +409,11 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
     if (wait) handoff_sync(kBarSFree);
     tc_fence_after();
   };
-  // The loop's numbers as the warp's own: a warp-uniform value that the compiler
-  // knows to be one keeps descriptors in uniform registers.
-  auto same = [](int v) { return __shfl_sync(~0u, v, 0); };
   // Test hook: `drain` receives no arrival before the end, so this wait runs
   // out and exercises the abort path.
   bool ok = !p.inject_stall || wait_bar_warp(&S->drain, 0, S, p.status);
-  const int end = same(S->last);
-  int x = same(S->first);
+  const int end = warp_uniform(S->last);
+  int x = warp_uniform(S->first);
   int s = 0, qc = 0;  // steps and query tiles so far
   bool ptwo = false, pacc = false;  // of the step whose PV is owed
   // PV_t of step i.
@@ -425,40 +427,37 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
     if (t == (int)two) mma_commit_warp(&S->v_empty[vs]);
   };
   Unit u;
-  while (ok && next_unit(p, x, end, &u)) {
-    const int n = same(u.n);
-    const bool two = same(u.two);
-    x = same(x);
+  while (warp_uniform(ok && next_unit(p, x, end, &u))) {
+    const int n = warp_uniform(u.n);
+    const bool two = warp_uniform(u.two);
+    x = warp_uniform(x);
     const int q0 = qc % L::kQ, q1 = (qc + 1) % L::kQ;
     qc += 1 + (int)two;
     const uint32_t aborted = read_abort(S);  // looked at after the unit
     for (int j = 0; j < n; ++j, ++s) {
       const int ks = s % L::kK;
-      if (j == 0) relay_sync(kBarQ + q0);
-      relay_sync(kBarK + ks);
-      take_s(s > 0);
-      qk(q_lo + q0 * kStage16, k_lo + ks * kStage16);
-      mma_commit_warp(&S->s_full[0]);
-      if (j == n - 1) mma_commit_warp(&S->q_empty[q0]);
-      if (!two) mma_commit_warp(&S->k_empty[ks]);
-      if (s > 0) owed(0, s - 1, ptwo);
-      if (two) {
-        if (j == 0) relay_sync(kBarQ + q1);
-        take_s(true);
-        qk(q_lo + q1 * kStage16, k_lo + ks * kStage16);
-        mma_commit_warp(&S->s_full[1]);
-        if (j == n - 1) mma_commit_warp(&S->q_empty[q1]);
-        mma_commit_warp(&S->k_empty[ks]);
+#pragma unroll kSides
+      for (int t = 0; t < 2; ++t) {
+        if (t <= (int)two) {
+          const int q = t == 0 ? q0 : q1;
+          if (j == 0) relay_sync(kBarQ + q);
+          if (t == 0) relay_sync(kBarK + ks);
+          take_s(s + t > 0);
+          qk(q_lo + q * kStage16, k_lo + ks * kStage16);
+          mma_commit_warp(&S->s_full[t]);
+          if (j == n - 1) mma_commit_warp(&S->q_empty[q]);
+          if (t == (int)two) mma_commit_warp(&S->k_empty[ks]);
+        }
+        if (s > 0 && t <= (int)ptwo) owed(t, s - 1, ptwo);
       }
-      if (s > 0 && ptwo) owed(1, s - 1, true);
       ptwo = two;
       pacc = j > 0;
     }
     if (__any_sync(~0u, aborted != 0)) ok = false;
   }
   if (ok && s > 0) {
-    owed(0, s - 1, ptwo);
-    if (ptwo) owed(1, s - 1, true);
+#pragma unroll 1
+    for (int t = 0; t <= (int)ptwo; ++t) owed(t, s - 1, ptwo);
   }
   mma_commit_warp(&S->drain);
   if ((threadIdx.x & 31) == 0) {
@@ -648,7 +647,8 @@ cross_tile_kernel(const __grid_constant__ CrossParams p) {
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   Shared* S = reinterpret_cast<Shared*>(smem + L::shared_off);
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = warp_uniform(threadIdx.x / 32);
+  const int lane = threadIdx.x % 32;
   if (warp == 9) {
     tmem_alloc(&S->tmem_base, kTmemCols);
     tmem_relinquish();
@@ -684,7 +684,7 @@ cross_tile_kernel(const __grid_constant__ CrossParams p) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = S->tmem_base;
+  const uint32_t tmem = warp_uniform(S->tmem_base);
   pdl_trigger();
   pdl_wait();
   if (warp < 2) {

@@ -264,7 +264,7 @@ __device__ __forceinline__ void mma_finish(Shared* S) {
 }
 
 __device__ __forceinline__ uint32_t setup(Shared* S, const BwdParams& p) {
-  const int warp = threadIdx.x / 32;
+  const int warp = warp_uniform(threadIdx.x / 32);
   if (warp == kMmaWarp) {
     tmem_alloc(&S->tmem_base, kTmemCols);
     tmem_relinquish();
@@ -297,7 +297,7 @@ __device__ __forceinline__ uint32_t setup(Shared* S, const BwdParams& p) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  return S->tmem_base;
+  return warp_uniform(S->tmem_base);
 }
 
 __device__ __forceinline__ void teardown(uint32_t tmem) {
@@ -430,7 +430,8 @@ __device__ __forceinline__ void dkdv_cta(const BwdParams& p, uint8_t* smem,
   using L = DkdvLayout<D>;
   using RQ = typename L::Q;
   using RO = typename L::O;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = warp_uniform(threadIdx.x / 32);
+  const int lane = threadIdx.x % 32;
   // parts of a key tile and key tiles of a head side by side: their CTAs share
   // query tiles in L2
   int x = blockIdx.x;
@@ -754,7 +755,8 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
   using RO = typename L::O;
   using RK = typename L::K;
   using RV = typename L::V;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = warp_uniform(threadIdx.x / 32);
+  const int lane = threadIdx.x % 32;
 
   if (warp == kWarpA || warp == kWarpB) {
     // K_0, Q, K_1, ... and V_0, dO, V_1, ...: a unit's first K and V can be on

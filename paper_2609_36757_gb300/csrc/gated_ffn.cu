@@ -233,7 +233,8 @@ pair_kernel(const __grid_constant__ PairParams p) {
   uint8_t* smem = reinterpret_cast<uint8_t*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   Shared* S = reinterpret_cast<Shared*>(smem + kSharedBytes);
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = warp_uniform(threadIdx.x / 32);
+  const int lane = threadIdx.x % 32;
   const int rank = (int)cluster_rank();
   const int pair = blockIdx.x / 2, pairs = gridDim.x / 2;
 

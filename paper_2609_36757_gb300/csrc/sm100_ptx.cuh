@@ -308,6 +308,15 @@ __device__ __forceinline__ void mma_ts_warp(uint32_t d_tmem, uint32_t a_tmem,
       : "memory");
 }
 
+// A value that all lanes of the warp hold, in a form that the compiler knows to be
+// the same for all: what hangs on it then stays in uniform registers and uniform
+// control flow, without which the descriptors of every MMA are moved there anew
+// (with the warp's number, of which its role follows, taken so, cross_attn.cu's
+// 1080p chunk took 46.2 us instead of 50.1).
+__device__ __forceinline__ int warp_uniform(int v) {
+  return __shfl_sync(~0u, v, 0);
+}
+
 // Arrive on `bar` once every tcgen05 op previously issued by the warp's
 // elected lane has completed (with the full warp active, `elect.sync` picks
 // the same lane as for the MMAs).
