@@ -380,11 +380,10 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
   using L = Layout<D>;
   constexpr uint32_t kIdescQK = idesc_bf16_f32(kBM, kBN, 0);
   constexpr uint32_t kIdescPV = idesc_bf16_f32(kBM, D, 1);
-  // Unrolled code is issued faster, but has to be fetched: with heads of 64, whose
-  // MMAs are half as long, one piece of code for both query tiles and four MMAs at
-  // a time take 82 us for 19456 tokens of 24 heads over 512 keys, the unrolled
-  // form 89; with 128 the unrolled one takes 49 us for 12 heads, the other 50.
-  constexpr int kSides = D == 64 ? 1 : 2, kMmas = D == 64 ? 4 : 8;
+  // Both query tiles' part of a step is unrolled, but for heads of 64, whose MMAs
+  // are half as long, fetching the code takes longer than is saved (67.9 us for
+  // 19456 tokens of 24 heads over 512 keys, unrolled 69.2).
+  constexpr int kSides = D == 64 ? 1 : 2;
   const uint32_t sbase = smem_addr(smem);
   const uint32_t hi = desc_hi_sw128(1024);
   const uint32_t q_lo = desc_lo(sbase, 16);
@@ -399,7 +398,7 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
     }
   };
   auto pv = [&](int t, uint32_t b0, bool acc) {
-#pragma unroll kMmas
+#pragma unroll
     for (int kk = 0; kk < kBN / 16; ++kk)
       mma_ts_warp(tmem + kTmemO + t * 128, tmem + kTmemP + t * 64 + kk * 8,
                   b0 + (uint32_t)(kk * 2048 >> 4), hi, kIdescPV,
@@ -508,7 +507,11 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
   const int r = wq * 32 + lane;  // row within the tile
   const float sl2 = p.scale_log2;
   const uint64_t sl2x2 = f2_pack(sl2, sl2);
-  const int end = S->last;
+  // With heads of 128 the loop over units has no registers to spare for uniform
+  // control flow (50.7 us over 512 keys instead of 49.2); with 64 it takes 68.6 us
+  // instead of 80.7.
+  auto uniform = [](int v) { return D == 64 ? warp_uniform(v) : v; };
+  const int end = uniform(S->last);
   int tiles = 0;  // key tiles of this query tile so far: barrier phases
   // the slot of the unit whose output is owed (-1: none), the row's sum
   int owed = -1;
@@ -533,14 +536,15 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
     get_unit(p, owed, end, &u);
     write_row<D>(exists(u) ? out_row(u) : nullptr, tO, owed_l, p.wide);
   };
-  for (int slot = S->first, next; ok && slot < end; slot = next) {
+  for (int slot = uniform(S->first), next; uniform(ok && slot < end);
+       slot = next) {
     int n, len;
     bool unfollowed;  // no QK^T follows this unit's last S of this tile
     {
       Unit u, v;
-      next = get_unit(p, slot, end, &u);
-      n = u.n;
-      len = u.len;
+      next = uniform(get_unit(p, slot, end, &u));
+      n = warp_uniform(u.n);
+      len = warp_uniform(u.len);
       if (n == 0) {  // sees no key
         if (exists(u)) {
           for (int c = 0; c < D; c += 8)
