@@ -19,14 +19,14 @@
 //   warps 0-3, 4-7  softmax and output of the first and second query tile
 // TMEM (512 columns): S | P_0 | P_1 | O_0 | O_1.
 //
-// What bounds a step of 128 keys is the softmax warps' own time, about 2100 clk
-// for the products' 2048 of both tiles (157 us for 19456 tokens of 12 heads over
-// 2048 keys, 1560 TFLOP/s), and at a unit's end the output: 32-byte pieces of 128
-// rows keep a query tile's warps for another 2400 clk (58 us over 512 keys, 52
-// without the stores; through shared memory and TMA stores, or by warps of their
-// own, it was no faster, 62 and 67 us).  The first copies take 3 to 4 us of a
-// launch.  With entries of different lengths CTAs take ranges of query tiles of
-// about equal work.
+// With many keys it runs at the rate of chunk_attn_fwd.cu's steps (145 us for 19456
+// tokens of 12 heads over 2048 keys, 1690 TFLOP/s; 8192 by 8192 of 57 heads 1880).
+// With few, a unit's end counts: the output keeps a query tile's warps from their
+// next scores (46.2 us over 512 keys, 41.0 without the stores; through shared memory
+// and TMA stores, or by warps of their own, it was no faster).  The first copies
+// take 3 to 4 us of a launch.  What the kernel is sensitive to is the MMA warp's
+// issue, see warp_uniform.  With entries of different lengths CTAs take ranges of
+// query tiles of about equal work.
 //
 // Waits on mbarriers are bounded; past the limit every role stops.  The MMA
 // warp waits on named barriers, which have no limit: after a failure the relay
@@ -466,11 +466,18 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
   __syncwarp();
 }
 
-// out = O / l from TMEM, a row of a thread in pieces of 32 bytes (whole sectors).
+// out = O / l from TMEM, where a lane has a row.  With heads of 128 lanes 2 i and
+// 2 i + 1 exchange pieces of 32 bytes (whole sectors), so that a store writes 64 bytes
+// of 16 rows, `first` being the even lane's row and `second` the odd one's, instead of
+// 32 bytes of 32 rows: 43.5 us instead of 46.0 for the 1080p chunk.  A row of 64 has
+// too few of them (69.9 us for 19456 tokens of 24 heads over 512 keys, 73.4 with the
+// exchange): `first` is the lane's own.
 template <int D>
-__device__ __forceinline__ void write_row(uint16_t* o, uint32_t tO, float l,
-                                          bool wide) {
+__device__ __forceinline__ void write_rows(uint16_t* first,
+                                           uint16_t* second, int lane,
+                                           uint32_t tO, float l, bool wide) {
   const float inv = 1.f / l;
+  const bool b = lane & 1;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
     uint32_t v[32], pk[16];
@@ -481,16 +488,16 @@ __device__ __forceinline__ void write_row(uint16_t* o, uint32_t tO, float l,
     for (int i = 0; i < 16; ++i)
       pk[i] = pack_bf16(__uint_as_float(v[2 * i]) * inv,
                         __uint_as_float(v[2 * i + 1]) * inv);
-    if (o != nullptr) {
-      if (wide) {
-        store_32b(o + c * 32, pk);
-        store_32b(o + c * 32 + 16, pk + 8);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<uint4*>(o + c * 32 + 8 * i) = make_uint4(
-              pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
+    if (D == 64) {
+      if (first != nullptr) {
+        store_piece(first + c * 32, pk, wide);
+        store_piece(first + c * 32 + 16, pk + 8, wide);
       }
+    } else {
+      swap_pieces(pk, b);
+      const int at = c * 32 + 16 * b;
+      if (first != nullptr) store_piece(first + at, pk, wide);
+      if (second != nullptr) store_piece(second + at, pk + 8, wide);
     }
   }
   __syncwarp();
@@ -519,22 +526,26 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
   bool ok = true;
   // A row's places in out and lse; computed anew where they are needed, since
   // the loop over the keys has no registers to hold them.
-  auto out_row = [&](const Unit& u) {
+  auto out_row = [&](const Unit& u, int row) {
     return p.o + (int64_t)u.b * p.o_str.batch +
-           (int64_t)(u.q0 + t * kBM + r) * p.o_str.token +
+           (int64_t)(u.q0 + t * kBM + row) * p.o_str.token +
            (int64_t)u.h * p.o_str.head;
   };
   auto lse_row = [&](const Unit& u) {
     return p.lse + ((int64_t)u.b * p.heads + u.h) * p.q_tokens + u.q0 +
            t * kBM + r;
   };
-  auto exists = [&](const Unit& u) {
-    return u.q0 + t * kBM + r < p.q_tokens && (t == 0 || u.two);
+  auto exists = [&](const Unit& u, int row) {
+    return u.q0 + t * kBM + row < p.q_tokens && (t == 0 || u.two);
   };
   auto write_owed = [&]() {
     Unit u;
     get_unit(p, owed, end, &u);
-    write_row<D>(exists(u) ? out_row(u) : nullptr, tO, owed_l, p.wide);
+    const int x = D == 64 ? r : r & ~1;
+    write_rows<D>(
+        exists(u, x) ? out_row(u, x) : nullptr,
+        D == 128 && exists(u, x + 1) ? out_row(u, x + 1) : nullptr, lane, tO,
+        owed_l, p.wide);
   };
   for (int slot = uniform(S->first), next; uniform(ok && slot < end);
        slot = next) {
@@ -546,9 +557,9 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
       n = warp_uniform(u.n);
       len = warp_uniform(u.len);
       if (n == 0) {  // sees no key
-        if (exists(u)) {
+        if (exists(u, r)) {
           for (int c = 0; c < D; c += 8)
-            *reinterpret_cast<uint4*>(out_row(u) + c) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(out_row(u, r) + c) = make_uint4(0, 0, 0, 0);
           if (p.lse != nullptr) *lse_row(u) = -INFINITY;
         }
         __syncwarp();
@@ -631,7 +642,7 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
     if (!ok) break;
     Unit u;
     get_unit(p, slot, end, &u);
-    if (exists(u) && p.lse != nullptr)
+    if (exists(u, r) && p.lse != nullptr)
       *lse_row(u) = (m_ref + __log2f(l)) * 0.6931471805599453f;
     owed = slot;
     owed_l = l;

@@ -395,10 +395,13 @@ __device__ __forceinline__ void dscores32(const uint32_t (&p)[32],
   }
 }
 
-// 32 scaled results of TMEM as bfloat16 to a row.
+// 32 scaled results of TMEM, where a lane has a row, as bfloat16 to rows `even` and
+// `odd` of the lane and its neighbour (null: no such row).  A lane writes 32 bytes
+// of both (cross_attn.cu): 291 us for 12288 tokens of 24 heads over 512 keys with the
+// forward, 292 without the exchange.
 __device__ __forceinline__ void store_cols32(uint32_t taddr, float mul,
-                                             bool zero, uint16_t* to, bool in,
-                                             bool wide) {
+                                             bool zero, uint16_t* even,
+                                             uint16_t* odd, bool wide) {
   uint32_t v[32], pk[16];
   __syncwarp();
   tmem_ld32(taddr, v);
@@ -408,16 +411,19 @@ __device__ __forceinline__ void store_cols32(uint32_t taddr, float mul,
     pk[i] = zero ? 0u
                  : pack_bf16(__uint_as_float(v[2 * i]) * mul,
                              __uint_as_float(v[2 * i + 1]) * mul);
-  if (!in) return;
-  if (wide) {
-    store_32b(to, pk);
-    store_32b(to + 16, pk + 8);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<uint4*>(to + 8 * i) = make_uint4(
-          pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
-  }
+  const bool b = threadIdx.x & 1;
+  swap_pieces(pk, b);
+  if (even != nullptr) store_piece(even + 16 * b, pk, wide);
+  if (odd != nullptr) store_piece(odd + 16 * b, pk + 8, wide);
+}
+// The two rows' places, from the first one's.
+struct Rows {
+  uint16_t *even, *odd;
+};
+__device__ __forceinline__ Rows rows_at(uint16_t* first, int64_t stride,
+                                        int row, int rows) {
+  return {row < rows ? first : nullptr,
+          row + 1 < rows ? first + stride : nullptr};
 }
 
 // ------------------------------------------------------------------ dK, dV
@@ -623,19 +629,22 @@ __device__ __forceinline__ void dkdv_cta(const BwdParams& p, uint8_t* smem,
       const int row = k0 + t;
       const bool zero = row >= len;
       if (p.parts == 1) {
-        uint16_t* dk = p.dk + (int64_t)b * p.dk_str.batch +
-                       (int64_t)row * p.dk_str.token +
-                       (int64_t)hk * p.dk_str.head;
-        uint16_t* dv = p.dv + (int64_t)b * p.dv_str.batch +
-                       (int64_t)row * p.dv_str.token +
-                       (int64_t)hk * p.dv_str.head;
-        const bool in = row < p.kv_tokens;
+        const int even = row & ~1;
+        const Rows dk = rows_at(p.dk + (int64_t)b * p.dk_str.batch +
+                                    (int64_t)even * p.dk_str.token +
+                                    (int64_t)hk * p.dk_str.head,
+                                p.dk_str.token, even, p.kv_tokens);
+        const Rows dv = rows_at(p.dv + (int64_t)b * p.dv_str.batch +
+                                    (int64_t)even * p.dv_str.token +
+                                    (int64_t)hk * p.dv_str.head,
+                                p.dv_str.token, even, p.kv_tokens);
+        auto at = [](uint16_t* o, int c) { return o ? o + c * 32 : o; };
 #pragma unroll 1
         for (int c = hf * D / 64; c < (hf + 1) * D / 64; ++c) {
-          store_cols32(row_t + 256 + c * 32, 1.f, zero, dv + c * 32, in,
-                       p.wide_v);
-          store_cols32(row_t + 384 + c * 32, p.scale, zero, dk + c * 32, in,
-                       p.wide_k);
+          store_cols32(row_t + 256 + c * 32, 1.f, zero, at(dv.even, c),
+                       at(dv.odd, c), p.wide_v);
+          store_cols32(row_t + 384 + c * 32, p.scale, zero, at(dk.even, c),
+                       at(dk.odd, c), p.wide_k);
         }
       } else {
         const int64_t at = (((int64_t)part * p.batch * p.kv_heads + bh) *
@@ -882,17 +891,25 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
     const int t = (warp % 4) * 32 + lane;
     const uint32_t row_t = tmem + ((uint32_t)((warp % 4) * 32) << 16);
     const uint64_t c2x2 = f2(p.scale_log2, p.scale_log2);
-    uint16_t* owed = nullptr;  // the last unit's row, still to be written
-    bool owed_in = false, ok = true;
+    int owed = -1;  // the unit whose dQ is still to be written
+    bool ok = true;
     int s = 0, done = 0;
     auto write_out = [&]() {
       if (!(ok = wait_bar_warp(&S->out_full, done & 1, S, p.status))) return;
       ++done;
       tc_fence_after();
+      Unit u;
+      get_unit(p, owed, &u);
+      const int even = u.q0 + (t & ~1);
+      const Rows o = rows_at(p.dq + (int64_t)u.b * p.dq_str.batch +
+                                 (int64_t)even * p.dq_str.token +
+                                 (int64_t)u.h * p.dq_str.head,
+                             p.dq_str.token, even, p.q_tokens);
 #pragma unroll 1
       for (int c = hf * D / 64; c < (hf + 1) * D / 64; ++c)
-        store_cols32(row_t + 256 + c * 32, p.scale, false, owed + c * 32,
-                     owed_in, p.wide_q);
+        store_cols32(row_t + 256 + c * 32, p.scale, false,
+                     o.even ? o.even + c * 32 : nullptr,
+                     o.odd ? o.odd + c * 32 : nullptr, p.wide_q);
       tc_fence_before();
     };
     // A unit's row values lie at kT times its number; the next one's are asked
@@ -902,16 +919,16 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
     for (int x = cta; ok && x < p.units; x += p.dq_ctas) {
       Unit u;
       get_unit(p, x, &u);
-      const int row = u.q0 + t;
-      uint16_t* dst = p.dq + (int64_t)u.b * p.dq_str.batch +
-                      (int64_t)row * p.dq_str.token +
-                      (int64_t)u.h * p.dq_str.head;
       const float nl_row = nl_next, nd_row = nd_next;
       if (x + p.dq_ctas < p.units) {
         nl_next = p.lse2[(int64_t)(x + p.dq_ctas) * kT + t];
         nd_next = p.delta[(int64_t)(x + p.dq_ctas) * kT + t];
       }
       if (u.n == 0) {  // sees no key
+        const int row = u.q0 + t;
+        uint16_t* dst = p.dq + (int64_t)u.b * p.dq_str.batch +
+                        (int64_t)row * p.dq_str.token +
+                        (int64_t)u.h * p.dq_str.head;
         if (row < p.q_tokens)
           for (int c = hf * D / 2; c < (hf + 1) * D / 2; c += 8)
             *reinterpret_cast<uint4*>(dst + c) = make_uint4(0, 0, 0, 0);
@@ -941,7 +958,7 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
         }
         tc_fence_before();
         compute_arrive(kBarP);
-        if (j == 0 && owed != nullptr) {
+        if (j == 0 && owed >= 0) {
           write_out();
           if (!ok) break;
         }
@@ -961,10 +978,9 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
         tc_fence_before();
         compute_arrive(kBarDS + (s & 1));
       }
-      owed = dst;
-      owed_in = row < p.q_tokens;
+      owed = x;
     }
-    if (ok && owed != nullptr) write_out();
+    if (ok && owed >= 0) write_out();
   }
 }
 

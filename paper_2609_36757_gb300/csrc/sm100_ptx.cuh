@@ -445,5 +445,30 @@ __device__ __forceinline__ void store_32b(void* p, const uint32_t* r) {
       : "memory");
 }
 
+// 32 bytes to a place that lies on 32 bytes, or (not `wide`) on 16.
+__device__ __forceinline__ void store_piece(void* p, const uint32_t* r,
+                                            bool wide) {
+  if (wide) {
+    store_32b(p, r);
+  } else {
+    uint4* q = static_cast<uint4*>(p);
+    q[0] = make_uint4(r[0], r[1], r[2], r[3]);
+    q[1] = make_uint4(r[4], r[5], r[6], r[7]);
+  }
+}
+
+// Two pieces of 8 words of a row to a lane: lanes 2 i and 2 i + 1 exchange them, so
+// that lane 2 i has the first piece of both rows, lane 2 i + 1 (`odd`) the second.
+__device__ __forceinline__ void swap_pieces(uint32_t (&v)[16], bool odd) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t got = __shfl_xor_sync(~0u, odd ? v[i] : v[8 + i], 1);
+    if (odd)
+      v[i] = got;
+    else
+      v[8 + i] = got;
+  }
+}
+
 }  // namespace sm100
 }  // namespace fastvr
