@@ -25,7 +25,7 @@
 // next scores (46.2 us over 512 keys, 41.0 without the stores; through shared memory
 // and TMA stores, or by warps of their own, it was no faster).  The first copies
 // take 3 to 4 us of a launch.  What the kernel is sensitive to is the MMA warp's
-// issue, see warp_uniform.  With entries of different lengths CTAs take ranges of
+// issue (warp_uniform).  With entries of different lengths CTAs take ranges of
 // query tiles of about equal work.
 //
 // Waits on mbarriers are bounded; past the limit every role stops.  The MMA
@@ -470,7 +470,7 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
 // 2 i + 1 exchange pieces of 32 bytes (whole sectors), so that a store writes 64 bytes
 // of 16 rows, `first` being the even lane's row and `second` the odd one's, instead of
 // 32 bytes of 32 rows: 43.5 us instead of 46.0 for the 1080p chunk.  A row of 64 has
-// too few of them (69.9 us for 19456 tokens of 24 heads over 512 keys, 73.4 with the
+// too few of them (67.9 us for 19456 tokens of 24 heads over 512 keys, 73.4 with the
 // exchange): `first` is the lane's own.
 template <int D>
 __device__ __forceinline__ void write_rows(uint16_t* first,
@@ -572,7 +572,7 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
     float m_ref = -INFINITY, l = 0.f;
     // A wait may run out for some lanes of a warp and end well for others, so none
     // leaves alone: the warp goes on and looks at the abort flag together, every
-    // kLook tiles (50.3 us for the 1080p chunk; 52.0 with a vote on every wait).
+    // kLook tiles (45.8 us for the 1080p chunk; 46.9 with a vote on every wait).
     for (int j = 0; ok && j < n;) {
       const int stop = min(n, j + kLook);
       const bool ends = unfollowed && stop == n;

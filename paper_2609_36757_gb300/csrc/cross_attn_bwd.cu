@@ -22,8 +22,8 @@
 //                 next unit's S and dP run before this one's last dQ, whose
 //                 result leaves between the next unit's P and dS.
 // Measured at 12288 tokens of 24 heads of 128 over 512 keys: rows_kernel 27 us
-// (O and dO at 5.6 TB/s), grads_kernel 185 (seven products of which dq's recompute
-// two; 63 % of the tensor pipe's cycles: a unit of dq has four steps between its
+// (O and dO at 5.6 TB/s), grads_kernel 182 (seven products of which dq's recompute
+// two; 64 % of the tensor pipe's cycles: a unit of dq has four steps between its
 // ends), join_kernel 10.
 //
 // Lanes of TMEM are independent, so key rows past an entry's last need no mask
