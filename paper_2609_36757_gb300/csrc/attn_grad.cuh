@@ -50,26 +50,34 @@ __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v 
 // nearest integer (x + 1.5 * 2^23 rounds it into the low mantissa bits) and
 // f in [-0.5, 0.5]; 2^f by a degree-3 polynomial (a relative-error minimax
 // fit on [-0.5, 0.5], at most 7.5e-5 relative error in fp32: far below the
-// 2^-9 of the bf16 P it feeds), then n added to its exponent field.  x is
-// first clamped to >= -126 so that the exponent cannot wrap (2^x there is
-// below 1.2e-38, against 0 from ex2.approx.ftz).  Some of the pairs take
-// this path instead of MUFU ex2: the exponential step is bounded by the
-// MUFU throughput, while the FMA pipe has room.
+// 2^-9 of the bf16 P it feeds), then times 2^n, whose exponent field is n's
+// low bits.  x is first clamped to >= -126 so that the exponent cannot wrap
+// (2^x there is below 1.2e-38, against 0 from ex2.approx.ftz); a NaN stays
+// NaN in the clamp and, 2^n being a factor instead of an integer added to the
+// result's bits, in what follows.  Some of the pairs take this path instead of
+// MUFU ex2: the exponential step is bounded by the MUFU throughput, while the
+// FMA pipe has room.
 constexpr float kExpC0 = 0.9999281168f, kExpC1 = 0.6932609677f,
                 kExpC2 = 0.2426105440f, kExpC3 = 0.0551713221f;
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ void exp2_poly(float& x0, float& x1) {
-  const uint64_t x = f2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+  const uint64_t x = f2(max_nan(x0, -126.f), max_nan(x1, -126.f));
   const uint64_t t = f2_add(x, f2(12582912.f, 12582912.f));
   const uint64_t fr = f2_fma(f2_add(t, f2(-12582912.f, -12582912.f)),
                              f2(-1.f, -1.f), x);
   uint64_t q = f2_fma(f2(kExpC3, kExpC3), fr, f2(kExpC2, kExpC2));
   q = f2_fma(q, fr, f2(kExpC1, kExpC1));
   q = f2_fma(q, fr, f2(kExpC0, kExpC0));
-  float p0, p1, t0, t1;
-  f2_split(q, p0, p1);
+  float t0, t1;
   f2_split(t, t0, t1);
-  x0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
-  x1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
+  const uint32_t one = 0x3f800000u;  // 1.f, whose exponent n is added to
+  f2_split(f2_mul(q, f2(__uint_as_float((__float_as_uint(t0) << 23) + one),
+                        __uint_as_float((__float_as_uint(t1) << 23) + one))),
+           x0, x1);
 }
 // Groups of four columns (of eight per 32) whose exponentials take the
 // polynomial path in the unmasked step: one (training clip backward +0.5 %;
