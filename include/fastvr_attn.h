@@ -302,6 +302,8 @@ FASTVR_API fastvr_status_t fastvr_get_device_status(void);
  * bounded wait runs out after wait_limit_ns (0 = the 4 s default), every
  * role stops, in-flight copies and MMAs are drained, tensor memory is
  * released and FASTVR_ERR_TIMEOUT is recorded for fastvr_get_device_status.
+ * With stall = 2 the cross attention's forward waits in the thread that loads the
+ * values instead, while the other warps are in the midst of their work.
  * No GPU fault or hang results.  stall = 0 restores normal operation.
  * Host only; always FASTVR_OK. */
 FASTVR_API fastvr_status_t fastvr_debug_inject_stall_noplan(

@@ -276,7 +276,8 @@ __device__ void v_producer(const CrossParams& p, uint8_t* smem, Shared* S) {
   const int end = S->last;
   int x = S->first, vc = 0;
   Unit u;
-  bool ok = true;
+  // Test hook: the others' waits run out too, the MMA warp amid a unit.
+  bool ok = p.inject_stall != 2 || wait_bar(&S->drain, 0, S, p.status);
   while (ok && next_unit(p, x, end, &u)) {
     const int hk = (int)fast_div(u.h, p.by_group);
     for (int j = 0; j < u.n; ++j) {
@@ -410,7 +411,7 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
   };
   // Test hook: `drain` receives no arrival before the end, so this wait runs
   // out and exercises the abort path.
-  bool ok = !p.inject_stall || wait_bar_warp(&S->drain, 0, S, p.status);
+  bool ok = p.inject_stall != 1 || wait_bar_warp(&S->drain, 0, S, p.status);
   const int end = warp_uniform(S->last);
   int x = warp_uniform(S->first);
   int s = 0, qc = 0;  // steps and query tiles so far
@@ -571,13 +572,15 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
     }
     float m_ref = -INFINITY, l = 0.f;
     // A wait may run out for some lanes of a warp and end well for others, so none
-    // leaves alone: the warp goes on and looks at the abort flag together, every
-    // kLook tiles (45.8 us for the 1080p chunk; 46.9 with a vote on every wait).
+    // leaves alone: the warp meets again, as the accesses to TMEM and the named
+    // barriers ask for, goes on, and looks at the abort flag together, every kLook
+    // tiles (a vote on every wait took 46.9 us for the 1080p chunk instead of 45.8).
     for (int j = 0; ok && j < n;) {
       const int stop = min(n, j + kLook);
       const bool ends = unfollowed && stop == n;
       for (; j < stop; ++j) {
         wait_bar(&S->s_full[t], tiles & 1, S, p.status);
+        __syncwarp();
         tc_fence_after();
         uint32_t s[4][32];
 #pragma unroll
@@ -609,6 +612,7 @@ __device__ void softmax_role(const CrossParams& p, Shared* S, uint32_t tmem,
         for (int c = 0; c < 2; ++c) exp_pack32(s[c], sl2x2, neg2, pk[c], acc);
         // this query tile's previous PV is done: P may be written, O is current
         if (tiles > 0) wait_bar(&S->p_free[t], (tiles - 1) & 1, S, p.status);
+        __syncwarp();
         tc_fence_after();
         if (j == 0) {
           if (owed >= 0) write_owed();

@@ -563,7 +563,7 @@ fastvr_status_t fastvr_get_device_status(void) {
 
 fastvr_status_t fastvr_debug_inject_stall_noplan(int32_t stall,
                                                  uint64_t wait_limit_ns) {
-  g_noplan_stall.store(stall != 0);
+  g_noplan_stall.store(stall);
   g_noplan_wait_ns.store(wait_limit_ns);
   return FASTVR_OK;
 }

@@ -1,0 +1,51 @@
+"""Cross attention's forward without its values: the softmax lanes' waits run out, each
+at its own time, while the MMA warp is amid a unit.  The failure is reported, every
+role leaves, and the same call gives its results again."""
+import time
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def _call(B, L, H, T, d, lens, seed=1):
+    from paper_2609_36757_gb300 import fastvr as FV
+    g = torch.Generator("cuda").manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, generator=g,
+                                 device="cuda").to(torch.bfloat16)
+    q, k, v = rnd(B, L, H, d), rnd(B, T, 1, d), rnd(B, T, 1, d)
+    n = None if lens is None else torch.tensor(lens, dtype=torch.int32,
+                                               device="cuda")
+    cfg = FV.make_cross_config()
+    return lambda: FV.cross_attention(cfg, q, k, v, n, want_lse=True)
+
+
+CASES = [
+    # B, L, H, T, d, lens
+    (1, 300, 2, 300, 128, None),
+    (1, 300, 2, 300, 64, None),
+    (3, 700, 4, 200, 128, [200, 0, 77]),
+    (3, 700, 60, 140, 64, [140, 0, 77]),  # several units to a CTA
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_stall_amid_a_unit_is_reported(case):
+    from paper_2609_36757_gb300 import fastvr as FV
+    call = _call(*case)
+    ref = call()
+    assert FV.fastvr_get_device_status() == FV.FASTVR_OK
+    FV.fastvr_debug_inject_stall_noplan(2, 20_000_000)  # 20 ms per wait
+    try:
+        t0 = time.perf_counter()
+        call()
+        status = FV.fastvr_get_device_status()
+        assert time.perf_counter() - t0 < 5.0
+    finally:
+        FV.fastvr_debug_inject_stall_noplan(0, 0)
+    assert status == FV.FASTVR_ERR_TIMEOUT
+    assert FV.fastvr_get_device_status() == FV.FASTVR_OK  # cleared
+    for a, b in zip(call(), ref):
+        assert torch.equal(a, b)
+    assert FV.fastvr_get_device_status() == FV.FASTVR_OK
