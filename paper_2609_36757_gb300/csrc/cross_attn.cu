@@ -56,6 +56,9 @@ constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kTmemS = 0, kTmemP = 128, kTmemO = 256;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr uint64_t kDefaultWaitLimitNs = 4000000000ull;
+// The relay keeps the MMA warp going for this and three waits: far longer than that
+// warp needs to see a failure, since a named barrier has no limit.
+constexpr uint64_t kReleaseNs = 1000000000ull;
 // Named barriers of the hand-offs to the MMA warp.
 constexpr int kBarSFree = 1;
 constexpr int kBarP = 2;   // + query tile
@@ -362,7 +365,9 @@ __device__ void relay_role(const CrossParams& p, uint8_t* smem, Shared* S,
       for (int id = kBarSFree; id < kBarK; ++id) handoff_arrive(id);
       for (int id = kBarK; id < kBars; ++id) relay_arrive(id);
     }
-    if (__any_sync(~0u, global_timer_ns() - t0 > 3 * S->wait_limit_ns)) break;
+    if (__any_sync(~0u, global_timer_ns() - t0 >
+                            3 * S->wait_limit_ns + kReleaseNs))
+      break;
     __nanosleep(200);
   }
 }
@@ -375,6 +380,9 @@ __device__ __forceinline__ uint32_t read_abort(const Shared* S) {
   return a;
 }
 
+// The MMA warp stops within twice this many key tiles of a failure, each of which
+// takes a few rounds of the relay's arrivals: a millisecond or two in all.
+constexpr int kIssue = 128;
 template <int D>
 __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
                            uint32_t tmem) {
@@ -433,27 +441,30 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
     x = warp_uniform(x);
     const int q0 = qc % L::kQ, q1 = (qc + 1) % L::kQ;
     qc += 1 + (int)two;
-    const uint32_t aborted = read_abort(S);  // looked at after the unit
-    for (int j = 0; j < n; ++j, ++s) {
-      const int ks = s % L::kK;
+    for (int j = 0; ok && j < n;) {
+      const uint32_t aborted = read_abort(S);  // looked at kIssue steps later
+      const int stop = min(n, j + kIssue);
+      for (; j < stop; ++j, ++s) {
+        const int ks = s % L::kK;
 #pragma unroll kSides
-      for (int t = 0; t < 2; ++t) {
-        if (t <= (int)two) {
-          const int q = t == 0 ? q0 : q1;
-          if (j == 0) relay_sync(kBarQ + q);
-          if (t == 0) relay_sync(kBarK + ks);
-          take_s(s + t > 0);
-          qk(q_lo + q * kStage16, k_lo + ks * kStage16);
-          mma_commit_warp(&S->s_full[t]);
-          if (j == n - 1) mma_commit_warp(&S->q_empty[q]);
-          if (t == (int)two) mma_commit_warp(&S->k_empty[ks]);
+        for (int t = 0; t < 2; ++t) {
+          if (t <= (int)two) {
+            const int q = t == 0 ? q0 : q1;
+            if (j == 0) relay_sync(kBarQ + q);
+            if (t == 0) relay_sync(kBarK + ks);
+            take_s(s + t > 0);
+            qk(q_lo + q * kStage16, k_lo + ks * kStage16);
+            mma_commit_warp(&S->s_full[t]);
+            if (j == n - 1) mma_commit_warp(&S->q_empty[q]);
+            if (t == (int)two) mma_commit_warp(&S->k_empty[ks]);
+          }
+          if (s > 0 && t <= (int)ptwo) owed(t, s - 1, ptwo);
         }
-        if (s > 0 && t <= (int)ptwo) owed(t, s - 1, ptwo);
+        ptwo = two;
+        pacc = j > 0;
       }
-      ptwo = two;
-      pacc = j > 0;
+      if (__any_sync(~0u, aborted != 0)) ok = false;
     }
-    if (__any_sync(~0u, aborted != 0)) ok = false;
   }
   if (ok && s > 0) {
 #pragma unroll 1

@@ -59,6 +59,7 @@ constexpr int kBox = 128 * 128;  // one TMA box: 128 rows x 64 bf16 (bytes)
 constexpr int kThreads = 384;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint64_t kDefaultWaitLimitNs = 4000000000ull;
+constexpr uint64_t kReleaseNs = 1000000000ull;  // cross_attn.cu
 constexpr int kWarpA = 8, kMmaWarp = 9, kWarpB = 10, kRelayWarp = 11;
 // Named barriers of the hand-offs to the MMA warp.  dq's dS has one for even and
 // one for odd steps: its next S and dP are issued before the MMA warp waits for
@@ -241,7 +242,9 @@ __device__ __forceinline__ void relay_release(Shared* S) {
       compute_arrive(kBarDS + 1);
       for (int id = kBarRing; id < kBars; ++id) relay_arrive(id);
     }
-    if (__any_sync(~0u, global_timer_ns() - t0 > 3 * S->wait_limit_ns)) break;
+    if (__any_sync(~0u, global_timer_ns() - t0 >
+                            3 * S->wait_limit_ns + kReleaseNs))
+      break;
     __nanosleep(200);
   }
 }

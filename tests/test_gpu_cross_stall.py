@@ -49,3 +49,24 @@ def test_stall_amid_a_unit_is_reported(case):
     for a, b in zip(call(), ref):
         assert torch.equal(a, b)
     assert FV.fastvr_get_device_status() == FV.FASTVR_OK
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_stall_amid_a_long_unit(d):
+    """The MMA warp leaves a unit of 1563 key tiles soon, whatever the limit: what
+    keeps it from waiting for arrivals that nobody makes lasts for a while only."""
+    from paper_2609_36757_gb300 import fastvr as FV
+    call = _call(1, 300, 1, 200_000, d, None)
+    ref = call()
+    FV.fastvr_debug_inject_stall_noplan(2, 1_000_000)  # 1 ms
+    try:
+        t0 = time.perf_counter()
+        call()
+        status = FV.fastvr_get_device_status()
+        assert time.perf_counter() - t0 < 0.5
+    finally:
+        FV.fastvr_debug_inject_stall_noplan(0, 0)
+    assert status == FV.FASTVR_ERR_TIMEOUT
+    for a, b in zip(call(), ref):
+        assert torch.equal(a, b)
+    assert FV.fastvr_get_device_status() == FV.FASTVR_OK
