@@ -277,8 +277,9 @@ FASTVR_API fastvr_status_t fastvr_plan_launch_count(fastvr_plan_t plan,
  * tensor memory is released and FASTVR_ERR_TIMEOUT is recorded for
  * fastvr_get_status.  The output of such a launch is undefined.  No GPU
  * fault or hang results.  wait_limit_ns = 0 keeps the default limit
- * (4 s per wait); stall = 0 with wait_limit_ns = 0 restores normal
- * operation.  Host only.  Errors: INVALID_ARG. */
+ * (4 s per wait), others are taken as 1 ms at least, within which copies in
+ * flight land, and 60 s at most; stall = 0 with wait_limit_ns = 0 restores
+ * normal operation.  Host only.  Errors: INVALID_ARG. */
 FASTVR_API fastvr_status_t fastvr_debug_inject_stall(fastvr_plan_t plan,
                                                      int32_t stall,
                                                      uint64_t wait_limit_ns);
@@ -299,8 +300,8 @@ FASTVR_API fastvr_status_t fastvr_get_device_status(void);
  * stall != 0 makes every following one-shot forward and backward launch
  * (and those of the cross attention's and gated feed-forward's tile kernels)
  * wait, in its MMA-issuing warp, on a barrier that nothing arrives on; the
- * bounded wait runs out after wait_limit_ns (0 = the 4 s default), every
- * role stops, in-flight copies and MMAs are drained, tensor memory is
+ * bounded wait runs out after wait_limit_ns (0 = the 4 s default, others as
+ * fastvr_debug_inject_stall takes them), every role stops, in-flight copies and MMAs are drained, tensor memory is
  * released and FASTVR_ERR_TIMEOUT is recorded for fastvr_get_device_status.
  * With stall = 2 the cross attention's forward waits in the thread that loads the
  * values instead, while the other warps are in the midst of their work.

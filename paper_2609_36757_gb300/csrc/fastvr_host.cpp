@@ -46,6 +46,14 @@ namespace {
 std::atomic<int32_t> g_noplan_stall{0};
 std::atomic<uint64_t> g_noplan_wait_ns{0};
 
+// A limit as the kernels take it.  They wait as long for the copies and MMAs in
+// flight before they leave, so it is no shorter than those may take; and no wait
+// lasts for ever.
+uint64_t wait_limit(uint64_t ns) {
+  constexpr uint64_t kLeast = 1000000, kMost = 60000000000ull;
+  return ns == 0 ? 0 : std::min(std::max(ns, kLeast), kMost);
+}
+
 // Visible segments of the newest chunk, in slot order, merged when adjacent.
 std::vector<Segment> visible_segments(const fastvr_plan_s& p) {
   std::vector<Segment> segs;
@@ -532,7 +540,7 @@ fastvr_status_t fastvr_debug_inject_stall(fastvr_plan_t p, int32_t stall,
                                           uint64_t wait_limit_ns) {
   if (p == nullptr) return FASTVR_ERR_INVALID_ARG;
   p->inject_stall = stall != 0;
-  p->wait_limit_ns = wait_limit_ns;
+  p->wait_limit_ns = wait_limit(wait_limit_ns);
   return FASTVR_OK;
 }
 
@@ -564,7 +572,7 @@ fastvr_status_t fastvr_get_device_status(void) {
 fastvr_status_t fastvr_debug_inject_stall_noplan(int32_t stall,
                                                  uint64_t wait_limit_ns) {
   g_noplan_stall.store(stall);
-  g_noplan_wait_ns.store(wait_limit_ns);
+  g_noplan_wait_ns.store(wait_limit(wait_limit_ns));
   return FASTVR_OK;
 }
 
