@@ -33,41 +33,28 @@
 
 #include "fastvr_internal.h"
 #include "ffn_act.cuh"
+#include "ffn_tiles.h"
 #include "sm100_ptx.cuh"
 
 namespace fastvr {
 namespace {
 
+using namespace ffn;
 using namespace sm100;
 
 constexpr int kThreads = 384;
 constexpr int kStages = 6;
-constexpr int kHalf = 128;              // rows of A and of B in one CTA
-constexpr int kStep = 64;               // of the summed axis in one stage
 constexpr int kOperand = kHalf * kStep * 2;  // bytes of one operand's stage
 constexpr uint32_t kTmemCols = 512;     // two tiles' results
 constexpr uint64_t kDefaultWaitLimitNs = 4000000000ull;
 constexpr uint64_t kAbortGraceNs = 1000000;
-constexpr int kGroupTiles = 8;  // row tiles that share their columns' tiles
-
-enum Kind { kFwd, kDx, kDw };
-
-// Tiles of one kind: results [rows, cols], rows of tiles by tiles across.
-struct Tiles {
-  int32_t rows, cols, mt, nt, count, steps;
-  int32_t narrow;  // 128 columns of results instead of 256
-};
 
 struct PairParams {
   // x; gate and up weights; dg and du, by rows (dx) and by columns (dW)
   CUtensorMap x, w[2], d[2], dt[2];
   // results: forward h, g, u; backward dx, dWg, dWu
   CUtensorMap out[3];
-  Tiles tile[2];              // forward: [0]; backward: those listed first, and
-  int32_t kind[2];            // the others
-  // Pairs from `heavy` on (0: all) have one tile fewer of the first list than the
-  // others and take `extra` of the second list before its common rounds.
-  int32_t heavy, extra;
+  Division div;             // which tiles a pair takes (ffn_tiles.h)
   int32_t half_steps;       // dx: steps of dg Wg
   int32_t save;             // forward: g and u are wanted
   // by columns, a copy takes all the columns that a CTA needs: dim, hidden are
@@ -122,46 +109,6 @@ __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity,
   const uint64_t t0 = global_timer_ns();
   while (!mbar_try_wait_cluster(bar, parity))
     if (global_timer_ns() - t0 > S->wait_limit_ns) return;
-}
-
-// The i-th tile of a pair of CTAs; false behind its last.
-struct Work {
-  int kind, m0, n0, steps, which, narrow;  // which: dWg or dWu
-};
-__host__ __device__ inline bool nth_tile(const PairParams& p, int pair,
-                                         int pairs, int i, Work* w) {
-  int list = 0, t = pair + i * pairs;
-  if (t >= p.tile[0].count) {
-    list = 1;
-    i -= (p.tile[0].count + pairs - 1 - pair) / pairs;  // had of the first
-    const int light = pairs - p.heavy;
-    const int ahead = min(p.tile[1].count, p.extra * light);
-    if (p.extra > 0 && pair >= p.heavy && i < p.extra) {
-      t = pair - p.heavy + i * light;
-      if (t >= ahead) return false;
-    } else {
-      if (p.extra > 0 && pair >= p.heavy) i -= p.extra;
-      // common rounds, the pairs with fewer tiles of the first list first
-      t = ahead + (pair >= p.heavy ? pair - p.heavy : pair + light) + i * pairs;
-    }
-    if (t >= p.tile[1].count) return false;
-  }
-  const Tiles& a = p.tile[list];
-  w->kind = p.kind[list];
-  w->steps = a.steps;
-  w->narrow = a.narrow;
-  w->which = 0;
-  if (w->kind == kDw) {
-    const int one = a.mt * a.nt;
-    w->which = t >= one;
-    t -= w->which * one;
-  }
-  const int across = kGroupTiles * a.nt;
-  const int first = t / across * kGroupTiles;
-  const int gm = min(kGroupTiles, a.mt - first), r = t % across;
-  w->m0 = (first + r % gm) * 2 * kHalf;
-  w->n0 = r / gm * ((w->kind == kFwd ? kHalf : 2 * kHalf) >> w->narrow);
-  return true;
 }
 
 // An operand by columns: `boxes` of 64 columns from col on, 64 rows from row on.
@@ -270,7 +217,7 @@ pair_kernel(const __grid_constant__ PairParams p) {
     if (lane == 0) {
       int it = 0;
       bool ok = true;
-      for (int i = 0; ok && nth_tile(p, pair, pairs, i, &w); ++i) {
+      for (int i = 0; ok && nth_tile(p.div, pair, pairs, i, &w); ++i) {
         const int b_boxes = 2 - w.narrow;
         for (int s = 0; s < w.steps; ++s, ++it) {
           const int st = it % kStages;
@@ -319,7 +266,7 @@ pair_kernel(const __grid_constant__ PairParams p) {
       bool ok = !p.inject_stall || wait_bar_warp(&S->drain, 0, S, p.status);
       int it = 0;
       Work next;
-      bool have = nth_tile(p, pair, pairs, 0, &next);
+      bool have = nth_tile(p.div, pair, pairs, 0, &next);
       for (int i = 0; ok && have; ++i) {
         w = next;
         const int buf = i & 1;
@@ -353,7 +300,7 @@ pair_kernel(const __grid_constant__ PairParams p) {
                              b_lo + k * b_step, hi, idesc, (s | k) != 0);
           mma_commit_pair_warp(&S->empty[st]);
           // found while the first step's products run
-          if (s == 0) have = nth_tile(p, pair, pairs, i + 1, &next);
+          if (s == 0) have = nth_tile(p.div, pair, pairs, i + 1, &next);
         }
         if (ok) mma_commit_pair_warp(&S->acc_full[buf]);
       }
@@ -368,11 +315,11 @@ pair_kernel(const __grid_constant__ PairParams p) {
     uint8_t* box = smem + kStaging + hf * kBoxBytes;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     bool ok = true;
-    for (int i = 0; ok && nth_tile(p, pair, pairs, i, &w); ++i) {
+    for (int i = 0; ok && nth_tile(p.div, pair, pairs, i, &w); ++i) {
       const int buf = i & 1;
       ok = wait_bar_warp(&S->acc_full[buf], (i >> 1) & 1, S, p.status);
       tc_fence_after();
-      const Tiles& shape = p.tile[kBackward && w.kind != p.kind[0]];
+      const Tiles& shape = p.div.tile[kBackward && w.kind != p.div.kind[0]];
       const int row = w.m0 + rank * kHalf;
       const uint32_t acc = tmem + buf * 256 + lanes;
       const uint32_t freed = cluster_addr(&S->acc_empty[buf], 0);
@@ -530,67 +477,15 @@ bool make_column_map(CUtensorMap* m, const void* base, int64_t rows,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-
-// `wide`: columns of a wide tile.
-Tiles make_tiles(int64_t rows, int64_t cols, int wide, int copies, int steps,
-                 int narrow) {
-  Tiles t;
-  t.rows = (int32_t)rows;
-  t.cols = (int32_t)cols;
-  t.mt = up(rows, 2 * kHalf);
-  t.nt = up(cols, wide >> narrow);
-  t.count = t.mt * t.nt * copies;
-  t.steps = steps;
-  t.narrow = narrow;
-  return t;
-}
-
-// The pairs' shares of two lists of tiles, and the time of the pair that ends
-// last in steps of wide tiles.  A narrow tile has half of the products but three
-// quarters of the loads, which bound it.
-struct Shares {
-  int pairs, heavy, extra;
-  double time;
-};
-Shares share(const Tiles& a, const Tiles& b, int sms) {
-  const int pairs = std::min(sms / 2, a.count + b.count);
-  const double ca = (a.steps + 8) * (a.narrow ? 0.75 : 1.0);
-  const double cb = (b.steps + 8) * (b.narrow ? 0.75 : 1.0);
-  const int heavy = a.count % pairs, light = pairs - heavy;
-  Shares best = {pairs, heavy, 0, 0.0};
-  // extra rounds that make up for a tile of the first list, or one more
-  const int most = b.count > 0 && heavy > 0 ? (int)(ca / cb) + 1 : 0;
-  for (int extra = std::max(0, most - 1); extra <= most; ++extra) {
-    const int ahead = (int)std::min<int64_t>(b.count, (int64_t)extra * light);
-    double time = 0.0;
-    for (int p = 0; p < pairs; ++p) {
-      const int own = p >= heavy ? p - heavy : p + light;
-      int64_t n = (b.count - ahead + pairs - 1 - own) / pairs;
-      if (extra > 0 && p >= heavy)
-        n += std::min(extra, (ahead - own + light - 1) / light);
-      time = std::max(time,
-                      (a.count + pairs - 1 - p) / pairs * ca + (double)n * cb);
-    }
-    if (extra == std::max(0, most - 1) || time < best.time) {
-      best.extra = extra;
-      best.time = time;
-    }
-  }
-  return best;
-}
-
 template <int kAct>
-cudaError_t launch_pairs(PairParams& p, const FfnArgs& a, cudaStream_t stream) {
-  const Shares s = share(p.tile[0], p.tile[1], a.sms);
-  p.heavy = s.heavy;
-  p.extra = s.extra;
+cudaError_t launch_pairs(PairParams& p, int pairs, const FfnArgs& a,
+                         cudaStream_t stream) {
   p.status = a.status;
   p.inject_stall = a.inject_stall;
   p.wait_limit_ns = a.wait_limit_ns;
   const cudaError_t e = allow_smem<pair_kernel<kAct>>(kSmem, a.device);
   if (e != cudaSuccess) return e;
-  return launch_pdl(pair_kernel<kAct>, dim3(2 * s.pairs), dim3(kThreads),
+  return launch_pdl(pair_kernel<kAct>, dim3(2 * pairs), dim3(kThreads),
                     kSmem, stream, p);
 }
 
@@ -600,18 +495,9 @@ cudaError_t launch_ffn_fwd(const FfnArgs& a, cudaStream_t stream) {
   if (ffn_few_rows(a.tokens)) return launch_ffn_rows(a, stream);
   PairParams p;
   memset(&p, 0, sizeof(p));
-  p.kind[0] = p.kind[1] = kFwd;
-  double best = 0.0;
-  for (int narrow = 0; narrow < 2; ++narrow) {
-    const Tiles t = make_tiles(a.tokens, a.hidden, kHalf, 1, up(a.dim, kStep),
-                               narrow);
-    const double time = share(t, p.tile[1], a.sms).time;
-    if (narrow == 0 || time < best) {
-      best = time;
-      p.tile[0] = t;
-    }
-  }
-  const int w_rows = kHalf >> p.tile[0].narrow;
+  int pairs;
+  p.div = divide_fwd(a.tokens, a.dim, a.hidden, a.sms, &pairs);
+  const int w_rows = kHalf >> p.div.tile[0].narrow;
   if (!make_map(&p.x, a.x, a.tokens, a.dim, a.x_row, kHalf) ||
       !make_map(&p.w[0], a.w_gate, a.hidden, a.dim, a.dim, w_rows) ||
       !make_map(&p.w[1], a.w_up, a.hidden, a.dim, a.dim, w_rows))
@@ -621,9 +507,9 @@ cudaError_t launch_ffn_fwd(const FfnArgs& a, cudaStream_t stream) {
   for (int i = 0; i < (p.save ? 3 : 1); ++i)
     if (!make_map(&p.out[i], out[i], a.tokens, a.hidden, a.hidden, kHalf))
       return cudaErrorInvalidValue;
-  return a.act == kActSilu   ? launch_pairs<kActSilu>(p, a, stream)
-         : a.act == kActGelu ? launch_pairs<kActGelu>(p, a, stream)
-                             : launch_pairs<kActGeluTanh>(p, a, stream);
+  return a.act == kActSilu   ? launch_pairs<kActSilu>(p, pairs, a, stream)
+         : a.act == kActGelu ? launch_pairs<kActGelu>(p, pairs, a, stream)
+                             : launch_pairs<kActGeluTanh>(p, pairs, a, stream);
 }
 
 cudaError_t launch_ffn_bwd(const FfnBwdArgs& b, cudaStream_t stream) {
@@ -640,27 +526,10 @@ cudaError_t launch_ffn_bwd(const FfnBwdArgs& b, cudaStream_t stream) {
   memset(&p, 0, sizeof(p));
   const int kinds = b.dw_gate != nullptr ? 2 : 1;
   p.half_steps = up(a.hidden, kStep);
-  // the tiles with the longer sums first, each kind as wide as ends first
-  double best = 0.0;
-  for (int narrow = 0; narrow < 4; ++narrow) {
-    const Tiles dx = make_tiles(a.tokens, a.dim, 2 * kHalf, 1,
-                                2 * p.half_steps, narrow & 1);
-    Tiles dw = make_tiles(a.hidden, a.dim, 2 * kHalf, 2, up(a.tokens, kStep),
-                          narrow >> 1);
-    if (kinds == 1) dw.count = 0;
-    const int first = kinds == 2 && dw.steps > dx.steps ? 1 : 0;
-    const Tiles& a0 = first ? dw : dx;
-    const Tiles& a1 = first ? dx : dw;
-    const double time = share(a0, a1, a.sms).time;
-    if (narrow > 0 && time >= best) continue;
-    best = time;
-    p.tile[0] = a0;
-    p.tile[1] = a1;
-    p.kind[first] = kDx;
-    p.kind[1 - first] = kDw;
-  }
-  const Tiles& dx = p.tile[p.kind[1] == kDx];
-  const Tiles& dw = p.tile[p.kind[1] == kDw];
+  int pairs;
+  p.div = divide_bwd(a.tokens, a.dim, a.hidden, kinds == 2, a.sms, &pairs);
+  const Tiles& dx = p.div.tile[p.div.kind[1] == kDx];
+  const Tiles& dw = p.div.tile[p.div.kind[1] == kDw];
   const int64_t M = a.tokens, F = a.hidden, D = a.dim;
   p.dim_boxes = D % 64 == 0;
   p.hidden_boxes = F % 64 == 0;
@@ -677,7 +546,7 @@ cudaError_t launch_ffn_bwd(const FfnBwdArgs& b, cudaStream_t stream) {
        (!make_map(&p.out[1], b.dw_gate, a.hidden, a.dim, a.dim, kHalf) ||
         !make_map(&p.out[2], b.dw_up, a.hidden, a.dim, a.dim, kHalf))))
     return cudaErrorInvalidValue;
-  return launch_pairs<-1>(p, a, stream);
+  return launch_pairs<-1>(p, pairs, a, stream);
 }
 
 }  // namespace fastvr
