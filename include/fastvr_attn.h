@@ -275,8 +275,9 @@ FASTVR_API fastvr_status_t fastvr_plan_launch_count(fastvr_plan_t plan,
  * nothing arrives on; the kernel's bounded wait runs out after
  * wait_limit_ns, every role stops, in-flight copies and MMAs are drained,
  * tensor memory is released and FASTVR_ERR_TIMEOUT is recorded for
- * fastvr_get_status.  The output of such a launch is undefined.  No GPU
- * fault or hang results.  wait_limit_ns = 0 keeps the default limit
+ * fastvr_get_status; with stall = 2 the thread that loads the values waits
+ * instead.  The output of such a launch is undefined.  No GPU fault or hang
+ * results.  wait_limit_ns = 0 keeps the default limit
  * (4 s per wait), others are taken as 1 ms at least, within which copies in
  * flight land, and 60 s at most; stall = 0 with wait_limit_ns = 0 restores
  * normal operation.  Host only.  Errors: INVALID_ARG. */
@@ -301,10 +302,11 @@ FASTVR_API fastvr_status_t fastvr_get_device_status(void);
  * (and those of the cross attention's and gated feed-forward's tile kernels)
  * wait, in its MMA-issuing warp, on a barrier that nothing arrives on; the
  * bounded wait runs out after wait_limit_ns (0 = the 4 s default, others as
- * fastvr_debug_inject_stall takes them), every role stops, in-flight copies and MMAs are drained, tensor memory is
- * released and FASTVR_ERR_TIMEOUT is recorded for fastvr_get_device_status.
- * With stall = 2 the cross attention's forward waits in the thread that loads the
- * values instead, while the other warps are in the midst of their work.
+ * fastvr_debug_inject_stall takes them), every role stops, in-flight copies and
+ * MMAs are drained, tensor memory is released and FASTVR_ERR_TIMEOUT is
+ * recorded for fastvr_get_device_status.
+ * With stall = 2 the one-shot forward and the cross attention's forward wait in the
+ * thread that loads the values instead, while the other warps are amid their work.
  * No GPU fault or hang results.  stall = 0 restores normal operation.
  * Host only; always FASTVR_OK. */
 FASTVR_API fastvr_status_t fastvr_debug_inject_stall_noplan(

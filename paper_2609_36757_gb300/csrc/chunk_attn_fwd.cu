@@ -78,6 +78,12 @@ constexpr uint32_t kTmemO = 256;
 constexpr float kRescaleThreshold = 8.0f;      // log2 units
 constexpr int kMinTilesPerPart = 4;             // key tiles per split part
 constexpr uint64_t kDefaultWaitLimitNs = 4000000000ull;  // 4 s per wait
+// After a failed wait the relay makes arrivals for this and three waits: far longer
+// than the MMA warp needs to see the failure, since a named barrier has no limit.
+constexpr uint64_t kReleaseNs = 1000000000ull;
+// Key tiles between two looks at the abort flag, by the MMA warp and by the softmax
+// warps.
+constexpr int kLook = 64;
 // Named (hardware) barriers of the softmax -> MMA hand-offs: S read (free
 // for the next QK^T) and P_t stored.  The four softmax warps of a tile
 // arrive, the MMA warp syncs: kHandoff threads per generation.
@@ -228,7 +234,7 @@ struct Shared {
   uint64_t s_full[kQTiles], p_free[kQTiles];
   uint64_t o_full, drain;
   uint32_t tmem_base;
-  int abort;
+  int abort, mma_done;
   uint64_t wait_limit_ns;
 };
 
@@ -315,7 +321,11 @@ __device__ void producer(const TcParams& p, uint8_t* smem, Shared* S,
   for (int s = 0; s < kMaxSegments; ++s)
     tma_prefetch_desc(kIsK ? &p.k_map[s] : &p.v_map[s]);
   int issued = 0;
-  for (int j = 0; j < w.n; ++j) {
+  // Test hook: without values the softmax warps' waits run out, the MMA warp amid
+  // its unit.
+  const bool ok = kIsK || p.inject_stall != 2 ||
+                  wait_bar(&S->drain, 0, S, p.status);
+  for (int j = 0; ok && j < w.n; ++j) {
     const int st = j % kStages;
     const uint32_t ph = (j / kStages) & 1;
     int seg, tok0, valid;
@@ -368,8 +378,8 @@ __device__ __forceinline__ bool wait_bar_warp(uint64_t* bar, uint32_t parity,
 // poll is a shared-memory access, and while SMEM x SMEM MMAs are queued every
 // such access waits behind their operand reads (~200 clk), which the issuer
 // cannot afford several times per key tile.  A named barrier has no time
-// limit, so the softmax warps make exactly the arrivals the MMA warp will
-// wait for on every path, also after a failed wait (see softmax_role).
+// limit: after a failed wait of any role the relay warp arrives on all of them
+// until the MMA warp has seen the failure and left (see relay_role).
 __device__ __forceinline__ void named_arrive(int id) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(kHandoff) : "memory");
 }
@@ -392,12 +402,13 @@ __device__ __forceinline__ void relay_sync(int id) {
 // barrier of its ring stage, so the MMA warp itself never polls a
 // shared-memory barrier.  A stage's barrier cannot be arrived at twice
 // before the MMA warp has synced on it: the producer refills the stage only
-// after the MMAs that read it.  After a failed wait the remaining arrivals
-// are still made (the MMA warp then computes on undefined data, and the
-// failure is recorded), so the MMA warp never waits for one that does not
-// come.
+// after the MMAs that read it.  After a failed wait the MMA warp may be at any
+// of its barriers, and a role that is behind it or ahead of it cannot count the
+// arrivals that it will wait for (one warp's arrivals at once may complete a
+// barrier that the MMA warp has not reached), so the relay arrives on all of them
+// again and again; the MMA warp goes on with undefined data until it looks at
+// the abort flag.
 __device__ void relay_role(const TcParams& p, Shared* S, int n) {
-  int k_arr = 0, v_arr = 0;
   bool ok = true;
   for (int j = 0; ok && j <= n; ++j) {
     if (j < n) {
@@ -405,7 +416,6 @@ __device__ void relay_role(const TcParams& p, Shared* S, int n) {
                                S, p.status)))
         break;
       relay_arrive(kBarKFull0 + j % kKStages);
-      ++k_arr;
     }
     const int jp = j - 1;
     if (jp >= 0) {
@@ -413,11 +423,31 @@ __device__ void relay_role(const TcParams& p, Shared* S, int n) {
                                (jp / kVStages) & 1, S, p.status)))
         break;
       relay_arrive(kBarVFull0 + jp % kVStages);
-      ++v_arr;
     }
   }
-  for (; k_arr < n; ++k_arr) relay_arrive(kBarKFull0 + k_arr % kKStages);
-  for (; v_arr < n; ++v_arr) relay_arrive(kBarVFull0 + v_arr % kVStages);
+  volatile int* done = &S->mma_done;
+  volatile int* abort = &S->abort;
+  const uint64_t t0 = global_timer_ns();
+  while (!__any_sync(0xffffffffu, *done != 0)) {
+    if (__any_sync(0xffffffffu, *abort != 0)) {
+      named_arrive(kBarSFree);
+      for (int t = 0; t < kQTiles; ++t) named_arrive(kBarPFull0 + t);
+      for (int st = 0; st < kKStages; ++st) relay_arrive(kBarKFull0 + st);
+      for (int st = 0; st < kVStages; ++st) relay_arrive(kBarVFull0 + st);
+    }
+    if (__any_sync(0xffffffffu, global_timer_ns() - t0 >
+                                    3 * S->wait_limit_ns + kReleaseNs))
+      break;
+    __nanosleep(200);
+  }
+}
+
+__device__ __forceinline__ uint32_t read_abort(const Shared* S) {
+  uint32_t a;
+  asm volatile("ld.volatile.shared.u32 %0, [%1];"
+               : "=r"(a)
+               : "r"(smem_addr(&S->abort)));
+  return a;
 }
 
 template <int D>
@@ -474,52 +504,60 @@ __device__ void mma_issuer(const TcParams& p, uint8_t* smem, Shared* S,
 
   // Test hook: o_full receives no arrival before the end of the stream, so
   // this wait runs out and exercises the abort path.
-  bool ok = !p.inject_stall || wait_bar_warp(&S->o_full, 0, S, p.status);
+  bool ok = p.inject_stall != 1 || wait_bar_warp(&S->o_full, 0, S, p.status);
   ok = ok && wait_bar_warp(&S->q_full, 0, S, p.status);
   // Issue order per key tile j: QK_0(j), PV_0(j-1), QK_1(j), PV_1(j-1).  A
   // tile's PV runs one key tile behind its QK^T, so the softmax of S_t(j)
   // has the MMAs of three other steps (about 2000 clk) to produce P_t(j)
   // before the pipe needs it, while S, which only has to survive until the
   // softmax has loaded it, alternates between the tiles.
-  for (int j = 0; ok && j <= n; ++j) {
-    const bool has_qk = j < n;
-    const int st = j % kKStages;
-    const int jp = j - 1;  // the key tile whose PV runs now
-    const int vs = jp % kVStages;
-    if (has_qk) {
-      relay_sync(kBarKFull0 + st);
-      take_s();
-      qk(0, st);
-      mma_commit_warp(&S->s_full[0]);
-      if (!two) mma_commit_warp(&S->k_empty[st]);
-    }
-    if (jp >= 0) {
-      relay_sync(kBarVFull0 + vs);
-      named_sync(kBarPFull0);
-      tc_fence_after();
-      pv(0, vs, jp > 0);
-      mma_commit_warp(&S->p_free[0]);
-      if (!two) mma_commit_warp(&S->v_empty[vs]);
-    }
-    if (two) {
+  for (int j = 0; ok && j <= n;) {
+    const uint32_t aborted = read_abort(S);  // looked at kLook tiles later
+    const int stop = min(n + 1, j + kLook);
+    for (; j < stop; ++j) {
+      const bool has_qk = j < n;
+      const int st = j % kKStages;
+      const int jp = j - 1;  // the key tile whose PV runs now
+      const int vs = jp % kVStages;
       if (has_qk) {
+        relay_sync(kBarKFull0 + st);
         take_s();
-        qk(1, st);
-        mma_commit_warp(&S->s_full[1]);
-        mma_commit_warp(&S->k_empty[st]);
+        qk(0, st);
+        mma_commit_warp(&S->s_full[0]);
+        if (!two) mma_commit_warp(&S->k_empty[st]);
       }
       if (jp >= 0) {
-        named_sync(kBarPFull0 + 1);
+        relay_sync(kBarVFull0 + vs);
+        named_sync(kBarPFull0);
         tc_fence_after();
-        pv(1, vs, jp > 0);
-        mma_commit_warp(&S->p_free[1]);
-        mma_commit_warp(&S->v_empty[vs]);
+        pv(0, vs, jp > 0);
+        mma_commit_warp(&S->p_free[0]);
+        if (!two) mma_commit_warp(&S->v_empty[vs]);
+      }
+      if (two) {
+        if (has_qk) {
+          take_s();
+          qk(1, st);
+          mma_commit_warp(&S->s_full[1]);
+          mma_commit_warp(&S->k_empty[st]);
+        }
+        if (jp >= 0) {
+          named_sync(kBarPFull0 + 1);
+          tc_fence_after();
+          pv(1, vs, jp > 0);
+          mma_commit_warp(&S->p_free[1]);
+          mma_commit_warp(&S->v_empty[vs]);
+        }
       }
     }
+    if (__any_sync(0xffffffffu, aborted != 0)) ok = false;
   }
   if (ok) mma_commit_warp(&S->o_full);
   mma_commit_warp(&S->drain);
-  if ((threadIdx.x & 31) == 0) drain_wait(&S->drain, 0, S);
+  if ((threadIdx.x & 31) == 0) {
+    drain_wait(&S->drain, 0, S);
+    *reinterpret_cast<volatile int*>(&S->mma_done) = 1;
+  }
   __syncwarp();
 }
 
@@ -560,10 +598,9 @@ __device__ void softmax_role(const TcParams& p, Shared* S, uint32_t tmem,
   float m_ref = -INFINITY;  // exp2-domain reference (scaled scores)
   float l = 0.f;
   bool ok = true;
-  // Arrivals the MMA warp waits for: one per S this tile reads, except the
-  // very last S of the unit (no QK^T follows it), and one per P_t.
-  const int s_expected = (t == nqt - 1) ? n - 1 : n;
-  int s_arrived = 0, p_arrived = 0;
+  // Every S that this tile reads is handed back, except the very last S of the
+  // unit: no QK^T follows it.
+  const int s_handed = (t == nqt - 1) ? n - 1 : n;
   int vis_lo = 0, vis_hi = 0;  // one-shot: this row's visible key tokens
   if (kOneShot) {
     const int row = min(q0 + t * kBM + wq * 32 + lane, p.q_tokens - 1);
@@ -571,103 +608,96 @@ __device__ void softmax_role(const TcParams& p, Shared* S, uint32_t tmem,
     vis_lo = p.window < 0 ? 0 : max(0, c - p.window) * p.chunk_tokens;
     vis_hi = min((c + 1) * p.chunk_tokens, p.seq_tokens);
   }
-  for (int j = 0; j < n; ++j) {
-    int seg, tok0, valid;
-    const int jt = rev ? n - 1 - j : j;  // the producers' order
-    if (kOneShot)
-      oneshot_tile(kv0, kv1, jt, seg, tok0, valid);
-    else
-      tile_coord(p, j0 + jt, seg, tok0, valid);
-    if (!(ok = wait_bar(&S->s_full[t], j & 1, S, p.status))) break;
-    tc_fence_after();
-    uint32_t s[4][32];
+  // A wait may run out for some lanes of a warp and end well for others, so none
+  // leaves alone: the warp meets again, as the accesses to TMEM and the named
+  // barriers ask for, goes on, and looks at the abort flag together.
+  for (int j = 0; ok && j < n;) {
+    const int stop = min(n, j + kLook);
+    for (; j < stop; ++j) {
+      int seg, tok0, valid;
+      const int jt = rev ? n - 1 - j : j;  // the producers' order
+      if (kOneShot)
+        oneshot_tile(kv0, kv1, jt, seg, tok0, valid);
+      else
+        tile_coord(p, j0 + jt, seg, tok0, valid);
+      wait_bar(&S->s_full[t], j & 1, S, p.status);
+      __syncwarp();
+      tc_fence_after();
+      uint32_t s[4][32];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, s[c]);
-    tmem_wait_ld();
-    // S is in registers: the next QK^T (of either tile) may overwrite it.
-    tc_fence_before();
-    if (s_arrived < s_expected) {
-      named_arrive(kBarSFree);
-      ++s_arrived;
-    }
-    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (kOneShot) {
-      const int lo = vis_lo - tok0;
-      const int hi = min(vis_hi - tok0, valid);
+      for (int c = 0; c < 4; ++c) tmem_ld32(tS + 32 * c, s[c]);
+      tmem_wait_ld();
+      // S is in registers: the next QK^T (of either tile) may overwrite it.
+      tc_fence_before();
+      if (j < s_handed) named_arrive(kBarSFree);
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (kOneShot) {
+        const int lo = vis_lo - tok0;
+        const int hi = min(vis_hi - tok0, valid);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) mask_range_max32(s[c], c, lo, hi, mx);
-    } else if (kStart) {
+        for (int c = 0; c < 4; ++c) mask_range_max32(s[c], c, lo, hi, mx);
+      } else if (kStart) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        mask_range_max32(s[c], c, kv0 - tok0, valid, mx);
-    } else {
+        for (int c = 0; c < 4; ++c)
+          mask_range_max32(s[c], c, kv0 - tok0, valid, mx);
+      } else {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) mask_max32(s[c], c, valid, mx);
-    }
-    const float mrow = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2;
-    // The reference moves only when a row max passes it by more than the
-    // threshold (decided per warp: TMEM accesses are warp-wide).
-    const bool rescale =
-        __any_sync(0xffffffffu, mrow > m_ref + kRescaleThreshold);
-    float alpha = 1.f;
-    if (rescale) {
-      const float m_new = fmaxf(m_ref, mrow);
-      alpha = ex2(m_ref - m_new);
-      if (kOneShot && m_new == -INFINITY) alpha = 1.f;  // still nothing seen
-      l *= alpha;
-      m_ref = m_new;
-    }
-    // A row that has seen no visible key yet exponentiates -inf against 0.
-    const float neg = (kOneShot && m_ref == -INFINITY) ? 0.f : -m_ref;
-    const uint64_t neg2 = f2_pack(neg, neg);
-    uint64_t acc[4] = {0, 0, 0, 0};
-    uint32_t pk[2][16];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) exp_pack32(s[c], sl2x2, neg2, pk[c], acc);
-    // P_t(j - 1) has been consumed and O_t holds PV_t(0 .. j-1) (PV_t(j-1)
-    // was issued right after this S, so this normally does not wait).
-    if (j > 0 && !(ok = wait_bar(&S->p_free[t], (j - 1) & 1, S, p.status)))
-      break;
-    tc_fence_after();
-    if (rescale && j > 0) {
-      // Scale O_t in place before PV_t(j) accumulates against the new
-      // reference.
-#pragma unroll 1
-      for (int c = 0; c < D / 8; ++c) {
-        uint32_t r[8];
-        tmem_ld8(tO + c * 8, r);
-        tmem_wait_ld();
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
-        tmem_st8(tO + c * 8, r);
+        for (int c = 0; c < 4; ++c) mask_max32(s[c], c, valid, mx);
       }
-    }
-    tmem_st16(tP, pk[0]);
-    tmem_st16(tP + 16, pk[1]);
+      const float mrow = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * sl2;
+      // The reference moves only when a row max passes it by more than the
+      // threshold (decided per warp: TMEM accesses are warp-wide).
+      const bool rescale =
+          __any_sync(0xffffffffu, mrow > m_ref + kRescaleThreshold);
+      float alpha = 1.f;
+      if (rescale) {
+        const float m_new = fmaxf(m_ref, mrow);
+        alpha = ex2(m_ref - m_new);
+        if (kOneShot && m_new == -INFINITY) alpha = 1.f;  // still nothing seen
+        l *= alpha;
+        m_ref = m_new;
+      }
+      // A row that has seen no visible key yet exponentiates -inf against 0.
+      const float neg = (kOneShot && m_ref == -INFINITY) ? 0.f : -m_ref;
+      const uint64_t neg2 = f2_pack(neg, neg);
+      uint64_t acc[4] = {0, 0, 0, 0};
+      uint32_t pk[2][16];
 #pragma unroll
-    for (int c = 2; c < 4; ++c) {
-      exp_pack32(s[c], sl2x2, neg2, pk[c - 2], acc);
-      tmem_st16(tP + 16 * c, pk[c - 2]);
+      for (int c = 0; c < 2; ++c) exp_pack32(s[c], sl2x2, neg2, pk[c], acc);
+      // P_t(j - 1) has been consumed and O_t holds PV_t(0 .. j-1) (PV_t(j-1)
+      // was issued right after this S, so this normally does not wait).
+      if (j > 0) wait_bar(&S->p_free[t], (j - 1) & 1, S, p.status);
+      __syncwarp();
+      tc_fence_after();
+      if (rescale && j > 0) {
+        // Scale O_t in place before PV_t(j) accumulates against the new
+        // reference.
+#pragma unroll 1
+        for (int c = 0; c < D / 8; ++c) {
+          uint32_t r[8];
+          tmem_ld8(tO + c * 8, r);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            r[i] = __float_as_uint(__uint_as_float(r[i]) * alpha);
+          tmem_st8(tO + c * 8, r);
+        }
+      }
+      tmem_st16(tP, pk[0]);
+      tmem_st16(tP + 16, pk[1]);
+#pragma unroll
+      for (int c = 2; c < 4; ++c) {
+        exp_pack32(s[c], sl2x2, neg2, pk[c - 2], acc);
+        tmem_st16(tP + 16 * c, pk[c - 2]);
+      }
+      l += acc_total(acc);
+      tmem_wait_st();
+      tc_fence_before();
+      named_arrive(kBarPFull0 + t);
     }
-    l += acc_total(acc);
-    tmem_wait_st();
-    tc_fence_before();
-    named_arrive(kBarPFull0 + t);
-    ++p_arrived;
+    ok = !__any_sync(0xffffffffu, read_abort(S) != 0);
   }
-  // After a failed wait the remaining hand-offs are still made (their
-  // contents are undefined, and so is the output), so that the MMA warp
-  // never waits for an arrival that does not come.
-  while (s_arrived < s_expected) {
-    named_arrive(kBarSFree);
-    ++s_arrived;
-  }
-  while (p_arrived < n) {
-    named_arrive(kBarPFull0 + t);
-    ++p_arrived;
-  }
-  const bool have = ok && wait_bar(&S->o_full, 0, S, p.status);
+  const bool have = ok && wait_bar_warp(&S->o_full, 0, S, p.status);
   const Work w = cta_work<kOneShot, kStart>(p);
   const int r_unit = t * kBM + wq * 32 + lane;  // row within the unit
   const int row = w.q0 + r_unit;
@@ -883,6 +913,7 @@ chunk_attn_tc_kernel(const __grid_constant__ TcParams p) {
     mbar_init(&S->o_full, 1);
     mbar_init(&S->drain, 1);
     S->abort = 0;
+    S->mma_done = 0;
     S->wait_limit_ns = p.wait_limit_ns ? p.wait_limit_ns : kDefaultWaitLimitNs;
     fence_barrier_init();
   }

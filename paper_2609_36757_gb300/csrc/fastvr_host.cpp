@@ -539,7 +539,7 @@ fastvr_status_t fastvr_plan_launch_count(fastvr_plan_t p, int64_t* launches) {
 fastvr_status_t fastvr_debug_inject_stall(fastvr_plan_t p, int32_t stall,
                                           uint64_t wait_limit_ns) {
   if (p == nullptr) return FASTVR_ERR_INVALID_ARG;
-  p->inject_stall = stall != 0;
+  p->inject_stall = stall;
   p->wait_limit_ns = wait_limit(wait_limit_ns);
   return FASTVR_OK;
 }
