@@ -84,6 +84,7 @@ constexpr int kComputeHandoff = 9 * 32;
 constexpr int kRelayHandoff = 2 * 32;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint64_t kWaitLimitNs = 4000000000ull;
+constexpr uint64_t kReleaseNs = 1000000000ull;  // chunk_attn_fwd.cu
 
 struct BwdParams {
   CUtensorMap q_map, k_map, v_map, do_map;  // {d, L, H, B} token-major
@@ -96,7 +97,7 @@ struct BwdParams {
   int32_t seq_tokens, heads, batch, chunk_tokens, window, tiles, padded;
   float scale, scale_log2;
   int* status;             // device status word (timeouts) or null
-  int32_t inject_stall;    // test hook: the MMA warp waits on o_full first
+  int32_t inject_stall;    // test hook: a role waits for what never comes
   uint64_t wait_limit_ns;  // 0 = kWaitLimitNs
 };
 
@@ -116,7 +117,7 @@ struct BwdShared {
   // row-vector warp, released by the compute warps after dS)
   uint64_t vec_full[2], vec_empty[2];
   uint32_t tmem_base;
-  int abort;
+  int abort, mma_done;
   int* status;
   uint64_t wait_limit_ns;
 };
@@ -229,24 +230,49 @@ __device__ __forceinline__ void relay_sync(int id) {
 // ring 1, the order in which the MMA warp needs them) and hands each stage
 // over through its named barrier.  A stage's barrier cannot be arrived at
 // twice before the MMA warp has synced on it: the producer refills a stage
-// only after the MMAs that read it.  Named barriers have no time limit, so
-// after a failed wait the relay still makes the remaining arrivals (the
-// MMA warp then computes on undefined data; the failure is recorded).
+// only after the MMAs that read it.  Named barriers have no time limit: after a
+// failed wait of any role the relay arrives on all of them again and again until
+// the MMA warp, which goes on with undefined data, has seen the failure and left
+// (chunk_attn_fwd.cu's relay_role).
 template <int kS0>
 __device__ void bwd_relay(BwdShared* S, int n) {
-  int a0 = 0, a1 = 0;
   bool ok = true;
   for (int j = 0; ok && j < n; ++j) {
     if (!(ok = wait_bar_warp(&S->full[0][j % kS0], (j / kS0) & 1, S))) break;
     relay_arrive(kBarRing0 + j % kS0);
-    ++a0;
     if (!(ok = wait_bar_warp(&S->full[1][j % kStages1], (j / kStages1) & 1, S)))
       break;
     relay_arrive(kBarRing1 + j % kStages1);
-    ++a1;
   }
-  for (; a0 < n; ++a0) relay_arrive(kBarRing0 + a0 % kS0);
-  for (; a1 < n; ++a1) relay_arrive(kBarRing1 + a1 % kStages1);
+  // `drain` completes when the MMA warp has left its loop and its MMAs are done.
+  volatile int* abort = &S->abort;
+  const uint64_t t0 = global_timer_ns();
+  bool done = false;
+  while (!done) {
+    if (__any_sync(0xffffffffu, *abort != 0)) {
+      compute_arrive(kBarP);
+      compute_arrive(kBarDS);
+      compute_arrive(kBarDSOdd);
+      for (int st = 0; st < kS0; ++st) relay_arrive(kBarRing0 + st);
+      for (int st = 0; st < kStages1; ++st) relay_arrive(kBarRing1 + st);
+      __nanosleep(200);
+      done = __any_sync(0xffffffffu,
+                        *reinterpret_cast<volatile int*>(&S->mma_done) != 0);
+    } else {
+      done = __all_sync(0xffffffffu, mbar_try_wait(&S->drain, 0));
+    }
+    if (__any_sync(0xffffffffu, global_timer_ns() - t0 >
+                                    3 * S->wait_limit_ns + kReleaseNs))
+      break;
+  }
+}
+
+__device__ __forceinline__ uint32_t read_abort(const BwdShared* S) {
+  uint32_t a;
+  asm volatile("ld.volatile.shared.u32 %0, [%1];"
+               : "=r"(a)
+               : "r"(smem_addr(&S->abort)));
+  return a;
 }
 
 __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity) {
@@ -306,6 +332,7 @@ __device__ __forceinline__ uint32_t bwd_setup(BwdShared* S,
     mbar_init(&S->o_full, 1);
     mbar_init(&S->drain, 1);
     S->abort = 0;
+    S->mma_done = 0;
     S->status = p.status;
     S->wait_limit_ns = p.wait_limit_ns ? p.wait_limit_ns : kWaitLimitNs;
     fence_barrier_init();
@@ -331,7 +358,7 @@ template <class L>
 __device__ void bwd_producer(uint8_t* smem, BwdShared* S, const CUtensorMap* f0,
                              const CUtensorMap* f1, int t_fixed,
                              const CUtensorMap* r0, const CUtensorMap* r1,
-                             int t0, int n, int h, int b) {
+                             int t0, int n, int h, int b, bool stall) {
   constexpr int kS0 = L::kS0;
   // The resident tiles are read by this CTA alone (evict first); the
   // streamed tiles of a head are read by every CTA of the head (evict last).
@@ -349,6 +376,9 @@ __device__ void bwd_producer(uint8_t* smem, BwdShared* S, const CUtensorMap* f0,
   int issued[2] = {0, 0};
   for (int j = 0; j < n; ++j) {
     const int s1 = j % kStages1, s0 = j % kS0;
+    // Test hook: without the second step's tiles waits run out, the MMA warp amid
+    // its work.
+    if (stall && j == 1 && !wait_bar(&S->drain, 0, S)) break;
     if (!wait_bar(&S->empty[1][s1], ((j / kStages1) & 1) ^ 1, S)) break;
     mbar_arrive_expect_tx(&S->full[1][s1], L::kNB * kBox);
     for (int bx = 0; bx < L::kNB; ++bx)
@@ -487,7 +517,7 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
   if (warp == kProducerWarp) {
     if (lane == 0)
       bwd_producer<L>(smem, S, &p.k_map, &p.v_map, k0, &p.q_map, &p.do_map,
-                      q0, n, h, b);
+                      q0, n, h, b, p.inject_stall == 2);
     __syncwarp();
   } else if (warp == kRelayWarp) {
     bwd_relay<kDkdvS0>(S, n);
@@ -520,7 +550,7 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
     // as soon as they finish this tile's dS.
     // Test hook: o_full receives no arrival before the end, so this wait
     // runs out and exercises the abort path.
-    bool ok = (!p.inject_stall || wait_bar_warp(&S->o_full, 0, S)) &&
+    bool ok = (p.inject_stall != 1 || wait_bar_warp(&S->o_full, 0, S)) &&
               wait_bar_warp(&S->fixed_full, 0, S);
     if (ok) {
       relay_sync(kBarRing0);
@@ -536,6 +566,7 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
       // Q (ring 0) and dO (ring 1) run at their own depths
       const int q_st = j % kDkdvS0, q_stn = (j + 1) % kDkdvS0;
       const int o_st = j % kStages1, o_stn = (j + 1) % kStages1;
+      const uint32_t aborted = read_abort(S);  // looked at after the step
       compute_sync(kBarP);
       tc_fence_after();
       mma_tn<D>(sbase, tmem, 256, 0, L::ring(o_st, 1, 0), j > 0);    // dV
@@ -556,10 +587,14 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
         mma_nt<D, L>(sbase, tmem, 128, 1, o_stn, 1);  // dP^T_{j+1}
         mma_commit_warp(&S->dp_ready[0]);
       }
+      if (__any_sync(0xffffffffu, aborted != 0)) ok = false;
     }
     if (ok) mma_commit_warp(&S->o_full);
     mma_commit_warp(&S->drain);
-    if (lane == 0) drain_wait(&S->drain, 0);
+    if (lane == 0) {
+      drain_wait(&S->drain, 0);
+      *reinterpret_cast<volatile int*>(&S->mma_done) = 1;
+    }
     __syncwarp();
   } else {
     // Compute warps: warp w owns key rows 32 (w % 4) .. + 31 (its TMEM
@@ -574,7 +609,6 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
     key_sees(p, k0 + t, vis_lo, vis_hi);
     const uint64_t c2x2 = f2(p.scale_log2, p.scale_log2);
     bool ok = true;
-    int p_arr = 0, ds_arr = 0;  // hand-offs made to the MMA warp
     for (int j = 0; j < n; ++j) {
       const int i0 = q0 + j * kT + 64 * hf;  // first query of this half
       const int sl = j & 1;
@@ -614,7 +648,6 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
       tmem_wait_st();
       tc_fence_before();
       compute_arrive(kBarP);
-      ++p_arr;
       // phase 2 (overlaps the dV and next S^T MMAs): dS^T over the first
       // half of dP^T; the D values are read ahead like the LSE values
 #pragma unroll
@@ -634,16 +667,10 @@ dkdv_kernel(const __grid_constant__ BwdParams p) {
       tmem_wait_st();
       tc_fence_before();
       compute_arrive(kBarDS);
-      ++ds_arr;
       // the row-vector slot is read for the last time
       __syncwarp();
       if (lane == 0) mbar_arrive(&S->vec_empty[sl]);
     }
-    // After a failed wait the remaining hand-offs are still made (with
-    // undefined contents), so that the MMA warp never waits for an arrival
-    // that does not come.
-    for (; p_arr < n; ++p_arr) compute_arrive(kBarP);
-    for (; ds_arr < n; ++ds_arr) compute_arrive(kBarDS);
     // dV and dK are staged in the first two Q stages (free once o_full has
     // completed: every MMA has read its operands) and leave as TMA stores;
     // rows past the sequence fall outside the map and are not written.
@@ -696,7 +723,7 @@ dq_kernel(const __grid_constant__ BwdParams p) {
   if (warp == kProducerWarp) {
     if (lane == 0)
       bwd_producer<L>(smem, S, &p.q_map, &p.do_map, q0, &p.k_map, &p.v_map,
-                      kv0, n, h, b);
+                      kv0, n, h, b, p.inject_stall == 2);
     __syncwarp();
   } else if (warp == kRelayWarp) {
     bwd_relay<kDqS0>(S, n);
@@ -710,7 +737,7 @@ dq_kernel(const __grid_constant__ BwdParams p) {
     // two buffers, so it need not wait for this tile's dQ to read dS.
     // Test hook: o_full receives no arrival before the end, so this wait
     // runs out and exercises the abort path.
-    bool ok = (!p.inject_stall || wait_bar_warp(&S->o_full, 0, S)) &&
+    bool ok = (p.inject_stall != 1 || wait_bar_warp(&S->o_full, 0, S)) &&
               wait_bar_warp(&S->fixed_full, 0, S);
     if (ok) {
       relay_sync(kBarRing0);
@@ -727,6 +754,7 @@ dq_kernel(const __grid_constant__ BwdParams p) {
       // K (ring 0) and V (ring 1) run at their own depths
       const int k_st = j % kDqS0, k_stn = (j + 1) % kDqS0;
       const int v_stn = (j + 1) % kStages1;
+      const uint32_t aborted = read_abort(S);  // looked at after the step
       compute_sync(kBarP);
       if (j + 1 < n) {
         relay_sync(kBarRing0 + k_stn);
@@ -744,10 +772,14 @@ dq_kernel(const __grid_constant__ BwdParams p) {
       tc_fence_after();
       mma_tn<D>(sbase, tmem, 256, dq_dp_col(j), L::ring(k_st, 0, 0), j > 0);  // dQ
       mma_commit_warp(&S->empty[0][k_st]);  // K_j read for the last time
+      if (__any_sync(0xffffffffu, aborted != 0)) ok = false;
     }
     if (ok) mma_commit_warp(&S->o_full);
     mma_commit_warp(&S->drain);
-    if (lane == 0) drain_wait(&S->drain, 0);
+    if (lane == 0) {
+      drain_wait(&S->drain, 0);
+      *reinterpret_cast<volatile int*>(&S->mma_done) = 1;
+    }
     __syncwarp();
   } else {
     // Compute warps: warp w owns query rows 32 (w % 4) .. + 31 and key
@@ -772,7 +804,6 @@ dq_kernel(const __grid_constant__ BwdParams p) {
     for (int q = 0; q < 8; ++q) nd_v[q] = make_float4(nd_row, nd_row, nd_row, nd_row);
     const uint64_t c2x2 = f2(p.scale_log2, p.scale_log2);
     bool ok = true;
-    int p_arr = 0, ds_arr = 0;  // hand-offs made to the MMA warp
     for (int j = 0; j < n; ++j) {
       const int tok0 = kv0 + j * kT + 64 * hf;
       if (!(ok = wait_bar_warp(&S->s_ready, j & 1, S))) break;
@@ -797,7 +828,6 @@ dq_kernel(const __grid_constant__ BwdParams p) {
       }
       tc_fence_before();
       compute_arrive(kBarP);
-      ++p_arr;
       // phase 2 (overlaps the next tile's S and dP MMAs): dS over this
       // step's dP buffer
       if (!(ok = wait_bar_warp(&S->dp_ready[j & 1], (j >> 1) & 1, S))) break;
@@ -813,13 +843,7 @@ dq_kernel(const __grid_constant__ BwdParams p) {
       tmem_wait_st();
       tc_fence_before();
       compute_arrive(dq_ds_bar(j));
-      ++ds_arr;
     }
-    // After a failed wait the remaining hand-offs are still made (with
-    // undefined contents), so that the MMA warp never waits for an arrival
-    // that does not come.
-    for (; p_arr < n; ++p_arr) compute_arrive(kBarP);
-    for (; ds_arr < n; ++ds_arr) compute_arrive(dq_ds_bar(ds_arr));
     // dQ is staged in the first K stage (free once o_full has completed)
     // and leaves as TMA stores; rows past the sequence are not written.
     uint8_t* const tiles[1] = {smem + L::ring(0, 0, 0)};

@@ -1,6 +1,7 @@
-"""The streamed and the one-shot forward without their values: waits run out while the
-MMA warp is amid a unit, the softmax lanes' each at its own time.  The failure is
-reported, every role leaves soon, and the same call gives its results again."""
+"""The streamed and the one-shot forward without their values, the one-shot backward
+without its second step's tiles: waits run out while the MMA warp is amid its work, the
+forward's softmax lanes' each at its own time.  The failure is reported, every role
+leaves soon, and the same call gives its results again."""
 import time
 
 import pytest
@@ -33,13 +34,22 @@ def _one_shot(chunks, n, heads, d, window):
             FV.fastvr_get_device_status, FV.fastvr_debug_inject_stall_noplan)
 
 
+def _backward(chunks, n, heads, d, window):
+    from paper_2609_36757_gb300 import fastvr as FV
+    cfg = FV.make_config(1, heads, d, n, 1, window, chunks)
+    q, k, v, do = (_rnd(i, 1, chunks * n, heads, d) for i in range(4))
+    out, lse = FV.blockcausal_attention(cfg, q, k, v, want_lse=True)
+    return (lambda: FV.blockcausal_attention_bwd(cfg, q, k, v, out, do, lse),
+            FV.fastvr_get_device_status, FV.fastvr_debug_inject_stall_noplan)
+
+
 @pytest.mark.parametrize("case", [
     # chunks, tokens of each, heads, window: whole units; units cut over CTAs and
     # merged; units of several hundred key tiles
     (3, 700, 2, -1), (2, 5000, 40, 1), (80, 200, 1, -1), (300, 200, 2, -1),
     (4, 20000, 1, -1)], ids=str)
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("make", [_streamed, _one_shot])
+@pytest.mark.parametrize("make", [_streamed, _one_shot, _backward])
 def test_stall_amid_a_unit_is_reported(make, d, case):
     from paper_2609_36757_gb300 import fastvr as FV
     chunks, n, heads, window = case
