@@ -305,9 +305,9 @@ FASTVR_API fastvr_status_t fastvr_get_device_status(void);
  * fastvr_debug_inject_stall takes them), every role stops, in-flight copies and
  * MMAs are drained, tensor memory is released and FASTVR_ERR_TIMEOUT is
  * recorded for fastvr_get_device_status.
- * With stall = 2 the one-shot forward and backward and the cross attention's
- * forward wait in a loading thread instead, while the other warps are amid their
- * work.
+ * With stall = 2 the one-shot forward and backward and those of the cross
+ * attention wait in a loading thread instead, while the other warps are amid
+ * their work.
  * No GPU fault or hang results.  stall = 0 restores normal operation.
  * Host only; always FASTVR_OK. */
 FASTVR_API fastvr_status_t fastvr_debug_inject_stall_noplan(

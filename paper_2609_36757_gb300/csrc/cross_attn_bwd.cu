@@ -486,6 +486,10 @@ __device__ __forceinline__ void dkdv_cta(const BwdParams& p, uint8_t* smem,
       for (int j = 0; j < n; ++j) {
         const int h = h0 + (int)fast_div(x0 + j, p.by_q_tiles);
         const int tok = (x0 + j - (h - h0) * p.q_tiles) * kT;
+        // Test hook: waits run out, the MMA warp amid its work.
+        if (p.inject_stall == 2 && j == 1 &&
+            !wait_bar(&S->drain, 0, S, p.status))
+          break;
         if (!ring_load<D, RO>(p, smem, S, &p.do_map, oc, tok, h,
                               b * p.do_batch, keep) ||
             !ring_load<D, RQ>(p, smem, S, &p.q_map, qc, tok, h, b * p.q_batch,
@@ -532,7 +536,7 @@ __device__ __forceinline__ void dkdv_cta(const BwdParams& p, uint8_t* smem,
     auto q_at = [](int c) { return RQ::off + c % RQ::depth * L::kTile; };
     auto o_at = [](int c) { return RO::off + c % RO::depth * L::kTile; };
     // Test hook: `out_full` receives no arrival before the end.
-    bool ok = (!p.inject_stall ||
+    bool ok = (p.inject_stall != 1 ||
                wait_bar_warp(&S->out_full, 0, S, p.status)) &&
               wait_bar_warp(&S->fixed_full, 0, S, p.status);
     if (ok) {
@@ -779,7 +783,8 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
                      keep = l2_policy_evict_last();
       int x = cta, c = 0, r = 0;
       Unit u;
-      bool ok = true;
+      bool ok = a || p.inject_stall != 2 ||  // test hook, as in dkdv_cta
+                wait_bar(&S->drain, 0, S, p.status);
       while (ok && next_unit(p, x, &u)) {
         const int hk = (int)fast_div(u.h, p.by_group);
         for (int j = 0; ok && j < u.n; ++j) {
@@ -837,7 +842,7 @@ __device__ __forceinline__ void dq_cta(const BwdParams& p, uint8_t* smem,
       return off + c % depth * L::kTile;
     };
     // Test hook: `drain` receives no arrival before the end.
-    bool ok = !p.inject_stall || wait_bar_warp(&S->drain, 0, S, p.status);
+    bool ok = p.inject_stall != 1 || wait_bar_warp(&S->drain, 0, S, p.status);
     int x = cta;
     Unit u, nu;
     bool have = next_unit(p, x, &u);

@@ -1,6 +1,7 @@
-"""Cross attention's forward without its values: the softmax lanes' waits run out, each
-at its own time, while the MMA warp is amid a unit.  The failure is reported, every
-role leaves, and the same call gives its results again."""
+"""Cross attention's forward without its values, and its gradients without some tiles:
+waits run out while the MMA warp is amid a unit, the forward's softmax lanes' each at
+its own time.  The failure is reported, every role leaves, and the same call gives its
+results again."""
 import time
 
 import pytest
@@ -9,7 +10,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 
-def _call(B, L, H, T, d, lens, seed=1):
+def _call(B, L, H, T, d, lens, seed=1, grads=False):
     from paper_2609_36757_gb300 import fastvr as FV
     g = torch.Generator("cuda").manual_seed(seed)
     rnd = lambda *s: torch.randn(*s, generator=g,
@@ -18,7 +19,11 @@ def _call(B, L, H, T, d, lens, seed=1):
     n = None if lens is None else torch.tensor(lens, dtype=torch.int32,
                                                device="cuda")
     cfg = FV.make_cross_config()
-    return lambda: FV.cross_attention(cfg, q, k, v, n, want_lse=True)
+    if not grads:
+        return lambda: FV.cross_attention(cfg, q, k, v, n, want_lse=True)
+    out, lse = FV.cross_attention(cfg, q, k, v, n, want_lse=True)
+    do = rnd(B, L, H, d)
+    return lambda: FV.cross_attention_bwd(cfg, q, k, v, out, do, lse, n)
 
 
 CASES = [
@@ -30,10 +35,11 @@ CASES = [
 ]
 
 
+@pytest.mark.parametrize("grads", [False, True])
 @pytest.mark.parametrize("case", CASES, ids=str)
-def test_stall_amid_a_unit_is_reported(case):
+def test_stall_amid_a_unit_is_reported(case, grads):
     from paper_2609_36757_gb300 import fastvr as FV
-    call = _call(*case)
+    call = _call(*case, grads=grads)
     ref = call()
     assert FV.fastvr_get_device_status() == FV.FASTVR_OK
     FV.fastvr_debug_inject_stall_noplan(2, 20_000_000)  # 20 ms per wait
@@ -51,12 +57,13 @@ def test_stall_amid_a_unit_is_reported(case):
     assert FV.fastvr_get_device_status() == FV.FASTVR_OK
 
 
+@pytest.mark.parametrize("grads", [False, True])
 @pytest.mark.parametrize("d", [64, 128])
-def test_stall_amid_a_long_unit(d):
+def test_stall_amid_a_long_unit(d, grads):
     """The MMA warp leaves a unit of 1563 key tiles soon, whatever the limit: what
     keeps it from waiting for arrivals that nobody makes lasts for a while only."""
     from paper_2609_36757_gb300 import fastvr as FV
-    call = _call(1, 300, 1, 200_000, d, None)
+    call = _call(1, 300, 1, 200_000, d, None, grads=grads)
     ref = call()
     FV.fastvr_debug_inject_stall_noplan(2, 1_000_000)  # 1 ms
     try:
