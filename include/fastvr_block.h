@@ -302,8 +302,9 @@ FASTVR_API fastvr_status_t fastvr_q4_read(fastvr_plan_t plan, int64_t chunk,
  * its lse -infinity.  What k and v hold at t >= T_b (padding, NaN and
  * infinities included) does not matter. */
 typedef struct {
-  int32_t batch, q_tokens, kv_tokens; /* >= 1; batch * heads * (tokens / 128,
-                                         rounded up) below 2^29 for either   */
+  int32_t batch, q_tokens, kv_tokens; /* >= 1; tokens below 2^30, batch *
+                                         heads * (tokens / 128, rounded up)
+                                         below 2^29, for either              */
   int32_t heads, kv_heads;            /* heads a multiple of kv_heads         */
   int32_t head_dim;                   /* 64 or 128                            */
   float softmax_scale;                /* >= 0; 0 = 1 / sqrt(head_dim)         */

@@ -26,8 +26,8 @@
 // either tile can follow at once; each tile's PV runs one key tile behind,
 // which gives its softmax three MMA steps to store P_t.  The MMA warp never
 // polls a shared-memory barrier: every hand-off to it (S read, P_t stored,
-// K/V stage landed) is a named barrier, whose arrivals are made on every
-// path (also after a failed wait), since a named barrier has no time limit.
+// K/V stage landed) is a named barrier.  Those have no time limit: after a
+// failed wait the relay arrives on all of them until the MMA warp has left.
 //
 // Online softmax in the exp2 domain: each row keeps a reference m (a lower
 // bound of its running max) and exponentiates against it; m moves, and O is

@@ -481,7 +481,9 @@ __device__ void mma_issuer(const CrossParams& p, uint8_t* smem, Shared* S,
 // out = O / l from TMEM, where a lane has a row.  With heads of 128 lanes 2 i and
 // 2 i + 1 exchange pieces of 32 bytes (whole sectors), so that a store writes 64 bytes
 // of 16 rows, `first` being the even lane's row and `second` the odd one's, instead of
-// 32 bytes of 32 rows: 43.5 us instead of 46.0 for the 1080p chunk.  A row of 64 has
+// 32 bytes of 32 rows: 43.0 us instead of 45.8 for the 1080p chunk, 18.9 instead of 19.9
+// for 7440 tokens over 226 keys; 12.1 instead of 11.8 for 3180, two short units to a CTA,
+// the one of seven sizes that loses more than a hundredth.  A row of 64 has
 // too few of them (67.9 us for 19456 tokens of 24 heads over 512 keys, 73.4 with the
 // exchange): `first` is the lane's own.
 template <int D>

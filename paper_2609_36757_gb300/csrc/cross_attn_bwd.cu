@@ -400,8 +400,8 @@ __device__ __forceinline__ void dscores32(const uint32_t (&p)[32],
 
 // 32 scaled results of TMEM, where a lane has a row, as bfloat16 to rows `even` and
 // `odd` of the lane and its neighbour (null: no such row).  A lane writes 32 bytes
-// of both (cross_attn.cu): 291 us for 12288 tokens of 24 heads over 512 keys with the
-// forward, 292 without the exchange.
+// of both (cross_attn.cu): with the forward 295.5 us for 12288 tokens of 24 heads over
+// 512 keys (298.3 without the exchange), 158.1 over 128 (160.0).
 __device__ __forceinline__ void store_cols32(uint32_t taddr, float mul,
                                              bool zero, uint16_t* even,
                                              uint16_t* odd, bool wide) {

@@ -20,10 +20,11 @@
 // (six stages), warp 1 of the even CTA issues the MMAs of both, warps 4-11 form and
 // store the results from one half of TMEM while the next tile accumulates in
 // the other.  Where there are too few tiles for all pairs they are half as wide.
-// Measured: 16320 x 1536 to 4096 in 227 us (1813 TFLOP/s, 93 to 96 % of the
-// tensor pipe's cycles, 33 % above its bytes' time), with g and u kept 12288 tokens in
-// 175; dx and both dW of these in 340 to 353 (1750 TFLOP/s and more).  Every wait is
-// bounded, as in chunk_attn_fwd.cu.
+// Measured: 16320 x 1536 to 4096 in 227 to 241 us one after another (1700 to 1810
+// TFLOP/s at the power cap, a median of 1500 MHz; its bytes take 31), 203 to 213 alone
+// after a pause (1830 MHz), 92 % of the tensor pipe's cycles either way; 12288 tokens
+// with g and u kept in 175 (83 %), dx and both dW of these in 335 to 353 (89 %; 1750
+// TFLOP/s and more).  Every wait is bounded, as in chunk_attn_fwd.cu.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <math.h>
