@@ -179,6 +179,7 @@ cross_rows_kernel(const __grid_constant__ RowsParams p) {
       o[n][2] *= alpha[1];
       o[n][3] *= alpha[1];
     }
+    // P in bfloat16, V's type; the sums above took it unrounded
     const uint32_t a0 = pack_bf16(s[0][0], s[0][1]),
                    a1 = pack_bf16(s[0][2], s[0][3]),
                    a2 = pack_bf16(s[1][0], s[1][1]),

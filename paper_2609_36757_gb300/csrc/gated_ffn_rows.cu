@@ -105,7 +105,7 @@ rows_kernel(const __grid_constant__ FfnArgs a) {
       const int64_t tok = i % kTok * 8 + 2 * t + e;
       if (tok >= a.tokens || col >= a.hidden) continue;
       const int64_t at = tok * a.hidden + col;
-      if (a.g != nullptr) {
+      if (a.g != nullptr) {  // in bfloat16, as gated_ffn.cu keeps them
         a.g[at] = __bfloat16_as_ushort(__float2bfloat16_rn(s[e]));
         a.u[at] = __bfloat16_as_ushort(__float2bfloat16_rn(s[2 + e]));
       }
