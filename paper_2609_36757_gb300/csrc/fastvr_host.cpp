@@ -46,6 +46,8 @@ namespace {
 std::atomic<int32_t> g_noplan_stall{0};
 std::atomic<uint64_t> g_noplan_wait_ns{0};
 
+// The hook's form: any value but 0 and 2 is 1.
+int32_t stall_form(int32_t stall) { return stall == 2 ? 2 : stall != 0; }
 // A limit as the kernels take it.  They wait as long for the copies and MMAs in
 // flight before they leave, so it is no shorter than those may take; and no wait
 // lasts for ever.
@@ -539,7 +541,7 @@ fastvr_status_t fastvr_plan_launch_count(fastvr_plan_t p, int64_t* launches) {
 fastvr_status_t fastvr_debug_inject_stall(fastvr_plan_t p, int32_t stall,
                                           uint64_t wait_limit_ns) {
   if (p == nullptr) return FASTVR_ERR_INVALID_ARG;
-  p->inject_stall = stall;
+  p->inject_stall = stall_form(stall);
   p->wait_limit_ns = wait_limit(wait_limit_ns);
   return FASTVR_OK;
 }
@@ -571,7 +573,7 @@ fastvr_status_t fastvr_get_device_status(void) {
 
 fastvr_status_t fastvr_debug_inject_stall_noplan(int32_t stall,
                                                  uint64_t wait_limit_ns) {
-  g_noplan_stall.store(stall);
+  g_noplan_stall.store(stall_form(stall));
   g_noplan_wait_ns.store(wait_limit(wait_limit_ns));
   return FASTVR_OK;
 }

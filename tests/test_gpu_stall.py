@@ -70,3 +70,19 @@ def test_stall_amid_a_unit_is_reported(make, d, case):
     for a, b in zip(call(), ref):
         assert torch.equal(a, b)
     assert status() == FV.FASTVR_OK
+
+
+@pytest.mark.parametrize("stall", [-1, 3, 1 << 20])
+@pytest.mark.parametrize("make", [_streamed, _one_shot, _backward])
+def test_any_other_value_stalls_the_mma_warp(make, stall):
+    from paper_2609_36757_gb300 import fastvr as FV
+    call, status, hook = make(3, 300, 2, 64, -1)
+    call()
+    hook(stall, 5_000_000)
+    try:
+        call()
+        assert status() == FV.FASTVR_ERR_TIMEOUT
+    finally:
+        hook(0, 0)
+    call()
+    assert status() == FV.FASTVR_OK
