@@ -43,7 +43,8 @@ extern "C" {
 
 /* Strides of a [batch, token, head, d] tensor in elements; the d elements of
  * a head are contiguous.  Every stride (of a dimension with more than one
- * entry) is a multiple of 16 bytes; an output's is not 0. */
+ * entry) is a multiple of 16 bytes; an output's is not 0, and its heads do not
+ * overlap one another. */
 typedef struct {
   int64_t batch, token, head;
 } fastvr_strides_t;
